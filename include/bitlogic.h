@@ -50,15 +50,16 @@ typedef enum {
     BITLOGIC_ERR_NULL = -1,       /* a required pointer is NULL */
     BITLOGIC_ERR_SHAPE = -2,      /* size <= 0, overflow, or w % C != 0 */
     BITLOGIC_ERR_FANIN = -3,      /* k outside 1..6, or k > w_in */
-    BITLOGIC_ERR_ALIGN = -4,      /* workspace not 16-byte aligned */
+    BITLOGIC_ERR_ALIGN = -4,      /* workspace not 16-byte aligned, or an array not as the call needs */
     BITLOGIC_ERR_WORKSPACE = -5,  /* workspace smaller than the query result */
     BITLOGIC_ERR_CUDA = -6,       /* a CUDA launch or copy failed */
     BITLOGIC_ERR_INDEX = -7,      /* index out of range (host-side check) */
     BITLOGIC_ERR_DEVICE = -8,     /* device-side index check tripped */
     BITLOGIC_ERR_THRESH = -9,     /* thresholds: b outside 1..32 */
     BITLOGIC_ERR_TOO_LARGE = -10, /* sizes beyond bitlogic_head_loss_noalloc's fixed scratch */
-    BITLOGIC_ERR_HYPER = -11,     /* optimizer hyperparameter out of range */
-    BITLOGIC_ERR_NODE = -12       /* unknown node form */
+    BITLOGIC_ERR_HYPER = -11,     /* optimizer or loss hyperparameter out of range */
+    BITLOGIC_ERR_NODE = -12,      /* unknown node form */
+    BITLOGIC_ERR_DTYPE = -13      /* logit type unknown, or not taken by the call */
 } bitlogic_status_t;
 
 /* Node forms of the LightLUT parameterization (§2 "Gradient-based LUT
@@ -534,6 +535,114 @@ int bitlogic_head_loss_noalloc(const float* Y, int32_t w, int64_t B, int32_t C, 
 int bitlogic_adamw_update(float* theta, float* m, float* v, const float* grad, int64_t n,
                           int64_t step, float lr, float beta1, float beta2, float eps,
                           float weight_decay, cudaStream_t stream);
+
+/* Operators on rows of logits: what a student learns from a teacher's
+ * answers, the record of those answers, and answers drawn by chance.  The
+ * logits may come from the group-sum head (bitlogic_head_loss_ex), from the
+ * hard head's counts (bitlogic_hard_forward) or from any other model.
+ *
+ *   X      device [T] rows of V classes, row t at X + t*ld elements (ld >= V),
+ *          aligned to the element (BITLOGIC_ERR_ALIGN otherwise);
+ *          1 <= V <= 2^20.  T == 0 writes nothing but a zero loss.
+ *   dtype  the type of X, a bitlogic_dtype_t (BITLOGIC_ERR_DTYPE otherwise).
+ *          Values are taken to fp32, and every sum, maximum and probability
+ *          is held in fp32 or wider.  In BITLOGIC_I32 the lowest int stands
+ *          for -inf.
+ * -inf marks a class that is masked.  Any other number, the type's lowest
+ * among them, is an ordinary logit.  No call needs a workspace, and results do
+ * not depend on the rows around a row. */
+typedef enum {
+    BITLOGIC_F32 = 0,
+    BITLOGIC_BF16 = 1,
+    BITLOGIC_F16 = 2,
+    BITLOGIC_I32 = 3    /* counts; bitlogic_top_logits and bitlogic_sample_logits */
+} bitlogic_dtype_t;
+
+/* The K largest logits of every row, in the order (value descending, class
+ * ascending), and the row's log-sum-exp: the record of a teacher's answers that
+ * bitlogic_distill_loss reads.
+ *   val  device fp32 [T][K]   the logits (not divided by the temperature)
+ *   idx  device int32 [T][K]  their classes
+ *   lse  device fp32 [T] or NULL: ln sum_v exp(X[t][v] / temperature)
+ * 1 <= K <= 256, K <= V.  -inf and NaN do not rank: a row with fewer than K
+ * other logits ends in val -inf, idx -1.  lse is -inf for a row of -inf, NaN
+ * when the row has a NaN, +inf when it has +inf and no NaN.
+ * Returns BITLOGIC_ERR_NULL, BITLOGIC_ERR_SHAPE, BITLOGIC_ERR_DTYPE,
+ * BITLOGIC_ERR_ALIGN, BITLOGIC_ERR_HYPER (temperature not positive and
+ * finite), BITLOGIC_ERR_CUDA. */
+int bitlogic_top_logits(const void* X, int32_t dtype, int64_t T, int32_t V, int64_t ld, int32_t K,
+                        float temperature, float* val, int32_t* idx, float* lse, cudaStream_t stream);
+
+/* Loss of a student's logits Z against a teacher's record and labels, with its
+ * gradient.  With y = z / temperature, p = softmax(y) and the record's classes
+ * v_k with a_k = teacher_val[t][k] / temperature:
+ *   teacher_lse NULL  q_k = softmax of a over the record, q_r = 0
+ *   teacher_lse given q_k = exp(a_k - teacher_lse[t]) (the log-sum-exp of all
+ *                     the teacher's logits at this temperature), and
+ *                     q_r = max(0, 1 - sum_k q_k) for the classes off the
+ *                     record taken together, whose share of p is r
+ *   KL          = sum_k q_k (ln q_k - ln p[v_k]) + q_r (ln q_r - ln r)
+ *   row_loss[t] = kd_weight temperature^2 KL
+ *                 + ce_weight (ln sum_v exp(z_v) - z[labels[t]])
+ *   loss        = sum_t w_t row_loss[t],  w_t = row_weight[t], or 1/T when NULL
+ *   dZ[t][v]    = grad_scale w_t d row_loss[t] / d z_v, rounded once to dtype
+ *   Z            as X above, BITLOGIC_F32, BITLOGIC_BF16 or BITLOGIC_F16
+ *   teacher_val  device fp32 [T][K], teacher_idx device int32 [T][K],
+ *                1 <= K <= 256 (K may exceed V: places without an entry hold a
+ *                negative class); teacher_lse device fp32 [T] or NULL
+ *   labels       device int32 [T] or NULL; negative: the row has no label
+ *   row_weight   device fp32 [T] or NULL
+ *   row_loss     device fp32 [T];  loss device fp32 [1]
+ *   dZ           device, of Z's type, or NULL (the loss alone): element (t, v)
+ *                at t*ldg + v*incg (incg = 1 for rows; ldg = 1, incg = T for
+ *                one row per class, as the layer backward reads them as
+ *                dY_grouped with grad_scale = 1 / tau).  It may be Z itself
+ *                with the same strides, and overlap Z in no other way.
+ * A row of weight 0 has loss and gradient 0 whatever its logits hold, and so
+ * has a row whose logits are all -inf.  A row without entries has no teacher
+ * term.  A teacher value of -inf has q = 0.  A class that is on the record more
+ * than once counts with the sum of its q.  A masked class has gradient
+ * -q times its factor, and a loss of +inf where q > 0 or where it is the
+ * label.  A row with a NaN or +inf logit has NaN in its loss and gradient.
+ * A class or label of V or more raises the device flag and is ignored.
+ * Sums run in a fixed order: results are the same from run to run.
+ * Returns BITLOGIC_ERR_NULL, BITLOGIC_ERR_SHAPE, BITLOGIC_ERR_DTYPE,
+ * BITLOGIC_ERR_ALIGN, BITLOGIC_ERR_HYPER (temperature not positive and finite,
+ * a weight or scale not finite), BITLOGIC_ERR_CUDA. */
+int bitlogic_distill_loss(const void* Z, int32_t dtype, int64_t T, int32_t V, int64_t ld,
+                          const float* teacher_val, const int32_t* teacher_idx, int32_t K,
+                          const float* teacher_lse, const int32_t* labels, const float* row_weight,
+                          float temperature, float kd_weight, float ce_weight,
+                          float* row_loss, float* loss, void* dZ, int64_t ldg, int64_t incg,
+                          float grad_scale, cudaStream_t stream);
+
+/* A class drawn per row from given random numbers.  With m the largest logit
+ * of the row, slope = (1 / temperature) log2(e) and
+ *   e_v = 2^((x_v - m) slope),   w_v = 2^40 e_v rounded to a whole number,
+ * the classes kept are, in this order,
+ *   1. the first top_k in the order (value descending, class ascending);
+ *   2. of these the shortest run from the front whose weights sum to at least
+ *      floor(top_p sum) of theirs (never less than one class);
+ *   3. of these the ones with e_v >= min_p,
+ * and the draw is the first class, by class, whose kept weights up to and
+ * including its own exceed floor(u sum of the kept).  u and top_p count with 24
+ * bits after the point.  The weights are whole numbers, so the sums are exact
+ * in any order and the draw does not depend on the batch or on how a row is
+ * split over threads.
+ *   u            device fp32 [T], in [0, 1) (clamped; NaN reads 0)
+ *   temperature  device fp32 [T] or NULL (1); not > 0: the first of the largest
+ *   top_k        device int32 [T] or NULL; <= 0: off
+ *   top_p        device fp32 [T] or NULL; >= 1 or NaN: off
+ *   min_p        device fp32 [T] or NULL; not > 0: off, above 1 reads 1
+ *   token        device int32 [T]; -1 when every logit is -inf or NaN
+ *   logprob      device fp32 [T] or NULL: ln of the probability with which the
+ *                class is drawn (-inf when token is -1)
+ * NaN and -inf are never drawn; with +inf the draw is the first of those.
+ * Returns BITLOGIC_ERR_NULL, BITLOGIC_ERR_SHAPE, BITLOGIC_ERR_DTYPE,
+ * BITLOGIC_ERR_ALIGN, BITLOGIC_ERR_CUDA. */
+int bitlogic_sample_logits(const void* X, int32_t dtype, int64_t T, int32_t V, int64_t ld, const float* u,
+                           const float* temperature, const int32_t* top_k, const float* top_p,
+                           const float* min_p, int32_t* token, float* logprob, cudaStream_t stream);
 
 /* Table discretization (§3: every surrogate discretizes to a 2^n-entry
  * truth table; App. C.1 extracts it once per layer): bit a of table[j] is 1

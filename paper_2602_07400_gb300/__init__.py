@@ -33,6 +33,7 @@ __all__ = [
     "bitlogic_lut_forward_bitrows", "bitlogic_lut_backward_bitrows", "bitrow_words",
     "bitlogic_lut_forward_codes", "bitlogic_codes_decode", "bitlogic_lut_forward_coded",
     "bitlogic_lut_backward_coded", "bitlogic_corner_reduce", "code_bytes",
+    "bitlogic_top_logits", "bitlogic_distill_loss", "bitlogic_sample_logits", "LOGIT_TYPES", "MAX_TOP",
     "bitlogic_head_loss", "bitlogic_binarize_tables", "bitlogic_pack_bits",
     "bitlogic_hard_forward", "bitlogic_build_csr", "bitlogic_csr_positions", "bitlogic_degree_order",
     "bitlogic_device_error",
@@ -49,6 +50,13 @@ LIB_PATH = _build.LIB
 # node forms (bitlogic_node_t): the soft LightLUT node and its
 # straight-through hard form
 NODE_FORMS = {"soft": 0, "st": 1}
+
+# types of a matrix of logits (bitlogic_dtype_t); int32 counts are taken by
+# bitlogic_top_logits and bitlogic_sample_logits
+LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int32: 3}
+
+# entries of a teacher's record per row, at most
+MAX_TOP = 256
 
 # instruction kinds of the issue-throughput probe (bitlogic_probe_t)
 PROBE_KINDS = {"lop3": 0, "imad": 1, "ffma": 2, "mux3": 3, "mix": 4}
@@ -120,6 +128,10 @@ _SIGS = {
     "bitlogic_head_loss_noalloc": ([_P, _I32, _I64, _I32, _F32, _P, _P, _P, _P, _P], ctypes.c_int),
     "bitlogic_head_loss": ([_P, _I32, _I64, _I32, _F32, _P, _P, _P, _P, _P, _SZ, _P],
                            ctypes.c_int),
+    "bitlogic_top_logits": ([_P, _I32, _I64, _I32, _I64, _I32, _F32, _P, _P, _P, _P], ctypes.c_int),
+    "bitlogic_distill_loss": ([_P, _I32, _I64, _I32, _I64, _P, _P, _I32, _P, _P, _P, _F32, _F32, _F32, _P, _P, _P,
+                               _I64, _I64, _F32, _P], ctypes.c_int),
+    "bitlogic_sample_logits": ([_P, _I32, _I64, _I32, _I64, _P, _P, _P, _P, _P, _P, _P, _P], ctypes.c_int),
     "bitlogic_binarize_tables": ([_P, _I32, _I32, _P, _P], ctypes.c_int),
     "bitlogic_pack_bits": ([_P, _I64, _I32, _P, _I32, _P, _P], ctypes.c_int),
     "bitlogic_hard_forward": ([_P, _I32, _I64, _P, _P, _I32, _I32, _P, _I32, _P, _P, _P],
@@ -842,6 +854,114 @@ def bitlogic_head_loss_noalloc(Y: torch.Tensor, labels: torch.Tensor, C: int, ta
     _check("bitlogic_head_loss_noalloc", load().bitlogic_head_loss_noalloc(
         _ptr(Y), w, B, C, float(tau), _ptr(labels), _ptr(logits), _ptr(loss), _ptr(dY),
         _stream(stream)))
+
+
+def _logits(x: torch.Tensor, name: str) -> Tuple[int, int, int, int]:
+    """Type code, rows, classes and row stride of a matrix of logits whose
+    classes are adjacent (rows may lie apart)."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    code = LOGIT_TYPES.get(x.dtype)
+    if code is None:
+        raise TypeError(f"{name}: expected one of {[str(t) for t in LOGIT_TYPES]}, got {x.dtype}")
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be on a CUDA device")
+    if x.dim() != 2:
+        raise ValueError(f"{name}: expected [rows, classes], got {x.dim()} dimensions")
+    T, V = x.shape
+    ld, inc = x.stride()
+    if V > 1 and inc != 1:
+        raise ValueError(f"{name}: the classes of a row must be adjacent (stride 1)")
+    if T <= 1:
+        ld = max(ld, V)
+    return code, T, V, ld
+
+
+def bitlogic_top_logits(logits: torch.Tensor, val: torch.Tensor, idx: torch.Tensor,
+                        lse: Optional[torch.Tensor] = None, temperature: float = 1.0, stream=None):
+    """The K largest logits of every row of ``logits`` [T, V] (fp32, bf16, fp16
+    or int32 counts), equal ones by class: values into val fp32 [T, K], classes
+    into idx int32 [T, K], and the rows' log-sum-exp at ``temperature`` into lse
+    fp32 [T]: a teacher's record, as bitlogic_distill_loss reads it."""
+    code, T, V, ld = _logits(logits, "logits")
+    K = val.shape[-1] if isinstance(val, torch.Tensor) and val.dim() == 2 else 0
+    _need(val, "val", torch.float32, (T, K))
+    _need(idx, "idx", torch.int32, (T, K))
+    if lse is not None:
+        _need(lse, "lse", torch.float32, (T,))
+    _check("bitlogic_top_logits", load().bitlogic_top_logits(
+        _ptr(logits), code, T, V, ld, K, float(temperature), _ptr(val), _ptr(idx), _ptr(lse), _stream(stream)))
+
+
+def bitlogic_distill_loss(logits: torch.Tensor, teacher_val: torch.Tensor, teacher_idx: torch.Tensor,
+                          row_loss: torch.Tensor, loss: torch.Tensor, grad: Optional[torch.Tensor] = None,
+                          teacher_lse: Optional[torch.Tensor] = None, labels: Optional[torch.Tensor] = None,
+                          row_weight: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                          kd_weight: float = 1.0, ce_weight: float = 0.0, grad_scale: float = 1.0, stream=None):
+    """Loss of a student's ``logits`` [T, V] (fp32, bf16 or fp16) against a
+    teacher's record (teacher_val fp32, teacher_idx int32 [T, K], and with
+    teacher_lse fp32 [T] the teacher's remaining probability) and against labels
+    int32 [T]; the gradient at the logits into ``grad``, of the logits' type and
+    shape, in any strides that keep its elements apart (e.g. the transpose of
+    [V, T] gradient rows per class)."""
+    code, T, V, ld = _logits(logits, "logits")
+    K = teacher_val.shape[-1] if isinstance(teacher_val, torch.Tensor) and teacher_val.dim() == 2 else 0
+    _need(teacher_val, "teacher_val", torch.float32, (T, K))
+    _need(teacher_idx, "teacher_idx", torch.int32, (T, K))
+    _need(row_loss, "row_loss", torch.float32, (T,))
+    _need(loss, "loss", torch.float32, (1,))
+    if teacher_lse is not None:
+        _need(teacher_lse, "teacher_lse", torch.float32, (T,))
+    if labels is not None:
+        _need(labels, "labels", torch.int32, (T,))
+    if row_weight is not None:
+        _need(row_weight, "row_weight", torch.float32, (T,))
+    ldg = incg = 1
+    if grad is not None:
+        if not isinstance(grad, torch.Tensor):
+            raise TypeError("grad must be a torch.Tensor")
+        if grad.dtype != logits.dtype:
+            raise TypeError(f"grad: expected {logits.dtype}, got {grad.dtype}")
+        if not grad.is_cuda:
+            raise ValueError("grad must be on a CUDA device")
+        if grad.shape != logits.shape:
+            raise ValueError(f"grad: expected shape {tuple(logits.shape)}, got {tuple(grad.shape)}")
+        ldg, incg = grad.stride()
+        if V <= 1:
+            incg = 1
+        if T <= 1:
+            ldg = max(ldg, (V - 1) * incg + 1)
+    _check("bitlogic_distill_loss", load().bitlogic_distill_loss(
+        _ptr(logits), code, T, V, ld, _ptr(teacher_val), _ptr(teacher_idx), K, _ptr(teacher_lse), _ptr(labels),
+        _ptr(row_weight), float(temperature), float(kd_weight), float(ce_weight), _ptr(row_loss), _ptr(loss),
+        _ptr(grad), ldg, incg, float(grad_scale), _stream(stream)))
+
+
+def bitlogic_sample_logits(logits: torch.Tensor, u: torch.Tensor, token: torch.Tensor,
+                           logprob: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None,
+                           top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                           min_p: Optional[torch.Tensor] = None, stream=None):
+    """A class per row of ``logits`` [T, V] (fp32, bf16, fp16 or int32 counts)
+    drawn with the random numbers u fp32 [T] in [0, 1), into token int32 [T],
+    and the logarithm of its probability into logprob fp32 [T].  Per row, each
+    optional: temperature fp32 (0: the first of the largest), top_k int32 (0:
+    off), top_p fp32 (1: off), min_p fp32 (0: off)."""
+    code, T, V, ld = _logits(logits, "logits")
+    _need(u, "u", torch.float32, (T,))
+    _need(token, "token", torch.int32, (T,))
+    if logprob is not None:
+        _need(logprob, "logprob", torch.float32, (T,))
+    if temperature is not None:
+        _need(temperature, "temperature", torch.float32, (T,))
+    if top_k is not None:
+        _need(top_k, "top_k", torch.int32, (T,))
+    if top_p is not None:
+        _need(top_p, "top_p", torch.float32, (T,))
+    if min_p is not None:
+        _need(min_p, "min_p", torch.float32, (T,))
+    _check("bitlogic_sample_logits", load().bitlogic_sample_logits(
+        _ptr(logits), code, T, V, ld, _ptr(u), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+        _ptr(token), _ptr(logprob), _stream(stream)))
 
 
 def bitlogic_binarize_tables(theta: torch.Tensor, table: torch.Tensor, stream=None):

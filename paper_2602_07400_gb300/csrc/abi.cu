@@ -35,6 +35,7 @@ extern "C" int bitlogic_internal_index_error_lut_through(cudaStream_t);
 extern "C" int bitlogic_internal_index_error_lut_bytes(cudaStream_t);
 extern "C" int bitlogic_internal_index_error_lut_codes(cudaStream_t);
 extern "C" int bitlogic_internal_index_error_lut_packed(cudaStream_t);
+extern "C" int bitlogic_internal_index_error_distill(cudaStream_t);
 
 extern "C" const char* bitlogic_status_string(int code) {
     switch (code) {
@@ -42,15 +43,16 @@ extern "C" const char* bitlogic_status_string(int code) {
         case BITLOGIC_ERR_NULL: return "a required pointer is NULL";
         case BITLOGIC_ERR_SHAPE: return "invalid shape (size <= 0, overflow, grid limit, or w % C != 0)";
         case BITLOGIC_ERR_FANIN: return "unsupported fan-in (k must be 1..6 and <= w_in)";
-        case BITLOGIC_ERR_ALIGN: return "workspace is not 16-byte aligned";
+        case BITLOGIC_ERR_ALIGN: return "workspace is not 16-byte aligned, or an array not aligned as the call needs";
         case BITLOGIC_ERR_WORKSPACE: return "workspace too small";
         case BITLOGIC_ERR_CUDA: return "CUDA launch or copy failed";
         case BITLOGIC_ERR_INDEX: return "index out of range";
         case BITLOGIC_ERR_DEVICE: return "a kernel met an out-of-range index (read as 0)";
         case BITLOGIC_ERR_THRESH: return "number of thresholds must be 1..32";
         case BITLOGIC_ERR_TOO_LARGE: return "sizes exceed the fixed scratch of the allocation-free entry point";
-        case BITLOGIC_ERR_HYPER: return "optimizer hyperparameter out of range";
+        case BITLOGIC_ERR_HYPER: return "optimizer or loss hyperparameter out of range";
         case BITLOGIC_ERR_NODE: return "unknown node form";
+        case BITLOGIC_ERR_DTYPE: return "logit type unknown or not taken by the call";
         default: return "unknown status";
     }
 }
@@ -104,7 +106,7 @@ extern "C" int bitlogic_degree_order(const int32_t* off_host, int32_t n, int32_t
 
 extern "C" int bitlogic_device_error(cudaStream_t stream) {
     int worst = BITLOGIC_OK;
-    const int r[10] = {bitlogic_internal_index_error_lut_soft(stream),
+    const int r[11] = {bitlogic_internal_index_error_lut_soft(stream),
                       bitlogic_internal_index_error_head(stream),
                       bitlogic_internal_index_error_encode(stream),
                       bitlogic_internal_index_error_hard(stream),
@@ -113,7 +115,8 @@ extern "C" int bitlogic_device_error(cudaStream_t stream) {
                       bitlogic_internal_index_error_lut_through(stream),
                       bitlogic_internal_index_error_lut_bytes(stream),
                       bitlogic_internal_index_error_lut_codes(stream),
-                       bitlogic_internal_index_error_lut_packed(stream)};
+                       bitlogic_internal_index_error_lut_packed(stream),
+                      bitlogic_internal_index_error_distill(stream)};
     for (int v : r) {
         if (v == BITLOGIC_ERR_CUDA) return v;
         if (v != BITLOGIC_OK) worst = v;
