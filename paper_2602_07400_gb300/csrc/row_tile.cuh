@@ -1,0 +1,221 @@
+// A row of logits held in the shared memory of one block, or of the blocks of
+// one cluster, each a contiguous slice.
+//
+// Slices are cut at 16-byte boundaries of memory, not of the row, so rows of
+// any alignment are copied with 16-byte cp.async; the pieces that reach over
+// the row's ends are filled by element, with -inf in the places that are not
+// the row's.  Every pass then works on whole pieces.
+#pragma once
+
+#include "logits.cuh"
+
+namespace bitlogic {
+
+constexpr int kMaxCluster = 8;
+
+__device__ __forceinline__ unsigned cluster_rank() {
+    unsigned r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ unsigned cluster_size() {
+    unsigned r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+// The cluster's barrier; writes to another block's shared memory before the
+// arrival are visible after the wait.  Every thread of every block takes part.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// The address of `p` (this block's shared memory) in block `rank`, and a
+// store of 4 bytes there.
+__device__ __forceinline__ void store_in_block(const void* p, unsigned rank, uint32_t v) {
+    const unsigned s = (unsigned)__cvta_generic_to_shared(p);
+    asm volatile("{\n.reg .b32 a;\nmapa.shared::cluster.u32 a, %0, %1;\nst.shared::cluster.u32 [a], %2;\n}\n"
+                 ::"r"(s), "r"(rank), "r"(v) : "memory");
+}
+// A struct of 4-byte words to the same place in block `rank`.
+template <typename S>
+__device__ __forceinline__ void put_in_block(S* p, unsigned rank, const S& v) {
+    static_assert(sizeof(S) % 4 == 0, "whole words");
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(S) / 4); ++i) store_in_block(reinterpret_cast<uint32_t*>(p) + i, rank, w[i]);
+}
+
+// 16 bytes of logits: their number, their values, their maximum, and the
+// rounding of values back into a piece.
+template <typename T> struct Piece;
+
+template <> struct Piece<float> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ void load(const uint4& u, float (&z)[4]) {
+        z[0] = __uint_as_float(u.x);
+        z[1] = __uint_as_float(u.y);
+        z[2] = __uint_as_float(u.z);
+        z[3] = __uint_as_float(u.w);
+    }
+    static __device__ __forceinline__ uint4 pack(const float (&g)[4]) {
+        return make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
+    }
+    using Max = float;
+    static __device__ __forceinline__ Max lowest() { return BITLOGIC_NEG_INF; }
+    static __device__ __forceinline__ Max largest(Max m, const uint4& u) {
+        return fmaxf(fmaxf(m, fmaxf(__uint_as_float(u.x), __uint_as_float(u.y))),
+                     fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
+    }
+    static __device__ __forceinline__ float value(Max m) { return m; }
+};
+template <> struct Piece<int> {
+    static constexpr int N = 4;
+    static __device__ __forceinline__ void load(const uint4& u, float (&z)[4]) {
+        z[0] = logit_value((int)u.x);
+        z[1] = logit_value((int)u.y);
+        z[2] = logit_value((int)u.z);
+        z[3] = logit_value((int)u.w);
+    }
+    using Max = int;
+    static __device__ __forceinline__ Max lowest() { return INT_MIN; }
+    static __device__ __forceinline__ Max largest(Max m, const uint4& u) {
+        return max(max(m, max((int)u.x, (int)u.y)), max((int)u.z, (int)u.w));
+    }
+    static __device__ __forceinline__ float value(Max m) { return logit_value(m); }
+};
+template <> struct Piece<__nv_bfloat16> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ void two(uint32_t u, float& a, float& b) {
+        a = __uint_as_float(u << 16);
+        b = __uint_as_float(u & 0xffff0000u);
+    }
+    static __device__ __forceinline__ void load(const uint4& u, float (&z)[8]) {
+        two(u.x, z[0], z[1]);
+        two(u.y, z[2], z[3]);
+        two(u.z, z[4], z[5]);
+        two(u.w, z[6], z[7]);
+    }
+    static __device__ __forceinline__ uint32_t pair(float a, float b) {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&p);
+    }
+    static __device__ __forceinline__ uint4 pack(const float (&g)[8]) {
+        return make_uint4(pair(g[0], g[1]), pair(g[2], g[3]), pair(g[4], g[5]), pair(g[6], g[7]));
+    }
+    using Max = __nv_bfloat162;
+    static __device__ __forceinline__ Max as(uint32_t u) { return *reinterpret_cast<const Max*>(&u); }
+    static __device__ __forceinline__ Max lowest() { return as(0xff80ff80u); }
+    static __device__ __forceinline__ Max largest(Max m, const uint4& u) {   // of two numbers: NaN is passed over
+        return __hmax2(__hmax2(m, __hmax2(as(u.x), as(u.y))), __hmax2(as(u.z), as(u.w)));
+    }
+    static __device__ __forceinline__ float value(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
+};
+template <> struct Piece<__half> {
+    static constexpr int N = 8;
+    static __device__ __forceinline__ __half2 as(uint32_t u) { return *reinterpret_cast<const __half2*>(&u); }
+    static __device__ __forceinline__ void load(const uint4& u, float (&z)[8]) {
+        const float2 a = __half22float2(as(u.x)), b = __half22float2(as(u.y)), c = __half22float2(as(u.z)),
+                     d = __half22float2(as(u.w));
+        z[0] = a.x; z[1] = a.y; z[2] = b.x; z[3] = b.y;
+        z[4] = c.x; z[5] = c.y; z[6] = d.x; z[7] = d.y;
+    }
+    static __device__ __forceinline__ uint32_t pair(float a, float b) {
+        const __half2 p = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&p);
+    }
+    static __device__ __forceinline__ uint4 pack(const float (&g)[8]) {
+        return make_uint4(pair(g[0], g[1]), pair(g[2], g[3]), pair(g[4], g[5]), pair(g[6], g[7]));
+    }
+    using Max = __half2;
+    static __device__ __forceinline__ Max lowest() { return as(0xfc00fc00u); }
+    static __device__ __forceinline__ Max largest(Max m, const uint4& u) {
+        return __hmax2(__hmax2(m, __hmax2(as(u.x), as(u.y))), __hmax2(as(u.z), as(u.w)));
+    }
+    static __device__ __forceinline__ float value(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
+};
+
+template <typename T> __device__ __forceinline__ T masked_logit();
+template <> __device__ __forceinline__ float masked_logit<float>() { return BITLOGIC_NEG_INF; }
+template <> __device__ __forceinline__ int masked_logit<int>() { return INT_MIN; }
+template <> __device__ __forceinline__ __nv_bfloat16 masked_logit<__nv_bfloat16>() { return __ushort_as_bfloat16(0xff80); }
+template <> __device__ __forceinline__ __half masked_logit<__half>() { return __ushort_as_half(0xfc00); }
+
+// A block's slice: pieces [0, n), piece j holding classes first + N j + i.
+template <typename T>
+struct RowSlice {
+    static constexpr int N = Piece<T>::N;
+    int first;   // class of the first place (below 0 where the row starts inside the piece)
+    int n;
+
+    __device__ __forceinline__ RowSlice(const T* x, int V, unsigned rank, unsigned blocks) {
+        const int shift = (int)((reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(T));
+        const int all = (shift + V + N - 1) / N, per = (all + (int)blocks - 1) / (int)blocks;
+        const int p0 = min(all, (int)rank * per);
+        n = min(all, p0 + per) - p0;
+        first = p0 * N - shift;
+    }
+    // Copies on their way; finish with cp_async_wait<0>() and a barrier.
+    __device__ __forceinline__ void copy(const T* x, int V, T* tile, int tid, int threads) const {
+        for (int j = tid; j < n; j += threads) {
+            const int v = first + j * N;
+            if (v >= 0 && v + N <= V) {
+                cp_async16(tile + j * N, x + v);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) tile[j * N + i] = v + i >= 0 && v + i < V ? x[v + i] : masked_logit<T>();
+            }
+        }
+        cp_async_commit();
+    }
+    // Place of class v in the slice, or -1.
+    __device__ __forceinline__ int place(int v) const {
+        const int p = v - first;
+        return v >= 0 && p >= 0 && p < n * N ? p : -1;
+    }
+};
+
+// Bytes of the longest slice of a row of V classes over `blocks` blocks, for
+// any alignment of the row.
+inline long long slice_bytes(long long V, int element, int blocks) {
+    const long long N = 16 / element, all = (N - 1 + V + N - 1) / N;
+    return (all + blocks - 1) / blocks * 16;
+}
+
+// Blocks per row: as many as the row needs for slices of `fit` bytes (so that
+// several blocks share an SM and one loads while another computes), and with
+// few rows as many as keep every SM busy on slices of at least `least` bytes.
+// 0: the row does not fit slices of `most` bytes.
+inline int blocks_per_row(long long T, long long V, int element, long long fit, long long most, long long least) {
+    int c = 1;
+    while (c < kMaxCluster && slice_bytes(V, element, c) > fit) c *= 2;
+    if (slice_bytes(V, element, c) > most) return 0;
+    while (c < kMaxCluster && T * c * 2 <= sm_count() && slice_bytes(V, element, 2 * c) >= least) c *= 2;
+    return c;
+}
+
+// Launch of a kernel over T rows with `blocks` blocks (one cluster) per row,
+// as a programmatic dependent launch (see launch_dependent).
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_rows(void (*kernel)(KArgs...), long long T, int blocks, int threads, size_t smem,
+                               cudaStream_t stream, Args... args) {
+    if (smem > 40 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(T * blocks));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)blocks;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = blocks > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+}  // namespace bitlogic
