@@ -44,6 +44,53 @@ __device__ __forceinline__ void put_in_block(S* p, unsigned rank, const S& v) {
     for (int i = 0; i < (int)(sizeof(S) / 4); ++i) store_in_block(reinterpret_cast<uint32_t*>(p) + i, rank, w[i]);
 }
 
+// Adds v to a counter in block `rank` and returns what it held.
+__device__ __forceinline__ unsigned add_in_block(unsigned* p, unsigned rank, unsigned v) {
+    const unsigned s = (unsigned)__cvta_generic_to_shared(p);
+    unsigned r;
+    asm volatile("{\n.reg .b32 a;\nmapa.shared::cluster.u32 a, %1, %2;\natom.shared::cluster.add.u32 %0, [a], %3;\n}\n"
+                 : "=r"(r) : "r"(s), "r"(rank), "r"(v) : "memory");
+    return r;
+}
+
+// Sorts a[0, size) in falling order, size a power of two (bitonic exchanges);
+// called by the whole block.
+__device__ __forceinline__ void block_sort_falling(unsigned long long* a, int size) {
+    for (int k = 2; k <= size; k <<= 1)
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < size / 2; i += blockDim.x) {
+                const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
+                const unsigned long long x = a[lo], y = a[hi];
+                if ((x < y) == ((lo & k) == 0)) {
+                    a[lo] = y;
+                    a[hi] = x;
+                }
+            }
+        }
+    __syncthreads();
+}
+
+// The logit of a key.
+__device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k ^ 0x80000000u) : ~k); }
+
+// A lower bound of the `need` largest of the values that the warp's lanes hold
+// two of each: the largest key of 16 leading bits that at least `need` of the
+// 64 reach (0 when fewer rank).
+__device__ __forceinline__ uint32_t warp_bound(float a, float b, int need) {
+    const uint32_t ka = logit_key(a) >> 16, kb = logit_key(b) >> 16;
+    uint32_t t = 0;
+#pragma unroll
+    for (uint32_t bit = 0x8000u; bit > 0; bit >>= 1) {
+        const uint32_t c = t | bit;
+        const int n = __popc(__ballot_sync(0xffffffffu, ka >= c)) + __popc(__ballot_sync(0xffffffffu, kb >= c));
+        if (n >= need) t = c;
+    }
+    return t << 16;
+}
+// The smallest logit that such a bound lets through.
+__device__ __forceinline__ float bound_logit(uint32_t key) { return key <= kKeyNegInf ? BITLOGIC_NEG_INF : key_logit(key); }
+
 // 16 bytes of logits: their number, their values, their maximum, and the
 // rounding of values back into a piece.
 template <typename T> struct Piece;
@@ -66,6 +113,7 @@ template <> struct Piece<float> {
                      fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
     }
     static __device__ __forceinline__ float value(Max m) { return m; }
+    static __device__ __forceinline__ float largest_of(const uint4& u) { return largest(__uint_as_float(u.x), u); }
 };
 template <> struct Piece<int> {
     static constexpr int N = 4;
@@ -81,6 +129,7 @@ template <> struct Piece<int> {
         return max(max(m, max((int)u.x, (int)u.y)), max((int)u.z, (int)u.w));
     }
     static __device__ __forceinline__ float value(Max m) { return logit_value(m); }
+    static __device__ __forceinline__ float largest_of(const uint4& u) { return value(largest((int)u.x, u)); }
 };
 template <> struct Piece<__nv_bfloat16> {
     static constexpr int N = 8;
@@ -108,6 +157,7 @@ template <> struct Piece<__nv_bfloat16> {
         return __hmax2(__hmax2(m, __hmax2(as(u.x), as(u.y))), __hmax2(as(u.z), as(u.w)));
     }
     static __device__ __forceinline__ float value(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
+    static __device__ __forceinline__ float largest_of(const uint4& u) { return value(largest(as(u.x), u)); }
 };
 template <> struct Piece<__half> {
     static constexpr int N = 8;
@@ -131,6 +181,7 @@ template <> struct Piece<__half> {
         return __hmax2(__hmax2(m, __hmax2(as(u.x), as(u.y))), __hmax2(as(u.z), as(u.w)));
     }
     static __device__ __forceinline__ float value(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
+    static __device__ __forceinline__ float largest_of(const uint4& u) { return value(largest(as(u.x), u)); }
 };
 
 template <typename T> __device__ __forceinline__ T masked_logit();
@@ -197,7 +248,7 @@ inline int blocks_per_row(long long T, long long V, int element, long long fit, 
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_rows(void (*kernel)(KArgs...), long long T, int blocks, int threads, size_t smem,
                                cudaStream_t stream, Args... args) {
-    if (smem > 40 * 1024) {
+    if (smem > 12 * 1024) {   // with the kernels' own arrays perhaps past the 48 KB that need no leave
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
