@@ -13,12 +13,12 @@
 // threads or the order of additions.  Bound by reading the logits once.
 #include <cfloat>
 
-#include "logits.cuh"
+#include "row_tile.cuh"
 
 namespace bitlogic {
 namespace {
 
-constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32;
+constexpr int kSampleThreads = 256, kSampleWarps = kSampleThreads / 32;
 constexpr uint32_t kNoCut = 0u;   // every key of a class with a weight lies above
 
 struct Settings {
@@ -28,102 +28,154 @@ struct Settings {
     const float* top_p;
     const float* min_p;
 };
+struct Draw {
+    int* token;
+    float* logprob;
+};
 
-// One block per row, any V: the row is read from memory in every pass.
+// A row's settings as the draw uses them.
+struct RowSettings {
+    float u, temp, p, floor_e;
+    int k;
+
+    __device__ __forceinline__ RowSettings(const Settings& s, long long row, int V) {
+        temp = s.temperature ? s.temperature[row] : 1.0f;
+        k = s.top_k ? s.top_k[row] : 0;
+        if (k <= 0 || k > V) k = V;
+        p = s.top_p ? s.top_p[row] : 1.0f;
+        p = p < 1.0f ? fmaxf(p, 0.f) : 1.0f;
+        floor_e = s.min_p ? s.min_p[row] : 0.0f;
+        floor_e = floor_e > 0.f ? fminf(floor_e, 1.0f) : 0.f;
+        u = s.u[row];
+        u = u > 0.f ? fminf(u, 0.99999994f) : 0.f;
+    }
+};
+
+// e_v about the row's largest logit.  A temperature that is not positive, or a
+// largest logit of +inf, leaves the first of the largest: k = 1.
+struct Power {
+    float m, slope;
+    __device__ __forceinline__ Power(float largest, RowSettings& set) {
+        slope = 0.f;
+        if (set.temp > 0.f && !isinf(largest)) slope = fminf((1.0f / set.temp) * kLog2E, FLT_MAX);
+        else set.k = 1;
+        m = isinf(largest) ? 0.f : largest;
+    }
+    // for a logit that ranks
+    __device__ __forceinline__ float operator()(float z) const { return exp2_unit((isinf(z) ? 0.f : z - m) * slope); }
+    // for any but +inf: 0 for -inf and NaN (0 slope included)
+    __device__ __forceinline__ float of(float z) const {
+        return z > BITLOGIC_NEG_INF ? exp2_unit((z - m) * slope) : 0.f;
+    }
+};
+
+// A sum of weights w = rint(2^40 e), 0 <= e <= 1, of at most 512 of them, in
+// fp32 and 32-bit integer operations: 32 + e rounds e to a multiple of 2^-18,
+// the remainder is exact, and 1.5 2^23 + 2^40 remainder rounds it to a whole
+// number as rint does.
+struct WeightSum {
+    uint32_t high = 0;
+    int low = 0;
+    __device__ __forceinline__ void add(float e) {
+        const float t = e + 32.0f, r = e - (t - 32.0f);
+        const float u = fmaf(r, 1099511627776.0f, 12582912.0f);
+        high += __float_as_uint(t) - 0x42000000u;
+        low += (int)(__float_as_uint(u) - 0x4b400000u);
+    }
+    __device__ __forceinline__ unsigned long long total() const {
+        return ((unsigned long long)high << 22) + (unsigned long long)(long long)low;
+    }
+};
+
+struct StreamScratch {
+    SelectScratch select;
+    float fbuf[kSampleWarps];
+    unsigned long long mass[kSampleWarps], ties[kSampleWarps];
+};
+
+__device__ __forceinline__ unsigned long long block_max(unsigned long long v, unsigned long long* buf) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const unsigned long long t = shuffle_xor(v, o);
+        v = t > v ? t : v;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+    __syncthreads();
+    for (int w = 0; w < kSampleWarps; ++w) v = buf[w] > v ? buf[w] : v;
+    return v;
+}
+
+// The inclusive sums of v over the lanes of a warp.
+__device__ __forceinline__ unsigned long long warp_upto(unsigned long long v, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long t = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += t;
+    }
+    return v;
+}
+
+// The draw of a row read from memory in every pass, for any row and settings.
+// Called by the whole block.
 template <typename T>
-__global__ void __launch_bounds__(kSampleThreads)
-sample_stream_kernel(const T* __restrict__ X, long long ld, int V, Settings set, int* __restrict__ token,
-                     float* __restrict__ logprob) {
-    __shared__ SelectScratch sc;
-    __shared__ float fbuf[kSampleWarps];
-    __shared__ unsigned long long mbuf[kSampleWarps], tbuf[kSampleWarps];
-    const long long row = blockIdx.x;
-    const T* x = X + row * ld;
+__device__ void sample_of_stream(const T* __restrict__ x, int V, RowSettings set, long long row, const Draw& out,
+                                 StreamScratch* sc) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    float temp = set.temperature ? set.temperature[row] : 1.0f;
-    int k = set.top_k ? set.top_k[row] : 0;
-    const float p = set.top_p ? set.top_p[row] : 1.0f;
-    float floor_e = set.min_p ? set.min_p[row] : 0.0f, u = set.u[row];
-    floor_e = floor_e > 0.f ? fminf(floor_e, 1.0f) : 0.f;
-    u = u > 0.f ? fminf(u, 0.99999994f) : 0.f;
     float m = BITLOGIC_NEG_INF;
     for (int v = tid; v < V; v += kSampleThreads) m = fmaxf(m, logit_value(x[v]));
-    m = block_largest(m, fbuf, kSampleWarps);
+    m = block_largest(m, sc->fbuf, kSampleWarps);
     if (m == BITLOGIC_NEG_INF) {   // nothing to draw from
         if (tid == 0) {
-            token[row] = -1;
-            if (logprob) logprob[row] = BITLOGIC_NEG_INF;
+            out.token[row] = -1;
+            if (out.logprob) out.logprob[row] = BITLOGIC_NEG_INF;
         }
         return;
     }
-    float slope = 0.f;
-    if (temp > 0.f && !isinf(m)) slope = fminf((1.0f / temp) * kLog2E, FLT_MAX);
-    else k = 1;   // the first of the largest
-    const float ms = isinf(m) ? 0.f : m;
+    const Power power(m, set);
     auto key_at = [&](int v) { return logit_key(logit_value(x[v])); };
     auto share = [&](int v) {   // e_v; 0 for what does not rank
         const float z = logit_value(x[v]);
-        return z > BITLOGIC_NEG_INF ? exp2_unit((isinf(z) ? 0.f : z - ms) * slope) : 0.f;
+        return z > BITLOGIC_NEG_INF ? power(z) : 0.f;
     };
     Cut cut = {kNoCut, 0};
     unsigned long long above;
-    if (k > 0 && k < V) {
+    if (set.k < V) {
         unsigned long long n = 0;
         for (int v = tid; v < V; v += kSampleThreads) n += ranks(key_at(v));
-        n = block_add(n, mbuf, kSampleWarps);
-        if ((unsigned long long)k < n) {
-            cut.key = select_key(key_at, [](int, uint32_t kk) { return ranks(kk) ? 1ull : 0ull; }, V, k, &sc, &above);
-            cut.ties = k - above;
+        n = block_add(n, sc->mass, kSampleWarps);
+        if ((unsigned long long)set.k < n) {
+            cut.key = select_key(key_at, [](int, uint32_t kk) { return ranks(kk) ? 1ull : 0ull; }, V, set.k, &sc->select, &above);
+            cut.ties = set.k - above;
         }
     }
-    if (p < 1.0f) {
+    if (set.p < 1.0f) {
         const uint32_t kt = cut.key;
-        unsigned long long mass = 0, we = 0;   // above the cut; the weight of a class at it
-        for (int v = tid; v < V; v += kSampleThreads) {
-            const uint32_t kk = key_at(v);
-            if (kk > kt) mass += draw_weight(share(v));
-            else if (kk == kt && cut.ties) we = draw_weight(share(v));
-        }
-        mass = block_add(mass, mbuf, kSampleWarps);
-        for (int o = 16; o > 0; o >>= 1) {
-            const unsigned long long t = shuffle_xor(we, o);
-            we = t > we ? t : we;
-        }
-        __syncthreads();
-        if (lane == 0) tbuf[warp] = we;
-        __syncthreads();
-        for (int w = 0; w < kSampleWarps; ++w) we = tbuf[w] > we ? tbuf[w] : we;
-        unsigned long long want = share_of(mass + cut.ties * we, fmaxf(p, 0.f));
+        unsigned long long mass = 0;   // above the cut
+        for (int v = tid; v < V; v += kSampleThreads)
+            if (key_at(v) > kt) mass += draw_weight(share(v));
+        mass = block_add(mass, sc->mass, kSampleWarps);
+        const unsigned long long we = cut.ties ? draw_weight(power(key_logit(kt))) : 0ull;
+        unsigned long long want = share_of(mass + cut.ties * we, set.p);
         if (want < 1) want = 1;
         if (want > mass) {   // reached among the ties of the top-k cut
             const unsigned long long need = we ? (want - mass + we - 1) / we : cut.ties;
             if (need < cut.ties) cut.ties = need;
         } else {
-            const uint32_t t = select_key(key_at, [&](int v, uint32_t kk) { return kk > kt ? draw_weight(share(v)) : 0ull; },
-                                          V, want, &sc, &above);
-            unsigned long long wt = 0;
-            for (int v = tid; v < V; v += kSampleThreads)
-                if (key_at(v) == t) wt = draw_weight(share(v));
-            for (int o = 16; o > 0; o >>= 1) {
-                const unsigned long long q = shuffle_xor(wt, o);
-                wt = q > wt ? q : wt;
-            }
-            __syncthreads();
-            if (lane == 0) tbuf[warp] = wt;
-            __syncthreads();
-            for (int w = 0; w < kSampleWarps; ++w) wt = tbuf[w] > wt ? tbuf[w] : wt;
-            cut.key = t;
+            cut.key = select_key(key_at, [&](int v, uint32_t kk) { return kk > kt ? draw_weight(share(v)) : 0ull; }, V, want,
+                                 &sc->select, &above);
+            const unsigned long long wt = draw_weight(power(key_logit(cut.key)));
             cut.ties = wt ? (want - above + wt - 1) / wt : 1;
         }
     }
     // every warp a contiguous part of the row: its weight above the cut, and its ties
-    const int part = (V + kSampleWarps - 1) / kSampleWarps, v0 = warp * part, v1 = min(V, v0 + part);
+    const int part = (V + kSampleWarps - 1) / kSampleWarps, v0 = min(V, warp * part), v1 = min(V, v0 + part);
     unsigned long long mass = 0, eq = 0;
     for (int v = v0 + lane; v < v1; v += 32) {
         const uint32_t kk = key_at(v);
         if (kk > cut.key) {
             const float e = share(v);
-            if (e >= floor_e) mass += draw_weight(e);
+            if (e >= set.floor_e) mass += draw_weight(e);
         } else if (kk == cut.key && cut.ties) {
             ++eq;
         }
@@ -132,18 +184,15 @@ sample_stream_kernel(const T* __restrict__ X, long long ld, int V, Settings set,
     eq = warp_add(eq);
     __syncthreads();
     if (lane == 0) {
-        mbuf[warp] = mass;
-        tbuf[warp] = eq;
+        sc->mass[warp] = mass;
+        sc->ties[warp] = eq;
     }
     __syncthreads();
     // weight of a tie: the same for all of them
     unsigned long long wt = 0;
     if (cut.ties) {
-        uint32_t kb = cut.key;
-        kb = (kb & 0x80000000u) ? (kb ^ 0x80000000u) : ~kb;
-        const float z = __uint_as_float(kb);
-        const float e = exp2_unit((isinf(z) ? 0.f : z - ms) * slope);
-        wt = e >= floor_e ? draw_weight(e) : 0ull;
+        const float e = power(key_logit(cut.key));
+        wt = e >= set.floor_e ? draw_weight(e) : 0ull;
     }
     unsigned long long total = 0, before = 0, left = cut.ties, my_left = 0;
     for (int w = 0; w < kSampleWarps; ++w) {
@@ -151,11 +200,11 @@ sample_stream_kernel(const T* __restrict__ X, long long ld, int V, Settings set,
             before = total;
             my_left = left;
         }
-        const unsigned long long q = tbuf[w] < left ? tbuf[w] : left;
-        total += mbuf[w] + q * wt;
+        const unsigned long long q = sc->ties[w] < left ? sc->ties[w] : left;
+        total += sc->mass[w] + q * wt;
         left -= q;
     }
-    const unsigned long long target = share_of(total, u);
+    const unsigned long long target = share_of(total, set.u);
     const unsigned long long mine = mass + (eq < my_left ? eq : my_left) * wt;
     if (target < before || target >= before + mine) return;
     // the warp that holds the class: 32 classes at a time, in order
@@ -168,20 +217,16 @@ sample_stream_kernel(const T* __restrict__ X, long long ld, int V, Settings set,
         unsigned long long w = 0;
         if (v < v1 && kk > cut.key) {
             const float e = share(v);
-            if (e >= floor_e) w = draw_weight(e);
+            if (e >= set.floor_e) w = draw_weight(e);
         } else if (same && __popc(mask & ((1u << lane) - 1u)) < my_left) {
             w = wt;
         }
-        unsigned long long upto = w;
-        for (int o = 1; o < 32; o <<= 1) {
-            const unsigned long long t = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += t;
-        }
+        const unsigned long long upto = warp_upto(w, lane);
         const unsigned hit = __ballot_sync(0xffffffffu, run + upto > target);
         if (hit) {
             if (lane == __ffs(hit) - 1) {
-                token[row] = v;
-                if (logprob) logprob[row] = logf((float)w / (float)total);
+                out.token[row] = v;
+                if (out.logprob) out.logprob[row] = logf((float)w / (float)total);
             }
             return;
         }
@@ -189,6 +234,719 @@ sample_stream_kernel(const T* __restrict__ X, long long ld, int V, Settings set,
         const unsigned used = __popc(mask);
         my_left = my_left > used ? my_left - used : 0;
     }
+}
+
+// Rows too long for the shared memory of a cluster.
+template <typename T>
+__global__ void __launch_bounds__(kSampleThreads)
+sample_stream_kernel(const T* __restrict__ X, long long ld, int V, Settings set, Draw out) {
+    __shared__ StreamScratch sc;
+    grid_dependency_wait();
+    allow_dependent_launch();
+    const long long row = blockIdx.x;
+    sample_of_stream(X + row * ld, V, RowSettings(set, row, V), row, out, &sc);
+}
+
+// ------------------------------------------------------------ rows on chip --
+
+constexpr int kList = 2048;       // entries that a cut or a draw looks at in the end
+constexpr int kListTop = 1024;    // largest top_k that goes by the list
+constexpr int kBinsPerOctave = 64, kBins = 42 * kBinsPerOctave;   // weights below 2^-41 are 0
+
+struct SampleShared {
+    union {
+        unsigned long long list[kList];   // key << 32 | ~class, of the row, in the first block
+        StreamScratch stream;
+    };
+    union {
+        unsigned long long local[kList];  // of the slice
+        unsigned bins[kBins];             // mass of the slice by the power's exponent
+        struct {
+            unsigned long long sums[kSampleWarps];
+        } scan;
+    };
+    struct Stats {
+        float m;
+        uint32_t bound;
+    } stats[kMaxCluster];
+    struct Sums {
+        unsigned long long mass;
+        unsigned ties, pad;
+    } sums[kMaxCluster];
+    unsigned long long warp_mass[kSampleWarps];
+    unsigned warp_ties[kSampleWarps];
+    float fbuf[kSampleWarps];
+    uint32_t bounds[kSampleWarps];
+    struct Found {
+        uint32_t key;
+        unsigned ties, slow, pad;
+    } found;
+    int bin;
+    unsigned n_list, n_local, base;
+};
+
+// Bin of a power's exponent y = (m - z) slope >= 0, and a bin's unit of mass: a
+// power in bin b counts e 2^(15 + b / 64) units (2^14 to 2^15 of them), so
+// that a bin sums in 32 bits and is right to 2^-15.
+__device__ __forceinline__ int bin_of(float y) { return (int)fminf(y * kBinsPerOctave, (float)(kBins - 1)); }
+__device__ __forceinline__ unsigned bin_units(float e, int b) {
+    return (unsigned)__float2uint_rn(e * __uint_as_float((unsigned)(127 + 15 + b / kBinsPerOctave) << 23));
+}
+__device__ __forceinline__ float bin_mass(unsigned units, int b) {
+    return (float)units * __uint_as_float((unsigned)(127 - 15 - b / kBinsPerOctave) << 23);
+}
+
+// The sum of v over the block's threads before this one, and over all of them.
+__device__ __forceinline__ unsigned long long block_before(unsigned long long v, unsigned long long* buf,
+                                                           unsigned long long* all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const unsigned long long upto = warp_upto(v, lane);
+    __syncthreads();
+    if (lane == 31) buf[warp] = upto;
+    __syncthreads();
+    unsigned long long before = 0, t = 0;
+    for (int w = 0; w < kSampleWarps; ++w) {
+        if (w == warp) before = t;
+        t += buf[w];
+    }
+    *all = t;
+    return before + upto - v;
+}
+
+__device__ __forceinline__ int power_of_two(unsigned n) { return n <= 32 ? 32 : 1 << (32 - __clz(n - 1)); }
+
+// The first block's work where the row's first k classes are all on its list:
+// the cut by rank and mass on the sorted list, then the draw among the kept
+// sorted by class.
+__device__ void sample_of_list(SampleShared* s, unsigned n, const RowSettings& set, const Power& power, long long row,
+                               const Draw& out) {
+    constexpr int kPer = kListTop / kSampleThreads;
+    const int tid = threadIdx.x;
+    const int size = power_of_two(n);
+    for (int i = n + tid; i < size; i += kSampleThreads) s->list[i] = 0ull;
+    block_sort_falling(s->list, size);
+    const int k = min((int)n, set.k);   // at most kListTop
+    unsigned long long w[kPer], sum = 0, all;
+    float e[kPer];
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+        const int i = tid * kPer + q;
+        e[q] = i < k ? power(key_logit((uint32_t)(s->list[i] >> 32))) : 0.f;
+        w[q] = i < k ? draw_weight(e[q]) : 0ull;
+        sum += w[q];
+    }
+    unsigned long long before = block_before(sum, s->scan.sums, &all);
+    unsigned long long want = set.p < 1.0f ? share_of(all, set.p) : all;
+    if (want < 1) want = 1;
+    int kept = 0;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+        const int i = tid * kPer + q;
+        if (i < k && (set.p >= 1.0f || before < want)) kept = i + 1;
+        before += w[q];
+    }
+    // the kept are a run from the front: its length
+    for (int o = 16; o > 0; o >>= 1) kept = max(kept, __shfl_xor_sync(0xffffffffu, kept, o));
+    __syncthreads();
+    if ((tid & 31) == 0) s->bounds[tid >> 5] = kept;
+    __syncthreads();
+    for (int v = 0; v < kSampleWarps; ++v) kept = max(kept, (int)s->bounds[v]);
+    // by class: ~class << 32 | key falls as the class rises
+    const int size2 = power_of_two(kept);
+    for (int i = tid; i < size2; i += kSampleThreads) {
+        const unsigned long long x = s->list[i];
+        s->list[i] = i < kept ? (x << 32) | (x >> 32) : 0ull;
+    }
+    block_sort_falling(s->list, size2);
+    sum = 0;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+        const int i = tid * kPer + q;
+        w[q] = 0ull;
+        if (i < kept) {
+            const float p = power(key_logit((uint32_t)s->list[i]));
+            if (p >= set.floor_e) w[q] = draw_weight(p);
+        }
+        sum += w[q];
+    }
+    before = block_before(sum, s->scan.sums, &all);
+    const unsigned long long target = share_of(all, set.u);
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+        if (target >= before && target < before + w[q]) {
+            out.token[row] = (int)~(uint32_t)(s->list[tid * kPer + q] >> 32);
+            if (out.logprob) out.logprob[row] = logf((float)w[q] / (float)all);
+        }
+        before += w[q];
+    }
+}
+
+// A row in the shared memory of one block or one cluster.  What it does past
+// the row's largest logit goes by the row's settings, alike in all its blocks:
+//   top_k up to 1024 (and greedy rows): the classes that pass a bound which at
+//     least k reach go to the first block, which cuts and draws among them;
+//   top_p alone: the weights by bins of 1/64 octave show where the mass is
+//     reached; the three bins around it go to the first block, which finds the
+//     cut to the class with exact sums; then every block sums its kept weights
+//     in the order of classes and the one that holds the draw finds it;
+//   neither: the last step alone.
+// A larger top_k, and a list that overflows (long runs of equal logits), are
+// drawn from memory by the first block.
+template <typename T>
+__global__ void __launch_bounds__(kSampleThreads)
+sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settings, Draw out) {
+    using P = Piece<T>;
+    extern __shared__ __align__(16) unsigned char raw[];
+    T* tile = reinterpret_cast<T*>(raw);
+    const uint4* tile16 = reinterpret_cast<const uint4*>(raw);
+    __shared__ SampleShared s;
+    grid_dependency_wait();
+    allow_dependent_launch();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const unsigned rank = cluster_rank(), blocks = cluster_size();
+    const long long row = blockIdx.x / blocks;
+    const T* x = X + row * ld;
+    const RowSlice<T> slice(x, V, rank, blocks);
+    slice.copy(x, V, tile, tid, kSampleThreads);
+    RowSettings set(settings, row, V);
+    auto row_barrier = [&]() {
+        if (blocks > 1) {
+            cluster_arrive();
+            cluster_wait();
+        } else {
+            __syncthreads();
+        }
+    };
+    if (tid == 0) s.n_list = s.n_local = 0;
+    cp_async_wait<0>();
+    __syncthreads();
+
+    // the largest, and a bound that the first k reach
+    const int k_asked = set.temp > 0.f ? set.k : 1;
+    typename P::Max ma = P::lowest(), mb = P::lowest();
+#pragma unroll 4
+    for (int j = tid; j < slice.n; j += 2 * kSampleThreads) {
+        ma = P::largest(ma, tile16[j]);
+        if (j + kSampleThreads < slice.n) mb = P::largest(mb, tile16[j + kSampleThreads]);
+    }
+    const float za = P::value(ma), zb = P::value(mb);
+    const int need = (k_asked + (int)blocks * kSampleWarps - 1) / ((int)blocks * kSampleWarps);
+    const uint32_t wb = need <= 64 ? warp_bound(za, zb, need) : 0u;
+    const float wm = warp_largest(fmaxf(za, zb));
+    if (lane == 0) {
+        s.fbuf[warp] = wm;
+        s.bounds[warp] = wb;
+    }
+    __syncthreads();
+    if (tid < (int)blocks) {
+        SampleShared::Stats st = {s.fbuf[0], s.bounds[0]};
+        for (int w = 1; w < kSampleWarps; ++w) {
+            st.m = fmaxf(st.m, s.fbuf[w]);
+            st.bound = min(st.bound, s.bounds[w]);
+        }
+        put_in_block(&s.stats[rank], tid, st);
+    }
+    row_barrier();
+    float m = s.stats[0].m;
+    uint32_t bound = s.stats[0].bound;
+    for (unsigned b = 1; b < blocks; ++b) {
+        m = fmaxf(m, s.stats[b].m);
+        bound = min(bound, s.stats[b].bound);
+    }
+    if (m == BITLOGIC_NEG_INF) {   // nothing to draw from
+        if (rank == 0 && tid == 0) {
+            out.token[row] = -1;
+            if (out.logprob) out.logprob[row] = BITLOGIC_NEG_INF;
+        }
+        return;
+    }
+    const Power power(m, set);
+    if (set.k == 1 && k_asked != 1) bound = 0xff800000u;   // a largest of +inf: nothing below it is needed
+
+    // entries of the slice with zmin <= z <= zmax to the first block's list
+    auto list_slice = [&](float zmin, float zmax) {
+        for (int j = tid; j < slice.n; j += kSampleThreads) {
+            const uint4 u = tile16[j];
+            if (P::largest_of(u) >= zmin) {
+                float z[P::N];
+                P::load(u, z);
+#pragma unroll
+                for (int i = 0; i < P::N; ++i)
+                    if (z[i] >= zmin && z[i] <= zmax && z[i] > BITLOGIC_NEG_INF) {
+                        const unsigned at = atomicAdd(&s.n_local, 1u);
+                        const int v = slice.first + j * P::N + i;
+                        if (at < kList) s.local[at] = ((unsigned long long)logit_key(z[i]) << 32) | (uint32_t)~v;
+                    }
+            }
+        }
+        __syncthreads();
+        const unsigned n = min(s.n_local, (unsigned)kList);
+        if (tid == 0) s.base = add_in_block(&s.n_list, 0, s.n_local);
+        __syncthreads();
+        for (unsigned i = tid; i < n; i += kSampleThreads)
+            if (s.base + i < kList) put_in_block(&s.list[s.base + i], 0, s.local[i]);
+    };
+
+    if (set.k < V) {
+        const bool listed = set.k <= kListTop;
+        if (listed) {
+            list_slice(bound_logit(bound), __int_as_float(0x7f800000));
+            row_barrier();
+        }
+        if (rank != 0) return;
+        const unsigned n = s.n_list;
+        __syncthreads();
+        if (listed && n <= kList) sample_of_list(&s, n, set, power, row, out);
+        else sample_of_stream(x, V, set, row, out, &s.stream);
+        return;
+    }
+
+    // every warp a contiguous part of the slice, so that sums follow the order
+    // of classes
+    const int part = (slice.n + kSampleWarps - 1) / kSampleWarps, j0 = min(slice.n, warp * part),
+              j1 = min(slice.n, j0 + part);
+    Cut cut = {kNoCut, 0};
+    float z_cut = BITLOGIC_NEG_INF;   // kept: above it, and the first ties at it
+    if (set.p < 1.0f) {
+        // the mass of the row
+        unsigned long long mass = 0;
+        for (int j = j0 + lane; j < j1;) {
+            WeightSum ws;
+#pragma unroll 2
+            for (int r = 0; r < 32 && j < j1; ++r, j += 32) {
+                float z[P::N];
+                P::load(tile16[j], z);
+#pragma unroll
+                for (int i = 0; i < P::N; ++i) ws.add(power.of(z[i]));
+            }
+            mass += ws.total();
+        }
+        mass = block_add(mass, s.warp_mass, kSampleWarps);
+        for (int b = tid; b < kBins; b += kSampleThreads) s.bins[b] = 0u;
+        if (tid < (int)blocks) put_in_block(&s.sums[rank], tid, SampleShared::Sums{mass, 0u, 0u});
+        row_barrier();
+        unsigned long long total = 0;
+        for (unsigned b = 0; b < blocks; ++b) total += s.sums[b].mass;
+        unsigned long long want = share_of(total, set.p);
+        if (want < 1) want = 1;
+        // classes with less than a V-th of what top_p leaves off come after it
+        const float left_off = fmaxf((float)(total - want) * (1.0f / 1099511627776.0f) / (float)V, 2.3e-13f);
+        const float y_max = fminf(-log2f(left_off) + 0.01f, 41.0f);
+        const float z_min = power.slope > 0.f ? power.m - fabsf(power.m) * 1e-6f - (y_max + 0.01f) / power.slope : BITLOGIC_NEG_INF;
+        for (int j = tid; j < slice.n; j += kSampleThreads) {
+            const uint4 u = tile16[j];
+            if (P::largest_of(u) >= z_min) {
+                float z[P::N];
+                P::load(u, z);
+#pragma unroll
+                for (int i = 0; i < P::N; ++i)
+                    if (z[i] >= z_min && z[i] > BITLOGIC_NEG_INF) {
+                        const int b = bin_of((power.m - z[i]) * power.slope);
+                        atomicAdd(&s.bins[b], bin_units(power.of(z[i]), b));
+                    }
+            }
+        }
+        __syncthreads();
+        // the bins of all blocks added up where the first one keeps its list (a
+        // sum past 32 bits, of more than 2^17 equal logits, picks a wrong bin,
+        // which the exact sums below show)
+        constexpr int kBinPer = (kBins + kSampleThreads - 1) / kSampleThreads;
+        unsigned* row_bins = reinterpret_cast<unsigned*>(s.list);
+        if (rank == 0)
+            for (int b = tid; b < kBins; b += kSampleThreads) row_bins[b] = 0u;
+        row_barrier();
+        for (int b = tid; b < kBins; b += kSampleThreads)
+            if (s.bins[b]) add_in_block(row_bins + b, 0, s.bins[b]);
+        row_barrier();
+        if (rank == 0) {
+            // the bin in which the mass is reached: thread t sums bins
+            // [t per, (t + 1) per)
+            float sum = 0.f;
+            for (int q = 0; q < kBinPer; ++q) {
+                const int b = tid * kBinPer + q;
+                if (b < kBins) sum += bin_mass(row_bins[b], b);
+            }
+            float upto = sum;
+            for (int o = 1; o < 32; o <<= 1) {
+                const float t = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += t;
+            }
+            if (lane == 31) s.fbuf[warp] = upto;
+            if (tid == 0) s.bin = kBins - 1;
+            __syncthreads();
+            float before = upto - sum;
+            for (int w = 0; w < warp; ++w) before += s.fbuf[w];
+            const float goal = (float)want * (1.0f / 1099511627776.0f);
+            for (int q = 0; q < kBinPer; ++q) {
+                const int b = tid * kBinPer + q;
+                if (b < kBins) {
+                    const float mb_ = bin_mass(row_bins[b], b);
+                    if (before < goal && before + mb_ >= goal) atomicMin(&s.bin, b);
+                    before += mb_;
+                }
+            }
+            __syncthreads();
+            const int b = s.bin;
+            if (tid < (int)blocks) store_in_block(&s.bin, tid, (uint32_t)b);
+            if (tid == 0) s.n_list = 0;
+        }
+        if (tid == 0) s.n_local = 0;
+        row_barrier();
+        // logits of bins bin - 1 to bin + 1: a bin's logits are those whose
+        // exponent rounds into it, so the test below is the bin's own
+        const int b0 = max(0, s.bin - 1), b1 = min(kBins - 1, s.bin + 1);
+        mass = 0;
+        for (int j = tid; j < slice.n; j += kSampleThreads) {
+            const uint4 u = tile16[j];
+            if (P::largest_of(u) >= z_min) {
+                float z[P::N];
+                P::load(u, z);
+#pragma unroll
+                for (int i = 0; i < P::N; ++i)
+                    if (z[i] >= z_min && z[i] > BITLOGIC_NEG_INF) {
+                        const int b = bin_of((power.m - z[i]) * power.slope);
+                        if (b < b0) {
+                            mass += draw_weight(power.of(z[i]));
+                        } else if (b <= b1) {
+                            const unsigned at = atomicAdd(&s.n_local, 1u);
+                            const int v = slice.first + j * P::N + i;
+                            if (at < kList) s.local[at] = ((unsigned long long)logit_key(z[i]) << 32) | (uint32_t)~v;
+                        }
+                    }
+            }
+        }
+        mass = block_add(mass, s.warp_mass, kSampleWarps);
+        const unsigned n = min(s.n_local, (unsigned)kList);
+        if (tid == 0) {
+            s.base = add_in_block(&s.n_list, 0, s.n_local);
+            put_in_block(&s.sums[rank], 0, SampleShared::Sums{mass, 0u, 0u});
+        }
+        __syncthreads();
+        for (unsigned i = tid; i < n; i += kSampleThreads)
+            if (s.base + i < kList) put_in_block(&s.list[s.base + i], 0, s.local[i]);
+        row_barrier();
+        if (rank == 0) {
+            constexpr int kPer = kList / kSampleThreads;
+            unsigned long long before = 0;
+            for (unsigned b = 0; b < blocks; ++b) before += s.sums[b].mass;
+            const unsigned long long first = before;
+            const unsigned listed = s.n_list;
+            if (tid == 0) s.found = {0u, 0u, 1u, 0u};   // not found: from memory
+            __syncthreads();
+            if (listed <= kList && listed > 0 && first < want) {
+                const int size = power_of_two(listed);
+                for (int i = listed + tid; i < size; i += kSampleThreads) s.list[i] = 0ull;
+                block_sort_falling(s.list, size);
+                unsigned long long w[kPer], sum = 0, all;
+#pragma unroll
+                for (int q = 0; q < kPer; ++q) {
+                    const int i = tid * kPer + q;
+                    w[q] = i < (int)listed ? draw_weight(power.of(key_logit((uint32_t)(s.list[i] >> 32)))) : 0ull;
+                    sum += w[q];
+                }
+                before = first + block_before(sum, s.scan.sums, &all);
+#pragma unroll
+                for (int q = 0; q < kPer; ++q) {
+                    const int i = tid * kPer + q;
+                    if (before < want && before + w[q] >= want) {   // the last one kept
+                        const uint32_t key = (uint32_t)(s.list[i] >> 32);
+                        unsigned ties = 1;   // with those of its key before it
+                        for (int r = i - 1; r >= 0 && (uint32_t)(s.list[r] >> 32) == key; --r) ++ties;
+                        s.found = {key, ties, 0u, 0u};
+                    }
+                    before += w[q];
+                }
+            }
+            __syncthreads();
+            const SampleShared::Found f = s.found;
+            if (tid < (int)blocks && tid > 0) put_in_block(&s.found, tid, f);
+        }
+        row_barrier();
+        if (s.found.slow) {
+            if (rank == 0) sample_of_stream(x, V, set, row, out, &s.stream);
+            return;
+        }
+        cut = {s.found.key, s.found.ties};
+        z_cut = key_logit(cut.key);
+    }
+
+    // kept weights and ties, by warp and by block
+    unsigned long long mass = 0;
+    unsigned eq = 0;
+    if (set.p >= 1.0f) {
+        for (int j = j0 + lane; j < j1;) {
+            WeightSum ws;
+#pragma unroll 2
+            for (int r = 0; r < 32 && j < j1; ++r, j += 32) {
+                float z[P::N];
+                P::load(tile16[j], z);
+#pragma unroll
+                for (int i = 0; i < P::N; ++i) {
+                    const float e = power.of(z[i]);
+                    ws.add(e >= set.floor_e ? e : 0.f);
+                }
+            }
+            mass += ws.total();
+        }
+    } else {
+        for (int j = j0 + lane; j < j1; j += 32) {
+            const uint4 u = tile16[j];
+            if (P::largest_of(u) >= z_cut) {
+                float z[P::N];
+                P::load(u, z);
+#pragma unroll
+                for (int i = 0; i < P::N; ++i) {
+                    if (z[i] > z_cut) {
+                        const float e = power.of(z[i]);
+                        if (e >= set.floor_e) mass += draw_weight(e);
+                    } else if (z[i] == z_cut) {
+                        ++eq;
+                    }
+                }
+            }
+        }
+    }
+    mass = warp_add(mass);
+    eq = __reduce_add_sync(0xffffffffu, eq);
+    __syncthreads();
+    if (lane == 0) {
+        s.warp_mass[warp] = mass;
+        s.warp_ties[warp] = eq;
+    }
+    __syncthreads();
+    if (tid < (int)blocks) {
+        SampleShared::Sums mine = {0ull, 0u, 0u};
+        for (int w = 0; w < kSampleWarps; ++w) {
+            mine.mass += s.warp_mass[w];
+            mine.ties += s.warp_ties[w];
+        }
+        put_in_block(&s.sums[rank], tid, mine);
+    }
+    row_barrier();
+    unsigned long long wt = 0;
+    if (cut.ties) {
+        const float e = power.of(z_cut);
+        wt = e >= set.floor_e ? draw_weight(e) : 0ull;
+    }
+    unsigned long long total = 0, before = 0, left = cut.ties, my_left = 0;
+    for (unsigned b = 0; b < blocks; ++b) {
+        if (b == rank) {
+            unsigned long long l = left;
+            before = total;
+            for (int w = 0; w < warp; ++w) {
+                const unsigned long long q = s.warp_ties[w] < l ? s.warp_ties[w] : l;
+                before += s.warp_mass[w] + q * wt;
+                l -= q;
+            }
+            my_left = l;
+        }
+        const unsigned long long q = s.sums[b].ties < left ? s.sums[b].ties : left;
+        total += s.sums[b].mass + q * wt;
+        left -= q;
+    }
+    const unsigned long long target = share_of(total, set.u);
+    const unsigned long long mine = mass + (eq < my_left ? eq : my_left) * wt;
+    if (target < before || target >= before + mine) return;
+    // the warp that holds the class: a piece per lane, in order
+    unsigned long long run = before;
+    for (int b = j0; b < j1; b += 32) {
+        const int j = b + lane;
+        float z[P::N];
+        P::load(j < j1 ? tile16[j] : make_uint4(0, 0, 0, 0), z);
+        unsigned long long w[P::N], sum = 0;
+        unsigned same = 0;
+#pragma unroll
+        for (int i = 0; i < P::N; ++i) same += j < j1 && cut.ties && z[i] == z_cut;
+        unsigned ties_before = same;
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned t = __shfl_up_sync(0xffffffffu, ties_before, o);
+            if (lane >= o) ties_before += t;
+        }
+        const unsigned ties_all = __shfl_sync(0xffffffffu, ties_before, 31);
+        ties_before -= same;
+#pragma unroll
+        for (int i = 0; i < P::N; ++i) {
+            w[i] = 0ull;
+            if (j < j1) {
+                if (z[i] > z_cut) {
+                    const float e = power.of(z[i]);
+                    if (e >= set.floor_e) w[i] = draw_weight(e);
+                } else if (cut.ties && z[i] == z_cut) {
+                    if (ties_before < my_left) w[i] = wt;
+                    ++ties_before;
+                }
+            }
+            sum += w[i];
+        }
+        const unsigned long long upto = warp_upto(sum, lane);
+        const unsigned hit = __ballot_sync(0xffffffffu, run + upto > target);
+        if (hit) {
+            if (lane == __ffs(hit) - 1) {
+                unsigned long long r = run + upto - sum;
+                bool done = false;
+#pragma unroll
+                for (int i = 0; i < P::N; ++i) {
+                    r += w[i];
+                    if (!done && r > target) {
+                        done = true;
+                        out.token[row] = slice.first + j * P::N + i;
+                        if (out.logprob) out.logprob[row] = logf((float)w[i] / (float)total);
+                    }
+                }
+            }
+            return;
+        }
+        run += __shfl_sync(0xffffffffu, upto, 31);
+        my_left = my_left > ties_all ? my_left - ties_all : 0;
+    }
+}
+
+// Rows of few classes: a warp per row, PER logits in the registers of a lane
+// (class 32 i + lane).
+constexpr int kNarrow = 1024, kNarrowWarps = 8;
+
+template <typename T, int PER>
+__global__ void __launch_bounds__(kNarrowWarps * 32)
+sample_narrow_kernel(const T* __restrict__ X, long long ld, int V, long long rows, Settings settings, Draw out) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    grid_dependency_wait();
+    allow_dependent_launch();
+    const long long row = (long long)blockIdx.x * kNarrowWarps + warp;
+    if (row >= rows) return;
+    const T* x = X + row * ld;
+    RowSettings set(settings, row, V);
+    float z[PER], m = BITLOGIC_NEG_INF;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) z[i] = 32 * i + lane < V ? logit_value(x[32 * i + lane]) : BITLOGIC_NEG_INF;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) m = fmaxf(m, z[i]);
+    m = warp_largest(m);
+    if (m == BITLOGIC_NEG_INF) {   // nothing to draw from
+        if (lane == 0) {
+            out.token[row] = -1;
+            if (out.logprob) out.logprob[row] = BITLOGIC_NEG_INF;
+        }
+        return;
+    }
+    const Power power(m, set);
+    auto share = [&](int i) { return z[i] > BITLOGIC_NEG_INF ? power(z[i]) : 0.f; };
+    Cut cut = {kNoCut, 0};
+    if (set.k < V) {
+        unsigned n = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) n += ranks(logit_key(z[i]));
+        n = __reduce_add_sync(0xffffffffu, n);
+        if ((unsigned)set.k < n) {
+            uint32_t t = 0;
+            unsigned reach = 0;
+            for (uint32_t bit = 0x80000000u; bit > 0 && reach != (unsigned)set.k; bit >>= 1) {
+                unsigned h = 0;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) h += logit_key(z[i]) >= (t | bit);
+                h = __reduce_add_sync(0xffffffffu, h);
+                if (h >= (unsigned)set.k) {
+                    t |= bit;
+                    reach = h;
+                }
+            }
+            unsigned above = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) above += logit_key(z[i]) > t;
+            above = __reduce_add_sync(0xffffffffu, above);
+            cut.key = t;
+            cut.ties = set.k - above;
+        }
+    }
+    if (set.p < 1.0f) {
+        unsigned long long mass = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (logit_key(z[i]) > cut.key) mass += draw_weight(share(i));
+        mass = warp_add(mass);
+        const unsigned long long we = cut.ties ? draw_weight(power(key_logit(cut.key))) : 0ull;
+        unsigned long long want = share_of(mass + cut.ties * we, set.p);
+        if (want < 1) want = 1;
+        if (want > mass) {
+            const unsigned long long nd = we ? (want - mass + we - 1) / we : cut.ties;
+            if (nd < cut.ties) cut.ties = nd;
+        } else {
+            // the largest key that the mass is reached at, a bit at a time
+            uint32_t t = 0;
+            for (uint32_t bit = 0x80000000u; bit > 0; bit >>= 1) {
+                unsigned long long h = 0;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const uint32_t kk = logit_key(z[i]);
+                    if (kk >= (t | bit) && kk > cut.key) h += draw_weight(share(i));
+                }
+                if (warp_add(h) >= want) t |= bit;
+            }
+            unsigned long long above = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (logit_key(z[i]) > t) above += draw_weight(share(i));
+            above = warp_add(above);
+            const unsigned long long wt = draw_weight(power(key_logit(t)));
+            cut.key = t;
+            cut.ties = wt ? (want - above + wt - 1) / wt : 1;
+        }
+    }
+    // kept weights in registers, then the draw, 32 classes at a time
+    unsigned long long total = 0;
+    float e[PER];
+    unsigned left = (unsigned)cut.ties;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const uint32_t kk = logit_key(z[i]);
+        const bool same = cut.ties && kk == cut.key;
+        const unsigned mask = __ballot_sync(0xffffffffu, same);
+        bool kept = kk > cut.key || (same && __popc(mask & ((1u << lane) - 1u)) < left);
+        left -= min(left, (unsigned)__popc(mask));
+        e[i] = kept ? share(i) : 0.f;
+        if (e[i] < set.floor_e) e[i] = 0.f;
+        total += draw_weight(e[i]);
+    }
+    total = warp_add(total);
+    const unsigned long long target = share_of(total, set.u);
+    unsigned long long run = 0;
+    bool done = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (!done) {
+            const unsigned long long w = draw_weight(e[i]);
+            const unsigned long long upto = warp_upto(w, lane);
+            const unsigned hit = __ballot_sync(0xffffffffu, run + upto > target);
+            if (hit) {
+                if (lane == __ffs(hit) - 1) {
+                    out.token[row] = 32 * i + lane;
+                    if (out.logprob) out.logprob[row] = logf((float)w / (float)total);
+                }
+                done = true;
+            }
+            run += __shfl_sync(0xffffffffu, upto, 31);
+        }
+    }
+}
+
+// Slices of at most kTileFit bytes leave room for three blocks on an SM beside
+// their lists.
+constexpr int kTileFit = 40 * 1024, kTileMost = 184 * 1024, kTileLeast = 8 * 1024;
+
+template <typename T>
+int launch_sample(const T* x, long long T_, int V, long long ld, const Settings& set, const Draw& out,
+                  cudaStream_t stream) {
+    cudaError_t e;
+    if (V <= kNarrow) {
+        auto kern = V <= 32 ? sample_narrow_kernel<T, 1> : V <= 128 ? sample_narrow_kernel<T, 4>
+                  : V <= 256 ? sample_narrow_kernel<T, 8> : sample_narrow_kernel<T, 32>;
+        e = launch_rows(kern, (T_ + kNarrowWarps - 1) / kNarrowWarps, 1, kNarrowWarps * 32, 0, stream, x, ld, V, T_, set, out);
+    } else if (const int blocks = blocks_per_row(T_, V, sizeof(T), kTileFit, kTileMost, kTileLeast)) {
+        e = launch_rows(sample_tile_kernel<T>, T_, blocks, kSampleThreads, (size_t)slice_bytes(V, sizeof(T), blocks), stream,
+                        x, ld, V, set, out);
+    } else {
+        e = launch_rows(sample_stream_kernel<T>, T_, 1, kSampleThreads, 0, stream, x, ld, V, set, out);
+    }
+    return e == cudaSuccess ? launch_status() : (int)BITLOGIC_ERR_CUDA;
 }
 
 }  // namespace
@@ -203,9 +961,8 @@ extern "C" int bitlogic_sample_logits(const void* X, int32_t dtype, int64_t T, i
     if (T == 0) return BITLOGIC_OK;
     if (!u || !token) return BITLOGIC_ERR_NULL;
     const Settings set = {u, temperature, top_k, top_p, min_p};
+    const Draw out = {token, logprob};
     return with_logit_type(dtype, true, [&](auto* type) {
-        const auto* x = static_cast<decltype(type)>(X);
-        sample_stream_kernel<<<(unsigned)T, kSampleThreads, 0, stream>>>(x, ld, V, set, token, logprob);
-        return launch_status();
+        return launch_sample(static_cast<decltype(type)>(X), T, V, ld, set, out, stream);
     });
 }
