@@ -74,19 +74,54 @@ __device__ __forceinline__ void block_sort_falling(unsigned long long* a, int si
 // The logit of a key.
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k ^ 0x80000000u) : ~k); }
 
-// A lower bound of the `need` largest of the values that the warp's lanes hold
-// two of each: the largest key of 16 leading bits that at least `need` of the
-// 64 reach (0 when fewer rank).
-__device__ __forceinline__ uint32_t warp_bound(float a, float b, int need) {
+// A bound of the largest values that a block's threads hold two of each: the
+// largest key of 16 leading bits that at least `need` of them reach (0 when
+// fewer rank), by 8 bits at a time.  Called by the whole block of 256 threads.
+struct BoundScratch {
+    unsigned bins[2][256];
+    unsigned digit[2], above;
+};
+__device__ __forceinline__ uint32_t block_bound(float a, float b, unsigned need, BoundScratch* s) {
     const uint32_t ka = logit_key(a) >> 16, kb = logit_key(b) >> 16;
-    uint32_t t = 0;
+    const int tid = threadIdx.x, lane = tid & 31;
+    s->bins[0][tid] = s->bins[1][tid] = 0u;
+    if (tid == 0) s->digit[0] = s->digit[1] = s->above = 0u;
+    __syncthreads();
 #pragma unroll
-    for (uint32_t bit = 0x8000u; bit > 0; bit >>= 1) {
-        const uint32_t c = t | bit;
-        const int n = __popc(__ballot_sync(0xffffffffu, ka >= c)) + __popc(__ballot_sync(0xffffffffu, kb >= c));
-        if (n >= need) t = c;
+    for (int pass = 0; pass < 2; ++pass) {
+        unsigned* bins = s->bins[pass];
+        const uint32_t top = s->digit[0];
+        if (pass == 0) {
+            atomicAdd(&bins[ka >> 8], 1u);
+            atomicAdd(&bins[kb >> 8], 1u);
+        } else {
+            if ((ka >> 8) == top) atomicAdd(&bins[ka & 255u], 1u);
+            if ((kb >> 8) == top) atomicAdd(&bins[kb & 255u], 1u);
+        }
+        __syncthreads();
+        if (tid < 32) {   // lane l: bins 255 - 8 l down to 248 - 8 l
+            const unsigned start = pass == 0 ? 0u : s->above;
+            unsigned own = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) own += bins[255 - 8 * lane - i];
+            unsigned upto = own;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const unsigned t = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += t;
+            }
+            const unsigned m = __ballot_sync(0xffffffffu, start + upto >= need);
+            if (m && lane == __ffs(m) - 1) {
+                unsigned n = start + upto - own;
+                int d = 255 - 8 * lane;
+                while (n + bins[d] < need) n += bins[d--];
+                s->digit[pass] = (unsigned)d;
+                s->above = n;
+            }
+        }
+        __syncthreads();
     }
-    return t << 16;
+    return (s->digit[0] << 24) | (s->digit[1] << 16);
 }
 // The smallest logit that such a bound lets through.
 __device__ __forceinline__ float bound_logit(uint32_t key) { return key <= kKeyNegInf ? BITLOGIC_NEG_INF : key_logit(key); }

@@ -260,6 +260,7 @@ struct SampleShared {
     };
     union {
         unsigned long long local[kList];  // of the slice
+        BoundScratch bound;
         unsigned bins[kBins];             // mass of the slice by the power's exponent
         struct {
             unsigned long long sums[kSampleWarps];
@@ -276,7 +277,7 @@ struct SampleShared {
     unsigned long long warp_mass[kSampleWarps];
     unsigned warp_ties[kSampleWarps];
     float fbuf[kSampleWarps];
-    uint32_t bounds[kSampleWarps];
+    int kept[kSampleWarps];
     struct Found {
         uint32_t key;
         unsigned ties, slow, pad;
@@ -348,9 +349,9 @@ __device__ void sample_of_list(SampleShared* s, unsigned n, const RowSettings& s
     // the kept are a run from the front: its length
     for (int o = 16; o > 0; o >>= 1) kept = max(kept, __shfl_xor_sync(0xffffffffu, kept, o));
     __syncthreads();
-    if ((tid & 31) == 0) s->bounds[tid >> 5] = kept;
+    if ((tid & 31) == 0) s->kept[tid >> 5] = kept;
     __syncthreads();
-    for (int v = 0; v < kSampleWarps; ++v) kept = max(kept, (int)s->bounds[v]);
+    for (int v = 0; v < kSampleWarps; ++v) kept = max(kept, s->kept[v]);
     // by class: ~class << 32 | key falls as the class rises
     const int size2 = power_of_two(kept);
     for (int i = tid; i < size2; i += kSampleThreads) {
@@ -430,20 +431,13 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
         if (j + kSampleThreads < slice.n) mb = P::largest(mb, tile16[j + kSampleThreads]);
     }
     const float za = P::value(ma), zb = P::value(mb);
-    const int need = (k_asked + (int)blocks * kSampleWarps - 1) / ((int)blocks * kSampleWarps);
-    const uint32_t wb = need <= 64 ? warp_bound(za, zb, need) : 0u;
+    const uint32_t bound_here = k_asked < V ? block_bound(za, zb, (k_asked + blocks - 1) / blocks, &s.bound) : 0u;
     const float wm = warp_largest(fmaxf(za, zb));
-    if (lane == 0) {
-        s.fbuf[warp] = wm;
-        s.bounds[warp] = wb;
-    }
+    if (lane == 0) s.fbuf[warp] = wm;
     __syncthreads();
     if (tid < (int)blocks) {
-        SampleShared::Stats st = {s.fbuf[0], s.bounds[0]};
-        for (int w = 1; w < kSampleWarps; ++w) {
-            st.m = fmaxf(st.m, s.fbuf[w]);
-            st.bound = min(st.bound, s.bounds[w]);
-        }
+        SampleShared::Stats st = {s.fbuf[0], bound_here};
+        for (int w = 1; w < kSampleWarps; ++w) st.m = fmaxf(st.m, s.fbuf[w]);
         put_in_block(&s.stats[rank], tid, st);
     }
     row_barrier();

@@ -108,21 +108,23 @@ struct TopShared {
         unsigned long long list[kTopList];   // of the row, in the cluster's first block
         TopScratch scratch;
     };
-    unsigned long long local[kTopList];      // of the slice
+    union {
+        unsigned long long local[kTopList];  // of the slice
+        BoundScratch bound;
+    };
     struct Stats {
         float m;
         uint32_t bound;
     } stats[kMaxCluster];
     float sums[kMaxCluster];
     float fbuf[kTopWarps];
-    uint32_t bounds[kTopWarps];
     unsigned n_list, n_local, base;
 };
 
 // A row in the shared memory of one block or one cluster.  Each thread's two
-// running maxima give a bound that at least K logits of the row reach: with
-// need = K / (blocks 8) rounded up, the largest key that `need` of a warp's 64
-// maxima reach, and the smallest of those over all warps.  For logits in no
+// running maxima give a bound that at least K logits of the row reach: the
+// largest key that K / blocks of a block's 512 maxima reach, and the smallest
+// of those over the row's blocks.  For logits in no
 // particular order little more than K pass it, so the selection sorts a few
 // hundred entries; rows on which more than 1024 pass (long runs of equal
 // logits, rows sorted by value) are selected from memory.
@@ -153,20 +155,13 @@ top_tile_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
         if (j + kTopThreads < slice.n) mb = P::largest(mb, tile16[j + kTopThreads]);
     }
     const float za = P::value(ma), zb = P::value(mb);
-    const int need = (K + (int)blocks * kTopWarps - 1) / ((int)blocks * kTopWarps);
-    const uint32_t wb = warp_bound(za, zb, need);
+    const uint32_t bound_here = block_bound(za, zb, (K + blocks - 1) / blocks, &s.bound);
     const float wm = warp_largest(fmaxf(za, zb));
-    if (lane == 0) {
-        s.fbuf[warp] = wm;
-        s.bounds[warp] = wb;
-    }
+    if (lane == 0) s.fbuf[warp] = wm;
     __syncthreads();
     if (tid < (int)blocks) {
-        TopShared::Stats st = {s.fbuf[0], s.bounds[0]};
-        for (int w = 1; w < kTopWarps; ++w) {
-            st.m = fmaxf(st.m, s.fbuf[w]);
-            st.bound = min(st.bound, s.bounds[w]);
-        }
+        TopShared::Stats st = {s.fbuf[0], bound_here};
+        for (int w = 1; w < kTopWarps; ++w) st.m = fmaxf(st.m, s.fbuf[w]);
         put_in_block(&s.stats[rank], tid, st);
     }
     if (blocks > 1) {
