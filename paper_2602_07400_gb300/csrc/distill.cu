@@ -23,8 +23,6 @@
 namespace bitlogic {
 namespace {
 
-constexpr int kDistillThreads = 512, kDistillWarps = kDistillThreads / 32;
-
 struct Distill {
     long long T;
     int V, K;
@@ -41,153 +39,314 @@ struct Distill {
     float grad_scale;
 };
 
-// An entry of the record: a repeated class is one entry with the sum of its
-// probabilities, kept by its first place.
-struct Entry {
-    int v;        // class, -1: none
-    float q;      // teacher's probability
-    float logq;   // its logarithm
+constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
+constexpr int kRing = 8;   // places of a thread's ring: one piece in use, the others in flight
+
+// Powers summed about a running base: the base moves up with the largest logit
+// seen, and the sums with it.
+struct RunningSum {
+    float m = BITLOGIC_NEG_INF;
+    f32x2 y0 = 0, y1 = 0, z0 = 0, z1 = 0;   // powers at tau and at 1, two zeros each
+
+    template <bool TWO>
+    __device__ __forceinline__ void raise(float to, float cy) {
+        const PowerBase oy(m, cy), oz(m, kLog2E), ny(to, cy), nz(to, kLog2E);
+        const float f = far_alike(oy, oz).to(far_alike(ny, nz));
+        y0 = mul2(y0, pack2(f, f));
+        y1 = mul2(y1, pack2(f, f));
+        if (TWO) {
+            const float h = far_alike(oz, oy).to(far_alike(nz, ny));
+            z0 = mul2(z0, pack2(h, h));
+            z1 = mul2(z1, pack2(h, h));
+        }
+        m = to;
+    }
 };
 
-// Rows too long for the shared memory of a cluster: one block per row, which
-// reads it from memory in every pass; the classes on the record are marked in
-// a bit map.
-template <typename T>
-__global__ void __launch_bounds__(kDistillThreads)
-distill_stream_kernel(const T* Z, T* dZ, Distill a) {
-    extern __shared__ unsigned on_record[];
-    __shared__ float fbuf[kDistillWarps];
-    __shared__ double dbuf[kDistillWarps];
+// Rows too long for the shared memory of a cluster: a block per row, which
+// streams it once for the statistics and a second time, from L2, for the
+// gradient.  The classes on the record are marked in a bit map by place, and the
+// marked ones of a piece are taken out of its sum.  (On shorter rows it takes
+// 983 us where the tile kernel takes 893, 8192 x 131072 bf16.)
+template <typename T, bool TWO>
+__global__ void __launch_bounds__(kRowThreads, 4)
+distill_row_kernel(const T* Z, T* dZ, Distill a) {
+    using P = Piece<T>;
+    constexpr int N = P::N, H = N / 2;
+    extern __shared__ __align__(16) unsigned char raw[];
+    uint4* ring = reinterpret_cast<uint4*>(raw) + threadIdx.x;   // this thread's places, kRowThreads apart
+    const uint8_t* marks8 = raw + kRing * kRowThreads * 16;
+    uint32_t* marks = reinterpret_cast<uint32_t*>(raw + kRing * kRowThreads * 16);
+    __shared__ float tbuf[kRowWarps], nbuf[kRowWarps], qbuf[kRowWarps], mbuf[kRowWarps], kbuf[kRowWarps];
+    __shared__ float rest_buf[kRowWarps], member_buf[kRowWarps], sz_buf[kRowWarps];
+    __shared__ double dbuf[kRowWarps];
     __shared__ int classes[kMaxTop];
-    __shared__ int repeated;
+    __shared__ float probs[kMaxTop];
+    __shared__ int any_s, label_on_s, repeated_s;
     grid_dependency_wait();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long row = blockIdx.x;
+    const int V = a.V, K = a.K;
     const T* z = Z + row * a.ld;
     T* g = dZ ? dZ + row * a.ldg : nullptr;
-    const int tid = threadIdx.x, V = a.V, K = a.K;
+    const RowSlice<T> slice(z, V, 0, 1);
+    const int w0 = slice.whole0(), w1 = slice.whole1(V);
+    const bool wide = a.incg == 1 && ((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(z)) & 15u) == 0;
     const float wt = a.weight ? a.weight[row] : 1.0f / (float)a.T;
-    if (wt == 0.f) {   // a row left out: whatever its logits hold
-        for (int v = tid; g && v < V; v += kDistillThreads) g[(long long)v * a.incg] = logit_of<T>(0.f);
-        if (tid == 0) a.row_loss[row] = 0.f;
-        return;
-    }
-    for (int i = tid; i < (V + 31) / 32; i += kDistillThreads) on_record[i] = 0u;
-    if (tid == 0) repeated = 0;
-    Entry e = {-1, 0.f, 0.f};
-    float t = BITLOGIC_NEG_INF;
-    if (tid < K) {
-        e.v = a.idx[row * K + tid];
-        if (e.v >= V) {
-            flag_index_error();
-            e.v = -1;
-        }
-        if (e.v < 0) e.v = -1;
-        else t = a.val[row * K + tid] * a.inv_tau;
-        classes[tid] = e.v;
-    }
-    __syncthreads();
-    if (e.v >= 0 && (atomicOr(&on_record[e.v >> 5], 1u << (e.v & 31)) >> (e.v & 31)) & 1u) repeated = 1;
-    // the teacher's probabilities
-    float norm, Q = 0.f, q_left = 0.f;
-    if (a.teacher_lse) {
-        norm = a.teacher_lse[row];
-        double q = 0.0;
-        if (t != BITLOGIC_NEG_INF) {
-            const double d = (double)a.val[row * K + tid] * a.inv_tau64 - (double)norm;
-            e.logq = (float)d;
-            q = exp(d);
-        }
-        e.q = (float)q;
-        const double sum = block_add(q, dbuf, kDistillWarps);
-        Q = (float)sum;
-        q_left = (float)fmax(1.0 - sum, 0.0);
-    } else {
-        const float tm = block_largest(t, fbuf, kDistillWarps), ts = isinf(tm) ? 0.f : tm;
-        norm = ts + logf(block_add(exp2_unit((t - ts) * kLog2E), fbuf, kDistillWarps));
-        e.logq = t - norm;
-        e.q = t == BITLOGIC_NEG_INF ? 0.f : exp2_unit(e.logq * kLog2E);
-        Q = block_add(e.q, fbuf, kDistillWarps);
-    }
-    const bool any = block_add(e.v >= 0 ? 1.f : 0.f, fbuf, kDistillWarps) > 0.f;
-    bool first = e.v >= 0;
-    float q_class = e.q;   // of all places of the class
-    __syncthreads();
-    if (repeated && e.v >= 0) {
-        q_class = 0.f;
-        for (int j = 0; j < K; ++j)
-            if (classes[j] == e.v) {
-                if (j < tid) first = false;
-                q_class += a.val[row * K + j] == BITLOGIC_NEG_INF ? 0.f : exp2_unit((a.val[row * K + j] * a.inv_tau - norm) * kLog2E);
-            }
-    }
-    // softmax statistics
-    float m = BITLOGIC_NEG_INF;
-    for (int v = tid; v < V; v += kDistillThreads) m = fmaxf(m, logit_value(z[v]));
-    m = block_largest(m, fbuf, kDistillWarps);
-    if (isinf(m) && m < 0.f) m = 0.f;
-    const float cy = kLog2E * a.inv_tau;
+    int ev = tid < K ? a.idx[row * K + tid] : -1;
+    const float tval = tid < K ? a.val[row * K + tid] : 0.f;
     const int label = a.labels && a.ce != 0.f ? a.labels[row] : -1;
-    float rest = 0.f, member = 0.f, sz = 0.f;
-    for (int v = tid; v < V; v += kDistillThreads) {
-        const float d = logit_value(z[v]) - m, ey = exp2_unit(d * cy);
-        if ((on_record[v >> 5] >> (v & 31)) & 1u) member += ey;
-        else rest += ey;
-        if (label >= 0) sz += exp2_unit(d * kLog2E);
-    }
-    rest = block_add(rest, fbuf, kDistillWarps);
-    const float s = rest + block_add(member, fbuf, kDistillWarps);
-    if (label >= 0) sz = block_add(sz, fbuf, kDistillWarps);
-    if (s == 0.f) {   // every class masked: no distribution, no loss
-        for (int v = tid; g && v < V; v += kDistillThreads) g[(long long)v * a.incg] = logit_of<T>(0.f);
+
+    // a piece at the row's ends, by element; places outside it are masked
+    auto end_piece = [&](int j) {
+        T x[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int v = slice.first + j * N + i;
+            x[i] = v >= 0 && v < V ? z[v] : masked_logit<T>();
+        }
+        return *reinterpret_cast<uint4*>(x);
+    };
+    // whole pieces by the ring, each thread its own: from `start` on, every
+    // piece handed to `use` while the ones after it are on their way
+    const T* from = z + slice.first;   // read at whole pieces
+    auto start = [&]() {
+#pragma unroll
+        for (int i = 0; i < kRing - 1; ++i) {
+            const int j = w0 + tid + i * kRowThreads;
+            if (j < w1) cp_async16(ring + i * kRowThreads, from + j * N);
+            cp_async_commit();
+        }
+    };
+    auto stream = [&](auto&& use) {
+        int at = 0;
+        for (int j = w0 + tid; j < w1; j += kRowThreads) {
+            cp_async_wait<kRing - 2>();
+            const uint4 u = ring[at * kRowThreads];
+            const int next = j + (kRing - 1) * kRowThreads;
+            if (next < w1) cp_async16(ring + (at == 0 ? kRing - 1 : at - 1) * kRowThreads, from + next * N);
+            cp_async_commit();
+            use(j, u);
+            at = at == kRing - 1 ? 0 : at + 1;
+        }
+        if (tid == 0 && w0 > 0) use(0, end_piece(0));   // the pieces at the row's ends
+        if (tid == 32 && w1 < slice.n) use(w1, end_piece(w1));
+    };
+    auto store = [&](int j, const float (&y)[N]) {
+        if (wide && j >= w0 && j < w1) {
+            __stcs(reinterpret_cast<uint4*>(g + slice.first) + j, P::pack(y));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int v = slice.first + j * N + i;
+                if (v >= 0 && v < V) g[(long long)v * a.incg] = logit_of<T>(y[i]);
+            }
+        }
+    };
+    auto zero_row = [&]() {
+        const float y[N] = {};
+        for (int j = tid; g && j < slice.n; j += kRowThreads) store(j, y);
         if (tid == 0) a.row_loss[row] = 0.f;
+    };
+    if (wt == 0.f) {   // a row left out: whatever its logits hold
+        zero_row();
         return;
     }
+    start();
+
+    // the record: thread k holds entry k
+    for (int i = tid; i < (slice.n * N + 31) / 32; i += kRowThreads) marks[i] = 0u;
+    if (tid == 0) any_s = label_on_s = repeated_s = 0;
+    if (ev >= V) {
+        flag_index_error();
+        ev = -1;
+    }
+    if (ev < 0) ev = -1;
+    const float t = ev >= 0 ? tval * a.inv_tau : BITLOGIC_NEG_INF;
+    const float zk = ev >= 0 ? logit_value(z[ev]) : 0.f;
     const bool label_ok = label >= 0 && label < V;
     if (label >= V && tid == 0) flag_index_error();
-    const float qr = a.teacher_lse && any && rest > 0.f ? q_left : 0.f;
-    const float log_s = logf(s);
-    // the loss
-    float kl = 0.f;
-    if (e.q > 0.f) kl = e.q * (e.logq - ((logit_value(z[e.v]) - m) * a.inv_tau - log_s));
-    kl = block_add(kl, fbuf, kDistillWarps);
-    if (qr > 0.f) kl += qr * (logf(qr) - logf(rest / s));
-    if (tid == 0) {
-        float loss = a.kd != 0.f ? a.kd * kl : 0.f;   // a loss of +inf without weight is none
-        if (label_ok) loss += a.ce * (logf(sz) - (logit_value(z[label]) - m));
-        a.row_loss[row] = (s != s) ? s : loss;
-    }
-    if (!g) return;
-    // the gradient
-    const float ay = wt * a.grad_scale * a.kd * a.inv_tau, az = label_ok ? wt * a.grad_scale * a.ce : 0.f;
-    const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) / s - (qr > 0.f ? qr / rest : 0.f));
-    const float iz = label_ok ? az / sz : 0.f;
-    const float z_first = first ? logit_value(z[e.v]) : 0.f, z_label = label_ok ? logit_value(z[label]) : 0.f;
-    __syncthreads();   // the gradient may take the logits' place
-    for (int v = tid; v < V; v += kDistillThreads) {
-        const float d = logit_value(z[v]) - m;
-        float x = exp2_unit(d * cy) * off;
-        if (label_ok) x += exp2_unit(d * kLog2E) * iz;
-        g[(long long)v * a.incg] = logit_of<T>(x);
+    const float z_label = label_ok ? logit_value(z[label]) : 0.f;
+    __syncthreads();
+    if (ev >= 0) {
+        any_s = 1;
+        if (ev == label) label_on_s = 1;
+        const int p = ev - slice.first;
+        if ((atomicOr(&marks[p >> 5], 1u << (p & 31)) >> (p & 31)) & 1u) repeated_s = 1;
     }
     __syncthreads();
-    if (first) {
-        const float d = z_first - m;
-        float x = exp2_unit(d * cy) * on - ay * q_class;
-        if (label_ok) x += exp2_unit(d * kLog2E) * iz - (e.v == label ? az : 0.f);
-        g[(long long)e.v * a.incg] = logit_of<T>(x);
+
+    // statistics, about a base of each thread's own
+    const float cy = kLog2E * a.inv_tau;
+    RunningSum run;
+    stream([&](int j, uint4 u) {
+        const unsigned on = ((unsigned)marks8[j * N / 8] >> (j * N % 8)) & ((1u << N) - 1u);
+        if (on) {
+            T* x = reinterpret_cast<T*>(&u);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if ((on >> i) & 1u) x[i] = masked_logit<T>();
+        }
+        const float top = P::largest_of(u);
+        if (top > run.m) run.raise<TWO>(top, cy);
+        const PowerBase by(run.m, cy), bz(run.m, kLog2E), ey = far_alike(by, bz), ez = far_alike(bz, by);
+        auto sums = [&](const auto& py, const auto& pz) {
+            f32x2 x[H];
+            load_pairs<T>(u, x);
+#pragma unroll
+            for (int i = 0; i < H; i += 2) {
+                run.y0 = add2(run.y0, py(x[i]));
+                run.y1 = add2(run.y1, py(x[i + 1]));
+                if (TWO) {
+                    run.z0 = add2(run.z0, pz(x[i]));
+                    run.z1 = add2(run.z1, pz(x[i + 1]));
+                }
+            }
+        };
+        if (ey.far) sums(FarPairs(ey), FarPairs(ez));
+        else sums(NearPairs(ey), NearPairs(ez));
+    });
+    if (g) start();   // the second time, while the statistics come together
+
+    // the teacher's probabilities
+    float q = 0.f, logq = 0.f, Q = 0.f, q_left = 0.f;
+    if (a.teacher_lse) {
+        double q64 = 0.0;
+        if (t != BITLOGIC_NEG_INF) {
+            const double d = (double)tval * a.inv_tau64 - (double)a.teacher_lse[row];
+            logq = (float)d;
+            q64 = exp(d);
+            q = (float)q64;
+        }
+        q64 = warp_add(q64);
+        if (lane == 0) dbuf[warp] = q64;
+    } else {   // softmax over the record
+        const float wm = warp_largest(t);
+        if (lane == 0) tbuf[warp] = wm;
+        __syncthreads();
+        float tm = tbuf[0];
+        for (int w = 1; w < kRowWarps; ++w) tm = fmaxf(tm, tbuf[w]);
+        const float ts = isinf(tm) ? 0.f : tm, ws = warp_add(exp2_unit((t - ts) * kLog2E));
+        if (lane == 0) nbuf[warp] = ws;
+        __syncthreads();
+        float sum = 0.f;
+        for (int w = 0; w < kRowWarps; ++w) sum += nbuf[w];
+        logq = t - (ts + logf(sum));
+        q = t == BITLOGIC_NEG_INF ? 0.f : exp2_unit(logq * kLog2E);
+        const float wq = warp_add(q);
+        if (lane == 0) qbuf[warp] = wq;
     }
-    if (tid == 0 && label_ok && !((on_record[label >> 5] >> (label & 31)) & 1u)) {
-        const float d = z_label - m;
-        g[(long long)label * a.incg] = logit_of<T>(exp2_unit(d * cy) * off + exp2_unit(d * kLog2E) * iz - az);
+    bool first = ev >= 0;
+    float q_class = q;   // of all places of the class
+    if (repeated_s) {
+        if (tid < K) {
+            classes[tid] = ev;
+            probs[tid] = q;
+        }
+        __syncthreads();
+        if (ev >= 0) {
+            q_class = 0.f;
+            for (int j = 0; j < K; ++j)
+                if (classes[j] == ev) {
+                    if (j < tid) first = false;
+                    q_class += probs[j];
+                }
+        }
+    }
+    // the row's base and sums
+    float m = warp_largest(ev >= 0 ? fmaxf(run.m, zk) : run.m);
+    if (lane == 0) mbuf[warp] = m;
+    __syncthreads();
+    for (int w = 0; w < kRowWarps; ++w) m = fmaxf(m, mbuf[w]);
+    const PowerBase ny(m, cy), nz(m, kLog2E), by = far_alike(ny, nz), bz = far_alike(nz, ny);
+    {
+        const PowerBase oy(run.m, cy), oz(run.m, kLog2E);
+        float ra, rb, sa, sb;
+        unpack2(add2(run.y0, run.y1), ra, rb);
+        unpack2(add2(run.z0, run.z1), sa, sb);
+        const float rest = warp_add((ra + rb) * far_alike(oy, oz).to(by));
+        const float member = warp_add(first ? by.power(zk) : 0.f);
+        const float sz = TWO ? warp_add((sa + sb) * far_alike(oz, oy).to(bz) + (first ? bz.power(zk) : 0.f)) : 0.f;
+        if (lane == 0) {
+            rest_buf[warp] = rest;
+            member_buf[warp] = member;
+            sz_buf[warp] = sz;
+        }
+    }
+    __syncthreads();
+    float rest = 0.f, s = 0.f, sz = 0.f;
+    double q_sum = 0.0;
+    for (int w = 0; w < kRowWarps; ++w) {
+        rest += rest_buf[w];
+        s += member_buf[w];
+        sz += sz_buf[w];
+        if (a.teacher_lse) q_sum += dbuf[w];
+        else Q += qbuf[w];
+    }
+    s += rest;
+    if (!TWO) sz = s;   // tau = 1 where a label is
+    if (a.teacher_lse) {
+        Q = (float)q_sum;
+        q_left = (float)fmax(1.0 - q_sum, 0.0);
+    }
+    const bool any = any_s != 0, label_on = label_on_s != 0;
+    allow_dependent_launch();
+    if (s == 0.f) {   // every class masked: no distribution, no loss
+        cp_async_wait<0>();
+        zero_row();
+        return;
+    }
+    const float qr = a.teacher_lse && any && rest > 0.f ? q_left : 0.f, log2_s = log2f(s);
+    const float kl_part = warp_add(q > 0.f ? q * (logq - kLn2 * (by.exponent(zk) - log2_s)) : 0.f);
+    if (lane == 0) kbuf[warp] = kl_part;
+    if (g) {
+        const float ay = wt * a.grad_scale * a.kd * a.inv_tau, az = label_ok ? wt * a.grad_scale * a.ce : 0.f;
+        const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) / s - (qr > 0.f ? qr / rest : 0.f));
+        const float iz = label_ok ? az / sz : 0.f, fy = TWO ? off : off + iz;
+        auto gradient = [&](const auto& py, const auto& pz) {
+            const f32x2 fy2 = pack2(fy, fy), fz2 = pack2(iz, iz);
+            stream([&](int j, uint4 u) {
+                f32x2 x[H];
+                load_pairs<T>(u, x);
+                float y[N];
+#pragma unroll
+                for (int i = 0; i < H; ++i) {
+                    f32x2 v = mul2(py(x[i]), fy2);
+                    if (TWO) v = fma2(pz(x[i]), fz2, v);
+                    unpack2(v, y[2 * i], y[2 * i + 1]);
+                }
+                store(j, y);
+            });
+        };
+        if (by.far) gradient(FarPairs(by), FarPairs(bz));
+        else gradient(NearPairs(by), NearPairs(bz));
+    }
+    __syncthreads();
+    if (g) {
+        // the record's classes and the label, over what the pass wrote there
+        if (first) {
+            float x = by.power(zk) * (wt * a.grad_scale * a.kd * a.inv_tau * (Q + qr) / s) - wt * a.grad_scale * a.kd * a.inv_tau * q_class;
+            if (label_ok) {
+                const float az = wt * a.grad_scale * a.ce;
+                x += bz.power(zk) * (az / sz) - (ev == label ? az : 0.f);
+            }
+            g[(long long)ev * a.incg] = logit_of<T>(x);
+        }
+        if (tid == 0 && label_ok && !label_on) {
+            const float ay = wt * a.grad_scale * a.kd * a.inv_tau, az = wt * a.grad_scale * a.ce;
+            const float off = ay * ((Q + qr) / s - (qr > 0.f ? qr / rest : 0.f));
+            g[(long long)label * a.incg] = logit_of<T>(by.power(z_label) * off + bz.power(z_label) * (az / sz) - az);
+        }
+    }
+    if (tid == 0) {
+        float kl = 0.f;
+        for (int w = 0; w < kRowWarps; ++w) kl += kbuf[w];
+        if (qr > 0.f) kl += qr * (logf(qr) - logf(rest / s));
+        float loss = a.kd != 0.f ? a.kd * kl : 0.f;   // a loss of +inf without weight is none
+        if (label_ok) loss += a.ce * kLn2 * (log2f(sz) - bz.exponent(z_label));
+        a.row_loss[row] = s != s ? s : loss;
     }
 }
-
-// Powers 2^(c (z - m)) of a slice about its largest.
-struct PowerBase {
-    float c, m;
-    __device__ __forceinline__ PowerBase(float m_, float c_) : c(c_), m(m_) {}
-    __device__ __forceinline__ float operator()(float z) const { return exp2_unit((z - m) * c); }
-};
 
 // What the blocks of a row tell each other.
 struct __align__(8) DistillStats {
@@ -199,6 +358,7 @@ struct __align__(8) DistillStats {
 };
 
 constexpr int kTileThreads = 256, kTileWarps = kTileThreads / 32;
+constexpr int kClassTable = 512;   // open-addressed, of at most kMaxTop classes
 
 // A row in the shared memory of one block or one cluster: the logits are read
 // once, and the gradient is written from the same copy.  The record's logits
@@ -207,18 +367,24 @@ constexpr int kTileThreads = 256, kTileWarps = kTileThreads / 32;
 // gradients are formed by the thread that holds the entry.
 // TWO: labels at a temperature other than 1, which need a second softmax.
 template <typename T, bool TWO>
-__global__ void __launch_bounds__(kTileThreads, 3)
+__global__ void __launch_bounds__(kTileThreads, TWO ? 4 : 5)
 distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     using P = Piece<T>;
+    constexpr int H = P::N / 2;
     extern __shared__ __align__(16) unsigned char raw[];
     T* tile = reinterpret_cast<T*>(raw);
     uint4* tile16 = reinterpret_cast<uint4*>(raw);
     __shared__ DistillStats stats[kMaxCluster];
-    __shared__ float kl_part[kMaxCluster];
-    __shared__ float fbuf[3][kTileWarps];
+    __shared__ float kl_part[kMaxCluster * kTileWarps];
+    __shared__ float mbuf[kTileWarps], tbuf[kTileWarps], nbuf[kTileWarps], qbuf[kTileWarps];
+    __shared__ float rest_buf[kTileWarps], member_buf[kTileWarps], sz_buf[kTileWarps];
     __shared__ double dbuf[kTileWarps];
+    __shared__ int table[kClassTable];
     __shared__ int classes[kMaxTop];
     __shared__ float probs[kMaxTop];
+    __shared__ double own_q[kMaxTop];
+    __shared__ float own_t[kMaxTop];
+    __shared__ int any_s, label_on_s, repeated_s, n_own;
     grid_dependency_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const unsigned rank = cluster_rank(), blocks = cluster_size();
@@ -227,21 +393,30 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     const T* z = Z + row * a.ld;
     T* g = dZ ? dZ + row * a.ldg : nullptr;
     const RowSlice<T> slice(z, V, rank, blocks);
+    const int w0 = slice.whole0(), w1 = slice.whole1(V);
     const bool wide = a.incg == 1 && ((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(z)) & 15u) == 0;
     const float wt = a.weight ? a.weight[row] : 1.0f / (float)a.T;
+    int ev = tid < K ? a.idx[row * K + tid] : -1;
+    const float tval = tid < K ? a.val[row * K + tid] : 0.f;
+    const int label = a.labels && a.ce != 0.f ? a.labels[row] : -1;
 
     // the gradient zero, for rows that do not count
     auto zero_row = [&]() {
-        if (g)
-            for (int j = tid; j < slice.n; j += kTileThreads) {
-                const int v = slice.first + j * P::N;
-                if (wide && v >= 0 && v + P::N <= V) {
-                    *reinterpret_cast<uint4*>(g + v) = make_uint4(0, 0, 0, 0);
-                } else {
-                    for (int i = 0; i < P::N; ++i)
-                        if (v + i >= 0 && v + i < V) g[(long long)(v + i) * a.incg] = logit_of<T>(0.f);
+        if (g) {
+            if (wide) {
+                for (int j = w0 + tid; j < w1; j += kTileThreads)
+                    *reinterpret_cast<uint4*>(g + slice.first + j * P::N) = make_uint4(0, 0, 0, 0);
+                if (tid < 2 * P::N) {
+                    const int j = tid < P::N ? 0 : slice.n - 1, v = slice.first + j * P::N + tid % P::N;
+                    if (slice.n > 0 && (j < w0 || j >= w1) && v >= 0 && v < V) g[v] = logit_of<T>(0.f);
+                }
+            } else {
+                for (int p = tid; p < slice.n * P::N; p += kTileThreads) {
+                    const int v = slice.first + p;
+                    if (v >= 0 && v < V) g[(long long)v * a.incg] = logit_of<T>(0.f);
                 }
             }
+        }
         if (rank == 0 && tid == 0) a.row_loss[row] = 0.f;
     };
     if (wt == 0.f) {   // the same for every block of the row
@@ -252,66 +427,84 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
 
     // the record: thread k holds entry k; it is this block's when its class
     // lies in the slice
-    int ev = -1, place = -1;
-    float t = BITLOGIC_NEG_INF, q = 0.f, logq = 0.f;
-    double q64 = 0.0;
-    if (tid < K) {
-        ev = a.idx[row * K + tid];
-        if (ev >= V) {
-            if (rank == 0) flag_index_error();
-            ev = -1;
-        }
-        if (ev < 0) {
-            ev = -1;
-        } else {
-            t = a.val[row * K + tid] * a.inv_tau;
-            place = slice.place(ev);
-        }
+    for (int i = tid; i < kClassTable; i += kTileThreads) table[i] = -1;
+    if (tid == 0) any_s = label_on_s = repeated_s = n_own = 0;
+    if (ev >= V) {
+        if (rank == 0) flag_index_error();
+        ev = -1;
     }
-    const int label = a.labels && a.ce != 0.f ? a.labels[row] : -1;
+    if (ev < 0) ev = -1;
+    const float t = ev >= 0 ? tval * a.inv_tau : BITLOGIC_NEG_INF;
+    const int place = slice.place(ev);
     const bool label_ok = label >= 0 && label < V;
     if (label >= V && rank == 0 && tid == 0) flag_index_error();
-    const bool any = __syncthreads_or(ev >= 0) != 0;
-    const bool label_on = label_ok && __syncthreads_or(ev == label) != 0;
-    float Q = 0.f;
+    const int label_place = label_ok ? slice.place(label) : -1;
+    float q = 0.f, logq = 0.f, Q = 0.f;
+    double q64 = 0.0;
     if (a.teacher_lse) {
-        if (place >= 0 && t != BITLOGIC_NEG_INF) {
-            const double d = (double)a.val[row * K + tid] * a.inv_tau64 - (double)a.teacher_lse[row];
-            logq = (float)d;
-            q64 = exp(d);
+        // the slice's entries side by side, so that few warps run the double
+        // precision exponentials (4 of 128 entries' warps, each a quarter
+        // full, kept the FP64 pipe busy for a third of the kernel)
+        const double norm = (double)a.teacher_lse[row];
+        const bool own = place >= 0 && t != BITLOGIC_NEG_INF;
+        __syncthreads();
+        int slot = 0;
+        if (own) {
+            slot = atomicAdd(&n_own, 1);
+            own_t[slot] = tval;
+        }
+        __syncthreads();
+        if (tid < n_own) own_q[tid] = exp((double)own_t[tid] * a.inv_tau64 - norm);
+        __syncthreads();
+        if (own) {
+            q64 = own_q[slot];
+            logq = (float)((double)tval * a.inv_tau64 - norm);
             q = (float)q64;
         }
-    } else {
-        const float tm = block_largest(t, fbuf[0], kTileWarps), ts = isinf(tm) ? 0.f : tm;
-        const float norm = ts + logf(block_add(exp2_unit((t - ts) * kLog2E), fbuf[1], kTileWarps));
-        logq = t - norm;
+    } else {   // softmax over the record
+        const float wm = warp_largest(t);
+        if (lane == 0) tbuf[warp] = wm;
+        __syncthreads();
+        float tm = tbuf[0];
+        for (int w = 1; w < kTileWarps; ++w) tm = fmaxf(tm, tbuf[w]);
+        const float ts = isinf(tm) ? 0.f : tm, ws = warp_add(exp2_unit((t - ts) * kLog2E));
+        if (lane == 0) nbuf[warp] = ws;
+        __syncthreads();
+        float sum = 0.f;
+        for (int w = 0; w < kTileWarps; ++w) sum += nbuf[w];
+        logq = t - (ts + logf(sum));
         q = t == BITLOGIC_NEG_INF ? 0.f : exp2_unit(logq * kLog2E);
-        Q = block_add(q, fbuf[2], kTileWarps);
+        const float wq = warp_add(q);
+        if (lane == 0) qbuf[warp] = wq;
+    }
+    // entries of one class: the second finds the first in the table
+    if (ev >= 0) any_s = 1;
+    if (label_ok && ev == label) label_on_s = 1;
+    if (place >= 0) {
+        unsigned h = ((unsigned)ev * 2654435761u) >> 23;
+        for (int i = 0; i < kClassTable; ++i, h = (h + 1) % kClassTable) {
+            const int was = atomicCAS(&table[h], -1, ev);
+            if (was == ev) repeated_s = 1;
+            if (was == -1 || was == ev) break;
+        }
     }
 
     cp_async_wait<0>();
     __syncthreads();
+    // the largest of the slice, and the logits that are taken out of it
     const float zk = place >= 0 ? logit_value(tile[place]) : 0.f;
-    const int label_place = label_ok ? slice.place(label) : -1;
     const float z_label = label_place >= 0 ? logit_value(tile[label_place]) : 0.f;
-    __syncthreads();
-    // entries of one class write their number to the same place: the ones that
-    // do not find it there again are repeated
-    auto mark = [&](int n) {
-        if constexpr (sizeof(T) == 4) reinterpret_cast<int*>(tile)[place] = n;
-        else reinterpret_cast<short*>(tile)[place] = (short)n;
-    };
-    auto marked = [&]() -> int {
-        if constexpr (sizeof(T) == 4) return reinterpret_cast<int*>(tile)[place];
-        else return reinterpret_cast<short*>(tile)[place];
-    };
-    if (place >= 0) mark(tid);
-    __syncthreads();
-    const bool repeated = __syncthreads_or(place >= 0 && marked() != tid) != 0;
-    if (place >= 0) tile[place] = masked_logit<T>();
+    typename P::Max mx = P::lowest();
+#pragma unroll 4
+    for (int j = tid; j < slice.n; j += kTileThreads) mx = P::largest(mx, tile16[j]);
+    float m = warp_largest(P::value(mx));
+    if (lane == 0) mbuf[warp] = m;
+    const bool any = any_s != 0, label_on = label_on_s != 0;
+    if (!a.teacher_lse)
+        for (int w = 0; w < kTileWarps; ++w) Q += qbuf[w];
     bool first = place >= 0;
     float q_class = q;   // of all places of the class
-    if (repeated) {
+    if (repeated_s) {
         if (tid < K) {
             classes[tid] = ev;
             probs[tid] = q;
@@ -327,54 +520,56 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
         }
     }
     __syncthreads();
+    if (place >= 0) tile[place] = masked_logit<T>();
+    for (int w = 0; w < kTileWarps; ++w) m = fmaxf(m, mbuf[w]);
+    __syncthreads();
 
-    // statistics of the slice about its own largest
-    typename P::Max mx = P::lowest();
-#pragma unroll 4
-    for (int j = tid; j < slice.n; j += kTileThreads) mx = P::largest(mx, tile16[j]);
-    float m = P::value(mx);
-    if (first) m = fmaxf(m, zk);
-    m = block_largest(m, fbuf[0], kTileWarps);
+    // powers of the slice about its own largest
     const float cy = kLog2E * a.inv_tau;
     {
-        const float ms = m == BITLOGIC_NEG_INF ? 0.f : m;
-        const PowerBase py(ms, cy), pz(ms, kLog2E);
-        float r0 = 0.f, r1 = 0.f, s0 = 0.f, s1 = 0.f;
+        const PowerBase by(m, cy), bz(m, kLog2E), ey = far_alike(by, bz), ez = far_alike(bz, by);
+        f32x2 r0 = 0, r1 = 0, s0 = 0, s1 = 0;   // two zeros each
+        auto sums = [&](const auto& py, const auto& pz) {
 #pragma unroll 2
-        for (int j = tid; j < slice.n; j += kTileThreads) {
-            float x[P::N];
-            P::load(tile16[j], x);
+            for (int j = tid; j < slice.n; j += kTileThreads) {
+                f32x2 x[H];
+                load_pairs<T>(tile16[j], x);
 #pragma unroll
-            for (int i = 0; i < P::N; i += 2) {
-                r0 += py(x[i]);
-                r1 += py(x[i + 1]);
-                if (TWO) {
-                    s0 += pz(x[i]);
-                    s1 += pz(x[i + 1]);
+                for (int i = 0; i < H; i += 2) {
+                    r0 = add2(r0, py(x[i]));
+                    r1 = add2(r1, py(x[i + 1]));
+                    if (TWO) {
+                        s0 = add2(s0, pz(x[i]));
+                        s1 = add2(s1, pz(x[i + 1]));
+                    }
                 }
             }
-        }
-        const float member = warp_add(first ? py(zk) : 0.f);
-        const float rest = warp_add(r0 + r1), sz = TWO ? warp_add(s0 + s1 + (first ? pz(zk) : 0.f)) : 0.f;
-        q64 = a.teacher_lse ? warp_add(q64) : 0.0;
-        __syncthreads();
+        };
+        if (ey.far) sums(FarPairs(ey), FarPairs(ez));
+        else sums(NearPairs(ey), NearPairs(ez));
+        float ra, rb, sa, sb;
+        unpack2(add2(r0, r1), ra, rb);
+        unpack2(add2(s0, s1), sa, sb);
+        const float rest = warp_add(ra + rb), member = warp_add(first ? ey.power(zk) : 0.f);
+        const float sz = TWO ? warp_add(sa + sb + (first ? ez.power(zk) : 0.f)) : 0.f;
+        if (a.teacher_lse) q64 = warp_add(q64);
         if (lane == 0) {
-            fbuf[0][warp] = rest;
-            fbuf[1][warp] = member;
-            fbuf[2][warp] = sz;
+            rest_buf[warp] = rest;
+            member_buf[warp] = member;
+            sz_buf[warp] = sz;
             dbuf[warp] = q64;
         }
-        __syncthreads();
-        if (tid < (int)blocks) {
-            DistillStats s = {0.0, m, 0.f, 0.f, 0.f, z_label, label_place >= 0};
-            for (int w = 0; w < kTileWarps; ++w) {
-                s.rest += fbuf[0][w];
-                s.member += fbuf[1][w];
-                s.sz += fbuf[2][w];
-                s.q += dbuf[w];
-            }
-            put_in_block(&stats[rank], tid, s);
+    }
+    __syncthreads();
+    if (tid < (int)blocks) {
+        DistillStats s = {0.0, m, 0.f, 0.f, 0.f, z_label, label_place >= 0};
+        for (int w = 0; w < kTileWarps; ++w) {
+            s.rest += rest_buf[w];
+            s.member += member_buf[w];
+            s.sz += sz_buf[w];
+            s.q += dbuf[w];
         }
+        put_in_block(&stats[rank], tid, s);
     }
     if (blocks > 1) {
         cluster_arrive();
@@ -386,15 +581,16 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     // statistics of the row
     m = stats[0].m;
     for (unsigned b = 1; b < blocks; ++b) m = fmaxf(m, stats[b].m);
-    if (m == BITLOGIC_NEG_INF) m = 0.f;
+    const PowerBase ny(m, cy), nz(m, kLog2E), by = far_alike(ny, nz), bz = far_alike(nz, ny);
     float rest = 0.f, s = 0.f, sz = 0.f, zl = 0.f;
     double q_sum = 0.0;
     for (unsigned b = 0; b < blocks; ++b) {
         const DistillStats& o = stats[b];
-        const float d = o.m == BITLOGIC_NEG_INF ? 0.f : o.m - m, f = exp2_unit(d * cy);
+        const PowerBase oy(o.m, cy), oz(o.m, kLog2E);
+        const float f = far_alike(oy, oz).to(by);
         rest += o.rest * f;
         s += o.member * f;
-        if (TWO) sz += o.sz * exp2_unit(d * kLog2E);
+        if (TWO) sz += o.sz * far_alike(oz, oy).to(bz);
         q_sum += o.q;
         if (o.has_label) zl = o.z_label;
     }
@@ -406,11 +602,11 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
         Q = (float)q_sum;
         if (any && rest > 0.f) qr = (float)fmax(1.0 - q_sum, 0.0);
     }
-    const float log_s = logf(s);
+    const float log2_s = log2f(s);
     {
-        const float term = place >= 0 && q > 0.f ? q * (logq - ((zk - m) * a.inv_tau - log_s)) : 0.f;
-        const float part = block_add(term, fbuf[0], kTileWarps);
-        if (tid == 0) put_in_block(&kl_part[rank], 0, part);
+        const float term = place >= 0 && q > 0.f ? q * (logq - kLn2 * (by.exponent(zk) - log2_s)) : 0.f;
+        const float part = warp_add(term);
+        if (lane == 0) store_in_block(&kl_part[rank * kTileWarps + warp], 0, __float_as_uint(part));
     }
     if (blocks > 1) cluster_arrive();
     else __syncthreads();
@@ -421,52 +617,59 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     } else if (g) {
         const float ay = wt * a.grad_scale * a.kd * a.inv_tau, az = label_ok ? wt * a.grad_scale * a.ce : 0.f;
         const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) / s - (qr > 0.f ? qr / rest : 0.f));
-        const float iz = label_ok ? az / sz : 0.f;
-        const PowerBase py(m, cy), pz(m, kLog2E);
-        const float fy = TWO ? off : off + iz;
+        const float iz = label_ok ? az / sz : 0.f, fy = TWO ? off : off + iz;
+        auto gradient = [&](const auto& py, const auto& pz) {
+            const f32x2 fy2 = pack2(fy, fy), fz2 = pack2(iz, iz);
+            uint4* to16 = wide ? reinterpret_cast<uint4*>(g + slice.first) : tile16;   // written at whole pieces
 #pragma unroll 2
-        for (int j = tid; j < slice.n; j += kTileThreads) {
-            float x[P::N];
-            P::load(tile16[j], x);
+            for (int j = tid; j < slice.n; j += kTileThreads) {
+                f32x2 x[H];
+                load_pairs<T>(tile16[j], x);
+                float y[P::N];
 #pragma unroll
-            for (int i = 0; i < P::N; ++i) x[i] = TWO ? fmaf(py(x[i]), fy, pz(x[i]) * iz) : py(x[i]) * fy;
-            const uint4 u = P::pack(x);
-            const int v = slice.first + j * P::N;
-            if (!wide) {
-                tile16[j] = u;
-            } else if (v >= 0 && v + P::N <= V) {
-                *reinterpret_cast<uint4*>(g + v) = u;
-            } else {
-#pragma unroll
-                for (int i = 0; i < P::N; ++i)
-                    if (v + i >= 0 && v + i < V) g[v + i] = logit_of<T>(x[i]);
+                for (int i = 0; i < H; ++i) {
+                    f32x2 v = mul2(py(x[i]), fy2);
+                    if (TWO) v = fma2(pz(x[i]), fz2, v);
+                    unpack2(v, y[2 * i], y[2 * i + 1]);
+                }
+                const uint4 u = P::pack(y);
+                if (!wide || (j >= w0 && j < w1)) to16[j] = u;
+                else tile16[j] = u;
             }
-        }
+        };
+        if (by.far) gradient(FarPairs(by), FarPairs(bz));
+        else gradient(NearPairs(by), NearPairs(bz));
         __syncthreads();
         // the record's classes and the label, over what the pass wrote there
-        T* to = wide ? g + slice.first : tile;
+        auto put = [&](int p, float x) {
+            const int j = p / P::N;
+            if (wide && j >= w0 && j < w1) g[slice.first + p] = logit_of<T>(x);
+            else tile[p] = logit_of<T>(x);
+        };
         if (first) {
-            float x = exp2_unit((zk - m) * cy) * on - ay * q_class;
-            if (label_ok) x += exp2_unit((zk - m) * kLog2E) * iz - (ev == label ? az : 0.f);
-            to[place] = logit_of<T>(x);
+            float x = by.power(zk) * on - ay * q_class;
+            if (label_ok) x += bz.power(zk) * iz - (ev == label ? az : 0.f);
+            put(place, x);
         }
-        if (tid == 0 && label_place >= 0 && !label_on)
-            to[label_place] = logit_of<T>(exp2_unit((z_label - m) * cy) * off + exp2_unit((z_label - m) * kLog2E) * iz - az);
+        if (tid == 0 && label_place >= 0 && !label_on) put(label_place, by.power(z_label) * off + bz.power(z_label) * iz - az);
+        __syncthreads();
         if (!wide) {   // gradient places apart from the logits' or at another alignment
-            __syncthreads();
             for (int p = tid; p < slice.n * P::N; p += kTileThreads) {
                 const int v = slice.first + p;
                 if (v >= 0 && v < V) g[(long long)v * a.incg] = tile[p];
             }
+        } else if (tid < 2 * P::N) {   // the pieces at the row's ends
+            const int j = tid < P::N ? 0 : slice.n - 1, p = j * P::N + tid % P::N, v = slice.first + p;
+            if (slice.n > 0 && (j < w0 || j >= w1) && v >= 0 && v < V) g[v] = tile[p];
         }
     }
     if (blocks > 1) cluster_wait();
     if (rank == 0 && tid == 0 && !empty) {
         float kl = 0.f;
-        for (unsigned b = 0; b < blocks; ++b) kl += kl_part[b];
+        for (unsigned b = 0; b < blocks * kTileWarps; ++b) kl += kl_part[b];
         if (qr > 0.f) kl += qr * (logf(qr) - logf(rest / s));
         float loss = a.kd != 0.f ? a.kd * kl : 0.f;
-        if (label_ok) loss += a.ce * (logf(sz) - (zl - m));
+        if (label_ok) loss += a.ce * kLn2 * (log2f(sz) - bz.exponent(zl));
         a.row_loss[row] = s != s ? s : loss;
     }
 }
@@ -665,14 +868,18 @@ distill_narrow_kernel(const T* Z, T* dZ, Distill a) {
     }
 }
 
-// Slices of at most this many bytes leave room for three blocks on an SM: one
-// loads while another computes or writes.
-constexpr int kTileFit = 70 * 1024, kTileMost = 208 * 1024, kTileLeast = 8 * 1024;
+// Blocks per row.  Slices up to 100 KB (two blocks on an SM) beat more and
+// shorter ones: what a block does besides its bytes takes 5 us or more, and the
+// more so the more blocks exchange statistics (bf16, 2^30 logits in all: rows of
+// 64 KB in one block 758 us, of 128 KB in two 835, of 256 KB in four 895; the
+// 256 KB rows in eight slices of 32 KB 1115 us; 509 fp32 rows of 200 KB in two
+// 51.7 us, in four 55.9 us).
+constexpr int kTileFit = 100 * 1024, kTileMost = 208 * 1024, kTileLeast = 8 * 1024;
 
 template <typename T, bool TWO>
 int launch_distill(const T* z, T* dz, const Distill& a, cudaStream_t stream) {
     cudaError_t e;
-    const int blocks = a.V <= kNarrow ? 1 : blocks_per_row(a.T, a.V, sizeof(T), kTileFit, kTileMost, kTileLeast);
+    const int blocks = blocks_per_row(a.T, a.V, sizeof(T), kTileFit, kTileMost, kTileLeast);
     if (a.V <= kNarrow) {
         const size_t smem = kNarrowWarps * (a.K * sizeof(NarrowEntry) + narrow_row_floats(a.V) * sizeof(float));
         e = launch_rows(distill_narrow_kernel<T, TWO>, (a.T + kNarrowWarps - 1) / kNarrowWarps, 1, kNarrowWarps * 32, smem,
@@ -681,8 +888,8 @@ int launch_distill(const T* z, T* dz, const Distill& a, cudaStream_t stream) {
         const size_t smem = (size_t)slice_bytes(a.V, sizeof(T), blocks);
         e = launch_rows(distill_tile_kernel<T, TWO>, a.T, blocks, kTileThreads, smem, stream, z, dz, a);
     } else {
-        const size_t smem = (size_t)(a.V + 31) / 32 * 4;
-        e = launch_rows(distill_stream_kernel<T>, a.T, 1, kDistillThreads, smem, stream, z, dz, a);
+        const size_t smem = kRing * kRowThreads * 16 + (size_t)(slice_bytes(a.V, sizeof(T), 1) / sizeof(T) + 31) / 32 * 4;   // and a bit per place
+        e = launch_rows(distill_row_kernel<T, TWO>, a.T, 1, kRowThreads, smem, stream, z, dz, a);
     }
     return e == cudaSuccess ? launch_status() : (int)BITLOGIC_ERR_CUDA;
 }

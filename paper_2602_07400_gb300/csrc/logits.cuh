@@ -9,6 +9,7 @@
 #include <cuda_fp16.h>
 
 #include <climits>
+#include <cmath>
 
 #include "common.cuh"
 
@@ -19,7 +20,7 @@ constexpr int kMaxTop = 256;           // entries of a record
 
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-#define BITLOGIC_NEG_INF (-__int_as_float(0x7f800000))
+#define BITLOGIC_NEG_INF (-HUGE_VALF)
 
 __device__ __forceinline__ float logit_value(float x) { return x; }
 __device__ __forceinline__ float logit_value(__nv_bfloat16 x) { return __bfloat162float(x); }

@@ -8,6 +8,7 @@
 #pragma once
 
 #include "logits.cuh"
+#include "packed.cuh"
 
 namespace bitlogic {
 
@@ -225,6 +226,62 @@ template <> __device__ __forceinline__ int masked_logit<int>() { return INT_MIN;
 template <> __device__ __forceinline__ __nv_bfloat16 masked_logit<__nv_bfloat16>() { return __ushort_as_bfloat16(0xff80); }
 template <> __device__ __forceinline__ __half masked_logit<__half>() { return __ushort_as_half(0xfc00); }
 
+// The values of a piece as pairs, and pairs rounded back into a piece.
+template <typename T>
+__device__ __forceinline__ void load_pairs(const uint4& u, f32x2 (&z)[Piece<T>::N / 2]) {
+    float x[Piece<T>::N];
+    Piece<T>::load(u, x);
+#pragma unroll
+    for (int i = 0; i < Piece<T>::N / 2; ++i) z[i] = pack2(x[2 * i], x[2 * i + 1]);
+}
+
+// 2^v of both elements
+__device__ __forceinline__ f32x2 exp2_pair(f32x2 v) {
+    float a, b;
+    unpack2(v, a, b);
+    return pack2(exp2_unit(a), exp2_unit(b));
+}
+
+// The exponents c z - base of a slice's powers, the base near c m for the
+// slice's largest logit m: one multiply-add each where c m is below 2^28 (the
+// base is then rint(c m), so that bases of slices differ by whole numbers), the
+// difference z - m first where it is not, which keeps the digits that equal or
+// nearby logits of that size differ in.
+struct PowerBase {
+    float c, m, b;
+    bool far, none;   // none: no logit in the sum
+    __device__ __forceinline__ PowerBase(float largest, float c_)
+        : c(c_), m(largest == BITLOGIC_NEG_INF ? 0.f : largest), none(largest == BITLOGIC_NEG_INF) {
+        const float mc = m * c;
+        far = !(fabsf(mc) < 268435456.0f);
+        b = far ? 0.f : rintf(mc);
+    }
+    __device__ __forceinline__ float exponent(float z) const { return far ? (z - m) * c : fmaf(z, c, -b); }
+    __device__ __forceinline__ float power(float z) const { return exp2_unit(exponent(z)); }
+    // the factor that takes a sum about this base to one about `row`
+    __device__ __forceinline__ float to(const PowerBase& row) const {
+        if (none) return 1.f;   // of a sum of 0, or of NaN
+        if (!row.far) return exp2_unit(far ? fmaf(m, c, -row.b) : b - row.b);
+        return exp2_unit((m - row.m) * c - (far ? 0.f : fmaf(m, c, -b)));
+    }
+};
+// `p`, far where either of two bases about one logit is.
+__device__ __forceinline__ PowerBase far_alike(PowerBase p, const PowerBase& other) {
+    p.far = p.far || other.far;
+    if (p.far) p.b = 0.f;
+    return p;
+}
+struct NearPairs {
+    f32x2 c, nb;
+    __device__ __forceinline__ explicit NearPairs(const PowerBase& p) : c(pack2(p.c, p.c)), nb(pack2(-p.b, -p.b)) {}
+    __device__ __forceinline__ f32x2 operator()(f32x2 z) const { return exp2_pair(fma2(z, c, nb)); }
+};
+struct FarPairs {
+    f32x2 c, m;
+    __device__ __forceinline__ explicit FarPairs(const PowerBase& p) : c(pack2(p.c, p.c)), m(pack2(p.m, p.m)) {}
+    __device__ __forceinline__ f32x2 operator()(f32x2 z) const { return exp2_pair(mul2(sub2(z, m), c)); }
+};
+
 // A block's slice: pieces [0, n), piece j holding classes first + N j + i.
 template <typename T>
 struct RowSlice {
@@ -239,18 +296,22 @@ struct RowSlice {
         n = min(all, p0 + per) - p0;
         first = p0 * N - shift;
     }
+    // Pieces [whole0, whole1) lie in the row in full; at most one before and
+    // one after do not.
+    __device__ __forceinline__ int whole0() const { return first < 0 && n > 0 ? 1 : 0; }
+    __device__ __forceinline__ int whole1(int V) const { return n > 0 && first + n * N > V ? max(whole0(), n - 1) : n; }
     // Copies on their way; finish with cp_async_wait<0>() and a barrier.
     __device__ __forceinline__ void copy(const T* x, int V, T* tile, int tid, int threads) const {
-        for (int j = tid; j < n; j += threads) {
-            const int v = first + j * N;
-            if (v >= 0 && v + N <= V) {
-                cp_async16(tile + j * N, x + v);
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) tile[j * N + i] = v + i >= 0 && v + i < V ? x[v + i] : masked_logit<T>();
-            }
-        }
+        const int w0 = whole0(), w1 = whole1(V);
+        const T* from = x + first;   // read at whole pieces only
+#pragma unroll 4
+        for (int j = w0 + tid; j < w1; j += threads) cp_async16(tile + j * N, from + j * N);
         cp_async_commit();
+        // the places of the pieces at the row's ends, by element
+        if (tid < 2 * N) {
+            const int j = tid < N ? 0 : n - 1, p = j * N + tid % N, v = first + p;
+            if (n > 0 && (j < w0 || j >= w1)) tile[p] = v >= 0 && v < V ? x[v] : masked_logit<T>();
+        }
     }
     // Place of class v in the slice, or -1.
     __device__ __forceinline__ int place(int v) const {
