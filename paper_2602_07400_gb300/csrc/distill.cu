@@ -40,43 +40,19 @@ struct Distill {
 };
 
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
-constexpr int kRing = 8;   // places of a thread's ring: one piece in use, the others in flight
-
-// Powers summed about a running base: the base moves up with the largest logit
-// seen, and the sums with it.
-struct RunningSum {
-    float m = BITLOGIC_NEG_INF;
-    f32x2 y0 = 0, y1 = 0, z0 = 0, z1 = 0;   // powers at tau and at 1, two zeros each
-
-    template <bool TWO>
-    __device__ __forceinline__ void raise(float to, float cy) {
-        const PowerBase oy(m, cy), oz(m, kLog2E), ny(to, cy), nz(to, kLog2E);
-        const float f = far_alike(oy, oz).to(far_alike(ny, nz));
-        y0 = mul2(y0, pack2(f, f));
-        y1 = mul2(y1, pack2(f, f));
-        if (TWO) {
-            const float h = far_alike(oz, oy).to(far_alike(nz, ny));
-            z0 = mul2(z0, pack2(h, h));
-            z1 = mul2(z1, pack2(h, h));
-        }
-        m = to;
-    }
-};
 
 // Rows too long for the shared memory of a cluster: a block per row, which
-// streams it once for the statistics and a second time, from L2, for the
-// gradient.  The classes on the record are marked in a bit map by place, and the
-// marked ones of a piece are taken out of its sum.  (On shorter rows it takes
-// 983 us where the tile kernel takes 893, 8192 x 131072 bf16.)
+// streams it from memory once for the statistics and a second time, most of it
+// from L2, for the gradient (8192 x 131072 bf16: 907 us, the tile kernel 893).
+// The classes on the record are
+// marked in a bit map by place, and the pieces that hold any in a mask per
+// thread, whose marked ones are taken out of their sum.
 template <typename T, bool TWO>
-__global__ void __launch_bounds__(kRowThreads, 4)
+__global__ void __launch_bounds__(kRowThreads, 3)
 distill_row_kernel(const T* Z, T* dZ, Distill a) {
     using P = Piece<T>;
     constexpr int N = P::N, H = N / 2;
     extern __shared__ __align__(16) unsigned char raw[];
-    uint4* ring = reinterpret_cast<uint4*>(raw) + threadIdx.x;   // this thread's places, kRowThreads apart
-    const uint8_t* marks8 = raw + kRing * kRowThreads * 16;
-    uint32_t* marks = reinterpret_cast<uint32_t*>(raw + kRing * kRowThreads * 16);
     __shared__ float tbuf[kRowWarps], nbuf[kRowWarps], qbuf[kRowWarps], mbuf[kRowWarps], kbuf[kRowWarps];
     __shared__ float rest_buf[kRowWarps], member_buf[kRowWarps], sz_buf[kRowWarps];
     __shared__ double dbuf[kRowWarps];
@@ -92,46 +68,18 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
     const RowSlice<T> slice(z, V, 0, 1);
     const int w0 = slice.whole0(), w1 = slice.whole1(V);
     const bool wide = a.incg == 1 && ((reinterpret_cast<uintptr_t>(g) ^ reinterpret_cast<uintptr_t>(z)) & 15u) == 0;
+    const PieceStream<T, kRowThreads> stream(z, slice, V, tid);
+    const int words = (stream.batches + 7) / 8;   // of a thread's mask
+    uint32_t* masks = reinterpret_cast<uint32_t*>(raw);              // [words][kRowThreads]
+    uint32_t* marks = masks + words * kRowThreads;                   // a bit per place
+    const uint8_t* marks8 = reinterpret_cast<const uint8_t*>(marks);
     const float wt = a.weight ? a.weight[row] : 1.0f / (float)a.T;
     int ev = tid < K ? a.idx[row * K + tid] : -1;
     const float tval = tid < K ? a.val[row * K + tid] : 0.f;
     const int label = a.labels && a.ce != 0.f ? a.labels[row] : -1;
+    // the pieces at the row's ends, of threads 0 and 32
+    const int j_end = tid == 0 && w0 > 0 ? 0 : tid == 32 && w1 < slice.n ? w1 : -1;
 
-    // a piece at the row's ends, by element; places outside it are masked
-    auto end_piece = [&](int j) {
-        T x[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int v = slice.first + j * N + i;
-            x[i] = v >= 0 && v < V ? z[v] : masked_logit<T>();
-        }
-        return *reinterpret_cast<uint4*>(x);
-    };
-    // whole pieces by the ring, each thread its own: from `start` on, every
-    // piece handed to `use` while the ones after it are on their way
-    const T* from = z + slice.first;   // read at whole pieces
-    auto start = [&]() {
-#pragma unroll
-        for (int i = 0; i < kRing - 1; ++i) {
-            const int j = w0 + tid + i * kRowThreads;
-            if (j < w1) cp_async16(ring + i * kRowThreads, from + j * N);
-            cp_async_commit();
-        }
-    };
-    auto stream = [&](auto&& use) {
-        int at = 0;
-        for (int j = w0 + tid; j < w1; j += kRowThreads) {
-            cp_async_wait<kRing - 2>();
-            const uint4 u = ring[at * kRowThreads];
-            const int next = j + (kRing - 1) * kRowThreads;
-            if (next < w1) cp_async16(ring + (at == 0 ? kRing - 1 : at - 1) * kRowThreads, from + next * N);
-            cp_async_commit();
-            use(j, u);
-            at = at == kRing - 1 ? 0 : at + 1;
-        }
-        if (tid == 0 && w0 > 0) use(0, end_piece(0));   // the pieces at the row's ends
-        if (tid == 32 && w1 < slice.n) use(w1, end_piece(w1));
-    };
     auto store = [&](int j, const float (&y)[N]) {
         if (wide && j >= w0 && j < w1) {
             __stcs(reinterpret_cast<uint4*>(g + slice.first) + j, P::pack(y));
@@ -152,10 +100,12 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
         zero_row();
         return;
     }
-    start();
+    uint4 ua[4], ub[4];
+    stream.load(0, ua);
+    stream.load(1, ub);
 
     // the record: thread k holds entry k
-    for (int i = tid; i < (slice.n * N + 31) / 32; i += kRowThreads) marks[i] = 0u;
+    for (int i = tid; i < words * kRowThreads + (slice.n * N + 31) / 32; i += kRowThreads) masks[i] = 0u;
     if (tid == 0) any_s = label_on_s = repeated_s = 0;
     if (ev >= V) {
         flag_index_error();
@@ -171,43 +121,13 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
     if (ev >= 0) {
         any_s = 1;
         if (ev == label) label_on_s = 1;
-        const int p = ev - slice.first;
+        const int p = ev - slice.first, j = p / N - w0;   // piece j: lane j % 32 of warp j / 128 % 8, its (j / 32 % 4)th of batch j / 1024
         if ((atomicOr(&marks[p >> 5], 1u << (p & 31)) >> (p & 31)) & 1u) repeated_s = 1;
-    }
-    __syncthreads();
-
-    // statistics, about a base of each thread's own
-    const float cy = kLog2E * a.inv_tau;
-    RunningSum run;
-    stream([&](int j, uint4 u) {
-        const unsigned on = ((unsigned)marks8[j * N / 8] >> (j * N % 8)) & ((1u << N) - 1u);
-        if (on) {
-            T* x = reinterpret_cast<T*>(&u);
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if ((on >> i) & 1u) x[i] = masked_logit<T>();
+        if (j >= 0 && j < w1 - w0) {
+            const int in = j % (4 * kRowThreads), nth = 4 * (j / (4 * kRowThreads)) + in % 128 / 32;
+            atomicOr(&masks[(nth >> 5) * kRowThreads + in / 128 * 32 + in % 32], 1u << (nth & 31));
         }
-        const float top = P::largest_of(u);
-        if (top > run.m) run.raise<TWO>(top, cy);
-        const PowerBase by(run.m, cy), bz(run.m, kLog2E), ey = far_alike(by, bz), ez = far_alike(bz, by);
-        auto sums = [&](const auto& py, const auto& pz) {
-            f32x2 x[H];
-            load_pairs<T>(u, x);
-#pragma unroll
-            for (int i = 0; i < H; i += 2) {
-                run.y0 = add2(run.y0, py(x[i]));
-                run.y1 = add2(run.y1, py(x[i + 1]));
-                if (TWO) {
-                    run.z0 = add2(run.z0, pz(x[i]));
-                    run.z1 = add2(run.z1, pz(x[i + 1]));
-                }
-            }
-        };
-        if (ey.far) sums(FarPairs(ey), FarPairs(ez));
-        else sums(NearPairs(ey), NearPairs(ez));
-    });
-    if (g) start();   // the second time, while the statistics come together
-
+    }
     // the teacher's probabilities
     float q = 0.f, logq = 0.f, Q = 0.f, q_left = 0.f;
     if (a.teacher_lse) {
@@ -220,6 +140,7 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
         }
         q64 = warp_add(q64);
         if (lane == 0) dbuf[warp] = q64;
+        __syncthreads();
     } else {   // softmax over the record
         const float wm = warp_largest(t);
         if (lane == 0) tbuf[warp] = wm;
@@ -236,6 +157,88 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
         const float wq = warp_add(q);
         if (lane == 0) qbuf[warp] = wq;
     }
+
+    // statistics, about a base of each thread's own that seldom moves
+    const float cy = kLog2E * a.inv_tau;
+    float seen = BITLOGIC_NEG_INF;   // the logit of the base, and the largest
+    typename P::Max mx = P::lowest();
+    PowerBase by(seen, cy), bz(seen, kLog2E);
+    f32x2 y0 = 0, y1 = 0, s0 = 0, s1 = 0;
+    auto sums = [&](const uint4& u, const auto& py, const auto& pz) {
+        f32x2 x[H];
+        load_pairs<T>(u, x);
+#pragma unroll
+        for (int i = 0; i < H; i += 2) {
+            y0 = add2(y0, py(x[i]));
+            y1 = add2(y1, py(x[i + 1]));
+            if (TWO) {
+                s0 = add2(s0, pz(x[i]));
+                s1 = add2(s1, pz(x[i + 1]));
+            }
+        }
+    };
+    auto add = [&](const uint4 (&u)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = P::largest(mx, u[i]);
+        const float top = P::value(mx);
+        if (!by.holds(top) || !bz.holds(top)) {
+            const PowerBase ny(top, cy), nz(top, kLog2E), uy = far_alike(ny, nz), uz = far_alike(nz, ny);
+            const float f = by.to(uy);
+            y0 = mul2(y0, pack2(f, f));
+            y1 = mul2(y1, pack2(f, f));
+            if (TWO) {
+                const float h = bz.to(uz);
+                s0 = mul2(s0, pack2(h, h));
+                s1 = mul2(s1, pack2(h, h));
+            }
+            by = uy;
+            bz = uz;
+        }
+        if (by.far) {
+            const FarPairs py(by), pz(bz);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sums(u[i], py, pz);
+        } else {
+            const NearPairs py(by), pz(bz);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sums(u[i], py, pz);
+        }
+    };
+    auto without_marked = [&](uint4& u, int j) {
+        const unsigned on = ((unsigned)marks8[j * N / 8] >> (j * N % 8)) & ((1u << N) - 1u);
+        T x[N];
+        memcpy(x, &u, 16);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if ((on >> i) & 1u) x[i] = masked_logit<T>();
+        memcpy(&u, x, 16);
+    };
+    auto use = [&](uint4 (&u)[4], int q_, uint32_t mask) {
+        const unsigned marked = (mask >> (4 * (q_ & 7))) & 15u;
+        if (marked) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if ((marked >> i) & 1u) without_marked(u[i], stream.piece(q_, i));
+        }
+        add(u);
+    };
+    for (int b = 0; b < stream.batches; b += 2) {
+        const uint32_t mask = masks[(b >> 3) * kRowThreads + tid];
+        use(ua, b, mask);
+        if (b + 2 < stream.batches) stream.load(b + 2, ua);
+        if (b + 1 < stream.batches) use(ub, b + 1, mask);
+        if (b + 3 < stream.batches) stream.load(b + 3, ub);
+    }
+    if (j_end >= 0) {
+        uint4 e[4] = {end_piece(z, V, slice.first + j_end * N), masked_piece<T>(), masked_piece<T>(), masked_piece<T>()};
+        without_marked(e[0], j_end);
+        add(e);
+    }
+    if (g) {   // the second time, while the statistics come together
+        stream.load(0, ua);
+        stream.load(1, ub);
+    }
+
     bool first = ev >= 0;
     float q_class = q;   // of all places of the class
     if (repeated_s) {
@@ -254,19 +257,18 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
         }
     }
     // the row's base and sums
-    float m = warp_largest(ev >= 0 ? fmaxf(run.m, zk) : run.m);
+    float m = warp_largest(fmaxf(P::value(mx), ev >= 0 ? zk : BITLOGIC_NEG_INF));
     if (lane == 0) mbuf[warp] = m;
     __syncthreads();
     for (int w = 0; w < kRowWarps; ++w) m = fmaxf(m, mbuf[w]);
-    const PowerBase ny(m, cy), nz(m, kLog2E), by = far_alike(ny, nz), bz = far_alike(nz, ny);
+    const PowerBase my(m, cy), mz(m, kLog2E), ry = far_alike(my, mz), rz = far_alike(mz, my);
     {
-        const PowerBase oy(run.m, cy), oz(run.m, kLog2E);
         float ra, rb, sa, sb;
-        unpack2(add2(run.y0, run.y1), ra, rb);
-        unpack2(add2(run.z0, run.z1), sa, sb);
-        const float rest = warp_add((ra + rb) * far_alike(oy, oz).to(by));
-        const float member = warp_add(first ? by.power(zk) : 0.f);
-        const float sz = TWO ? warp_add((sa + sb) * far_alike(oz, oy).to(bz) + (first ? bz.power(zk) : 0.f)) : 0.f;
+        unpack2(add2(y0, y1), ra, rb);
+        unpack2(add2(s0, s1), sa, sb);
+        const float rest = warp_add((ra + rb) * by.to(ry));
+        const float member = warp_add(first ? ry.power(zk) : 0.f);
+        const float sz = TWO ? warp_add((sa + sb) * bz.to(rz) + (first ? rz.power(zk) : 0.f)) : 0.f;
         if (lane == 0) {
             rest_buf[warp] = rest;
             member_buf[warp] = member;
@@ -292,20 +294,19 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
     const bool any = any_s != 0, label_on = label_on_s != 0;
     allow_dependent_launch();
     if (s == 0.f) {   // every class masked: no distribution, no loss
-        cp_async_wait<0>();
         zero_row();
         return;
     }
     const float qr = a.teacher_lse && any && rest > 0.f ? q_left : 0.f, log2_s = log2f(s);
-    const float kl_part = warp_add(q > 0.f ? q * (logq - kLn2 * (by.exponent(zk) - log2_s)) : 0.f);
+    const float kl_part = warp_add(q > 0.f ? q * (logq - kLn2 * (ry.exponent(zk) - log2_s)) : 0.f);
     if (lane == 0) kbuf[warp] = kl_part;
+    const float ay = wt * a.grad_scale * a.kd * a.inv_tau, az = label_ok ? wt * a.grad_scale * a.ce : 0.f;
+    const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) / s - (qr > 0.f ? qr / rest : 0.f));
+    const float iz = label_ok ? az / sz : 0.f, fy = TWO ? off : off + iz;
     if (g) {
-        const float ay = wt * a.grad_scale * a.kd * a.inv_tau, az = label_ok ? wt * a.grad_scale * a.ce : 0.f;
-        const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) / s - (qr > 0.f ? qr / rest : 0.f));
-        const float iz = label_ok ? az / sz : 0.f, fy = TWO ? off : off + iz;
         auto gradient = [&](const auto& py, const auto& pz) {
             const f32x2 fy2 = pack2(fy, fy), fz2 = pack2(iz, iz);
-            stream([&](int j, uint4 u) {
+            auto one = [&](const uint4& u, int j) {
                 f32x2 x[H];
                 load_pairs<T>(u, x);
                 float y[N];
@@ -316,34 +317,40 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
                     unpack2(v, y[2 * i], y[2 * i + 1]);
                 }
                 store(j, y);
-            });
+            };
+            auto all = [&](const uint4 (&u)[4], int b) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (stream.piece(b, i) < stream.j1) one(u[i], stream.piece(b, i));
+            };
+            for (int b = 0; b < stream.batches; b += 2) {
+                all(ua, b);
+                if (b + 2 < stream.batches) stream.load(b + 2, ua);
+                if (b + 1 < stream.batches) all(ub, b + 1);
+                if (b + 3 < stream.batches) stream.load(b + 3, ub);
+            }
+            if (j_end >= 0) one(end_piece(z, V, slice.first + j_end * N), j_end);
         };
-        if (by.far) gradient(FarPairs(by), FarPairs(bz));
-        else gradient(NearPairs(by), NearPairs(bz));
+        if (ry.far) gradient(FarPairs(ry), FarPairs(rz));
+        else gradient(NearPairs(ry), NearPairs(rz));
     }
     __syncthreads();
     if (g) {
         // the record's classes and the label, over what the pass wrote there
         if (first) {
-            float x = by.power(zk) * (wt * a.grad_scale * a.kd * a.inv_tau * (Q + qr) / s) - wt * a.grad_scale * a.kd * a.inv_tau * q_class;
-            if (label_ok) {
-                const float az = wt * a.grad_scale * a.ce;
-                x += bz.power(zk) * (az / sz) - (ev == label ? az : 0.f);
-            }
+            float x = ry.power(zk) * on - ay * q_class;
+            if (label_ok) x += rz.power(zk) * iz - (ev == label ? az : 0.f);
             g[(long long)ev * a.incg] = logit_of<T>(x);
         }
-        if (tid == 0 && label_ok && !label_on) {
-            const float ay = wt * a.grad_scale * a.kd * a.inv_tau, az = wt * a.grad_scale * a.ce;
-            const float off = ay * ((Q + qr) / s - (qr > 0.f ? qr / rest : 0.f));
-            g[(long long)label * a.incg] = logit_of<T>(by.power(z_label) * off + bz.power(z_label) * (az / sz) - az);
-        }
+        if (tid == 0 && label_ok && !label_on)
+            g[(long long)label * a.incg] = logit_of<T>(ry.power(z_label) * off + rz.power(z_label) * iz - az);
     }
     if (tid == 0) {
         float kl = 0.f;
         for (int w = 0; w < kRowWarps; ++w) kl += kbuf[w];
         if (qr > 0.f) kl += qr * (logf(qr) - logf(rest / s));
         float loss = a.kd != 0.f ? a.kd * kl : 0.f;   // a loss of +inf without weight is none
-        if (label_ok) loss += a.ce * kLn2 * (log2f(sz) - bz.exponent(z_label));
+        if (label_ok) loss += a.ce * kLn2 * (log2f(sz) - rz.exponent(z_label));
         a.row_loss[row] = s != s ? s : loss;
     }
 }
@@ -888,7 +895,9 @@ int launch_distill(const T* z, T* dz, const Distill& a, cudaStream_t stream) {
         const size_t smem = (size_t)slice_bytes(a.V, sizeof(T), blocks);
         e = launch_rows(distill_tile_kernel<T, TWO>, a.T, blocks, kTileThreads, smem, stream, z, dz, a);
     } else {
-        const size_t smem = kRing * kRowThreads * 16 + (size_t)(slice_bytes(a.V, sizeof(T), 1) / sizeof(T) + 31) / 32 * 4;   // and a bit per place
+        // a thread's mask bits, by 32 of its pieces, and a bit per place of the row
+        const long long pieces = slice_bytes(a.V, sizeof(T), 1) / 16, words = (pieces + 32 * kRowThreads - 1) / (32 * kRowThreads);
+        const size_t smem = (size_t)(words * kRowThreads + (pieces * (16 / sizeof(T)) + 31) / 32) * 4;
         e = launch_rows(distill_row_kernel<T, TWO>, a.T, 1, kRowThreads, smem, stream, z, dz, a);
     }
     return e == cudaSuccess ? launch_status() : (int)BITLOGIC_ERR_CUDA;

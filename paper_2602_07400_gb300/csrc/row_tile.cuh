@@ -55,11 +55,12 @@ __device__ __forceinline__ unsigned add_in_block(unsigned* p, unsigned rank, uns
 }
 
 // Sorts a[0, size) in falling order, size a power of two (bitonic exchanges);
-// called by the whole block.
+// called by the whole block.  Exchanges over 32 places or fewer stay within the
+// 64 places that a warp's 32 pairs cover, so they need no barrier of the block.
 __device__ __forceinline__ void block_sort_falling(unsigned long long* a, int size) {
+    __syncthreads();
     for (int k = 2; k <= size; k <<= 1)
         for (int j = k >> 1; j > 0; j >>= 1) {
-            __syncthreads();
             for (int i = threadIdx.x; i < size / 2; i += blockDim.x) {
                 const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
                 const unsigned long long x = a[lo], y = a[hi];
@@ -68,6 +69,8 @@ __device__ __forceinline__ void block_sort_falling(unsigned long long* a, int si
                     a[hi] = x;
                 }
             }
+            if (j > 32 || (j == 1 && k >= 64)) __syncthreads();   // the next exchange may span warps
+            else __syncwarp();
         }
     __syncthreads();
 }
@@ -75,15 +78,18 @@ __device__ __forceinline__ void block_sort_falling(unsigned long long* a, int si
 // The logit of a key.
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k ^ 0x80000000u) : ~k); }
 
-// A bound of the largest values that a block's threads hold two of each: the
+// A bound of the largest values that a block's threads hold G of each: the
 // largest key of 16 leading bits that at least `need` of them reach (0 when
 // fewer rank), by 8 bits at a time.  Called by the whole block of 256 threads.
 struct BoundScratch {
     unsigned bins[2][256];
     unsigned digit[2], above;
 };
-__device__ __forceinline__ uint32_t block_bound(float a, float b, unsigned need, BoundScratch* s) {
-    const uint32_t ka = logit_key(a) >> 16, kb = logit_key(b) >> 16;
+template <int G>
+__device__ __forceinline__ uint32_t block_bound(const float (&v)[G], unsigned need, BoundScratch* s) {
+    uint32_t key[G];
+#pragma unroll
+    for (int i = 0; i < G; ++i) key[i] = logit_key(v[i]) >> 16;
     const int tid = threadIdx.x, lane = tid & 31;
     s->bins[0][tid] = s->bins[1][tid] = 0u;
     if (tid == 0) s->digit[0] = s->digit[1] = s->above = 0u;
@@ -92,12 +98,10 @@ __device__ __forceinline__ uint32_t block_bound(float a, float b, unsigned need,
     for (int pass = 0; pass < 2; ++pass) {
         unsigned* bins = s->bins[pass];
         const uint32_t top = s->digit[0];
-        if (pass == 0) {
-            atomicAdd(&bins[ka >> 8], 1u);
-            atomicAdd(&bins[kb >> 8], 1u);
-        } else {
-            if ((ka >> 8) == top) atomicAdd(&bins[ka & 255u], 1u);
-            if ((kb >> 8) == top) atomicAdd(&bins[kb & 255u], 1u);
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            if (pass == 0) atomicAdd(&bins[key[i] >> 8], 1u);
+            else if ((key[i] >> 8) == top) atomicAdd(&bins[key[i] & 255u], 1u);
         }
         __syncthreads();
         if (tid < 32) {   // lane l: bins 255 - 8 l down to 248 - 8 l
@@ -127,8 +131,9 @@ __device__ __forceinline__ uint32_t block_bound(float a, float b, unsigned need,
 // The smallest logit that such a bound lets through.
 __device__ __forceinline__ float bound_logit(uint32_t key) { return key <= kKeyNegInf ? BITLOGIC_NEG_INF : key_logit(key); }
 
-// 16 bytes of logits: their number, their values, their maximum, and the
-// rounding of values back into a piece.
+// 16 bytes of logits: their number, their values, their maximum (in two parts,
+// each of half the piece's logits), and the rounding of values back into a
+// piece.
 template <typename T> struct Piece;
 
 template <> struct Piece<float> {
@@ -142,14 +147,19 @@ template <> struct Piece<float> {
     static __device__ __forceinline__ uint4 pack(const float (&g)[4]) {
         return make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
     }
-    using Max = float;
-    static __device__ __forceinline__ Max lowest() { return BITLOGIC_NEG_INF; }
+    struct Max {
+        float a, b;
+    };
+    static __device__ __forceinline__ Max lowest() { return {BITLOGIC_NEG_INF, BITLOGIC_NEG_INF}; }
     static __device__ __forceinline__ Max largest(Max m, const uint4& u) {
-        return fmaxf(fmaxf(m, fmaxf(__uint_as_float(u.x), __uint_as_float(u.y))),
-                     fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
+        return {fmaxf(m.a, fmaxf(__uint_as_float(u.x), __uint_as_float(u.y))),
+                fmaxf(m.b, fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)))};
     }
-    static __device__ __forceinline__ float value(Max m) { return m; }
-    static __device__ __forceinline__ float largest_of(const uint4& u) { return largest(__uint_as_float(u.x), u); }
+    static __device__ __forceinline__ void parts(Max m, float& a, float& b) { a = m.a, b = m.b; }
+    static __device__ __forceinline__ float value(Max m) { return fmaxf(m.a, m.b); }
+    static __device__ __forceinline__ float largest_of(const uint4& u) {
+        return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
+    }
 };
 template <> struct Piece<int> {
     static constexpr int N = 4;
@@ -159,13 +169,16 @@ template <> struct Piece<int> {
         z[2] = logit_value((int)u.z);
         z[3] = logit_value((int)u.w);
     }
-    using Max = int;
-    static __device__ __forceinline__ Max lowest() { return INT_MIN; }
+    struct Max {
+        int a, b;
+    };
+    static __device__ __forceinline__ Max lowest() { return {INT_MIN, INT_MIN}; }
     static __device__ __forceinline__ Max largest(Max m, const uint4& u) {
-        return max(max(m, max((int)u.x, (int)u.y)), max((int)u.z, (int)u.w));
+        return {max(m.a, max((int)u.x, (int)u.y)), max(m.b, max((int)u.z, (int)u.w))};
     }
-    static __device__ __forceinline__ float value(Max m) { return logit_value(m); }
-    static __device__ __forceinline__ float largest_of(const uint4& u) { return value(largest((int)u.x, u)); }
+    static __device__ __forceinline__ void parts(Max m, float& a, float& b) { a = logit_value(m.a), b = logit_value(m.b); }
+    static __device__ __forceinline__ float value(Max m) { return logit_value(max(m.a, m.b)); }
+    static __device__ __forceinline__ float largest_of(const uint4& u) { return value(largest({(int)u.x, (int)u.z}, u)); }
 };
 template <> struct Piece<__nv_bfloat16> {
     static constexpr int N = 8;
@@ -192,6 +205,7 @@ template <> struct Piece<__nv_bfloat16> {
     static __device__ __forceinline__ Max largest(Max m, const uint4& u) {   // of two numbers: NaN is passed over
         return __hmax2(__hmax2(m, __hmax2(as(u.x), as(u.y))), __hmax2(as(u.z), as(u.w)));
     }
+    static __device__ __forceinline__ void parts(Max m, float& a, float& b) { a = __low2float(m), b = __high2float(m); }
     static __device__ __forceinline__ float value(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
     static __device__ __forceinline__ float largest_of(const uint4& u) { return value(largest(as(u.x), u)); }
 };
@@ -216,6 +230,7 @@ template <> struct Piece<__half> {
     static __device__ __forceinline__ Max largest(Max m, const uint4& u) {
         return __hmax2(__hmax2(m, __hmax2(as(u.x), as(u.y))), __hmax2(as(u.z), as(u.w)));
     }
+    static __device__ __forceinline__ void parts(Max m, float& a, float& b) { a = __low2float(m), b = __high2float(m); }
     static __device__ __forceinline__ float value(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
     static __device__ __forceinline__ float largest_of(const uint4& u) { return value(largest(as(u.x), u)); }
 };
@@ -258,6 +273,12 @@ struct PowerBase {
     }
     __device__ __forceinline__ float exponent(float z) const { return far ? (z - m) * c : fmaf(z, c, -b); }
     __device__ __forceinline__ float power(float z) const { return exp2_unit(exponent(z)); }
+    // whether powers of logits up to `z` about this base stay well inside fp32
+    __device__ __forceinline__ bool holds(float z) const { return !none && (far ? z <= m : fmaf(z, c, -b) <= 64.f); }
+    // ln of a sum of powers about this base, taken to logits (c = log2(e) / tau)
+    __device__ __forceinline__ float log_of(float sum, float inv_tau) const {
+        return far ? m * inv_tau + logf(sum) : kLn2 * (b + log2f(sum));
+    }
     // the factor that takes a sum about this base to one about `row`
     __device__ __forceinline__ float to(const PowerBase& row) const {
         if (none) return 1.f;   // of a sum of 0, or of NaN
@@ -320,6 +341,53 @@ struct RowSlice {
     }
 };
 
+// A piece of masked logits.
+template <typename T>
+__device__ __forceinline__ uint4 masked_piece() {
+    constexpr uint32_t w = std::is_same_v<T, float> ? 0xff800000u : std::is_same_v<T, int> ? 0x80000000u
+                         : std::is_same_v<T, __nv_bfloat16> ? 0xff80ff80u : 0xfc00fc00u;
+    return make_uint4(w, w, w, w);
+}
+
+// The whole pieces of a row streamed through registers by a block of kThreads:
+// batches of four pieces of every thread, a warp's 128 pieces of a batch side by
+// side, a batch loaded while the one before it is used.
+template <typename T, int kThreads>
+struct PieceStream {
+    static constexpr int N = Piece<T>::N;
+    const uint4* from;   // piece 0, read at whole pieces
+    int j0, j1;          // this thread's first piece, and the end of the whole ones
+    int batches;         // that cover all threads' pieces
+
+    static __device__ __forceinline__ int first_of(int tid) { return (tid >> 5) * 128 + (tid & 31); }
+
+    __device__ __forceinline__ PieceStream(const T* x, const RowSlice<T>& slice, int V, int tid)
+        : from(reinterpret_cast<const uint4*>(x + slice.first)), j0(slice.whole0() + first_of(tid)), j1(slice.whole1(V)),
+          batches((max(0, slice.whole1(V) - slice.whole0()) + 4 * kThreads - 1) / (4 * kThreads)) {}
+    __device__ __forceinline__ int piece(int q, int i) const { return j0 + 4 * kThreads * q + 32 * i; }
+    __device__ __forceinline__ void load(int q, uint4 (&u)[4]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = piece(q, i);
+            u[i] = j < j1 ? __ldcg(from + j) : masked_piece<T>();
+        }
+    }
+};
+
+// A piece at the row's ends, by element; places outside the row are masked.
+template <typename T>
+__device__ __forceinline__ uint4 end_piece(const T* x, int V, int first_class) {
+    T e[Piece<T>::N];
+#pragma unroll
+    for (int i = 0; i < Piece<T>::N; ++i) {
+        const int v = first_class + i;
+        e[i] = v >= 0 && v < V ? x[v] : masked_logit<T>();
+    }
+    uint4 u;
+    memcpy(&u, e, 16);
+    return u;
+}
+
 // Bytes of the longest slice of a row of V classes over `blocks` blocks, for
 // any alignment of the row.
 inline long long slice_bytes(long long V, int element, int blocks) {
@@ -344,7 +412,7 @@ inline int blocks_per_row(long long T, long long V, int element, long long fit, 
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_rows(void (*kernel)(KArgs...), long long T, int blocks, int threads, size_t smem,
                                cudaStream_t stream, Args... args) {
-    if (smem > 12 * 1024) {   // with the kernels' own arrays perhaps past the 48 KB that need no leave
+    if (smem > 4 * 1024) {   // with the kernels' own arrays perhaps past the 48 KB that need no leave
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }

@@ -69,21 +69,48 @@ struct Power {
     }
 };
 
-// A sum of weights w = rint(2^40 e), 0 <= e <= 1, of at most 512 of them, in
-// fp32 and 32-bit integer operations: 32 + e rounds e to a multiple of 2^-18,
+// Sums of weights w = rint(2^40 e), 0 <= e <= 1, of at most 1024 of them, in
+// fp32 and 32-bit integer operations: 16 + e rounds e to a multiple of 2^-19,
 // the remainder is exact, and 1.5 2^23 + 2^40 remainder rounds it to a whole
-// number as rint does.
+// number as rint does; so w = 2^21 high + low with the offsets of the two
+// floats' bits taken off, in arithmetic modulo 2^32.
 struct WeightSum {
-    uint32_t high = 0;
-    int low = 0;
-    __device__ __forceinline__ void add(float e) {
-        const float t = e + 32.0f, r = e - (t - 32.0f);
-        const float u = fmaf(r, 1099511627776.0f, 12582912.0f);
-        high += __float_as_uint(t) - 0x42000000u;
-        low += (int)(__float_as_uint(u) - 0x4b400000u);
+    uint32_t high = 0, low = 0;
+    __device__ __forceinline__ void add(f32x2 e) {
+        const f32x2 c16 = pack2(16.0f, 16.0f), scale = pack2(1099511627776.0f, 1099511627776.0f),
+                    whole = pack2(12582912.0f, 12582912.0f);
+        const f32x2 t = add2(e, c16), r = sub2(e, sub2(t, c16)), u = fma2(r, scale, whole);
+        float a, b;
+        unpack2(t, a, b);
+        high += __float_as_uint(a) + __float_as_uint(b) - 2u * 0x41800000u;
+        unpack2(u, a, b);
+        low += __float_as_uint(a) + __float_as_uint(b) - 2u * 0x4b400000u;
     }
     __device__ __forceinline__ unsigned long long total() const {
-        return ((unsigned long long)high << 22) + (unsigned long long)(long long)low;
+        return ((unsigned long long)high << 21) + (unsigned long long)(long long)(int)low;
+    }
+    // the sum over a warp (of at most 1024 weights), in every lane
+    __device__ __forceinline__ unsigned long long warp_total() const {
+        WeightSum s;
+        s.high = __reduce_add_sync(0xffffffffu, high);
+        s.low = __reduce_add_sync(0xffffffffu, low);
+        return s.total();
+    }
+};
+
+// e of two logits, rounded as Power does one; 0 for -inf and NaN.
+struct PowerPairs {
+    f32x2 m, slope;
+    __device__ __forceinline__ explicit PowerPairs(const Power& p) : m(pack2(p.m, p.m)), slope(pack2(p.slope, p.slope)) {}
+    __device__ __forceinline__ f32x2 operator()(f32x2 z) const {
+        float a, b;
+        unpack2(mul2(sub2(z, m), slope), a, b);
+        return pack2(fmaxf(exp2_unit(a), 0.f), fmaxf(exp2_unit(b), 0.f));
+    }
+    __device__ __forceinline__ f32x2 at_least(f32x2 z, float floor_e) const {
+        float a, b;
+        unpack2((*this)(z), a, b);
+        return pack2(a >= floor_e ? a : 0.f, b >= floor_e ? b : 0.f);
     }
 };
 
@@ -236,17 +263,6 @@ __device__ void sample_of_stream(const T* __restrict__ x, int V, RowSettings set
     }
 }
 
-// Rows too long for the shared memory of a cluster.
-template <typename T>
-__global__ void __launch_bounds__(kSampleThreads)
-sample_stream_kernel(const T* __restrict__ X, long long ld, int V, Settings set, Draw out) {
-    __shared__ StreamScratch sc;
-    grid_dependency_wait();
-    allow_dependent_launch();
-    const long long row = blockIdx.x;
-    sample_of_stream(X + row * ld, V, RowSettings(set, row, V), row, out, &sc);
-}
-
 // ------------------------------------------------------------ rows on chip --
 
 constexpr int kList = 2048;       // entries that a cut or a draw looks at in the end
@@ -319,7 +335,8 @@ __device__ __forceinline__ int power_of_two(unsigned n) { return n <= 32 ? 32 : 
 // The first block's work where the row's first k classes are all on its list:
 // the cut by rank and mass on the sorted list, then the draw among the kept
 // sorted by class.
-__device__ void sample_of_list(SampleShared* s, unsigned n, const RowSettings& set, const Power& power, long long row,
+template <typename S>
+__device__ void sample_of_list(S* s, unsigned n, const RowSettings& set, const Power& power, long long row,
                                const Draw& out) {
     constexpr int kPer = kListTop / kSampleThreads;
     const int tid = threadIdx.x;
@@ -431,7 +448,7 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
         if (j + kSampleThreads < slice.n) mb = P::largest(mb, tile16[j + kSampleThreads]);
     }
     const float za = P::value(ma), zb = P::value(mb);
-    const uint32_t bound_here = k_asked < V ? block_bound(za, zb, (k_asked + blocks - 1) / blocks, &s.bound) : 0u;
+    const uint32_t bound_here = k_asked < V ? block_bound({za, zb}, (k_asked + blocks - 1) / blocks, &s.bound) : 0u;
     const float wm = warp_largest(fmaxf(za, zb));
     if (lane == 0) s.fbuf[warp] = wm;
     __syncthreads();
@@ -455,6 +472,7 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
         return;
     }
     const Power power(m, set);
+    const PowerPairs pairs(power);
     if (set.k == 1 && k_asked != 1) bound = 0xff800000u;   // a largest of +inf: nothing below it is needed
 
     // entries of the slice with zmin <= z <= zmax to the first block's list
@@ -506,12 +524,12 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
         unsigned long long mass = 0;
         for (int j = j0 + lane; j < j1;) {
             WeightSum ws;
-#pragma unroll 2
-            for (int r = 0; r < 32 && j < j1; ++r, j += 32) {
-                float z[P::N];
-                P::load(tile16[j], z);
+#pragma unroll 4
+            for (int r = 0; r < 64 && j < j1; ++r, j += 32) {
+                f32x2 z[P::N / 2];
+                load_pairs<T>(tile16[j], z);
 #pragma unroll
-                for (int i = 0; i < P::N; ++i) ws.add(power.of(z[i]));
+                for (int i = 0; i < P::N / 2; ++i) ws.add(pairs(z[i]));
             }
             mass += ws.total();
         }
@@ -670,15 +688,12 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
     if (set.p >= 1.0f) {
         for (int j = j0 + lane; j < j1;) {
             WeightSum ws;
-#pragma unroll 2
-            for (int r = 0; r < 32 && j < j1; ++r, j += 32) {
-                float z[P::N];
-                P::load(tile16[j], z);
+#pragma unroll 4
+            for (int r = 0; r < 64 && j < j1; ++r, j += 32) {
+                f32x2 z[P::N / 2];
+                load_pairs<T>(tile16[j], z);
 #pragma unroll
-                for (int i = 0; i < P::N; ++i) {
-                    const float e = power.of(z[i]);
-                    ws.add(e >= set.floor_e ? e : 0.f);
-                }
+                for (int i = 0; i < P::N / 2; ++i) ws.add(pairs.at_least(z[i], set.floor_e));
             }
             mass += ws.total();
         }
@@ -784,6 +799,423 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
                     if (!done && r > target) {
                         done = true;
                         out.token[row] = slice.first + j * P::N + i;
+                        if (out.logprob) out.logprob[row] = logf((float)w[i] / (float)total);
+                    }
+                }
+            }
+            return;
+        }
+        run += __shfl_sync(0xffffffffu, upto, 31);
+        my_left = my_left > ties_all ? my_left - ties_all : 0;
+    }
+}
+
+// ------------------------------------------------------ rows by one block --
+
+constexpr int kRowList = 4096;   // entries that a cut or a draw looks at in the end
+
+struct SampleRowShared {
+    union {
+        unsigned long long list[kRowList];   // key << 32 | ~class
+        StreamScratch stream;
+    };
+    union {
+        BoundScratch bound;
+        unsigned short groups[4 * kSampleThreads];
+        unsigned bins[kBins];   // mass by the power's exponent
+        struct {
+            unsigned long long sums[kSampleWarps];
+        } scan;
+    };
+    float fbuf[kSampleWarps];
+    unsigned long long mass[kSampleWarps];
+    int kept[kSampleWarps];
+    unsigned n, n_groups, ties;
+    int bin;
+    struct {
+        uint32_t key;
+        unsigned ties, slow;
+    } found;
+};
+
+// The classes in order of their pieces: chunk 0 is the piece at the row's front
+// that is not whole, chunk 1 + 8 q + w the 128 pieces of warp w's batch q, and
+// the last chunk the piece at the end.
+//
+// Many rows, of any length: a block per row.  It streams the row once from
+// memory for the largest and for the maxima of 2048 groups; what else a row
+// needs streams it again from L2:
+//   top_k up to 1024 (and greedy rows): the groups that reach the bound are
+//     read again, and their entries cut and drawn among as a list;
+//   top_p alone: the mass of the row; then its bins of 1/64 octave down to
+//     where top_p can end; then the exact mass above the bin in which it does,
+//     by chunk, and that bin's entries as a list, in which the cut is found;
+//   neither: the weights by chunk.
+// The chunk that holds the draw is read once more by a warp.
+template <typename T>
+__global__ void __launch_bounds__(kSampleThreads, 4)
+sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings settings, Draw out) {
+    using P = Piece<T>;
+    constexpr int N = P::N, H = N / 2;
+    extern __shared__ __align__(16) unsigned char raw[];
+    unsigned long long* chunks = reinterpret_cast<unsigned long long*>(raw);   // kept weight by chunk
+    __shared__ SampleRowShared s;
+    grid_dependency_wait();
+    allow_dependent_launch();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const long long row = blockIdx.x;
+    const T* x = X + row * ld;
+    const RowSlice<T> slice(x, V, 0, 1);
+    const PieceStream<T, kSampleThreads> stream(x, slice, V, tid);
+    uint4 ua[4], ub[4];
+    stream.load(0, ua);
+    stream.load(1, ub);
+    RowSettings set(settings, row, V);
+    if (tid == 0) s.n = s.n_groups = s.ties = 0u;
+    // every batch of the row to `use`, of which the first two are loaded
+    auto stream_row = [&](auto&& use) {
+        for (int q = 0; q < stream.batches; q += 2) {
+            use(ua, q);
+            if (q + 2 < stream.batches) stream.load(q + 2, ua);
+            if (q + 1 < stream.batches) use(ub, q + 1);
+            if (q + 3 < stream.batches) stream.load(q + 3, ub);
+        }
+    };
+    // the pieces at the row's ends, of threads 0 and 32
+    const int j_end = tid == 0 && slice.whole0() > 0 ? 0 : tid == 32 && slice.whole1(V) < slice.n ? slice.whole1(V) : -1;
+    const uint4 u_end = j_end >= 0 ? end_piece(x, V, slice.first + j_end * N) : masked_piece<T>();
+    const int last_chunk = 1 + kSampleWarps * stream.batches, end_chunk = tid == 0 ? 0 : last_chunk;
+
+    typename P::Max mx[4] = {P::lowest(), P::lowest(), P::lowest(), P::lowest()};
+    stream_row([&](const uint4 (&u)[4], int) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx[i] = P::largest(mx[i], u[i]);
+    });
+    float group[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) group[i] = P::value(mx[i]);
+    const float m = block_largest(fmaxf(fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3])), P::largest_of(u_end)), s.fbuf, kSampleWarps);
+    if (m == BITLOGIC_NEG_INF) {   // nothing to draw from
+        if (tid == 0) {
+            out.token[row] = -1;
+            if (out.logprob) out.logprob[row] = BITLOGIC_NEG_INF;
+        }
+        return;
+    }
+    const Power power(m, set);
+    const PowerPairs pairs(power);
+
+    auto list_entry = [&](float z, int v) {
+        const unsigned at = atomicAdd(&s.n, 1u);
+        if (at < kRowList) s.list[at] = ((unsigned long long)logit_key(z) << 32) | (uint32_t)~v;
+    };
+    if (set.k < V) {
+        if (set.k > kListTop) {
+            sample_of_stream(x, V, set, row, out, &s.stream);
+            return;
+        }
+        float part[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) P::parts(mx[i], part[2 * i], part[2 * i + 1]);
+        const float z_min = set.k == 1 ? m : bound_logit(block_bound(part, set.k, &s.bound));
+        __syncthreads();
+        auto take = [&](const uint4& u, int j) {
+            if (P::largest_of(u) >= z_min) {
+                float z[N];
+                P::load(u, z);
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (z[i] >= z_min && z[i] > BITLOGIC_NEG_INF) list_entry(z[i], slice.first + j * N + i);
+            }
+        };
+        if (j_end >= 0) take(u_end, j_end);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (group[i] >= z_min && group[i] > BITLOGIC_NEG_INF) s.groups[atomicAdd(&s.n_groups, 1u)] = (unsigned short)(4 * tid + i);
+        __syncthreads();
+        const unsigned pieces = s.n_groups * (unsigned)stream.batches;
+        for (unsigned p = tid; p < pieces; p += kSampleThreads) {
+            const unsigned which = p / (unsigned)stream.batches, g = s.groups[which];
+            const int j = slice.whole0() + stream.first_of((int)(g >> 2)) + 4 * kSampleThreads * (int)(p - which * (unsigned)stream.batches) + 32 * (int)(g & 3u);
+            if (j < stream.j1) take(__ldcg(stream.from + j), j);
+        }
+        __syncthreads();
+        const unsigned n = s.n;
+        __syncthreads();
+        if (n <= kRowList) sample_of_list(&s, n, set, power, row, out);
+        else sample_of_stream(x, V, set, row, out, &s.stream);
+        return;
+    }
+
+    Cut cut = {kNoCut, 0};
+    float z_cut = BITLOGIC_NEG_INF;   // kept: above it, and the first ties at it
+    stream.load(0, ua);
+    stream.load(1, ub);
+    if (set.p < 1.0f) {
+        // the mass of the row
+        for (int b = tid; b < kBins; b += kSampleThreads) s.bins[b] = 0u;
+        unsigned long long mass = 0;
+        stream_row([&](const uint4 (&u)[4], int) {
+            WeightSum ws;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f32x2 z[H];
+                load_pairs<T>(u[i], z);
+#pragma unroll
+                for (int e = 0; e < H; ++e) ws.add(pairs(z[e]));
+            }
+            mass += ws.total();
+        });
+        stream.load(0, ua);
+        stream.load(1, ub);
+        {
+            WeightSum ws;
+            f32x2 z[H];
+            load_pairs<T>(u_end, z);
+#pragma unroll
+            for (int e = 0; e < H; ++e) ws.add(pairs(z[e]));
+            mass += ws.total();
+        }
+        const unsigned long long total = block_add(mass, s.mass, kSampleWarps);
+        unsigned long long want = share_of(total, set.p);
+        if (want < 1) want = 1;
+        // classes with less than a V-th of what top_p leaves off come after it
+        const float left_off = fmaxf((float)(total - want) * (1.0f / 1099511627776.0f) / (float)V, 2.3e-13f);
+        const float y_max = fminf(-log2f(left_off) + 0.01f, 41.0f);
+        const float z_min = power.slope > 0.f ? power.m - fabsf(power.m) * 1e-6f - (y_max + 0.01f) / power.slope : BITLOGIC_NEG_INF;
+        auto count = [&](const uint4& u) {
+            if (P::largest_of(u) >= z_min) {
+                float z[N];
+                P::load(u, z);
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (z[i] >= z_min && z[i] > BITLOGIC_NEG_INF) {
+                        const int b = bin_of((power.m - z[i]) * power.slope);
+                        atomicAdd(&s.bins[b], bin_units(power.of(z[i]), b));
+                    }
+            }
+        };
+        stream_row([&](const uint4 (&u)[4], int) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) count(u[i]);
+        });
+        stream.load(0, ua);
+        stream.load(1, ub);
+        count(u_end);
+        if (tid == 0) s.bin = kBins - 1;
+        __syncthreads();
+        // the bin in which the mass is reached
+        constexpr int kBinPer = (kBins + kSampleThreads - 1) / kSampleThreads;
+        float sum = 0.f;
+        for (int q = 0; q < kBinPer; ++q) {
+            const int b = tid * kBinPer + q;
+            if (b < kBins) sum += bin_mass(s.bins[b], b);
+        }
+        float upto = sum;
+        for (int o = 1; o < 32; o <<= 1) {
+            const float t = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += t;
+        }
+        if (lane == 31) s.fbuf[warp] = upto;
+        __syncthreads();
+        float before_bin = upto - sum;
+        for (int w = 0; w < warp; ++w) before_bin += s.fbuf[w];
+        const float goal = (float)want * (1.0f / 1099511627776.0f);
+        for (int q = 0; q < kBinPer; ++q) {
+            const int b = tid * kBinPer + q;
+            if (b < kBins) {
+                const float mb = bin_mass(s.bins[b], b);
+                if (before_bin < goal && before_bin + mb >= goal) atomicMin(&s.bin, b);
+                before_bin += mb;
+            }
+        }
+        __syncthreads();
+        // the exact mass above the bins around it, by chunk where it is kept,
+        // and the entries of those bins
+        const int b0 = max(0, s.bin - 1), b1 = min(kBins - 1, s.bin + 1);
+        mass = 0;
+        auto above = [&](const uint4& u, int j, WeightSum& kept) {
+            if (P::largest_of(u) < z_min) return;
+            float z[N];
+            P::load(u, z);
+#pragma unroll
+            for (int i = 0; i < N; i += 2) {
+                float e[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const bool in = z[i + h] >= z_min && z[i + h] > BITLOGIC_NEG_INF;
+                    const int b = in ? bin_of((power.m - z[i + h]) * power.slope) : kBins;
+                    if (b >= b0 && b <= b1) list_entry(z[i + h], slice.first + j * N + i + h);
+                    e[h] = b < b0 ? power.of(z[i + h]) : 0.f;
+                    if (e[h] < set.floor_e) {
+                        mass += draw_weight(e[h]);   // counts for the cut, but is not kept
+                        e[h] = 0.f;
+                    }
+                }
+                kept.add(pack2(e[0], e[1]));
+            }
+        };
+        stream_row([&](const uint4 (&u)[4], int q) {
+            WeightSum kept;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) above(u[i], stream.piece(q, i), kept);
+            const unsigned long long w = kept.warp_total();
+            if (lane == 0) {
+                chunks[1 + kSampleWarps * q + warp] = w;
+                mass += w;
+            }
+        });
+        if (tid == 0) chunks[0] = chunks[last_chunk] = 0ull;
+        __syncthreads();
+        if (j_end >= 0) {
+            WeightSum kept;
+            above(u_end, j_end, kept);
+            chunks[end_chunk] = kept.total();
+            mass += kept.total();
+        }
+        const unsigned long long first = block_add(mass, s.mass, kSampleWarps);
+        const unsigned listed = s.n;
+        if (tid == 0) s.found = {0u, 0u, 1u};   // not found: from memory
+        __syncthreads();
+        constexpr int kPer = kRowList / kSampleThreads;
+        if (listed <= kRowList && listed > 0 && first < want) {
+            const int size = power_of_two(listed);
+            for (int i = listed + tid; i < size; i += kSampleThreads) s.list[i] = 0ull;
+            block_sort_falling(s.list, size);
+            unsigned long long part = 0, all;
+            for (int q = 0; q < kPer; ++q) {
+                const int i = tid * kPer + q;
+                if (i < (int)listed) part += draw_weight(power.of(key_logit((uint32_t)(s.list[i] >> 32))));
+            }
+            unsigned long long run = first + block_before(part, s.scan.sums, &all);
+            for (int q = 0; q < kPer; ++q) {
+                const int i = tid * kPer + q;
+                if (i >= (int)listed) break;
+                const uint32_t key = (uint32_t)(s.list[i] >> 32);
+                const float e = power.of(key_logit(key));
+                const unsigned long long w = draw_weight(e);
+                if (run < want) {   // kept: its weight to its chunk
+                    if (e >= set.floor_e && w) {
+                        const int p = (int)~(uint32_t)s.list[i] - slice.first, j = p / N - slice.whole0();
+                        const int c = j < 0 ? 0 : j >= slice.whole1(V) - slice.whole0() ? last_chunk : 1 + j / 128;
+                        atomicAdd(&chunks[c], w);
+                    }
+                    if (run + w >= want) {   // the last one
+                        unsigned ties = 1;   // with those of its key before it
+                        for (int r = i - 1; r >= 0 && (uint32_t)(s.list[r] >> 32) == key; --r) ++ties;
+                        s.found = {key, ties, 0u};
+                    }
+                }
+                run += w;
+            }
+        }
+        __syncthreads();
+        if (s.found.slow) {
+            sample_of_stream(x, V, set, row, out, &s.stream);
+            return;
+        }
+        cut = {s.found.key, s.found.ties};
+        z_cut = key_logit(cut.key);
+    } else {
+        stream_row([&](const uint4 (&u)[4], int q) {
+            WeightSum ws;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f32x2 z[H];
+                load_pairs<T>(u[i], z);
+#pragma unroll
+                for (int e = 0; e < H; ++e) ws.add(pairs.at_least(z[e], set.floor_e));
+            }
+            const unsigned long long w = ws.warp_total();
+            if (lane == 0) chunks[1 + kSampleWarps * q + warp] = w;
+        });
+        if (tid == 0) chunks[0] = chunks[last_chunk] = 0ull;
+        __syncthreads();
+        if (j_end >= 0) {
+            WeightSum ws;
+            f32x2 z[H];
+            load_pairs<T>(u_end, z);
+#pragma unroll
+            for (int e = 0; e < H; ++e) ws.add(pairs.at_least(z[e], set.floor_e));
+            chunks[end_chunk] = ws.total();
+        }
+        __syncthreads();
+    }
+
+    // the chunk that holds the draw, and what lies before it
+    const int per = (last_chunk + kSampleThreads) / kSampleThreads;
+    unsigned long long own = 0, total;
+    for (int i = tid * per; i < min(last_chunk + 1, (tid + 1) * per); ++i) own += chunks[i];
+    unsigned long long before = block_before(own, s.mass, &total);
+    const unsigned long long target = share_of(total, set.u);
+    if (tid == 0) s.kept[1] = -1;
+    __syncthreads();
+    if (target >= before && target < before + own) {
+        int i = tid * per;
+        while (target >= before + chunks[i]) before += chunks[i++];
+        s.kept[0] = i;
+        s.kept[1] = 0;
+        s.mass[0] = before;
+    }
+    __syncthreads();
+    if (warp != 0 || s.kept[1] < 0) return;
+    // read by one warp, a piece per lane, in order
+    const int chunk = s.kept[0], w0 = slice.whole0();
+    const int c0 = chunk == 0 ? 0 : chunk == last_chunk ? slice.whole1(V) : w0 + (chunk - 1) * 128;
+    const int c1 = chunk == 0 ? w0 : chunk == last_chunk ? slice.n : min(slice.whole1(V), c0 + 128);
+    unsigned long long run = s.mass[0];
+    unsigned my_left = 0;
+    unsigned long long wt = 0;
+    if (cut.ties) {
+        const float e = power.of(z_cut);
+        wt = e >= set.floor_e ? draw_weight(e) : 0ull;
+        // ties before the chunk: all of them are on the list
+        const int v_first = slice.first + c0 * N;
+        unsigned ties = 0;
+        for (unsigned i = lane; i < s.n; i += 32)
+            ties += (uint32_t)(s.list[i] >> 32) == cut.key && (int)~(uint32_t)s.list[i] < v_first;
+        ties = __reduce_add_sync(0xffffffffu, ties);
+        my_left = (unsigned)cut.ties > ties ? (unsigned)cut.ties - ties : 0u;
+    }
+    for (int b = c0; b < c1; b += 32) {
+        const int j = b + lane;
+        float z[N];
+        P::load(j >= c1 ? masked_piece<T>() : j >= w0 && j < slice.whole1(V) ? __ldcg(stream.from + j) : end_piece(x, V, slice.first + j * N), z);
+        unsigned long long w[N], sum = 0;
+        unsigned same = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) same += cut.ties && z[i] == z_cut;
+        unsigned ties_before = same;
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned t = __shfl_up_sync(0xffffffffu, ties_before, o);
+            if (lane >= o) ties_before += t;
+        }
+        const unsigned ties_all = __shfl_sync(0xffffffffu, ties_before, 31);
+        ties_before -= same;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            w[i] = 0ull;
+            if (z[i] > z_cut) {
+                const float e = power.of(z[i]);
+                if (e >= set.floor_e) w[i] = draw_weight(e);
+            } else if (cut.ties && z[i] == z_cut) {
+                if (ties_before < my_left) w[i] = wt;
+                ++ties_before;
+            }
+            sum += w[i];
+        }
+        const unsigned long long upto = warp_upto(sum, lane);
+        const unsigned hit = __ballot_sync(0xffffffffu, run + upto > target);
+        if (hit) {
+            if (lane == __ffs(hit) - 1) {
+                unsigned long long r = run + upto - sum;
+                bool done = false;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    r += w[i];
+                    if (!done && r > target) {
+                        done = true;
+                        out.token[row] = slice.first + j * N + i;
                         if (out.logprob) out.logprob[row] = logf((float)w[i] / (float)total);
                     }
                 }
@@ -934,11 +1366,16 @@ int launch_sample(const T* x, long long T_, int V, long long ld, const Settings&
         auto kern = V <= 32 ? sample_narrow_kernel<T, 1> : V <= 128 ? sample_narrow_kernel<T, 4>
                   : V <= 256 ? sample_narrow_kernel<T, 8> : sample_narrow_kernel<T, 32>;
         e = launch_rows(kern, (T_ + kNarrowWarps - 1) / kNarrowWarps, 1, kNarrowWarps * 32, 0, stream, x, ld, V, T_, set, out);
-    } else if (const int blocks = blocks_per_row(T_, V, sizeof(T), kTileFit, kTileMost, kTileLeast)) {
-        e = launch_rows(sample_tile_kernel<T>, T_, blocks, kSampleThreads, (size_t)slice_bytes(V, sizeof(T), blocks), stream,
-                        x, ld, V, set, out);
     } else {
-        e = launch_rows(sample_stream_kernel<T>, T_, 1, kSampleThreads, 0, stream, x, ld, V, set, out);
+        const int blocks = 2 * T_ <= sm_count() ? blocks_per_row(T_, V, sizeof(T), kTileFit, kTileMost, kTileLeast) : 0;
+        if (blocks > 0) {
+            e = launch_rows(sample_tile_kernel<T>, T_, blocks, kSampleThreads, (size_t)slice_bytes(V, sizeof(T), blocks),
+                            stream, x, ld, V, set, out);
+        } else {
+            const long long pieces = slice_bytes(V, sizeof(T), 1) / 16, batches = (pieces + 4 * kSampleThreads - 1) / (4 * kSampleThreads);
+            e = launch_rows(sample_row_kernel<T>, T_, 1, kSampleThreads, (size_t)(2 + kSampleWarps * batches) * 8, stream, x, ld, V,
+                            set, out);
+        }
     }
     return e == cudaSuccess ? launch_status() : (int)BITLOGIC_ERR_CUDA;
 }

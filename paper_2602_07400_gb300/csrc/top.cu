@@ -28,6 +28,17 @@ struct TopScratch {
     unsigned n_above;
 };
 
+// ln sum exp of a row that holds +inf: +inf, or NaN with a NaN.
+template <typename T>
+__device__ float lse_of_inf(const T* x, int V) {
+    float s = 0.f;
+    for (int v = 0; v < V; ++v) {
+        const float z = logit_value(x[v]);
+        if (z != z) s = z;
+    }
+    return s != s ? s : -BITLOGIC_NEG_INF;
+}
+
 // The selection of a row read from memory in every pass, for any row: the
 // exact key of the last rank by radix selection, then the classes above it and
 // the first ones at it.  Called by the whole block.
@@ -79,29 +90,195 @@ __device__ void top_of_stream(const T* __restrict__ x, int V, const TopOut& o, l
     }
 }
 
-// Rows too long for the shared memory of a cluster.
+// The largest of a sorted or short list to their ranks; the places that no
+// class takes are filled.  Called by the whole block; the list has room for
+// the next power of two.
+__device__ __forceinline__ void write_top(unsigned long long* list, unsigned total, const TopOut& o, long long row) {
+    const int tid = threadIdx.x, K = o.K;
+    if (total <= 256) {   // every entry to the place of its rank
+        const unsigned long long e = tid < (int)total ? list[tid] : 0ull;
+        unsigned r = 0;
+        for (unsigned j = 0; j < total; ++j) r += list[j] > e;
+        if (tid < (int)total && r < (unsigned)K) {
+            o.val[row * K + r] = key_logit((uint32_t)(e >> 32));
+            o.idx[row * K + r] = (int)~(uint32_t)e;
+        }
+    } else {
+        const int size = 1 << (32 - __clz(total - 1));
+        for (int i = total + tid; i < size; i += kTopThreads) list[i] = 0ull;
+        block_sort_falling(list, size);
+        if (tid < K) {
+            o.val[row * K + tid] = key_logit((uint32_t)(list[tid] >> 32));
+            o.idx[row * K + tid] = (int)~(uint32_t)list[tid];
+        }
+    }
+    if (tid < K && tid >= (int)total) {
+        o.val[row * K + tid] = BITLOGIC_NEG_INF;
+        o.idx[row * K + tid] = -1;
+    }
+}
+
+constexpr int kRowList = 2048;   // entries of a row
+
+struct TopRowShared {
+    union {
+        unsigned long long list[kRowList];
+        TopScratch scratch;
+    };
+    BoundScratch bound;
+    unsigned short groups[4 * kTopThreads];
+    float m[kTopWarps], s[kTopWarps];
+    unsigned n, n_groups, inf;
+};
+
+// Many rows, of any length: a block per row, which streams it once, keeping
+// four running maxima of two parts per thread.  These 2048 maxima of the row's
+// groups of pieces give a bound that K logits reach, and the groups whose maximum
+// reaches it are read again (an eighth of a row of 2^17 bf16 at K = 128), from
+// L2, for the entries: little more than K for logits in no particular order.  A
+// row on which more than 2048 pass is selected from memory.  Taking entries
+// while streaming, under a bound from the row's beginning that is raised as it
+// goes, met four times as many and took 554 us where this takes 248 us
+// (4096 x 131072 bf16).
 template <typename T>
-__global__ void __launch_bounds__(kTopThreads)
-top_stream_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
-    __shared__ TopScratch s;
+__global__ void __launch_bounds__(kTopThreads, 4)
+top_row_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
+    using P = Piece<T>;
+    constexpr int N = P::N, H = N / 2;
+    __shared__ TopRowShared s;
     grid_dependency_wait();
+    allow_dependent_launch();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, K = o.K;
     const long long row = blockIdx.x;
     const T* x = X + row * ld;
-    if (o.lse) {
-        float m = BITLOGIC_NEG_INF;
-        for (int v = threadIdx.x; v < V; v += kTopThreads) m = fmaxf(m, logit_value(x[v]));
-        m = block_largest(m, s.fbuf, kTopWarps);
-        const float ms = isinf(m) ? 0.f : m, c = kLog2E * o.inv_tau;
-        float sum = 0.f;
-        for (int v = threadIdx.x; v < V; v += kTopThreads) sum += exp2_unit((logit_value(x[v]) - ms) * c);
-        sum = block_add(sum, s.fbuf, kTopWarps);
-        if (threadIdx.x == 0) o.lse[row] = ms * o.inv_tau + logf(sum);
+    const RowSlice<T> slice(x, V, 0, 1);
+    const PieceStream<T, kTopThreads> stream(x, slice, V, tid);
+    uint4 ua[4], ub[4];
+    stream.load(0, ua);
+    stream.load(1, ub);
+    if (tid == 0) s.n = s.n_groups = s.inf = 0u;
+    __syncthreads();
+
+    // powers about a base of the warp's, which seldom moves
+    const float c = kLog2E * o.inv_tau;
+    PowerBase base(BITLOGIC_NEG_INF, c);
+    f32x2 y0 = 0, y1 = 0;
+    typename P::Max mx[4] = {P::lowest(), P::lowest(), P::lowest(), P::lowest()};
+    auto sums = [&](const uint4& u, const auto& power) {
+        f32x2 z[H];
+        load_pairs<T>(u, z);
+#pragma unroll
+        for (int i = 0; i < H; i += 2) {
+            y0 = add2(y0, power(z[i]));
+            y1 = add2(y1, power(z[i + 1]));
+        }
+    };
+    auto add = [&](const uint4 (&u)[4], float top) {   // `top`: of these or more
+        if (!base.holds(top)) {
+            if (isinf(top) && top > 0.f) {   // the sum is +inf, or NaN
+                s.inf = 1u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float z[N];
+                    P::load(u[i], z);
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (z[e] != z[e]) y0 = pack2(z[e], z[e]);
+                }
+                return;
+            }
+            const PowerBase up(top, c);
+            const float f = base.to(up);
+            y0 = mul2(y0, pack2(f, f));
+            y1 = mul2(y1, pack2(f, f));
+            base = up;
+        }
+        if (base.far) {
+            const FarPairs power(base);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sums(u[i], power);
+        } else {
+            const NearPairs power(base);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sums(u[i], power);
+        }
+    };
+    auto use = [&](const uint4 (&u)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx[i] = P::largest(mx[i], u[i]);
+        if (o.lse) add(u, fmaxf(fmaxf(P::value(mx[0]), P::value(mx[1])), fmaxf(P::value(mx[2]), P::value(mx[3]))));
+    };
+    for (int q = 0; q < stream.batches; q += 2) {
+        use(ua);
+        if (q + 2 < stream.batches) stream.load(q + 2, ua);
+        if (q + 1 < stream.batches) use(ub);
+        if (q + 3 < stream.batches) stream.load(q + 3, ub);
     }
-    top_of_stream(x, V, o, row, &s);
+    const float group[4] = {P::value(mx[0]), P::value(mx[1]), P::value(mx[2]), P::value(mx[3])};
+    // the pieces at the row's ends, of threads 0 and 32
+    const int j_end = tid == 0 && slice.whole0() > 0 ? 0 : tid == 32 && slice.whole1(V) < slice.n ? slice.whole1(V) : -1;
+    uint4 u_end = masked_piece<T>();
+    if (j_end >= 0) {
+        u_end = end_piece(x, V, slice.first + j_end * N);
+        const uint4 e[4] = {u_end, masked_piece<T>(), masked_piece<T>(), masked_piece<T>()};
+        if (o.lse) add(e, fmaxf(base.none ? BITLOGIC_NEG_INF : base.m, P::largest_of(u_end)));
+    }
+
+    float part[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) P::parts(mx[i], part[2 * i], part[2 * i + 1]);
+    const float z_min = bound_logit(block_bound(part, K, &s.bound));
+    auto take = [&](const uint4& u, int j) {
+        if (P::largest_of(u) >= z_min) {
+            float z[N];
+            P::load(u, z);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (z[i] >= z_min && z[i] > BITLOGIC_NEG_INF) {
+                    const unsigned at = atomicAdd(&s.n, 1u);
+                    if (at < kRowList) s.list[at] = ((unsigned long long)logit_key(z[i]) << 32) | (uint32_t)~(slice.first + j * N + i);
+                }
+        }
+    };
+    if (j_end >= 0) take(u_end, j_end);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (group[i] >= z_min && group[i] > BITLOGIC_NEG_INF) s.groups[atomicAdd(&s.n_groups, 1u)] = (unsigned short)(4 * tid + i);
+    __syncthreads();
+    const unsigned pieces = s.n_groups * (unsigned)stream.batches;
+    for (unsigned p = tid; p < pieces; p += kTopThreads) {
+        const unsigned which = p / (unsigned)stream.batches, g = s.groups[which];
+        const int j = slice.whole0() + stream.first_of((int)(g >> 2)) + 4 * kTopThreads * (int)(p - which * (unsigned)stream.batches) + 32 * (int)(g & 3u);
+        if (j < stream.j1) take(__ldcg(stream.from + j), j);
+    }
+    if (o.lse) {
+        float m = warp_largest(base.none ? BITLOGIC_NEG_INF : base.m), a, b;
+        if (lane == 0) s.m[warp] = m;
+        __syncthreads();
+        for (int w = 0; w < kTopWarps; ++w) m = fmaxf(m, s.m[w]);
+        const PowerBase all(m, c);
+        unpack2(add2(y0, y1), a, b);
+        const float sum = warp_add((a + b) * base.to(all));
+        if (lane == 0) s.s[warp] = sum;
+        __syncthreads();
+        if (tid == 0) {
+            float t = 0.f;
+            for (int w = 0; w < kTopWarps; ++w) t += s.s[w];
+            o.lse[row] = t != t ? t : s.inf ? -BITLOGIC_NEG_INF : all.log_of(t, o.inv_tau);
+        }
+    } else {
+        __syncthreads();
+    }
+    const unsigned total = s.n;
+    __syncthreads();
+    if (total > kRowList) top_of_stream(x, V, o, row, &s.scratch);
+    else write_top(s.list, total, o, row);
 }
 
 // Entries (key << 32 | ~class) that a row's selection looks at in the end.
 constexpr int kTopList = 1024;
+
+constexpr int kPieces = 1024;    // pieces of a slice that hold an entry
 
 struct TopShared {
     union {
@@ -112,13 +289,14 @@ struct TopShared {
         unsigned long long local[kTopList];  // of the slice
         BoundScratch bound;
     };
+    unsigned short pieces[kPieces];
     struct Stats {
         float m;
         uint32_t bound;
     } stats[kMaxCluster];
     float sums[kMaxCluster];
     float fbuf[kTopWarps];
-    unsigned n_list, n_local, base;
+    unsigned n_list, n_local, n_pieces, base;
 };
 
 // A row in the shared memory of one block or one cluster.  Each thread's two
@@ -144,7 +322,7 @@ top_tile_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
     const T* x = X + row * ld;
     const RowSlice<T> slice(x, V, rank, blocks);
     slice.copy(x, V, tile, tid, kTopThreads);
-    if (tid == 0) s.n_list = s.n_local = 0;
+    if (tid == 0) s.n_list = s.n_local = s.n_pieces = 0;
     cp_async_wait<0>();
     __syncthreads();
 
@@ -155,7 +333,7 @@ top_tile_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
         if (j + kTopThreads < slice.n) mb = P::largest(mb, tile16[j + kTopThreads]);
     }
     const float za = P::value(ma), zb = P::value(mb);
-    const uint32_t bound_here = block_bound(za, zb, (K + blocks - 1) / blocks, &s.bound);
+    const uint32_t bound_here = block_bound({za, zb}, (K + blocks - 1) / blocks, &s.bound);
     const float wm = warp_largest(fmaxf(za, zb));
     if (lane == 0) s.fbuf[warp] = wm;
     __syncthreads();
@@ -176,32 +354,51 @@ top_tile_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
         m = fmaxf(m, s.stats[b].m);
         bound = min(bound, s.stats[b].bound);
     }
-    const float ms = isinf(m) ? 0.f : m, c = kLog2E * o.inv_tau, zb_min = bound_logit(bound);
+    const float c = kLog2E * o.inv_tau, z_min = bound_logit(bound);
 
-    float s0 = 0.f, s1 = 0.f;
+    // the powers, and the pieces that hold an entry; their entries after the
+    // pass, by threads side by side (a thread that met one in the pass would
+    // hold up its warp)
+    const PowerBase base(m, c);
+    f32x2 y0 = 0, y1 = 0;
+    auto pass = [&](const auto& power) {
 #pragma unroll 2
-    for (int j = tid; j < slice.n; j += kTopThreads) {
-        const uint4 u = tile16[j];
-        float z[P::N];
-        P::load(u, z);
-        if (o.lse) {
+        for (int j = tid; j < slice.n; j += kTopThreads) {
+            const uint4 u = tile16[j];
+            if (o.lse) {
+                f32x2 z[P::N / 2];
+                load_pairs<T>(u, z);
 #pragma unroll
-            for (int i = 0; i < P::N; i += 2) {
-                s0 += exp2_unit((z[i] - ms) * c);
-                s1 += exp2_unit((z[i + 1] - ms) * c);
+                for (int i = 0; i < P::N / 2; i += 2) {
+                    y0 = add2(y0, power(z[i]));
+                    y1 = add2(y1, power(z[i + 1]));
+                }
+            }
+            if (P::largest_of(u) >= z_min) {
+                const unsigned at = atomicAdd(&s.n_pieces, 1u);
+                if (at < kPieces) s.pieces[at] = (unsigned short)j;
             }
         }
-        if (P::largest_of(u) >= zb_min) {
-#pragma unroll
-            for (int i = 0; i < P::N; ++i)
-                if (z[i] >= zb_min && z[i] > BITLOGIC_NEG_INF) {
-                    const unsigned at = atomicAdd(&s.n_local, 1u);
-                    const int v = slice.first + j * P::N + i;
-                    if (at < kTopList) s.local[at] = ((unsigned long long)logit_key(z[i]) << 32) | (uint32_t)~v;
-                }
+    };
+    if (base.far) pass(FarPairs(base));
+    else pass(NearPairs(base));
+    float sum_a, sum_b;
+    unpack2(add2(y0, y1), sum_a, sum_b);
+    const float sum = block_add(sum_a + sum_b, s.fbuf, kTopWarps);
+    const unsigned n_pieces = s.n_pieces;
+    if (n_pieces <= kPieces) {
+        for (unsigned i = tid; i < n_pieces * P::N; i += kTopThreads) {
+            const int p = s.pieces[i / P::N] * P::N + i % P::N;
+            const float v = logit_value(tile[p]);
+            if (v >= z_min && v > BITLOGIC_NEG_INF) {
+                const unsigned at = atomicAdd(&s.n_local, 1u);
+                if (at < kTopList) s.local[at] = ((unsigned long long)logit_key(v) << 32) | (uint32_t)~(slice.first + p);
+            }
         }
+    } else if (tid == 0) {
+        s.n_local = kTopList + 1;   // more than the list holds
     }
-    const float sum = block_add(s0 + s1, s.fbuf, kTopWarps);
+    __syncthreads();
     // the slice's entries to the first block
     const unsigned n = min(s.n_local, (unsigned)kTopList);
     if (tid == 0) {
@@ -222,7 +419,7 @@ top_tile_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
     if (o.lse && tid == 0) {
         float t = 0.f;
         for (unsigned b = 0; b < blocks; ++b) t += s.sums[b];
-        o.lse[row] = ms * o.inv_tau + logf(t);
+        o.lse[row] = isinf(m) && m > 0.f ? lse_of_inf(x, V) : base.log_of(t, o.inv_tau);
     }
     const unsigned total = s.n_list;
     __syncthreads();
@@ -230,28 +427,7 @@ top_tile_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
         top_of_stream(x, V, o, row, &s.scratch);
         return;
     }
-    if (total <= 256) {
-        // every entry to the place of its rank
-        const unsigned long long e = tid < (int)total ? s.list[tid] : 0ull;
-        unsigned r = 0;
-        for (unsigned j = 0; j < total; ++j) r += s.list[j] > e;
-        if (tid < (int)total && r < (unsigned)K) {
-            o.val[row * K + r] = key_logit((uint32_t)(e >> 32));
-            o.idx[row * K + r] = (int)~(uint32_t)e;
-        }
-    } else {
-        const int size = total <= 512 ? 512 : 1024;
-        for (int i = total + tid; i < size; i += kTopThreads) s.list[i] = 0ull;
-        block_sort_falling(s.list, size);
-        if (tid < K) {
-            o.val[row * K + tid] = key_logit((uint32_t)(s.list[tid] >> 32));
-            o.idx[row * K + tid] = (int)~(uint32_t)s.list[tid];
-        }
-    }
-    if (tid < K && tid >= (int)total) {
-        o.val[row * K + tid] = BITLOGIC_NEG_INF;
-        o.idx[row * K + tid] = -1;
-    }
+    write_top(s.list, total, o, row);
 }
 
 // Rows of few classes: a warp per row, PER keys in the registers of a lane.
@@ -338,7 +514,11 @@ top_narrow_kernel(const T* __restrict__ X, long long ld, int V, long long rows, 
     }
 }
 
-// Slices of at most kTileFit bytes leave room for three blocks on an SM.
+// Few rows go by clusters, so that several SMs share one (16 rows of 2^17 bf16
+// 9.7 against 17.2 us in a block each, 64 rows 13.5 against 17.6); from half a
+// row per SM on a block per row is faster (100 rows 17.6 against 20.3 us, 4096
+// rows 248 against 490).  Slices of at most kTileFit bytes leave room for three
+// blocks on an SM.
 constexpr int kTileFit = 56 * 1024, kTileMost = 200 * 1024, kTileLeast = 8 * 1024;
 
 template <typename T>
@@ -350,11 +530,13 @@ int launch_top(const T* x, long long T_, int V, long long ld, const TopOut& o, c
         auto kern = V <= 32 ? top_narrow_kernel<T, 1> : V <= 128 ? top_narrow_kernel<T, 4>
                   : V <= 256 ? top_narrow_kernel<T, 8> : top_narrow_kernel<T, 32>;
         e = launch_rows(kern, grid, 1, kNarrowWarps * 32, smem, stream, x, ld, V, T_, o);
-    } else if (const int blocks = blocks_per_row(T_, V, sizeof(T), kTileFit, kTileMost, kTileLeast)) {
-        e = launch_rows(top_tile_kernel<T>, T_, blocks, kTopThreads, (size_t)slice_bytes(V, sizeof(T), blocks), stream,
-                        x, ld, V, o);
     } else {
-        e = launch_rows(top_stream_kernel<T>, T_, 1, kTopThreads, 0, stream, x, ld, V, o);
+        const int blocks = 2 * T_ <= sm_count() ? blocks_per_row(T_, V, sizeof(T), kTileFit, kTileMost, kTileLeast) : 0;
+        if (blocks > 0)
+            e = launch_rows(top_tile_kernel<T>, T_, blocks, kTopThreads, (size_t)slice_bytes(V, sizeof(T), blocks), stream,
+                            x, ld, V, o);
+        else
+            e = launch_rows(top_row_kernel<T>, T_, 1, kTopThreads, 0, stream, x, ld, V, o);
     }
     return e == cudaSuccess ? launch_status() : (int)BITLOGIC_ERR_CUDA;
 }
