@@ -267,7 +267,7 @@ __device__ void sample_of_stream(const T* __restrict__ x, int V, RowSettings set
 
 constexpr int kList = 2048;       // entries that a cut or a draw looks at in the end
 constexpr int kListTop = 1024;    // largest top_k that goes by the list
-constexpr int kBinsPerOctave = 64, kBins = 42 * kBinsPerOctave;   // weights below 2^-41 are 0
+constexpr int kBinsPerOctave = 64, kBins = 42 * kBinsPerOctave;   // weights of powers below 2^-41 are 0
 
 struct SampleShared {
     union {
@@ -302,15 +302,52 @@ struct SampleShared {
     unsigned n_list, n_local, base;
 };
 
-// Bin of a power's exponent y = (m - z) slope >= 0, and a bin's unit of mass: a
-// power in bin b counts e 2^(15 + b / 64) units (2^14 to 2^15 of them), so
-// that a bin sums in 32 bits and is right to 2^-15.
-__device__ __forceinline__ int bin_of(float y) { return (int)fminf(y * kBinsPerOctave, (float)(kBins - 1)); }
-__device__ __forceinline__ unsigned bin_units(float e, int b) {
-    return (unsigned)__float2uint_rn(e * __uint_as_float((unsigned)(127 + 15 + b / kBinsPerOctave) << 23));
-}
+// Bins of the powers e, falling: by the exponent and the 6 leading bits of the
+// mantissa, so that the powers above bin b are those with e > bin_above(b); bin
+// 64 is the first below 1.  A power counts its mantissa's 15 leading bits, so
+// that a bin of 2^17 of them sums in 32 bits and is right to 2^-14 of itself.
+__device__ __forceinline__ int bin_of(float e) { return min((int)((0x3fffffffu - __float_as_uint(e)) >> 17), kBins - 1); }
+__device__ __forceinline__ unsigned bin_units(float e) { return (((__float_as_uint(e) & 0x7fffffu) | 0x800000u) + 256u) >> 9; }
 __device__ __forceinline__ float bin_mass(unsigned units, int b) {
-    return (float)units * __uint_as_float((unsigned)(127 - 15 - b / kBinsPerOctave) << 23);
+    return (float)units * __uint_as_float((unsigned)(127 - 14 - b / kBinsPerOctave) << 23);
+}
+__device__ __forceinline__ float bin_above(int b) { return __uint_as_float(0x3fffffffu - ((unsigned)b << 17)); }
+
+// A logit below which no power exceeds e (some of those above it may not).
+__device__ __forceinline__ float logit_below(float e, const Power& p) {
+    return p.slope > 0.f ? p.m - fabsf(p.m) * 1e-6f - (0.02f - 1.000001f * log2f(e)) / p.slope : BITLOGIC_NEG_INF;
+}
+
+// The bin in which a mass is reached from the largest power down (the last one
+// if none), into *bin.  Called by the whole block.
+__device__ __forceinline__ void find_bin(const unsigned* bins, float goal, int* bin, float* fbuf) {
+    constexpr int kPer = (kBins + kSampleThreads - 1) / kSampleThreads;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    float sum = 0.f;
+    for (int q = 0; q < kPer; ++q) {
+        const int b = tid * kPer + q;
+        if (b < kBins) sum += bin_mass(bins[b], b);
+    }
+    float upto = sum;
+    for (int o = 1; o < 32; o <<= 1) {
+        const float t = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += t;
+    }
+    if (lane == 31) fbuf[warp] = upto;
+    if (tid == 0) *bin = kBins - 1;
+    __syncthreads();
+    float before = upto - sum;
+    for (int w = 0; w < warp; ++w) before += fbuf[w];
+    if (before < goal && before + sum >= goal * 0.9999f)
+        for (int q = 0; q < kPer; ++q) {
+            const int b = tid * kPer + q;
+            if (b < kBins) {
+                const float m = bin_mass(bins[b], b);
+                if (before < goal && before + m >= goal) atomicMin(bin, b);
+                before += m;
+            }
+        }
+    __syncthreads();
 }
 
 // The sum of v over the block's threads before this one, and over all of them.
@@ -331,6 +368,38 @@ __device__ __forceinline__ unsigned long long block_before(unsigned long long v,
 }
 
 __device__ __forceinline__ int power_of_two(unsigned n) { return n <= 32 ? 32 : 1 << (32 - __clz(n - 1)); }
+
+// The last class kept by mass: the exact mass before the list is `first`, the
+// list is sorted here, and `kept(entry, e, w)` is called for every class kept
+// on it.  found->slow stays set where the mass is not reached on it.  Called by
+// the whole block.
+template <typename Found, typename Kept>
+__device__ __forceinline__ void find_cut(unsigned long long* list, unsigned listed, unsigned long long first,
+                                         unsigned long long want, const Power& power, unsigned long long* sums,
+                                         Found* found, Kept&& kept) {
+    const int tid = threadIdx.x, size = power_of_two(listed), per = ((int)listed + kSampleThreads - 1) / kSampleThreads;
+    for (int i = listed + tid; i < size; i += kSampleThreads) list[i] = 0ull;
+    block_sort_falling(list, size);
+    const int i0 = tid * per, i1 = min((int)listed, i0 + per);
+    unsigned long long own = 0, all;
+    for (int i = i0; i < i1; ++i) own += draw_weight(power.of(key_logit((uint32_t)(list[i] >> 32))));
+    unsigned long long run = first + block_before(own, sums, &all);
+    for (int i = i0; i < i1 && run < want; ++i) {
+        const uint32_t key = (uint32_t)(list[i] >> 32);
+        const float e = power.of(key_logit(key));
+        const unsigned long long w = draw_weight(e);
+        kept(list[i], e, w);
+        if (run + w >= want) {   // the last one
+            unsigned ties = 1;   // with those of its key before it
+            for (int r = i - 1; r >= 0 && (uint32_t)(list[r] >> 32) == key; --r) ++ties;
+            found->key = key;
+            found->ties = ties;
+            found->slow = 0u;
+        }
+        run += w;
+    }
+    __syncthreads();
+}
 
 // The first block's work where the row's first k classes are all on its list:
 // the cut by rank and mass on the sorted list, then the draw among the kept
@@ -534,7 +603,8 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
             mass += ws.total();
         }
         mass = block_add(mass, s.warp_mass, kSampleWarps);
-        for (int b = tid; b < kBins; b += kSampleThreads) s.bins[b] = 0u;
+        unsigned* row_bins = reinterpret_cast<unsigned*>(s.list);
+        for (int b = tid; b < kBins; b += kSampleThreads) s.bins[b] = row_bins[b] = 0u;
         if (tid < (int)blocks) put_in_block(&s.sums[rank], tid, SampleShared::Sums{mass, 0u, 0u});
         row_barrier();
         unsigned long long total = 0;
@@ -543,91 +613,68 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
         if (want < 1) want = 1;
         // classes with less than a V-th of what top_p leaves off come after it
         const float left_off = fmaxf((float)(total - want) * (1.0f / 1099511627776.0f) / (float)V, 2.3e-13f);
-        const float y_max = fminf(-log2f(left_off) + 0.01f, 41.0f);
-        const float z_min = power.slope > 0.f ? power.m - fabsf(power.m) * 1e-6f - (y_max + 0.01f) / power.slope : BITLOGIC_NEG_INF;
+        const float z_min = logit_below(left_off, power);
         for (int j = tid; j < slice.n; j += kSampleThreads) {
             const uint4 u = tile16[j];
             if (P::largest_of(u) >= z_min) {
-                float z[P::N];
-                P::load(u, z);
+                f32x2 z[P::N / 2];
+                load_pairs<T>(u, z);
 #pragma unroll
-                for (int i = 0; i < P::N; ++i)
-                    if (z[i] >= z_min && z[i] > BITLOGIC_NEG_INF) {
-                        const int b = bin_of((power.m - z[i]) * power.slope);
-                        atomicAdd(&s.bins[b], bin_units(power.of(z[i]), b));
-                    }
+                for (int i = 0; i < P::N / 2; ++i) {
+                    float a, b;
+                    unpack2(pairs(z[i]), a, b);
+                    if (a >= left_off) atomicAdd(&s.bins[bin_of(a)], bin_units(a));
+                    if (b >= left_off) atomicAdd(&s.bins[bin_of(b)], bin_units(b));
+                }
             }
         }
         __syncthreads();
         // the bins of all blocks added up where the first one keeps its list (a
         // sum past 32 bits, of more than 2^17 equal logits, picks a wrong bin,
         // which the exact sums below show)
-        constexpr int kBinPer = (kBins + kSampleThreads - 1) / kSampleThreads;
-        unsigned* row_bins = reinterpret_cast<unsigned*>(s.list);
-        if (rank == 0)
-            for (int b = tid; b < kBins; b += kSampleThreads) row_bins[b] = 0u;
-        row_barrier();
         for (int b = tid; b < kBins; b += kSampleThreads)
             if (s.bins[b]) add_in_block(row_bins + b, 0, s.bins[b]);
         row_barrier();
         if (rank == 0) {
-            // the bin in which the mass is reached: thread t sums bins
-            // [t per, (t + 1) per)
-            float sum = 0.f;
-            for (int q = 0; q < kBinPer; ++q) {
-                const int b = tid * kBinPer + q;
-                if (b < kBins) sum += bin_mass(row_bins[b], b);
-            }
-            float upto = sum;
-            for (int o = 1; o < 32; o <<= 1) {
-                const float t = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += t;
-            }
-            if (lane == 31) s.fbuf[warp] = upto;
-            if (tid == 0) s.bin = kBins - 1;
-            __syncthreads();
-            float before = upto - sum;
-            for (int w = 0; w < warp; ++w) before += s.fbuf[w];
-            const float goal = (float)want * (1.0f / 1099511627776.0f);
-            for (int q = 0; q < kBinPer; ++q) {
-                const int b = tid * kBinPer + q;
-                if (b < kBins) {
-                    const float mb_ = bin_mass(row_bins[b], b);
-                    if (before < goal && before + mb_ >= goal) atomicMin(&s.bin, b);
-                    before += mb_;
-                }
-            }
-            __syncthreads();
+            find_bin(row_bins, (float)want * (1.0f / 1099511627776.0f), &s.bin, s.fbuf);
             const int b = s.bin;
             if (tid < (int)blocks) store_in_block(&s.bin, tid, (uint32_t)b);
             if (tid == 0) s.n_list = 0;
         }
         if (tid == 0) s.n_local = 0;
         row_barrier();
-        // logits of bins bin - 1 to bin + 1: a bin's logits are those whose
-        // exponent rounds into it, so the test below is the bin's own
-        const int b0 = max(0, s.bin - 1), b1 = min(kBins - 1, s.bin + 1);
-        mass = 0;
+        // the exact mass above bins bin - 1 to bin + 1, and their entries
+        const float e_above = bin_above(max(0, s.bin - 1)), e_list = bin_above(min(kBins, s.bin + 2)), z_list = logit_below(e_list, power);
+        WeightSum ws;
         for (int j = tid; j < slice.n; j += kSampleThreads) {
             const uint4 u = tile16[j];
-            if (P::largest_of(u) >= z_min) {
-                float z[P::N];
-                P::load(u, z);
+            if (P::largest_of(u) >= z_list) {
+                f32x2 z[P::N / 2];
+                load_pairs<T>(u, z);
+                bool any = false;
 #pragma unroll
-                for (int i = 0; i < P::N; ++i)
-                    if (z[i] >= z_min && z[i] > BITLOGIC_NEG_INF) {
-                        const int b = bin_of((power.m - z[i]) * power.slope);
-                        if (b < b0) {
-                            mass += draw_weight(power.of(z[i]));
-                        } else if (b <= b1) {
+                for (int i = 0; i < P::N / 2; ++i) {
+                    float a, b;
+                    unpack2(pairs(z[i]), a, b);
+                    ws.add(pack2(a > e_above ? a : 0.f, b > e_above ? b : 0.f));
+                    any |= (a > e_list && a <= e_above) || (b > e_list && b <= e_above);
+                }
+                if (any) {
+                    float x_[P::N];
+                    P::load(u, x_);
+#pragma unroll
+                    for (int i = 0; i < P::N; ++i) {
+                        const float e = power.of(x_[i]);
+                        if (e > e_list && e <= e_above) {
                             const unsigned at = atomicAdd(&s.n_local, 1u);
                             const int v = slice.first + j * P::N + i;
-                            if (at < kList) s.local[at] = ((unsigned long long)logit_key(z[i]) << 32) | (uint32_t)~v;
+                            if (at < kList) s.local[at] = ((unsigned long long)logit_key(x_[i]) << 32) | (uint32_t)~v;
                         }
                     }
+                }
             }
         }
-        mass = block_add(mass, s.warp_mass, kSampleWarps);
+        mass = block_add(ws.total(), s.warp_mass, kSampleWarps);
         const unsigned n = min(s.n_local, (unsigned)kList);
         if (tid == 0) {
             s.base = add_in_block(&s.n_list, 0, s.n_local);
@@ -638,38 +685,13 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
             if (s.base + i < kList) put_in_block(&s.list[s.base + i], 0, s.local[i]);
         row_barrier();
         if (rank == 0) {
-            constexpr int kPer = kList / kSampleThreads;
-            unsigned long long before = 0;
-            for (unsigned b = 0; b < blocks; ++b) before += s.sums[b].mass;
-            const unsigned long long first = before;
+            unsigned long long first = 0;
+            for (unsigned b = 0; b < blocks; ++b) first += s.sums[b].mass;
             const unsigned listed = s.n_list;
             if (tid == 0) s.found = {0u, 0u, 1u, 0u};   // not found: from memory
             __syncthreads();
-            if (listed <= kList && listed > 0 && first < want) {
-                const int size = power_of_two(listed);
-                for (int i = listed + tid; i < size; i += kSampleThreads) s.list[i] = 0ull;
-                block_sort_falling(s.list, size);
-                unsigned long long w[kPer], sum = 0, all;
-#pragma unroll
-                for (int q = 0; q < kPer; ++q) {
-                    const int i = tid * kPer + q;
-                    w[q] = i < (int)listed ? draw_weight(power.of(key_logit((uint32_t)(s.list[i] >> 32)))) : 0ull;
-                    sum += w[q];
-                }
-                before = first + block_before(sum, s.scan.sums, &all);
-#pragma unroll
-                for (int q = 0; q < kPer; ++q) {
-                    const int i = tid * kPer + q;
-                    if (before < want && before + w[q] >= want) {   // the last one kept
-                        const uint32_t key = (uint32_t)(s.list[i] >> 32);
-                        unsigned ties = 1;   // with those of its key before it
-                        for (int r = i - 1; r >= 0 && (uint32_t)(s.list[r] >> 32) == key; --r) ++ties;
-                        s.found = {key, ties, 0u, 0u};
-                    }
-                    before += w[q];
-                }
-            }
-            __syncthreads();
+            if (listed <= kList && listed > 0 && first < want)
+                find_cut(s.list, listed, first, want, power, s.scan.sums, &s.found, [](unsigned long long, float, unsigned long long) {});
             const SampleShared::Found f = s.found;
             if (tid < (int)blocks && tid > 0) put_in_block(&s.found, tid, f);
         }
@@ -698,22 +720,23 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
             mass += ws.total();
         }
     } else {
+        WeightSum ws;
         for (int j = j0 + lane; j < j1; j += 32) {
             const uint4 u = tile16[j];
             if (P::largest_of(u) >= z_cut) {
-                float z[P::N];
-                P::load(u, z);
+                f32x2 z[P::N / 2];
+                load_pairs<T>(u, z);
 #pragma unroll
-                for (int i = 0; i < P::N; ++i) {
-                    if (z[i] > z_cut) {
-                        const float e = power.of(z[i]);
-                        if (e >= set.floor_e) mass += draw_weight(e);
-                    } else if (z[i] == z_cut) {
-                        ++eq;
-                    }
+                for (int i = 0; i < P::N / 2; ++i) {
+                    float a, b, za_, zb_;
+                    unpack2(pairs.at_least(z[i], set.floor_e), a, b);
+                    unpack2(z[i], za_, zb_);
+                    ws.add(pack2(za_ > z_cut ? a : 0.f, zb_ > z_cut ? b : 0.f));
+                    eq += (za_ == z_cut) + (zb_ == z_cut);
                 }
             }
         }
+        mass = ws.total();
     }
     mass = warp_add(mass);
     eq = __reduce_add_sync(0xffffffffu, eq);
@@ -981,18 +1004,18 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
         if (want < 1) want = 1;
         // classes with less than a V-th of what top_p leaves off come after it
         const float left_off = fmaxf((float)(total - want) * (1.0f / 1099511627776.0f) / (float)V, 2.3e-13f);
-        const float y_max = fminf(-log2f(left_off) + 0.01f, 41.0f);
-        const float z_min = power.slope > 0.f ? power.m - fabsf(power.m) * 1e-6f - (y_max + 0.01f) / power.slope : BITLOGIC_NEG_INF;
+        const float z_min = logit_below(left_off, power);
         auto count = [&](const uint4& u) {
             if (P::largest_of(u) >= z_min) {
-                float z[N];
-                P::load(u, z);
+                f32x2 z[H];
+                load_pairs<T>(u, z);
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (z[i] >= z_min && z[i] > BITLOGIC_NEG_INF) {
-                        const int b = bin_of((power.m - z[i]) * power.slope);
-                        atomicAdd(&s.bins[b], bin_units(power.of(z[i]), b));
-                    }
+                for (int i = 0; i < H; ++i) {
+                    float a, b;
+                    unpack2(pairs(z[i]), a, b);
+                    if (a >= left_off) atomicAdd(&s.bins[bin_of(a)], bin_units(a));
+                    if (b >= left_off) atomicAdd(&s.bins[bin_of(b)], bin_units(b));
+                }
             }
         };
         stream_row([&](const uint4 (&u)[4], int) {
@@ -1002,63 +1025,43 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
         stream.load(0, ua);
         stream.load(1, ub);
         count(u_end);
-        if (tid == 0) s.bin = kBins - 1;
         __syncthreads();
-        // the bin in which the mass is reached
-        constexpr int kBinPer = (kBins + kSampleThreads - 1) / kSampleThreads;
-        float sum = 0.f;
-        for (int q = 0; q < kBinPer; ++q) {
-            const int b = tid * kBinPer + q;
-            if (b < kBins) sum += bin_mass(s.bins[b], b);
-        }
-        float upto = sum;
-        for (int o = 1; o < 32; o <<= 1) {
-            const float t = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += t;
-        }
-        if (lane == 31) s.fbuf[warp] = upto;
+        find_bin(s.bins, (float)want * (1.0f / 1099511627776.0f), &s.bin, s.fbuf);
+        // the exact mass above bins bin - 1 to bin + 1, and its kept part by
+        // chunk; the pieces that hold entries of those bins wait until the pass
+        // is over (where the bins were)
+        const float e_above = bin_above(max(0, s.bin - 1)), e_list = bin_above(min(kBins, s.bin + 2)), z_list = logit_below(e_list, power);
         __syncthreads();
-        float before_bin = upto - sum;
-        for (int w = 0; w < warp; ++w) before_bin += s.fbuf[w];
-        const float goal = (float)want * (1.0f / 1099511627776.0f);
-        for (int q = 0; q < kBinPer; ++q) {
-            const int b = tid * kBinPer + q;
-            if (b < kBins) {
-                const float mb = bin_mass(s.bins[b], b);
-                if (before_bin < goal && before_bin + mb >= goal) atomicMin(&s.bin, b);
-                before_bin += mb;
-            }
-        }
-        __syncthreads();
-        // the exact mass above the bins around it, by chunk where it is kept,
-        // and the entries of those bins
-        const int b0 = max(0, s.bin - 1), b1 = min(kBins - 1, s.bin + 1);
         mass = 0;
-        auto above = [&](const uint4& u, int j, WeightSum& kept) {
-            if (P::largest_of(u) < z_min) return;
-            float z[N];
-            P::load(u, z);
+        auto above = [&](const uint4& u, int j, WeightSum& kept, WeightSum& cut_off) {
+            if (P::largest_of(u) < z_list) return;
+            f32x2 z[H];
+            load_pairs<T>(u, z);
+            bool any = false;
 #pragma unroll
-            for (int i = 0; i < N; i += 2) {
-                float e[2];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const bool in = z[i + h] >= z_min && z[i + h] > BITLOGIC_NEG_INF;
-                    const int b = in ? bin_of((power.m - z[i + h]) * power.slope) : kBins;
-                    if (b >= b0 && b <= b1) list_entry(z[i + h], slice.first + j * N + i + h);
-                    e[h] = b < b0 ? power.of(z[i + h]) : 0.f;
-                    if (e[h] < set.floor_e) {
-                        mass += draw_weight(e[h]);   // counts for the cut, but is not kept
-                        e[h] = 0.f;
-                    }
+            for (int i = 0; i < H; ++i) {
+                float a, b;
+                unpack2(pairs(z[i]), a, b);
+                any |= (a > e_list && a <= e_above) || (b > e_list && b <= e_above);
+                a = a > e_above ? a : 0.f;
+                b = b > e_above ? b : 0.f;
+                if (set.floor_e > 0.f) {   // counts for the cut, but is not kept
+                    cut_off.add(pack2(a < set.floor_e ? a : 0.f, b < set.floor_e ? b : 0.f));
+                    a = a < set.floor_e ? 0.f : a;
+                    b = b < set.floor_e ? 0.f : b;
                 }
-                kept.add(pack2(e[0], e[1]));
+                kept.add(pack2(a, b));
+            }
+            if (any) {
+                const unsigned at = atomicAdd(&s.n_groups, 1u);
+                if (at < kBins) s.bins[at] = (unsigned)j;
             }
         };
         stream_row([&](const uint4 (&u)[4], int q) {
-            WeightSum kept;
+            WeightSum kept, cut_off;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) above(u[i], stream.piece(q, i), kept);
+            for (int i = 0; i < 4; ++i) above(u[i], stream.piece(q, i), kept, cut_off);
+            mass += cut_off.total();
             const unsigned long long w = kept.warp_total();
             if (lane == 0) {
                 chunks[1 + kSampleWarps * q + warp] = w;
@@ -1068,48 +1071,31 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
         if (tid == 0) chunks[0] = chunks[last_chunk] = 0ull;
         __syncthreads();
         if (j_end >= 0) {
-            WeightSum kept;
-            above(u_end, j_end, kept);
+            WeightSum kept, cut_off;
+            above(u_end, j_end, kept, cut_off);
             chunks[end_chunk] = kept.total();
-            mass += kept.total();
+            mass += kept.total() + cut_off.total();
         }
         const unsigned long long first = block_add(mass, s.mass, kSampleWarps);
-        const unsigned listed = s.n;
-        if (tid == 0) s.found = {0u, 0u, 1u};   // not found: from memory
-        __syncthreads();
-        constexpr int kPer = kRowList / kSampleThreads;
-        if (listed <= kRowList && listed > 0 && first < want) {
-            const int size = power_of_two(listed);
-            for (int i = listed + tid; i < size; i += kSampleThreads) s.list[i] = 0ull;
-            block_sort_falling(s.list, size);
-            unsigned long long part = 0, all;
-            for (int q = 0; q < kPer; ++q) {
-                const int i = tid * kPer + q;
-                if (i < (int)listed) part += draw_weight(power.of(key_logit((uint32_t)(s.list[i] >> 32))));
-            }
-            unsigned long long run = first + block_before(part, s.scan.sums, &all);
-            for (int q = 0; q < kPer; ++q) {
-                const int i = tid * kPer + q;
-                if (i >= (int)listed) break;
-                const uint32_t key = (uint32_t)(s.list[i] >> 32);
-                const float e = power.of(key_logit(key));
-                const unsigned long long w = draw_weight(e);
-                if (run < want) {   // kept: its weight to its chunk
-                    if (e >= set.floor_e && w) {
-                        const int p = (int)~(uint32_t)s.list[i] - slice.first, j = p / N - slice.whole0();
-                        const int c = j < 0 ? 0 : j >= slice.whole1(V) - slice.whole0() ? last_chunk : 1 + j / 128;
-                        atomicAdd(&chunks[c], w);
-                    }
-                    if (run + w >= want) {   // the last one
-                        unsigned ties = 1;   // with those of its key before it
-                        for (int r = i - 1; r >= 0 && (uint32_t)(s.list[r] >> 32) == key; --r) ++ties;
-                        s.found = {key, ties, 0u};
-                    }
-                }
-                run += w;
+        const unsigned waiting = s.n_groups;
+        for (unsigned i = tid; i < min(waiting, (unsigned)kBins) * N; i += kSampleThreads) {
+            const int v = slice.first + (int)s.bins[i / N] * N + (int)(i % N);
+            if (v >= 0 && v < V) {
+                const float z = logit_value(x[v]), e = power.of(z);
+                if (e > e_list && e <= e_above) list_entry(z, v);
             }
         }
+        if (tid == 0) s.found = {0u, 0u, 1u};   // not found: from memory
         __syncthreads();
+        const unsigned listed = s.n;
+        __syncthreads();
+        if (waiting <= kBins && listed <= kRowList && listed > 0 && first < want)
+            find_cut(s.list, listed, first, want, power, s.scan.sums, &s.found, [&](unsigned long long entry, float e, unsigned long long w) {
+                if (e >= set.floor_e && w) {   // its weight to its chunk
+                    const int j = ((int)~(uint32_t)entry - slice.first) / N - slice.whole0();
+                    atomicAdd(&chunks[j < 0 ? 0 : j >= slice.whole1(V) - slice.whole0() ? last_chunk : 1 + j / 128], w);
+                }
+            });
         if (s.found.slow) {
             sample_of_stream(x, V, set, row, out, &s.stream);
             return;
@@ -1227,13 +1213,15 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
     }
 }
 
-// Rows of few classes: a warp per row, PER logits in the registers of a lane
-// (class 32 i + lane).
+// Rows of few classes: a warp per row, PER keys and weights in the registers of
+// a lane (class 32 i + lane).  A weight is held as w = 2^21 high + low (see
+// WeightSum), so that a warp's sums are two 32-bit reductions.
 constexpr int kNarrow = 1024, kNarrowWarps = 8;
 
 template <typename T, int PER>
 __global__ void __launch_bounds__(kNarrowWarps * 32)
 sample_narrow_kernel(const T* __restrict__ X, long long ld, int V, long long rows, Settings settings, Draw out) {
+    constexpr int kKeyBits = sizeof(T) == 2 ? 19 : 32;   // leading bits of a key that differ (fp16 fills 19)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     grid_dependency_wait();
     allow_dependent_launch();
@@ -1255,102 +1243,118 @@ sample_narrow_kernel(const T* __restrict__ X, long long ld, int V, long long row
         return;
     }
     const Power power(m, set);
-    auto share = [&](int i) { return z[i] > BITLOGIC_NEG_INF ? power(z[i]) : 0.f; };
-    Cut cut = {kNoCut, 0};
-    if (set.k < V) {
-        unsigned n = 0;
+    uint32_t key[PER], high[PER];
+    int low[PER];
+    unsigned ranked = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) n += ranks(logit_key(z[i]));
-        n = __reduce_add_sync(0xffffffffu, n);
-        if ((unsigned)set.k < n) {
-            uint32_t t = 0;
-            unsigned reach = 0;
-            for (uint32_t bit = 0x80000000u; bit > 0 && reach != (unsigned)set.k; bit >>= 1) {
-                unsigned h = 0;
-#pragma unroll
-                for (int i = 0; i < PER; ++i) h += logit_key(z[i]) >= (t | bit);
-                h = __reduce_add_sync(0xffffffffu, h);
-                if (h >= (unsigned)set.k) {
-                    t |= bit;
-                    reach = h;
-                }
-            }
-            unsigned above = 0;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) above += logit_key(z[i]) > t;
-            above = __reduce_add_sync(0xffffffffu, above);
-            cut.key = t;
-            cut.ties = set.k - above;
-        }
+    for (int i = 0; i < PER; ++i) {
+        key[i] = logit_key(z[i]);
+        ranked += ranks(key[i]);
+        const float e = ranks(key[i]) ? power(z[i]) : 0.f, t = e + 16.0f;
+        high[i] = __float_as_uint(t) - 0x41800000u;
+        low[i] = (int)(__float_as_uint(fmaf(e - (t - 16.0f), 1099511627776.0f, 12582912.0f)) - 0x4b400000u);
+        if (!ranks(key[i])) key[i] = 0u;
     }
-    if (set.p < 1.0f) {
-        unsigned long long mass = 0;
+    // the weight of the keys that `in` takes, over the warp
+    auto weigh = [&](auto&& in) {
+        unsigned h = 0;
+        int l = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            if (logit_key(z[i]) > cut.key) mass += draw_weight(share(i));
-        mass = warp_add(mass);
-        const unsigned long long we = cut.ties ? draw_weight(power(key_logit(cut.key))) : 0ull;
-        unsigned long long want = share_of(mass + cut.ties * we, set.p);
-        if (want < 1) want = 1;
-        if (want > mass) {
-            const unsigned long long nd = we ? (want - mass + we - 1) / we : cut.ties;
-            if (nd < cut.ties) cut.ties = nd;
-        } else {
-            // the largest key that the mass is reached at, a bit at a time
-            uint32_t t = 0;
-            for (uint32_t bit = 0x80000000u; bit > 0; bit >>= 1) {
-                unsigned long long h = 0;
-#pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const uint32_t kk = logit_key(z[i]);
-                    if (kk >= (t | bit) && kk > cut.key) h += draw_weight(share(i));
-                }
-                if (warp_add(h) >= want) t |= bit;
+            if (in(key[i])) {
+                h += high[i];
+                l += low[i];
             }
-            unsigned long long above = 0;
+        h = __reduce_add_sync(0xffffffffu, h);
+        l = (int)__reduce_add_sync(0xffffffffu, (unsigned)l);
+        return ((unsigned long long)h << 21) + (unsigned long long)(long long)l;
+    };
+    Cut cut = {kNoCut, 0};
+    unsigned long long wt = 0;   // of a class at the cut
+    auto weight_at = [&](uint32_t k) { return draw_weight(power(key_logit(k))); };
+    if (set.k < V && (unsigned)set.k < __reduce_add_sync(0xffffffffu, ranked)) {
+        uint32_t t = 0;
+        unsigned reach = 0;
+#pragma unroll 1
+        for (uint32_t bit = 0x80000000u; bit > 0 && reach != (unsigned)set.k; bit >>= 1) {
+            unsigned h = 0;
 #pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (logit_key(z[i]) > t) above += draw_weight(share(i));
-            above = warp_add(above);
-            const unsigned long long wt = draw_weight(power(key_logit(t)));
+            for (int i = 0; i < PER; ++i) h += key[i] >= (t | bit);
+            h = __reduce_add_sync(0xffffffffu, h);
+            if (h >= (unsigned)set.k) {
+                t |= bit;
+                reach = h;
+            }
+        }
+        unsigned above = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) above += key[i] > t;
+        above = __reduce_add_sync(0xffffffffu, above);
+        cut.key = t;
+        cut.ties = set.k - above;
+        if (cut.ties) wt = weight_at(cut.key);
+    }
+    if (set.p < 1.0f) {
+        const uint32_t kt = cut.key;
+        const unsigned long long mass = weigh([&](uint32_t k) { return k > kt; });
+        unsigned long long want = share_of(mass + cut.ties * wt, set.p);
+        if (want < 1) want = 1;
+        if (want > mass) {   // reached among the ties of the top-k cut
+            const unsigned long long need = wt ? (want - mass + wt - 1) / wt : cut.ties;
+            if (need < cut.ties) cut.ties = need;
+        } else {
+            // the largest key that the mass is reached at, a bit at a time; the
+            // bits of a key that the type does not fill follow the sign
+            uint32_t t = 0;
+#pragma unroll 1
+            for (uint32_t bit = 0x80000000u; bit >= 1u << (32 - kKeyBits); bit >>= 1) {
+                const uint32_t c = t | bit;
+                if (weigh([&](uint32_t k) { return k >= c && k > kt; }) >= want) t = c;
+                if (bit == 1u) break;
+            }
+            uint32_t lowest = 0xffffffffu;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) lowest = key[i] >= t && key[i] > kt ? min(lowest, key[i]) : lowest;
+            t = __reduce_min_sync(0xffffffffu, lowest);
+            const unsigned long long above = weigh([&](uint32_t k) { return k > t; });
+            wt = weight_at(t);
             cut.key = t;
             cut.ties = wt ? (want - above + wt - 1) / wt : 1;
         }
     }
-    // kept weights in registers, then the draw, 32 classes at a time
-    unsigned long long total = 0;
-    float e[PER];
+    // kept weights, then the draw: the 32 classes it falls in, and the class
     unsigned left = (unsigned)cut.ties;
+    const float floor_e = set.floor_e;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const uint32_t kk = logit_key(z[i]);
-        const bool same = cut.ties && kk == cut.key;
+        const bool same = cut.ties && key[i] == cut.key;
         const unsigned mask = __ballot_sync(0xffffffffu, same);
-        bool kept = kk > cut.key || (same && __popc(mask & ((1u << lane) - 1u)) < left);
+        const bool kept = (key[i] > cut.key || (same && __popc(mask & ((1u << lane) - 1u)) < left)) &&
+                          (floor_e == 0.f || power(key_logit(key[i])) >= floor_e);
         left -= min(left, (unsigned)__popc(mask));
-        e[i] = kept ? share(i) : 0.f;
-        if (e[i] < set.floor_e) e[i] = 0.f;
-        total += draw_weight(e[i]);
+        if (!kept || !ranks(key[i])) high[i] = 0u, low[i] = 0;
     }
-    total = warp_add(total);
-    const unsigned long long target = share_of(total, set.u);
-    unsigned long long run = 0;
-    bool done = false;
+    const unsigned long long total = weigh([](uint32_t) { return true; }), target = share_of(total, set.u);
+    unsigned long long before = 0, w = 0;
+    int at = -1;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        if (!done) {
-            const unsigned long long w = draw_weight(e[i]);
-            const unsigned long long upto = warp_upto(w, lane);
-            const unsigned hit = __ballot_sync(0xffffffffu, run + upto > target);
-            if (hit) {
-                if (lane == __ffs(hit) - 1) {
-                    out.token[row] = 32 * i + lane;
-                    if (out.logprob) out.logprob[row] = logf((float)w / (float)total);
-                }
-                done = true;
+    for (int i = 0; i < PER; ++i)
+        if (at < 0) {
+            const unsigned h = __reduce_add_sync(0xffffffffu, high[i]);
+            const int l = (int)__reduce_add_sync(0xffffffffu, (unsigned)low[i]);
+            const unsigned long long sum = ((unsigned long long)h << 21) + (unsigned long long)(long long)l;
+            if (before + sum > target) {
+                at = i;
+                w = ((unsigned long long)high[i] << 21) + (unsigned long long)(long long)low[i];
+            } else {
+                before += sum;
             }
-            run += __shfl_sync(0xffffffffu, upto, 31);
         }
+    const unsigned long long upto = warp_upto(w, lane);
+    const unsigned hit = __ballot_sync(0xffffffffu, before + upto > target);
+    if (hit && lane == __ffs(hit) - 1) {
+        out.token[row] = 32 * at + lane;
+        if (out.logprob) out.logprob[row] = logf((float)w / (float)total);
     }
 }
 
