@@ -15,7 +15,7 @@
 //            = (sum_k q_k + q_r) p_v - q_r p_v / r  off it
 // r is summed over the classes off the record, not formed as 1 - sum_k p_k,
 // which would leave no digits of a small remainder; for the same reason q_r is
-// formed in double precision.
+// formed from pairs of fp32 numbers.
 //
 // Bound by reading the logits and writing the gradient once.
 #include "row_tile.cuh"
@@ -32,12 +32,20 @@ struct Distill {
     const float* teacher_lse;
     const int* labels;
     const float* weight;
-    double inv_tau64;
+    Pair inv_tau2;           // 1 / tau
     float inv_tau, kd, ce;   // kd = kd_weight tau^2
     float* row_loss;
     long long ldg, incg;
     float grad_scale;
 };
+
+// ln q and q of an entry of logit `val` under the teacher's log-sum-exp.
+__device__ __forceinline__ Pair teacher_log(float val, const Distill& a, float lse) {
+    const Pair p = exact_product(val, a.inv_tau2.hi);
+    return pair_add(Pair{p.hi, fmaf(val, a.inv_tau2.lo, p.lo)}, Pair{-lse, 0.f});
+}
+// max(0, 1 - Q)
+__device__ __forceinline__ float left_of(Pair Q) { return fmaxf(pair_add(Pair{1.f, 0.f}, Pair{-Q.hi, -Q.lo}).hi, 0.f); }
 
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
 
@@ -55,7 +63,7 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
     extern __shared__ __align__(16) unsigned char raw[];
     __shared__ float tbuf[kRowWarps], nbuf[kRowWarps], qbuf[kRowWarps], mbuf[kRowWarps], kbuf[kRowWarps];
     __shared__ float rest_buf[kRowWarps], member_buf[kRowWarps], sz_buf[kRowWarps];
-    __shared__ double dbuf[kRowWarps];
+    __shared__ Pair dbuf[kRowWarps];
     __shared__ int classes[kMaxTop];
     __shared__ float probs[kMaxTop];
     __shared__ int any_s, label_on_s, repeated_s;
@@ -131,15 +139,15 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
     // the teacher's probabilities
     float q = 0.f, logq = 0.f, Q = 0.f, q_left = 0.f;
     if (a.teacher_lse) {
-        double q64 = 0.0;
+        Pair q2 = {0.f, 0.f};
         if (t != BITLOGIC_NEG_INF) {
-            const double d = (double)tval * a.inv_tau64 - (double)a.teacher_lse[row];
-            logq = (float)d;
-            q64 = exp(d);
-            q = (float)q64;
+            const Pair d = teacher_log(tval, a, a.teacher_lse[row]);
+            logq = d.hi;
+            q2 = exp_pair(d);
+            q = q2.hi;
         }
-        q64 = warp_add(q64);
-        if (lane == 0) dbuf[warp] = q64;
+        q2 = warp_add(q2);
+        if (lane == 0) dbuf[warp] = q2;
         __syncthreads();
     } else {   // softmax over the record
         const float wm = warp_largest(t);
@@ -277,19 +285,19 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
     }
     __syncthreads();
     float rest = 0.f, s = 0.f, sz = 0.f;
-    double q_sum = 0.0;
+    Pair q_sum = {0.f, 0.f};
     for (int w = 0; w < kRowWarps; ++w) {
         rest += rest_buf[w];
         s += member_buf[w];
         sz += sz_buf[w];
-        if (a.teacher_lse) q_sum += dbuf[w];
+        if (a.teacher_lse) q_sum = pair_add(q_sum, dbuf[w]);
         else Q += qbuf[w];
     }
     s += rest;
     if (!TWO) sz = s;   // tau = 1 where a label is
     if (a.teacher_lse) {
-        Q = (float)q_sum;
-        q_left = (float)fmax(1.0 - q_sum, 0.0);
+        Q = q_sum.hi;
+        q_left = left_of(q_sum);
     }
     const bool any = any_s != 0, label_on = label_on_s != 0;
     allow_dependent_launch();
@@ -356,8 +364,8 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
 }
 
 // What the blocks of a row tell each other.
-struct __align__(8) DistillStats {
-    double q;               // sum of q of the entries in the slice (with teacher_lse)
+struct DistillStats {
+    Pair q;                 // sum of q of the entries in the slice (with teacher_lse)
     float m;                // largest logit
     float rest, member, sz; // powers at tau off and on the record, powers at 1
     float z_label;
@@ -385,13 +393,11 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     __shared__ float kl_part[kMaxCluster * kTileWarps];
     __shared__ float mbuf[kTileWarps], tbuf[kTileWarps], nbuf[kTileWarps], qbuf[kTileWarps];
     __shared__ float rest_buf[kTileWarps], member_buf[kTileWarps], sz_buf[kTileWarps];
-    __shared__ double dbuf[kTileWarps];
+    __shared__ Pair dbuf[kTileWarps];
     __shared__ int table[kClassTable];
     __shared__ int classes[kMaxTop];
     __shared__ float probs[kMaxTop];
-    __shared__ double own_q[kMaxTop];
-    __shared__ float own_t[kMaxTop];
-    __shared__ int any_s, label_on_s, repeated_s, n_own;
+    __shared__ int any_s, label_on_s, repeated_s;
     grid_dependency_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const unsigned rank = cluster_rank(), blocks = cluster_size();
@@ -435,7 +441,7 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     // the record: thread k holds entry k; it is this block's when its class
     // lies in the slice
     for (int i = tid; i < kClassTable; i += kTileThreads) table[i] = -1;
-    if (tid == 0) any_s = label_on_s = repeated_s = n_own = 0;
+    if (tid == 0) any_s = label_on_s = repeated_s = 0;
     if (ev >= V) {
         if (rank == 0) flag_index_error();
         ev = -1;
@@ -447,27 +453,15 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     if (label >= V && rank == 0 && tid == 0) flag_index_error();
     const int label_place = label_ok ? slice.place(label) : -1;
     float q = 0.f, logq = 0.f, Q = 0.f;
-    double q64 = 0.0;
+    Pair q2 = {0.f, 0.f};
     if (a.teacher_lse) {
-        // the slice's entries side by side, so that few warps run the double
-        // precision exponentials (4 of 128 entries' warps, each a quarter
-        // full, kept the FP64 pipe busy for a third of the kernel)
-        const double norm = (double)a.teacher_lse[row];
-        const bool own = place >= 0 && t != BITLOGIC_NEG_INF;
-        __syncthreads();
-        int slot = 0;
-        if (own) {
-            slot = atomicAdd(&n_own, 1);
-            own_t[slot] = tval;
+        if (place >= 0 && t != BITLOGIC_NEG_INF) {
+            const Pair d = teacher_log(tval, a, a.teacher_lse[row]);
+            logq = d.hi;
+            q2 = exp_pair(d);
+            q = q2.hi;
         }
         __syncthreads();
-        if (tid < n_own) own_q[tid] = exp((double)own_t[tid] * a.inv_tau64 - norm);
-        __syncthreads();
-        if (own) {
-            q64 = own_q[slot];
-            logq = (float)((double)tval * a.inv_tau64 - norm);
-            q = (float)q64;
-        }
     } else {   // softmax over the record
         const float wm = warp_largest(t);
         if (lane == 0) tbuf[warp] = wm;
@@ -559,22 +553,22 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
         unpack2(add2(s0, s1), sa, sb);
         const float rest = warp_add(ra + rb), member = warp_add(first ? ey.power(zk) : 0.f);
         const float sz = TWO ? warp_add(sa + sb + (first ? ez.power(zk) : 0.f)) : 0.f;
-        if (a.teacher_lse) q64 = warp_add(q64);
+        if (a.teacher_lse) q2 = warp_add(q2);
         if (lane == 0) {
             rest_buf[warp] = rest;
             member_buf[warp] = member;
             sz_buf[warp] = sz;
-            dbuf[warp] = q64;
+            dbuf[warp] = q2;
         }
     }
     __syncthreads();
     if (tid < (int)blocks) {
-        DistillStats s = {0.0, m, 0.f, 0.f, 0.f, z_label, label_place >= 0};
+        DistillStats s = {{0.f, 0.f}, m, 0.f, 0.f, 0.f, z_label, label_place >= 0};
         for (int w = 0; w < kTileWarps; ++w) {
             s.rest += rest_buf[w];
             s.member += member_buf[w];
             s.sz += sz_buf[w];
-            s.q += dbuf[w];
+            if (a.teacher_lse) s.q = pair_add(s.q, dbuf[w]);
         }
         put_in_block(&stats[rank], tid, s);
     }
@@ -590,7 +584,7 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     for (unsigned b = 1; b < blocks; ++b) m = fmaxf(m, stats[b].m);
     const PowerBase ny(m, cy), nz(m, kLog2E), by = far_alike(ny, nz), bz = far_alike(nz, ny);
     float rest = 0.f, s = 0.f, sz = 0.f, zl = 0.f;
-    double q_sum = 0.0;
+    Pair q_sum = {0.f, 0.f};
     for (unsigned b = 0; b < blocks; ++b) {
         const DistillStats& o = stats[b];
         const PowerBase oy(o.m, cy), oz(o.m, kLog2E);
@@ -598,7 +592,7 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
         rest += o.rest * f;
         s += o.member * f;
         if (TWO) sz += o.sz * far_alike(oz, oy).to(bz);
-        q_sum += o.q;
+        if (a.teacher_lse) q_sum = pair_add(q_sum, o.q);
         if (o.has_label) zl = o.z_label;
     }
     s += rest;
@@ -606,8 +600,8 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     const bool empty = s == 0.f;   // every class masked
     float qr = 0.f;
     if (a.teacher_lse) {
-        Q = (float)q_sum;
-        if (any && rest > 0.f) qr = (float)fmax(1.0 - q_sum, 0.0);
+        Q = q_sum.hi;
+        if (any && rest > 0.f) qr = left_of(q_sum);
     }
     const float log2_s = log2f(s);
     {
@@ -732,20 +726,20 @@ distill_narrow_kernel(const T* Z, T* dZ, Distill a) {
         // the teacher's probabilities
         float Q = 0.f, q_left = 0.f;
         if (a.teacher_lse) {
-            const double norm = (double)a.teacher_lse[row];
-            double sum = 0.0;
+            const float norm = a.teacher_lse[row];
+            Pair sum = {0.f, 0.f};
             for (int k = lane; k < K; k += 32) {
                 const float t = entries[k].logq;
                 if (t != BITLOGIC_NEG_INF) {
-                    const double d = (double)t * a.inv_tau64 - norm, q = exp(d);
-                    entries[k].logq = (float)d;
-                    entries[k].q = (float)q;
-                    sum += q;
+                    const Pair d = teacher_log(t, a, norm), q = exp_pair(d);
+                    entries[k].logq = d.hi;
+                    entries[k].q = q.hi;
+                    sum = pair_add(sum, q);
                 }
             }
             sum = warp_add(sum);
-            Q = (float)sum;
-            q_left = (float)fmax(1.0 - sum, 0.0);
+            Q = sum.hi;
+            q_left = left_of(sum);
         } else {
             tm = warp_largest(tm);
             const float ts = isinf(tm) ? 0.f : tm;
@@ -941,7 +935,10 @@ extern "C" int bitlogic_distill_loss(const void* Z, int32_t dtype, int64_t T, in
         if (T > 1 && V > 1 && ldg < (V - 1) * incg + 1 && incg < (T - 1) * ldg + 1) return BITLOGIC_ERR_SHAPE;
         if (reinterpret_cast<uintptr_t>(dZ) % logit_bytes(dtype)) return BITLOGIC_ERR_ALIGN;
     }
-    Distill a = {T, V, K, ld, teacher_val, teacher_idx, teacher_lse, labels, row_weight, 1.0 / (double)temperature, 1.0f / temperature,
+    const double inv_tau = 1.0 / (double)temperature;
+    Distill a = {T, V, K, ld, teacher_val, teacher_idx, teacher_lse, labels, row_weight,
+                 {(float)inv_tau, (float)(inv_tau - (double)(float)inv_tau)},
+                 1.0f / temperature,
                  kd_weight * temperature * temperature, ce_weight, row_loss, ldg, incg, grad_scale};
     if (T > 0) {
         const int st = with_logit_type(dtype, false, [&](auto* type) {

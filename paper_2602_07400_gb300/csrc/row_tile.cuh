@@ -388,6 +388,66 @@ __device__ __forceinline__ uint4 end_piece(const T* x, int V, int first_class) {
     return u;
 }
 
+// Pairs hi + lo of fp32 numbers (lo below half an ulp of hi), by the error-free
+// sum and product of Knuth and Dekker: 48 bits of mantissa on the fp32 pipe, for
+// the few numbers of a row that need more than fp32.
+struct Pair {
+    float hi, lo;
+};
+__device__ __forceinline__ Pair exact_sum(float a, float b) {
+    const float s = a + b, t = s - a;
+    return {s, (a - (s - t)) + (b - t)};
+}
+__device__ __forceinline__ Pair exact_product(float a, float b) {
+    const float p = a * b;
+    return {p, fmaf(a, b, -p)};
+}
+__device__ __forceinline__ Pair pair_add(Pair x, Pair y) {
+    const Pair s = exact_sum(x.hi, y.hi);
+    const float lo = s.lo + (x.lo + y.lo), hi = s.hi + lo;
+    return {hi, lo - (hi - s.hi)};
+}
+__device__ __forceinline__ Pair pair_multiply(Pair x, Pair y) {
+    const Pair p = exact_product(x.hi, y.hi);
+    const float lo = p.lo + (x.hi * y.lo + x.lo * y.hi), hi = p.hi + lo;
+    return {hi, lo - (hi - p.hi)};
+}
+__device__ __forceinline__ Pair warp_add(Pair v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = pair_add(v, Pair{shuffle_xor(v.hi, o), shuffle_xor(v.lo, o)});
+    return v;
+}
+
+
+// e^x to about 2^-44 of itself, for x of a few ulps above 0 at most: x = n ln 2
+// + r, and the exponential series of r (|r| <= 0.35), whose terms from r^7 / 7!
+// on (below 2e-7) are summed in fp32.
+__device__ __forceinline__ Pair exp_pair(Pair x) {
+    if (!(x.hi > -80.f)) return {x.hi != x.hi ? x.hi : 0.f, 0.f};
+    const float n = rintf(x.hi * kLog2E);
+    // ln 2 in parts of 11, 24 and 24 bits: n times the first is exact
+    constexpr double kLn2Exact = 0.693147180559945309417;
+    constexpr float l1 = 0.693359375f, l2 = (float)(kLn2Exact - 0.693359375),
+                    l3 = (float)(kLn2Exact - 0.693359375 - (double)l2);
+    Pair r = exact_sum(fmaf(-n, l1, x.hi), x.lo);
+    const Pair p = exact_product(-n, l2);
+    r = pair_add(r, Pair{p.hi, fmaf(-n, l3, p.lo)});
+    const float t = r.hi;
+    float s = 1.f / 6227020800.f;                      // 1/13!
+    s = fmaf(s, t, 1.f / 479001600.f);
+    s = fmaf(s, t, 1.f / 39916800.f);
+    s = fmaf(s, t, 1.f / 3628800.f);
+    s = fmaf(s, t, 1.f / 362880.f);
+    s = fmaf(s, t, 1.f / 40320.f);
+    s = fmaf(s, t, 1.f / 5040.f);                      // the series from r^7 on, over r^7
+    Pair e = {s, 0.f};
+    constexpr double k[7] = {1.0, 1.0, 0.5, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720};
+#pragma unroll
+    for (int i = 6; i >= 0; --i) e = pair_add(pair_multiply(e, r), Pair{(float)k[i], (float)(k[i] - (double)(float)k[i])});
+    const float scale = __int_as_float(((int)n + 127) << 23);
+    return {e.hi * scale, e.lo * scale};
+}
+
 // Bytes of the longest slice of a row of V classes over `blocks` blocks, for
 // any alignment of the row.
 inline long long slice_bytes(long long V, int element, int blocks) {

@@ -516,9 +516,11 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
         ma = P::largest(ma, tile16[j]);
         if (j + kSampleThreads < slice.n) mb = P::largest(mb, tile16[j + kSampleThreads]);
     }
-    const float za = P::value(ma), zb = P::value(mb);
-    const uint32_t bound_here = k_asked < V ? block_bound({za, zb}, (k_asked + blocks - 1) / blocks, &s.bound) : 0u;
-    const float wm = warp_largest(fmaxf(za, zb));
+    float part[4];
+    P::parts(ma, part[0], part[1]);
+    P::parts(mb, part[2], part[3]);
+    const uint32_t bound_here = k_asked < V ? block_bound(part, (k_asked + blocks - 1) / blocks, &s.bound) : 0u;
+    const float wm = warp_largest(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])));
     if (lane == 0) s.fbuf[warp] = wm;
     __syncthreads();
     if (tid < (int)blocks) {
@@ -584,8 +586,8 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
 
     // every warp a contiguous part of the slice, so that sums follow the order
     // of classes
-    const int part = (slice.n + kSampleWarps - 1) / kSampleWarps, j0 = min(slice.n, warp * part),
-              j1 = min(slice.n, j0 + part);
+    const int run_of = (slice.n + kSampleWarps - 1) / kSampleWarps, j0 = min(slice.n, warp * run_of),
+              j1 = min(slice.n, j0 + run_of);
     Cut cut = {kNoCut, 0};
     float z_cut = BITLOGIC_NEG_INF;   // kept: above it, and the first ties at it
     if (set.p < 1.0f) {
@@ -1372,7 +1374,7 @@ int launch_sample(const T* x, long long T_, int V, long long ld, const Settings&
         e = launch_rows(kern, (T_ + kNarrowWarps - 1) / kNarrowWarps, 1, kNarrowWarps * 32, 0, stream, x, ld, V, T_, set, out);
     } else {
         const int blocks = 2 * T_ <= sm_count() ? blocks_per_row(T_, V, sizeof(T), kTileFit, kTileMost, kTileLeast) : 0;
-        if (blocks > 0) {
+        if (blocks > 1) {
             e = launch_rows(sample_tile_kernel<T>, T_, blocks, kSampleThreads, (size_t)slice_bytes(V, sizeof(T), blocks),
                             stream, x, ld, V, set, out);
         } else {

@@ -300,8 +300,8 @@ struct TopShared {
 };
 
 // A row in the shared memory of one block or one cluster.  Each thread's two
-// running maxima give a bound that at least K logits of the row reach: the
-// largest key that K / blocks of a block's 512 maxima reach, and the smallest
+// running maxima of two parts give a bound that at least K logits of the row
+// reach: the largest key that K / blocks of a block's 1024 maxima reach, and the smallest
 // of those over the row's blocks.  For logits in no
 // particular order little more than K pass it, so the selection sorts a few
 // hundred entries; rows on which more than 1024 pass (long runs of equal
@@ -332,9 +332,11 @@ top_tile_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
         ma = P::largest(ma, tile16[j]);
         if (j + kTopThreads < slice.n) mb = P::largest(mb, tile16[j + kTopThreads]);
     }
-    const float za = P::value(ma), zb = P::value(mb);
-    const uint32_t bound_here = block_bound({za, zb}, (K + blocks - 1) / blocks, &s.bound);
-    const float wm = warp_largest(fmaxf(za, zb));
+    float part[4];
+    P::parts(ma, part[0], part[1]);
+    P::parts(mb, part[2], part[3]);
+    const uint32_t bound_here = block_bound(part, (K + blocks - 1) / blocks, &s.bound);
+    const float wm = warp_largest(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])));
     if (lane == 0) s.fbuf[warp] = wm;
     __syncthreads();
     if (tid < (int)blocks) {
@@ -532,7 +534,7 @@ int launch_top(const T* x, long long T_, int V, long long ld, const TopOut& o, c
         e = launch_rows(kern, grid, 1, kNarrowWarps * 32, smem, stream, x, ld, V, T_, o);
     } else {
         const int blocks = 2 * T_ <= sm_count() ? blocks_per_row(T_, V, sizeof(T), kTileFit, kTileMost, kTileLeast) : 0;
-        if (blocks > 0)
+        if (blocks > 1)
             e = launch_rows(top_tile_kernel<T>, T_, blocks, kTopThreads, (size_t)slice_bytes(V, sizeof(T), blocks), stream,
                             x, ld, V, o);
         else
