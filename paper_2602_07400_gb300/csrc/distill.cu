@@ -372,20 +372,19 @@ struct DistillStats {
     int has_label;
 };
 
-constexpr int kTileThreads = 256, kTileWarps = kTileThreads / 32;
-constexpr int kClassTable = 512;   // open-addressed, of at most kMaxTop classes
-
 // A row in the shared memory of one block or one cluster: the logits are read
 // once, and the gradient is written from the same copy.  The record's logits
 // are taken out of the slice first (they become -inf), so the passes over the
 // slice see the classes off the record only, and the record's own terms and
 // gradients are formed by the thread that holds the entry.
 // TWO: labels at a temperature other than 1, which need a second softmax.
-template <typename T, bool TWO>
-__global__ void __launch_bounds__(kTileThreads, TWO ? 4 : 5)
+// kTileThreads: 256, or 128 or 64 for shorter rows, so that as many threads as an
+// SM holds work on rows that are too short to keep 256 in step; at least K.
+template <typename T, bool TWO, int kTileThreads>
+__global__ void __launch_bounds__(kTileThreads, kTileThreads == 64 ? (TWO ? 14 : 16) : kTileThreads == 128 ? (TWO ? 8 : 10) : (TWO ? 4 : 5))
 distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     using P = Piece<T>;
-    constexpr int H = P::N / 2;
+    constexpr int H = P::N / 2, kTileWarps = kTileThreads / 32, kClassTable = 2 * kTileThreads;   // open-addressed, of at most K classes
     extern __shared__ __align__(16) unsigned char raw[];
     T* tile = reinterpret_cast<T*>(raw);
     uint4* tile16 = reinterpret_cast<uint4*>(raw);
@@ -395,8 +394,8 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     __shared__ float rest_buf[kTileWarps], member_buf[kTileWarps], sz_buf[kTileWarps];
     __shared__ Pair dbuf[kTileWarps];
     __shared__ int table[kClassTable];
-    __shared__ int classes[kMaxTop];
-    __shared__ float probs[kMaxTop];
+    __shared__ int classes[kTileThreads];
+    __shared__ float probs[kTileThreads];
     __shared__ int any_s, label_on_s, repeated_s;
     grid_dependency_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -482,7 +481,7 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     if (ev >= 0) any_s = 1;
     if (label_ok && ev == label) label_on_s = 1;
     if (place >= 0) {
-        unsigned h = ((unsigned)ev * 2654435761u) >> 23;
+        unsigned h = (((unsigned)ev * 2654435761u) >> 16) % kClassTable;
         for (int i = 0; i < kClassTable; ++i, h = (h + 1) % kClassTable) {
             const int was = atomicCAS(&table[h], -1, ev);
             if (was == ev) repeated_s = 1;
@@ -886,8 +885,14 @@ int launch_distill(const T* z, T* dz, const Distill& a, cudaStream_t stream) {
         e = launch_rows(distill_narrow_kernel<T, TWO>, (a.T + kNarrowWarps - 1) / kNarrowWarps, 1, kNarrowWarps * 32, smem,
                         stream, z, dz, a);
     } else if (blocks > 0) {
-        const size_t smem = (size_t)slice_bytes(a.V, sizeof(T), blocks);
-        e = launch_rows(distill_tile_kernel<T, TWO>, a.T, blocks, kTileThreads, smem, stream, z, dz, a);
+        // (bf16: 9024 rows of 6644 classes 57.2 us in 64 threads, 63.1 in 128,
+        // 96.7 in 256; 8192 rows of 16384 classes 100.4, 97.7 and 114.8 us)
+        const long long bytes = slice_bytes(a.V, sizeof(T), blocks);
+        auto kern = a.K <= 64 && bytes <= 16 * 1024    ? distill_tile_kernel<T, TWO, 64>
+                    : a.K <= 128 && bytes <= 40 * 1024 ? distill_tile_kernel<T, TWO, 128>
+                                                       : distill_tile_kernel<T, TWO, 256>;
+        const int threads = a.K <= 64 && bytes <= 16 * 1024 ? 64 : a.K <= 128 && bytes <= 40 * 1024 ? 128 : 256;
+        e = launch_rows(kern, a.T, blocks, threads, (size_t)bytes, stream, z, dz, a);
     } else {
         // a thread's mask bits, by 32 of its pieces, and a bit per place of the row
         const long long pieces = slice_bytes(a.V, sizeof(T), 1) / 16, words = (pieces + 32 * kRowThreads - 1) / (32 * kRowThreads);

@@ -80,7 +80,7 @@ __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float(
 
 // A bound of the largest values that a block's threads hold G of each: the
 // largest key of 16 leading bits that at least `need` of them reach (0 when
-// fewer rank), by 8 bits at a time.  Called by the whole block of 256 threads.
+// fewer rank), by 8 bits at a time.  Called by the whole block.
 struct BoundScratch {
     unsigned bins[2][256];
     unsigned digit[2], above;
@@ -91,7 +91,7 @@ __device__ __forceinline__ uint32_t block_bound(const float (&v)[G], unsigned ne
 #pragma unroll
     for (int i = 0; i < G; ++i) key[i] = logit_key(v[i]) >> 16;
     const int tid = threadIdx.x, lane = tid & 31;
-    s->bins[0][tid] = s->bins[1][tid] = 0u;
+    for (int i = tid; i < 256; i += blockDim.x) s->bins[0][i] = s->bins[1][i] = 0u;
     if (tid == 0) s->digit[0] = s->digit[1] = s->above = 0u;
     __syncthreads();
 #pragma unroll
