@@ -534,7 +534,7 @@ int launch_top(const T* x, long long T_, int V, long long ld, const TopOut& o, c
         const long long grid = (T_ + kNarrowWarps - 1) / kNarrowWarps;
         const size_t smem = (size_t)kNarrowWarps * o.K * 8;
         auto kern = V <= 32 ? top_narrow_kernel<T, 1> : V <= 128 ? top_narrow_kernel<T, 4>
-                  : V <= 256 ? top_narrow_kernel<T, 8> : top_narrow_kernel<T, 32>;
+                  : V <= 256 ? top_narrow_kernel<T, 8> : V <= 512 ? top_narrow_kernel<T, 16> : top_narrow_kernel<T, 32>;
         e = launch_rows(kern, grid, 1, kNarrowWarps * 32, smem, stream, x, ld, V, T_, o);
     } else {
         const int blocks = 2 * T_ <= sm_count() ? blocks_per_row(T_, V, sizeof(T), kTileFit, kTileMost, kTileLeast) : 0;

@@ -5,13 +5,17 @@ paper's protocol (§4 "Architecture": encoder -> logic layer -> logic layer
 -> head): thermometer encode, two LUT forwards, group-sum head with
 cross-entropy, two LUT backwards.  ``HardInfer`` runs the hard bit-packed
 evaluation (App. C.1): binarize tables, encode + pack, hard layer 1, hard
-layer 2 with the fused popcount head and argmax.  Buffers are allocated once
+layer 2 with the fused popcount head and argmax.  ``DistillStep`` is the
+training step of a student that learns from a teacher's recorded answers
+(``TeacherRecord``), and ``HardInfer.draw`` answers by chance instead of the
+argmax.  Buffers are allocated once
 (torch provides the device memory); every step only enqueues library calls
 on the current stream, so a step can be captured once as a CUDA graph and
 replayed (``capture``), which removes the host work between the launches.
 """
 from __future__ import annotations
 
+import contextlib
 from typing import Optional, Sequence
 
 import numpy as np
@@ -27,7 +31,8 @@ from . import (NODE_FORMS, bitlogic_adamw_update, bitlogic_binarize_tables, bitl
                bitlogic_lut_forward_u8, bitlogic_encode_thermometer_bitrows, bitlogic_lut_forward_bitrows,
                bitlogic_lut_backward_bitrows, bitrow_words, bitlogic_degree_order,
                bitlogic_lut_forward_codes, bitlogic_lut_forward_coded, bitlogic_lut_backward_coded,
-               bitlogic_corner_reduce, bitlogic_codes_decode, code_bytes)
+               bitlogic_corner_reduce, bitlogic_codes_decode, code_bytes,
+               bitlogic_top_logits, bitlogic_distill_loss, bitlogic_sample_logits)
 
 
 def _nomark(name: str) -> None:
@@ -486,6 +491,80 @@ class TrainStep:
         return 7 + (0 if (self.fuse_dy1 or self.through) else 1) + (1 if self.dbits is not None else 0)
 
 
+class TeacherRecord:
+    """The answers of a teacher on a batch of B samples, as a student reads
+    them: per sample the K largest logits with their classes, and the
+    log-sum-exp of all of them at the distillation's temperature
+    (``val``, ``idx``, ``lse``)."""
+
+    def __init__(self, B: int, K: int, temperature: float = 1.0, device="cuda"):
+        dev = torch.device(device)
+        self.temperature = float(temperature)
+        self.val = torch.zeros(B, K, dtype=torch.float32, device=dev)
+        self.idx = torch.full((B, K), -1, dtype=torch.int32, device=dev)
+        self.lse = torch.zeros(B, dtype=torch.float32, device=dev)
+
+    def take(self, logits: torch.Tensor, unit: float = 1.0, stream=None):
+        """Records ``logits`` [B, C] (fp32, bf16, fp16, or the int32 counts of a
+        hard network, whose ``unit`` is the temperature of its group-sum head:
+        its logits are the counts divided by it)."""
+        bitlogic_top_logits(logits, self.val, self.idx, self.lse, temperature=self.temperature * unit, stream=stream)
+        if unit != 1.0:
+            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+                self.val.div_(unit)
+
+    def load(self, val: torch.Tensor, idx: torch.Tensor, lse: torch.Tensor, non_blocking: bool = False):
+        """A record made elsewhere."""
+        self.val.copy_(val, non_blocking=non_blocking)
+        self.idx.copy_(idx, non_blocking=non_blocking)
+        self.lse.copy_(lse, non_blocking=non_blocking)
+
+
+class DistillStep(TrainStep):
+    """A training step that learns from a teacher's record and from labels:
+    TrainStep with the head's loss and class gradients replaced by
+    ``bitlogic_distill_loss`` on the head's logits.
+
+    ``teacher`` is a TeacherRecord of the batch (K of its classes).  The loss is
+    ``kd_weight`` times the divergence from the teacher (times the squared
+    temperature) plus ``ce_weight`` times the cross-entropy against the labels
+    (negative: the sample has none), averaged over the batch or weighted by
+    ``row_weight`` (fp32 [B], 0 leaves a sample out); ``row_loss`` holds it per
+    sample.  With ``tail`` the teacher's probability off the record counts as
+    one further class."""
+
+    def __init__(self, net: Network, B: int, d: int, thresholds: Sequence[int], C: int, tau: float,
+                 teacher: TeacherRecord, kd_weight: float = 0.5, ce_weight: float = 0.5, tail: bool = True,
+                 row_weight: Optional[torch.Tensor] = None, device="cuda", **route):
+        super().__init__(net, B, d, thresholds, C, tau, device=device, **route)
+        self.teacher, self.tail = teacher, bool(tail)
+        self.kd_weight, self.ce_weight = float(kd_weight), float(ce_weight)
+        self.row_weight = row_weight
+        self.row_loss = torch.zeros(B, dtype=torch.float32, device=torch.device(device))
+        # what the head takes for a sample without a label
+        self._head_labels = torch.zeros_like(self.labels)
+
+    def forward(self, stream=None, mark=_nomark):
+        # the head's own loss and gradients are overwritten below; it takes
+        # labels in range, whatever the samples carry
+        labels, self.labels = self.labels, self._head_labels
+        try:
+            super().forward(stream, mark)
+        finally:
+            self.labels = labels
+        t = self.teacher
+        bitlogic_distill_loss(self.logits, t.val, t.idx, self.row_loss, self.loss, self.dyg.t(),
+                              teacher_lse=t.lse if self.tail else None, labels=labels, row_weight=self.row_weight,
+                              temperature=t.temperature, kd_weight=self.kd_weight, ce_weight=self.ce_weight,
+                              grad_scale=1.0 / self.tau, stream=stream)
+        mark("distill")
+
+    # and the distillation and its sum over the batch
+    @property
+    def kernels_per_run(self) -> int:
+        return super().kernels_per_run + 2
+
+
 class RoutedNetwork:
     """A two-layer LUT network with learnable routing (§3 "Connectivity"):
     per node slot a candidate pool (int32 [w*k, Kc]) and routing logits
@@ -651,6 +730,17 @@ class HardInfer:
         bitlogic_hard_forward(self.yp1, self.N, n.conn2, self.table2, yp=self.yp2, C=self.C,
                               counts=self.counts, pred=self.pred, stream=stream)
         mark("hard2")
+
+    def draw(self, u: torch.Tensor, token: torch.Tensor, logprob: Optional[torch.Tensor] = None,
+             temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+             top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, stream=None):
+        """A class per sample drawn from the last pass's counts with the random
+        numbers u fp32 [N], in place of the argmax ``pred``: into token int32
+        [N], and the logarithm of its probability into logprob.  Settings per
+        sample as in bitlogic_sample_logits; a temperature is in counts (the
+        head's tau times the softmax temperature)."""
+        bitlogic_sample_logits(self.counts, u, token, logprob, temperature=temperature, top_k=top_k, top_p=top_p,
+                               min_p=min_p, stream=stream)
 
     def capture(self, binarize: bool = True) -> torch.cuda.CUDAGraph:
         """One hard pass (with the table binarization when ``binarize``) as a
