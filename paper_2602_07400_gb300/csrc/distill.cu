@@ -695,37 +695,48 @@ distill_narrow_kernel(const T* Z, T* dZ, Distill a) {
     float* x = rows + warp * stride;
     grid_dependency_wait();
     const long long row0 = (long long)blockIdx.x * kNarrowWarps, row = row0 + warp;
-    const float wt = row >= a.T ? 0.f : a.weight ? a.weight[row] : 1.0f / (float)a.T;
-    float loss = 0.f;
-    bool counts = wt != 0.f;
-    if (counts) {
+    // all that the row needs of memory is asked for at once
+    const bool in = row < a.T;
+    const float wt = !in ? 0.f : a.weight ? a.weight[row] : 1.0f / (float)a.T;
+    const int label = in && a.labels && a.ce != 0.f ? a.labels[row] : -1;
+    const float norm = in && a.teacher_lse ? a.teacher_lse[row] : 0.f;
+    if (in) {
         const T* z = Z + row * a.ld;
 #pragma unroll 4
         for (int v = lane; v < V; v += 32) x[v] = logit_value(z[v]);
-        const int label = a.labels && a.ce != 0.f ? a.labels[row] : -1;
+        for (int k = lane; k < K; k += 32) {
+            NarrowEntry e = {a.idx[row * K + k], 0.f, a.val[row * K + k], 0.f};
+            if (e.v < 0) e.v = -1, e.logq = BITLOGIC_NEG_INF;
+            entries[k] = e;
+        }
+    }
+    __syncwarp();
+    float loss = 0.f;
+    bool counts = wt != 0.f;
+    if (counts) {
         const bool label_ok = label >= 0 && label < V;
         float tm = BITLOGIC_NEG_INF;
         bool bad = label >= V;
         unsigned any = 0, label_on = 0;
         for (int b = 0; b < K; b += 32) {
             const int k = b + lane;
-            NarrowEntry e = {-1, 0.f, BITLOGIC_NEG_INF, 0.f};
+            int v = -1;
             if (k < K) {
-                e.v = a.idx[row * K + k];
-                if (e.v >= V) bad = true;
-                if (e.v < 0 || e.v >= V) e.v = -1;
-                else e.logq = a.val[row * K + k];
-                entries[k] = e;
-                tm = fmaxf(tm, e.logq * a.inv_tau);
+                v = entries[k].v;
+                if (v >= V) {
+                    bad = true;
+                    entries[k].v = v = -1;
+                    entries[k].logq = BITLOGIC_NEG_INF;
+                }
+                tm = fmaxf(tm, entries[k].logq * a.inv_tau);
             }
-            any |= __ballot_sync(0xffffffffu, e.v >= 0);
-            label_on |= __ballot_sync(0xffffffffu, label_ok && e.v == label);
+            any |= __ballot_sync(0xffffffffu, v >= 0);
+            label_on |= __ballot_sync(0xffffffffu, label_ok && v == label);
         }
         if (bad) flag_index_error();
         // the teacher's probabilities
         float Q = 0.f, q_left = 0.f;
         if (a.teacher_lse) {
-            const float norm = a.teacher_lse[row];
             Pair sum = {0.f, 0.f};
             for (int k = lane; k < K; k += 32) {
                 const float t = entries[k].logq;
@@ -744,12 +755,12 @@ distill_narrow_kernel(const T* Z, T* dZ, Distill a) {
             const float ts = isinf(tm) ? 0.f : tm;
             float sum = 0.f;
             for (int k = lane; k < K; k += 32) sum += exp2_unit((entries[k].logq * a.inv_tau - ts) * kLog2E);
-            const float norm = ts + logf(warp_add(sum));
+            const float log_sum = ts + logf(warp_add(sum));
             for (int k = lane; k < K; k += 32) {
                 const float t = entries[k].logq * a.inv_tau;
                 if (t != BITLOGIC_NEG_INF) {
-                    entries[k].logq = t - norm;
-                    entries[k].q = exp2_unit((t - norm) * kLog2E);
+                    entries[k].logq = t - log_sum;
+                    entries[k].q = exp2_unit((t - log_sum) * kLog2E);
                     Q += entries[k].q;
                 }
             }
