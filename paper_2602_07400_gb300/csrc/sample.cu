@@ -306,7 +306,7 @@ struct SampleShared {
 // mantissa, so that the powers above bin b are those with e > bin_above(b); bin
 // 64 is the first below 1.  A power counts its mantissa's 15 leading bits, so
 // that a bin of 2^17 of them sums in 32 bits and is right to 2^-14 of itself.
-__device__ __forceinline__ int bin_of(float e) { return min((int)((0x3fffffffu - __float_as_uint(e)) >> 17), kBins - 1); }
+__device__ __forceinline__ int bin_of(float e) { return (int)((0x3fffffffu - __float_as_uint(e)) >> 17); }   // 2^-41 <= e <= 1
 __device__ __forceinline__ unsigned bin_units(float e) { return (((__float_as_uint(e) & 0x7fffffu) | 0x800000u) + 256u) >> 9; }
 __device__ __forceinline__ float bin_mass(unsigned units, int b) {
     return (float)units * __uint_as_float((unsigned)(127 - 14 - b / kBinsPerOctave) << 23);
@@ -318,8 +318,10 @@ __device__ __forceinline__ float logit_below(float e, const Power& p) {
     return p.slope > 0.f ? p.m - fabsf(p.m) * 1e-6f - (0.02f - 1.000001f * log2f(e)) / p.slope : BITLOGIC_NEG_INF;
 }
 
-// The bin in which a mass is reached from the largest power down (the last one
-// if none), into *bin.  Called by the whole block.
+// The bins in which a mass is reached from the largest power down, into *bin: 4
+// times the bin (the last one if none), and 1 or 2 where the mass comes so near
+// to its beginning or end that the bin before or after it may be the one (the
+// bins' sums are right to some 2^-13).  Called by the whole block.
 __device__ __forceinline__ void find_bin(const unsigned* bins, float goal, int* bin, float* fbuf) {
     constexpr int kPer = (kBins + kSampleThreads - 1) / kSampleThreads;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -334,7 +336,7 @@ __device__ __forceinline__ void find_bin(const unsigned* bins, float goal, int* 
         if (lane >= o) upto += t;
     }
     if (lane == 31) fbuf[warp] = upto;
-    if (tid == 0) *bin = kBins - 1;
+    if (tid == 0) *bin = 4 * (kBins - 1) + 3;
     __syncthreads();
     float before = upto - sum;
     for (int w = 0; w < warp; ++w) before += fbuf[w];
@@ -343,12 +345,16 @@ __device__ __forceinline__ void find_bin(const unsigned* bins, float goal, int* 
             const int b = tid * kPer + q;
             if (b < kBins) {
                 const float m = bin_mass(bins[b], b);
-                if (before < goal && before + m >= goal) atomicMin(bin, b);
+                const float near = goal * 0.0005f;
+                if (before < goal && before + m >= goal)
+                    atomicMin(bin, 4 * b + (goal - before < near) + 2 * (before + m - goal < near));
                 before += m;
             }
         }
     __syncthreads();
 }
+__device__ __forceinline__ int first_bin(int found) { return max(0, found / 4 - (found & 1)); }
+__device__ __forceinline__ int end_bin(int found) { return min(kBins, found / 4 + 1 + (found >> 1 & 1)); }
 
 // The sum of v over the block's threads before this one, and over all of them.
 __device__ __forceinline__ unsigned long long block_before(unsigned long long v, unsigned long long* buf,
@@ -614,7 +620,7 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
         unsigned long long want = share_of(total, set.p);
         if (want < 1) want = 1;
         // classes with less than a V-th of what top_p leaves off come after it
-        const float left_off = fmaxf((float)(total - want) * (1.0f / 1099511627776.0f) / (float)V, 2.3e-13f);
+        const float left_off = fmaxf((float)(total - want) * (1.0f / 1099511627776.0f) / (float)V, 4.5474735e-13f);   // 2^-41 at least
         const float z_min = logit_below(left_off, power);
         for (int j = tid; j < slice.n; j += kSampleThreads) {
             const uint4 u = tile16[j];
@@ -645,8 +651,8 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
         }
         if (tid == 0) s.n_local = 0;
         row_barrier();
-        // the exact mass above bins bin - 1 to bin + 1, and their entries
-        const float e_above = bin_above(max(0, s.bin - 1)), e_list = bin_above(min(kBins, s.bin + 2)), z_list = logit_below(e_list, power);
+        // the exact mass above the bins found, and their entries
+        const float e_above = bin_above(first_bin(s.bin)), e_list = bin_above(end_bin(s.bin)), z_list = logit_below(e_list, power);
         WeightSum ws;
         for (int j = tid; j < slice.n; j += kSampleThreads) {
             const uint4 u = tile16[j];
@@ -1005,7 +1011,7 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
         unsigned long long want = share_of(total, set.p);
         if (want < 1) want = 1;
         // classes with less than a V-th of what top_p leaves off come after it
-        const float left_off = fmaxf((float)(total - want) * (1.0f / 1099511627776.0f) / (float)V, 2.3e-13f);
+        const float left_off = fmaxf((float)(total - want) * (1.0f / 1099511627776.0f) / (float)V, 4.5474735e-13f);   // 2^-41 at least
         const float z_min = logit_below(left_off, power);
         auto count = [&](const uint4& u) {
             if (P::largest_of(u) >= z_min) {
@@ -1029,24 +1035,25 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
         count(u_end);
         __syncthreads();
         find_bin(s.bins, (float)want * (1.0f / 1099511627776.0f), &s.bin, s.fbuf);
-        // the exact mass above bins bin - 1 to bin + 1, and its kept part by
+        // the exact mass above the bins found, and its kept part by
         // chunk; the pieces that hold entries of those bins wait until the pass
         // is over (where the bins were)
-        const float e_above = bin_above(max(0, s.bin - 1)), e_list = bin_above(min(kBins, s.bin + 2)), z_list = logit_below(e_list, power);
+        const float e_above = bin_above(first_bin(s.bin)), e_list = bin_above(end_bin(s.bin)), z_list = logit_below(e_list, power);
         __syncthreads();
         mass = 0;
         auto above = [&](const uint4& u, int j, WeightSum& kept, WeightSum& cut_off) {
             if (P::largest_of(u) < z_list) return;
             f32x2 z[H];
             load_pairs<T>(u, z);
-            bool any = false;
+            float rest = 0.f;   // the largest that is not above
 #pragma unroll
             for (int i = 0; i < H; ++i) {
                 float a, b;
                 unpack2(pairs(z[i]), a, b);
-                any |= (a > e_list && a <= e_above) || (b > e_list && b <= e_above);
-                a = a > e_above ? a : 0.f;
-                b = b > e_above ? b : 0.f;
+                const float ra = a > e_above ? 0.f : a, rb = b > e_above ? 0.f : b;
+                rest = fmaxf(rest, fmaxf(ra, rb));
+                a -= ra;
+                b -= rb;
                 if (set.floor_e > 0.f) {   // counts for the cut, but is not kept
                     cut_off.add(pack2(a < set.floor_e ? a : 0.f, b < set.floor_e ? b : 0.f));
                     a = a < set.floor_e ? 0.f : a;
@@ -1054,7 +1061,7 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
                 }
                 kept.add(pack2(a, b));
             }
-            if (any) {
+            if (rest > e_list) {
                 const unsigned at = atomicAdd(&s.n_groups, 1u);
                 if (at < kBins) s.bins[at] = (unsigned)j;
             }
@@ -1305,14 +1312,25 @@ sample_narrow_kernel(const T* __restrict__ X, long long ld, int V, long long row
             const unsigned long long need = wt ? (want - mass + wt - 1) / wt : cut.ties;
             if (need < cut.ties) cut.ties = need;
         } else {
-            // the largest key that the mass is reached at, a bit at a time; the
-            // bits of a key that the type does not fill follow the sign
+            // the largest key that the mass is reached at, a bit at a time (the
+            // bits of a key that the type does not fill follow the sign), until
+            // one key is left in [t, t + bit)
             uint32_t t = 0;
 #pragma unroll 1
             for (uint32_t bit = 0x80000000u; bit >= 1u << (32 - kKeyBits); bit >>= 1) {
                 const uint32_t c = t | bit;
                 if (weigh([&](uint32_t k) { return k >= c && k > kt; }) >= want) t = c;
                 if (bit == 1u) break;
+                if (bit & 0x00888800u) {   // a look at what is left, now and then
+                    uint32_t lo = 0xffffffffu, hi = 0u;
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) {
+                        const bool left = key[i] >= t && key[i] > kt && key[i] - t < bit;
+                        lo = left ? min(lo, key[i]) : lo;
+                        hi = left ? max(hi, key[i]) : hi;
+                    }
+                    if (__reduce_min_sync(0xffffffffu, lo) == __reduce_max_sync(0xffffffffu, hi)) break;
+                }
             }
             uint32_t lowest = 0xffffffffu;
 #pragma unroll
