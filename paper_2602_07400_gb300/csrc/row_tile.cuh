@@ -155,6 +155,7 @@ template <> struct Piece<float> {
         return {fmaxf(m.a, fmaxf(__uint_as_float(u.x), __uint_as_float(u.y))),
                 fmaxf(m.b, fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)))};
     }
+    static __device__ __forceinline__ Max either(Max m, Max n) { return {fmaxf(m.a, n.a), fmaxf(m.b, n.b)}; }
     static __device__ __forceinline__ void parts(Max m, float& a, float& b) { a = m.a, b = m.b; }
     static __device__ __forceinline__ float value(Max m) { return fmaxf(m.a, m.b); }
     static __device__ __forceinline__ float largest_of(const uint4& u) {
@@ -176,6 +177,7 @@ template <> struct Piece<int> {
     static __device__ __forceinline__ Max largest(Max m, const uint4& u) {
         return {max(m.a, max((int)u.x, (int)u.y)), max(m.b, max((int)u.z, (int)u.w))};
     }
+    static __device__ __forceinline__ Max either(Max m, Max n) { return {max(m.a, n.a), max(m.b, n.b)}; }
     static __device__ __forceinline__ void parts(Max m, float& a, float& b) { a = logit_value(m.a), b = logit_value(m.b); }
     static __device__ __forceinline__ float value(Max m) { return logit_value(max(m.a, m.b)); }
     static __device__ __forceinline__ float largest_of(const uint4& u) { return value(largest({(int)u.x, (int)u.z}, u)); }
@@ -205,6 +207,7 @@ template <> struct Piece<__nv_bfloat16> {
     static __device__ __forceinline__ Max largest(Max m, const uint4& u) {   // of two numbers: NaN is passed over
         return __hmax2(__hmax2(m, __hmax2(as(u.x), as(u.y))), __hmax2(as(u.z), as(u.w)));
     }
+    static __device__ __forceinline__ Max either(Max m, Max n) { return __hmax2(m, n); }
     static __device__ __forceinline__ void parts(Max m, float& a, float& b) { a = __low2float(m), b = __high2float(m); }
     static __device__ __forceinline__ float value(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
     static __device__ __forceinline__ float largest_of(const uint4& u) { return value(largest(as(u.x), u)); }
@@ -230,6 +233,7 @@ template <> struct Piece<__half> {
     static __device__ __forceinline__ Max largest(Max m, const uint4& u) {
         return __hmax2(__hmax2(m, __hmax2(as(u.x), as(u.y))), __hmax2(as(u.z), as(u.w)));
     }
+    static __device__ __forceinline__ Max either(Max m, Max n) { return __hmax2(m, n); }
     static __device__ __forceinline__ void parts(Max m, float& a, float& b) { a = __low2float(m), b = __high2float(m); }
     static __device__ __forceinline__ float value(Max m) { return fmaxf(__low2float(m), __high2float(m)); }
     static __device__ __forceinline__ float largest_of(const uint4& u) { return value(largest(as(u.x), u)); }

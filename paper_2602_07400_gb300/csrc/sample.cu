@@ -852,7 +852,7 @@ struct SampleRowShared {
     };
     union {
         BoundScratch bound;
-        unsigned short groups[4 * kSampleThreads];
+        unsigned short groups[8 * kSampleThreads];
         unsigned bins[kBins];   // mass by the power's exponent
         struct {
             unsigned long long sums[kSampleWarps];
@@ -917,15 +917,22 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
     const uint4 u_end = j_end >= 0 ? end_piece(x, V, slice.first + j_end * N) : masked_piece<T>();
     const int last_chunk = 1 + kSampleWarps * stream.batches, end_chunk = tid == 0 ? 0 : last_chunk;
 
-    typename P::Max mx[4] = {P::lowest(), P::lowest(), P::lowest(), P::lowest()};
-    stream_row([&](const uint4 (&u)[4], int) {
+    typename P::Max mx[8];   // of even and of odd batches
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mx[i] = P::largest(mx[i], u[i]);
+    for (int i = 0; i < 8; ++i) mx[i] = P::lowest();
+    stream_row([&](const uint4 (&u)[4], int q) {
+        if (q & 1) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mx[4 + i] = P::largest(mx[4 + i], u[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mx[i] = P::largest(mx[i], u[i]);
+        }
     });
-    float group[4];
+    float m = P::largest_of(u_end);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) group[i] = P::value(mx[i]);
-    const float m = block_largest(fmaxf(fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3])), P::largest_of(u_end)), s.fbuf, kSampleWarps);
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, P::value(mx[i]));
+    m = block_largest(m, s.fbuf, kSampleWarps);
     if (m == BITLOGIC_NEG_INF) {   // nothing to draw from
         if (tid == 0) {
             out.token[row] = -1;
@@ -947,7 +954,7 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
         }
         float part[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) P::parts(mx[i], part[2 * i], part[2 * i + 1]);
+        for (int i = 0; i < 4; ++i) P::parts(P::either(mx[i], mx[4 + i]), part[2 * i], part[2 * i + 1]);
         const float z_min = set.k == 1 ? m : bound_logit(block_bound(part, set.k, &s.bound));
         __syncthreads();
         auto take = [&](const uint4& u, int j) {
@@ -961,13 +968,15 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
         };
         if (j_end >= 0) take(u_end, j_end);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (group[i] >= z_min && group[i] > BITLOGIC_NEG_INF) s.groups[atomicAdd(&s.n_groups, 1u)] = (unsigned short)(4 * tid + i);
+        for (int i = 0; i < 8; ++i) {
+            const float group = P::value(mx[i]);
+            if (group >= z_min && group > BITLOGIC_NEG_INF) s.groups[atomicAdd(&s.n_groups, 1u)] = (unsigned short)(8 * tid + i);
+        }
         __syncthreads();
-        const unsigned pieces = s.n_groups * (unsigned)stream.batches;
+        const unsigned half = ((unsigned)stream.batches + 1) / 2, pieces = s.n_groups * half;
         for (unsigned p = tid; p < pieces; p += kSampleThreads) {
-            const unsigned which = p / (unsigned)stream.batches, g = s.groups[which];
-            const int j = slice.whole0() + stream.first_of((int)(g >> 2)) + 4 * kSampleThreads * (int)(p - which * (unsigned)stream.batches) + 32 * (int)(g & 3u);
+            const unsigned which = p / half, g = s.groups[which], q = 2 * (p - which * half) + (g >> 2 & 1u);
+            const int j = slice.whole0() + stream.first_of((int)(g >> 3)) + 4 * kSampleThreads * (int)q + 32 * (int)(g & 3u);
             if (j < stream.j1) take(__ldcg(stream.from + j), j);
         }
         __syncthreads();

@@ -130,19 +130,19 @@ struct TopRowShared {
         TopScratch scratch;
     };
     BoundScratch bound;
-    unsigned short groups[4 * kTopThreads];
+    unsigned short groups[8 * kTopThreads];
     float m[kTopWarps], s[kTopWarps];
     unsigned n, n_groups, inf;
 };
 
 // Many rows, of any length: a block per row, which streams it once, keeping
-// four running maxima of two parts per thread.  These 2048 maxima of the row's
-// groups of pieces give a bound that K logits reach, and the groups whose maximum
-// reaches it are read again (an eighth of a row of 2^17 bf16 at K = 128), from
+// eight running maxima per thread.  Joined by twos, and in two parts each, the
+// 2048 maxima of the row's groups of pieces give a bound that K logits reach, and the groups whose maximum
+// reaches it are read again (a sixteenth of a row of 2^17 bf16 at K = 128), from
 // L2, for the entries: little more than K for logits in no particular order.  A
 // row on which more than 2048 pass is selected from memory.  Taking entries
 // while streaming, under a bound from the row's beginning that is raised as it
-// goes, met four times as many and took 554 us where this takes 248 us
+// goes, met four times as many and took 554 us where this takes 221 us
 // (4096 x 131072 bf16).
 template <typename T, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
@@ -167,7 +167,9 @@ top_row_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
     const float c = kLog2E * o.inv_tau;
     PowerBase base(BITLOGIC_NEG_INF, c);
     f32x2 y0 = 0, y1 = 0;
-    typename P::Max mx[4] = {P::lowest(), P::lowest(), P::lowest(), P::lowest()};
+    typename P::Max mx[8];   // of even and of odd batches
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mx[i] = P::lowest();
     auto sums = [&](const uint4& u, const auto& power) {
         f32x2 z[H];
         load_pairs<T>(u, z);
@@ -207,18 +209,19 @@ top_row_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
             for (int i = 0; i < 4; ++i) sums(u[i], power);
         }
     };
-    auto use = [&](const uint4 (&u)[4]) {
+    auto use = [&](const uint4 (&u)[4], int odd) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mx[i] = P::largest(mx[i], u[i]);
-        if (o.lse) add(u, fmaxf(fmaxf(P::value(mx[0]), P::value(mx[1])), fmaxf(P::value(mx[2]), P::value(mx[3]))));
+        for (int i = 0; i < 4; ++i) mx[4 * odd + i] = P::largest(mx[4 * odd + i], u[i]);
+        if (o.lse)
+            add(u, fmaxf(fmaxf(P::value(mx[4 * odd]), P::value(mx[4 * odd + 1])),
+                         fmaxf(P::value(mx[4 * odd + 2]), P::value(mx[4 * odd + 3]))));
     };
     for (int q = 0; q < stream.batches; q += 2) {
-        use(ua);
+        use(ua, 0);
         if (q + 2 < stream.batches) stream.load(q + 2, ua);
-        if (q + 1 < stream.batches) use(ub);
+        if (q + 1 < stream.batches) use(ub, 1);
         if (q + 3 < stream.batches) stream.load(q + 3, ub);
     }
-    const float group[4] = {P::value(mx[0]), P::value(mx[1]), P::value(mx[2]), P::value(mx[3])};
     // the pieces at the row's ends, of threads 0 and 32
     const int j_end = tid == 0 && slice.whole0() > 0 ? 0 : tid == 32 && slice.whole1(V) < slice.n ? slice.whole1(V) : -1;
     uint4 u_end = masked_piece<T>();
@@ -230,7 +233,7 @@ top_row_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
 
     float part[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) P::parts(mx[i], part[2 * i], part[2 * i + 1]);
+    for (int i = 0; i < 4; ++i) P::parts(P::either(mx[i], mx[4 + i]), part[2 * i], part[2 * i + 1]);
     const float z_min = bound_logit(block_bound(part, K, &s.bound));
     auto take = [&](const uint4& u, int j) {
         if (P::largest_of(u) >= z_min) {
@@ -246,13 +249,15 @@ top_row_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
     };
     if (j_end >= 0) take(u_end, j_end);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (group[i] >= z_min && group[i] > BITLOGIC_NEG_INF) s.groups[atomicAdd(&s.n_groups, 1u)] = (unsigned short)(4 * tid + i);
+    for (int i = 0; i < 8; ++i) {
+        const float group = P::value(mx[i]);
+        if (group >= z_min && group > BITLOGIC_NEG_INF) s.groups[atomicAdd(&s.n_groups, 1u)] = (unsigned short)(8 * tid + i);
+    }
     __syncthreads();
-    const unsigned pieces = s.n_groups * (unsigned)stream.batches;
+    const unsigned half = ((unsigned)stream.batches + 1) / 2, pieces = s.n_groups * half;
     for (unsigned p = tid; p < pieces; p += kThreads) {
-        const unsigned which = p / (unsigned)stream.batches, g = s.groups[which];
-        const int j = slice.whole0() + stream.first_of((int)(g >> 2)) + 4 * kThreads * (int)(p - which * (unsigned)stream.batches) + 32 * (int)(g & 3u);
+        const unsigned which = p / half, g = s.groups[which], q = 2 * (p - which * half) + (g >> 2 & 1u);
+        const int j = slice.whole0() + stream.first_of((int)(g >> 3)) + 4 * kThreads * (int)q + 32 * (int)(g & 3u);
         if (j < stream.j1) take(__ldcg(stream.from + j), j);
     }
     if (o.lse) {
@@ -523,7 +528,7 @@ top_narrow_kernel(const T* __restrict__ X, long long ld, int V, long long rows, 
 // Few rows go by clusters, so that several SMs share one (16 rows of 2^17 bf16
 // 9.7 against 17.2 us in a block each, 64 rows 13.5 against 17.6); from half a
 // row per SM on a block per row is faster (100 rows 17.6 against 20.3 us, 4096
-// rows 248 against 490).  Slices of at most kTileFit bytes leave room for three
+// rows 221 against 490).  Slices of at most kTileFit bytes leave room for three
 // blocks on an SM.
 constexpr int kTileFit = 56 * 1024, kTileMost = 200 * 1024, kTileLeast = 8 * 1024;
 
