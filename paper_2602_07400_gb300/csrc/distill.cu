@@ -51,7 +51,7 @@ constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
 
 // Rows too long for the shared memory of a cluster: a block per row, which
 // streams it from memory once for the statistics and a second time, most of it
-// from L2, for the gradient (8192 x 131072 bf16: 907 us, the tile kernel 893).
+// from L2, for the gradient (8192 x 131072 bf16: 907 us, the tile kernel 881).
 // The classes on the record are
 // marked in a bit map by place, and the pieces that hold any in a mask per
 // thread, whose marked ones are taken out of their sum.
