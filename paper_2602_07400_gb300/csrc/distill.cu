@@ -52,9 +52,8 @@ constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
 // Rows too long for the shared memory of a cluster: a block per row, which
 // streams it from memory once for the statistics and a second time, most of it
 // from L2, for the gradient (8192 x 131072 bf16: 907 us, the tile kernel 881).
-// The classes on the record are
-// marked in a bit map by place, and the pieces that hold any in a mask per
-// thread, whose marked ones are taken out of their sum.
+// The classes on the record are marked in a bit map by place, and the pieces that
+// hold any in a mask per thread; the marked ones are taken out of their sums.
 template <typename T, bool TWO>
 __global__ void __launch_bounds__(kRowThreads, 3)
 distill_row_kernel(const T* Z, T* dZ, Distill a) {
