@@ -434,6 +434,7 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
         zero_row();
         return;
     }
+    report_running(blocks);
     slice.copy(z, V, tile, tid, kTileThreads);
 
     // the record: thread k holds entry k; it is this block's when its class
@@ -560,6 +561,7 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
         }
     }
     __syncthreads();
+    wait_all_running(blocks);
     if (tid < (int)blocks) {
         DistillStats s = {{0.f, 0.f}, m, 0.f, 0.f, 0.f, z_label, label_place >= 0};
         for (int w = 0; w < kTileWarps; ++w) {

@@ -29,6 +29,16 @@ __device__ __forceinline__ unsigned cluster_size() {
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
+// Another block's shared memory may be touched only once that block runs: each
+// block of a cluster reports at its kernel's start, behind which it asks for its
+// slice, and waits for the others just before its first store to one of them.
+__device__ __forceinline__ void report_running(unsigned blocks) {
+    if (blocks > 1) cluster_arrive();
+}
+__device__ __forceinline__ void wait_all_running(unsigned blocks) {
+    if (blocks > 1) cluster_wait();
+}
+
 // The address of `p` (this block's shared memory) in block `rank`, and a
 // store of 4 bytes there.
 __device__ __forceinline__ void store_in_block(const void* p, unsigned rank, uint32_t v) {

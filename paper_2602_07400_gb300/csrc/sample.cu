@@ -500,6 +500,7 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
     const long long row = blockIdx.x / blocks;
     const T* x = X + row * ld;
     const RowSlice<T> slice(x, V, rank, blocks);
+    report_running(blocks);
     slice.copy(x, V, tile, tid, kSampleThreads);
     RowSettings set(settings, row, V);
     auto row_barrier = [&]() {
@@ -529,6 +530,7 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
     const float wm = warp_largest(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])));
     if (lane == 0) s.fbuf[warp] = wm;
     __syncthreads();
+    wait_all_running(blocks);
     if (tid < (int)blocks) {
         SampleShared::Stats st = {s.fbuf[0], bound_here};
         for (int w = 1; w < kSampleWarps; ++w) st.m = fmaxf(st.m, s.fbuf[w]);

@@ -330,6 +330,7 @@ top_tile_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
     const long long row = blockIdx.x / blocks;
     const T* x = X + row * ld;
     const RowSlice<T> slice(x, V, rank, blocks);
+    report_running(blocks);
     slice.copy(x, V, tile, tid, kTopThreads);
     if (tid == 0) s.n_list = s.n_local = s.n_pieces = 0;
     cp_async_wait<0>();
@@ -348,6 +349,7 @@ top_tile_kernel(const T* __restrict__ X, long long ld, int V, TopOut o) {
     const float wm = warp_largest(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])));
     if (lane == 0) s.fbuf[warp] = wm;
     __syncthreads();
+    wait_all_running(blocks);
     if (tid < (int)blocks) {
         TopShared::Stats st = {s.fbuf[0], bound_here};
         for (int w = 1; w < kTopWarps; ++w) st.m = fmaxf(st.m, s.fbuf[w]);
