@@ -581,6 +581,7 @@ int bitlogic_top_logits(const void* X, int32_t dtype, int64_t T, int32_t V, int6
  *                     the teacher's logits at this temperature), and
  *                     q_r = max(0, 1 - sum_k q_k) for the classes off the
  *                     record taken together, whose share of p is r
+ *                     (0 where all of those are masked)
  *   KL          = sum_k q_k (ln q_k - ln p[v_k]) + q_r (ln q_r - ln r)
  *   row_loss[t] = kd_weight temperature^2 KL
  *                 + ce_weight (ln sum_v exp(z_v) - z[labels[t]])

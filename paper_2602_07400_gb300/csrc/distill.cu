@@ -15,7 +15,14 @@
 //            = (sum_k q_k + q_r) p_v - q_r p_v / r  off it
 // r is summed over the classes off the record, not formed as 1 - sum_k p_k,
 // which would leave no digits of a small remainder; for the same reason q_r is
-// formed from pairs of fp32 numbers.
+// formed from pairs of fp32 numbers.  The sum runs about the largest logit off the
+// record: about the row's, it underflows where all of them lie 87 tau below, and
+// q_r / r overflows before.  With S that sum and F = 2^(base off the record - base
+// of the row), r = S F / s and p_v = power F / s, power about the base off the
+// record, so the gradient there is power ((sum_k q_k + q_r) F / s - q_r / S).
+// Logarithms are taken as (z - m) / tau less that of the sum about the row's largest
+// m (and r's with the largest off the record for z): c z overflows before they do.
+// Where every class off the record is masked, q_r = 0.
 //
 // Bound by reading the logits and writing the gradient once.
 #include "row_tile.cuh"
@@ -47,6 +54,12 @@ __device__ __forceinline__ Pair teacher_log(float val, const Distill& a, float l
 // max(0, 1 - Q)
 __device__ __forceinline__ float left_of(Pair Q) { return fmaxf(pair_add(Pair{1.f, 0.f}, Pair{-Q.hi, -Q.lo}).hi, 0.f); }
 
+// ln of a sum of powers about a base, less the base's own logit over tau.
+__device__ __forceinline__ float log_about(const PowerBase& p, float sum) { return kLn2 * (log2f(sum) - p.exponent(p.m)); }
+
+// The factor from a base off the record to the row's, 0 where no class is off it.
+__device__ __forceinline__ float factor_of(const PowerBase& off, const PowerBase& row) { return off.none ? 0.f : off.to(row); }
+
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
 
 // Rows too long for the shared memory of a cluster: a block per row, which
@@ -60,7 +73,7 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
     using P = Piece<T>;
     constexpr int N = P::N, H = N / 2;
     extern __shared__ __align__(16) unsigned char raw[];
-    __shared__ float tbuf[kRowWarps], nbuf[kRowWarps], qbuf[kRowWarps], mbuf[kRowWarps], kbuf[kRowWarps];
+    __shared__ float tbuf[kRowWarps], nbuf[kRowWarps], qbuf[kRowWarps], mbuf[kRowWarps], obuf[kRowWarps], kbuf[kRowWarps];
     __shared__ float rest_buf[kRowWarps], member_buf[kRowWarps], sz_buf[kRowWarps];
     __shared__ Pair dbuf[kRowWarps];
     __shared__ int classes[kMaxTop];
@@ -263,17 +276,24 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
                 }
         }
     }
-    // the row's base and sums
-    float m = warp_largest(fmaxf(P::value(mx), ev >= 0 ? zk : BITLOGIC_NEG_INF));
-    if (lane == 0) mbuf[warp] = m;
+    // the bases of the row and of its classes off the record, and the sums
+    float m_off = warp_largest(P::value(mx)), m = warp_largest(ev >= 0 ? zk : BITLOGIC_NEG_INF);
+    if (lane == 0) {
+        obuf[warp] = m_off;
+        mbuf[warp] = m;
+    }
     __syncthreads();
-    for (int w = 0; w < kRowWarps; ++w) m = fmaxf(m, mbuf[w]);
-    const PowerBase my(m, cy), mz(m, kLog2E), ry = far_alike(my, mz), rz = far_alike(mz, my);
+    for (int w = 0; w < kRowWarps; ++w) {
+        m_off = fmaxf(m_off, obuf[w]);
+        m = fmaxf(m, mbuf[w]);
+    }
+    m = fmaxf(m, m_off);
+    const PowerBase ry(m, cy), rz(m, kLog2E), ny(m_off, cy), nz(m_off, kLog2E), oy = far_alike(ny, nz), oz = far_alike(nz, ny);
     {
         float ra, rb, sa, sb;
         unpack2(add2(y0, y1), ra, rb);
         unpack2(add2(s0, s1), sa, sb);
-        const float rest = warp_add((ra + rb) * by.to(ry));
+        const float rest = warp_add((ra + rb) * by.to(oy));
         const float member = warp_add(first ? ry.power(zk) : 0.f);
         const float sz = TWO ? warp_add((sa + sb) * bz.to(rz) + (first ? rz.power(zk) : 0.f)) : 0.f;
         if (lane == 0) {
@@ -292,7 +312,7 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
         if (a.teacher_lse) q_sum = pair_add(q_sum, dbuf[w]);
         else Q += qbuf[w];
     }
-    s += rest;
+    s += rest * oy.to(ry);
     if (!TWO) sz = s;   // tau = 1 where a label is
     if (a.teacher_lse) {
         Q = q_sum.hi;
@@ -304,15 +324,15 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
         zero_row();
         return;
     }
-    const float qr = a.teacher_lse && any && rest > 0.f ? q_left : 0.f, log2_s = log2f(s);
-    const float kl_part = warp_add(q > 0.f ? q * (logq - kLn2 * (ry.exponent(zk) - log2_s)) : 0.f);
+    const float qr = a.teacher_lse && any && !oy.none ? q_left : 0.f, log_s = log_about(ry, s);
+    const float kl_part = warp_add(q > 0.f ? q * (logq - ((zk - m) * a.inv_tau - log_s)) : 0.f);
     if (lane == 0) kbuf[warp] = kl_part;
     const float ay = wt * a.grad_scale * a.kd * a.inv_tau, az = label_ok ? wt * a.grad_scale * a.ce : 0.f;
-    const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) / s - (qr > 0.f ? qr / rest : 0.f));
-    const float iz = label_ok ? az / sz : 0.f, fy = TWO ? off : off + iz;
+    const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) * factor_of(oy, ry) / s - (qr > 0.f ? qr / rest : 0.f));
+    const float iz = label_ok ? az / sz : 0.f, iz_off = iz * factor_of(oz, rz), fy = TWO ? off : off + iz_off;
     if (g) {
         auto gradient = [&](const auto& py, const auto& pz) {
-            const f32x2 fy2 = pack2(fy, fy), fz2 = pack2(iz, iz);
+            const f32x2 fy2 = pack2(fy, fy), fz2 = pack2(iz_off, iz_off);
             auto one = [&](const uint4& u, int j) {
                 f32x2 x[H];
                 load_pairs<T>(u, x);
@@ -338,26 +358,27 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
             }
             if (j_end >= 0) one(end_piece(z, V, slice.first + j_end * N), j_end);
         };
-        if (ry.far) gradient(FarPairs(ry), FarPairs(rz));
-        else gradient(NearPairs(ry), NearPairs(rz));
+        if (oy.far) gradient(FarPairs(oy), FarPairs(oz));
+        else gradient(NearPairs(oy), NearPairs(oz));
     }
     __syncthreads();
     if (g) {
-        // the record's classes and the label, over what the pass wrote there
+        // the record's classes (whose powers about the base off the record may
+        // have overflowed) and the label, over what the pass wrote there
         if (first) {
             float x = ry.power(zk) * on - ay * q_class;
             if (label_ok) x += rz.power(zk) * iz - (ev == label ? az : 0.f);
             g[(long long)ev * a.incg] = logit_of<T>(x);
         }
         if (tid == 0 && label_ok && !label_on)
-            g[(long long)label * a.incg] = logit_of<T>(ry.power(z_label) * off + rz.power(z_label) * iz - az);
+            g[(long long)label * a.incg] = logit_of<T>(oy.power(z_label) * off + oz.power(z_label) * iz_off - az);
     }
     if (tid == 0) {
         float kl = 0.f;
         for (int w = 0; w < kRowWarps; ++w) kl += kbuf[w];
-        if (qr > 0.f) kl += qr * (logf(qr) - logf(rest / s));
+        if (qr > 0.f) kl += qr * (logf(qr) - ((m_off - m) * a.inv_tau + log_about(oy, rest) - log_s));
         float loss = a.kd != 0.f ? a.kd * kl : 0.f;   // a loss of +inf without weight is none
-        if (label_ok) loss += a.ce * kLn2 * (log2f(sz) - rz.exponent(z_label));
+        if (label_ok) loss += a.ce * (log_about(rz, sz) - (z_label - m));
         a.row_loss[row] = s != s ? s : loss;
     }
 }
@@ -365,8 +386,9 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
 // What the blocks of a row tell each other.
 struct DistillStats {
     Pair q;                 // sum of q of the entries in the slice (with teacher_lse)
-    float m;                // largest logit
-    float rest, member, sz; // powers at tau off and on the record, powers at 1
+    float m, m_off;         // largest logit, and the largest off the record
+    float rest;             // powers at tau off the record, about m_off
+    float member, sz;       // powers at tau on it, and at 1 of all, about m
     float z_label;
     int has_label;
 };
@@ -389,7 +411,7 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     uint4* tile16 = reinterpret_cast<uint4*>(raw);
     __shared__ DistillStats stats[kMaxCluster];
     __shared__ float kl_part[kMaxCluster * kTileWarps];
-    __shared__ float mbuf[kTileWarps], tbuf[kTileWarps], nbuf[kTileWarps], qbuf[kTileWarps];
+    __shared__ float mbuf[kTileWarps], obuf[kTileWarps], tbuf[kTileWarps], nbuf[kTileWarps], qbuf[kTileWarps];
     __shared__ float rest_buf[kTileWarps], member_buf[kTileWarps], sz_buf[kTileWarps];
     __shared__ Pair dbuf[kTileWarps];
     __shared__ int table[kClassTable];
@@ -491,14 +513,11 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
 
     cp_async_wait<0>();
     __syncthreads();
-    // the largest of the slice, and the logits that are taken out of it
-    const float zk = place >= 0 ? logit_value(tile[place]) : 0.f;
+    // the record's logits out of the slice
+    const float zk = place >= 0 ? logit_value(tile[place]) : BITLOGIC_NEG_INF;
     const float z_label = label_place >= 0 ? logit_value(tile[label_place]) : 0.f;
-    typename P::Max mx = P::lowest();
-#pragma unroll 4
-    for (int j = tid; j < slice.n; j += kTileThreads) mx = P::largest(mx, tile16[j]);
-    float m = warp_largest(P::value(mx));
-    if (lane == 0) mbuf[warp] = m;
+    if (repeated_s || label_on_s) __syncthreads();   // a place that several threads read
+    if (place >= 0) tile[place] = masked_logit<T>();
     const bool any = any_s != 0, label_on = label_on_s != 0;
     if (!a.teacher_lse)
         for (int w = 0; w < kTileWarps; ++w) Q += qbuf[w];
@@ -520,14 +539,26 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
         }
     }
     __syncthreads();
-    if (place >= 0) tile[place] = masked_logit<T>();
-    for (int w = 0; w < kTileWarps; ++w) m = fmaxf(m, mbuf[w]);
+    // the largest of what is left, and of the slice
+    typename P::Max mx = P::lowest();
+#pragma unroll 4
+    for (int j = tid; j < slice.n; j += kTileThreads) mx = P::largest(mx, tile16[j]);
+    float m_off = warp_largest(P::value(mx)), m = warp_largest(zk);
+    if (lane == 0) {
+        obuf[warp] = m_off;
+        mbuf[warp] = m;
+    }
     __syncthreads();
+    for (int w = 0; w < kTileWarps; ++w) {
+        m_off = fmaxf(m_off, obuf[w]);
+        m = fmaxf(m, mbuf[w]);
+    }
+    m = fmaxf(m, m_off);
 
-    // powers of the slice about its own largest
+    // powers of the slice
     const float cy = kLog2E * a.inv_tau;
     {
-        const PowerBase by(m, cy), bz(m, kLog2E), ey = far_alike(by, bz), ez = far_alike(bz, by);
+        const PowerBase by(m_off, cy), bz(m_off, kLog2E), ey = far_alike(by, bz), ez = far_alike(bz, by), my(m, cy), mz(m, kLog2E);
         f32x2 r0 = 0, r1 = 0, s0 = 0, s1 = 0;   // two zeros each
         auto sums = [&](const auto& py, const auto& pz) {
 #pragma unroll 2
@@ -550,8 +581,8 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
         float ra, rb, sa, sb;
         unpack2(add2(r0, r1), ra, rb);
         unpack2(add2(s0, s1), sa, sb);
-        const float rest = warp_add(ra + rb), member = warp_add(first ? ey.power(zk) : 0.f);
-        const float sz = TWO ? warp_add(sa + sb + (first ? ez.power(zk) : 0.f)) : 0.f;
+        const float rest = warp_add(ra + rb), member = warp_add(first ? my.power(zk) : 0.f);
+        const float sz = TWO ? warp_add((sa + sb) * ez.to(mz) + (first ? mz.power(zk) : 0.f)) : 0.f;
         if (a.teacher_lse) q2 = warp_add(q2);
         if (lane == 0) {
             rest_buf[warp] = rest;
@@ -563,7 +594,7 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     __syncthreads();
     wait_all_running(blocks);
     if (tid < (int)blocks) {
-        DistillStats s = {{0.f, 0.f}, m, 0.f, 0.f, 0.f, z_label, label_place >= 0};
+        DistillStats s = {{0.f, 0.f}, m, m_off, 0.f, 0.f, 0.f, z_label, label_place >= 0};
         for (int w = 0; w < kTileWarps; ++w) {
             s.rest += rest_buf[w];
             s.member += member_buf[w];
@@ -581,31 +612,33 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
 
     // statistics of the row
     m = stats[0].m;
-    for (unsigned b = 1; b < blocks; ++b) m = fmaxf(m, stats[b].m);
-    const PowerBase ny(m, cy), nz(m, kLog2E), by = far_alike(ny, nz), bz = far_alike(nz, ny);
+    m_off = stats[0].m_off;
+    for (unsigned b = 1; b < blocks; ++b) {
+        m = fmaxf(m, stats[b].m);
+        m_off = fmaxf(m_off, stats[b].m_off);
+    }
+    const PowerBase by(m, cy), bz(m, kLog2E), ny(m_off, cy), nz(m_off, kLog2E), oy = far_alike(ny, nz), oz = far_alike(nz, ny);
     float rest = 0.f, s = 0.f, sz = 0.f, zl = 0.f;
     Pair q_sum = {0.f, 0.f};
     for (unsigned b = 0; b < blocks; ++b) {
         const DistillStats& o = stats[b];
-        const PowerBase oy(o.m, cy), oz(o.m, kLog2E);
-        const float f = far_alike(oy, oz).to(by);
-        rest += o.rest * f;
-        s += o.member * f;
-        if (TWO) sz += o.sz * far_alike(oz, oy).to(bz);
+        rest += o.rest * far_alike(PowerBase(o.m_off, cy), PowerBase(o.m_off, kLog2E)).to(oy);
+        s += o.member * PowerBase(o.m, cy).to(by);
+        if (TWO) sz += o.sz * PowerBase(o.m, kLog2E).to(bz);
         if (a.teacher_lse) q_sum = pair_add(q_sum, o.q);
         if (o.has_label) zl = o.z_label;
     }
-    s += rest;
+    s += rest * oy.to(by);
     if (!TWO) sz = s;   // tau = 1 where a label is
     const bool empty = s == 0.f;   // every class masked
     float qr = 0.f;
     if (a.teacher_lse) {
         Q = q_sum.hi;
-        if (any && rest > 0.f) qr = left_of(q_sum);
+        if (any && !oy.none) qr = left_of(q_sum);
     }
-    const float log2_s = log2f(s);
+    const float log_s = log_about(by, s);
     {
-        const float term = place >= 0 && q > 0.f ? q * (logq - kLn2 * (by.exponent(zk) - log2_s)) : 0.f;
+        const float term = place >= 0 && q > 0.f ? q * (logq - ((zk - m) * a.inv_tau - log_s)) : 0.f;
         const float part = warp_add(term);
         if (lane == 0) store_in_block(&kl_part[rank * kTileWarps + warp], 0, __float_as_uint(part));
     }
@@ -617,10 +650,10 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
         zero_row();
     } else if (g) {
         const float ay = wt * a.grad_scale * a.kd * a.inv_tau, az = label_ok ? wt * a.grad_scale * a.ce : 0.f;
-        const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) / s - (qr > 0.f ? qr / rest : 0.f));
-        const float iz = label_ok ? az / sz : 0.f, fy = TWO ? off : off + iz;
+        const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) * factor_of(oy, by) / s - (qr > 0.f ? qr / rest : 0.f));
+        const float iz = label_ok ? az / sz : 0.f, iz_off = iz * factor_of(oz, bz), fy = TWO ? off : off + iz_off;
         auto gradient = [&](const auto& py, const auto& pz) {
-            const f32x2 fy2 = pack2(fy, fy), fz2 = pack2(iz, iz);
+            const f32x2 fy2 = pack2(fy, fy), fz2 = pack2(iz_off, iz_off);
             uint4* to16 = wide ? reinterpret_cast<uint4*>(g + slice.first) : tile16;   // written at whole pieces
 #pragma unroll 2
             for (int j = tid; j < slice.n; j += kTileThreads) {
@@ -638,8 +671,8 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
                 else tile16[j] = u;
             }
         };
-        if (by.far) gradient(FarPairs(by), FarPairs(bz));
-        else gradient(NearPairs(by), NearPairs(bz));
+        if (oy.far) gradient(FarPairs(oy), FarPairs(oz));
+        else gradient(NearPairs(oy), NearPairs(oz));
         __syncthreads();
         // the record's classes and the label, over what the pass wrote there
         auto put = [&](int p, float x) {
@@ -652,7 +685,7 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
             if (label_ok) x += bz.power(zk) * iz - (ev == label ? az : 0.f);
             put(place, x);
         }
-        if (tid == 0 && label_place >= 0 && !label_on) put(label_place, by.power(z_label) * off + bz.power(z_label) * iz - az);
+        if (tid == 0 && label_place >= 0 && !label_on) put(label_place, oy.power(z_label) * off + oz.power(z_label) * iz_off - az);
         __syncthreads();
         if (!wide) {   // gradient places apart from the logits' or at another alignment
             for (int p = tid; p < slice.n * P::N; p += kTileThreads) {
@@ -668,9 +701,9 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     if (rank == 0 && tid == 0 && !empty) {
         float kl = 0.f;
         for (unsigned b = 0; b < blocks * kTileWarps; ++b) kl += kl_part[b];
-        if (qr > 0.f) kl += qr * (logf(qr) - logf(rest / s));
+        if (qr > 0.f) kl += qr * (logf(qr) - ((m_off - m) * a.inv_tau + log_about(oy, rest) - log_s));
         float loss = a.kd != 0.f ? a.kd * kl : 0.f;
-        if (label_ok) loss += a.ce * kLn2 * (log2f(sz) - bz.exponent(zl));
+        if (label_ok) loss += a.ce * (log_about(bz, sz) - (zl - m));
         a.row_loss[row] = s != s ? s : loss;
     }
 }
@@ -797,20 +830,26 @@ distill_narrow_kernel(const T* Z, T* dZ, Distill a) {
                 }
             return first;
         };
-        float m = BITLOGIC_NEG_INF;
-        for (int v = lane; v < V; v += 32) m = fmaxf(m, x[v]);
+        float mo = BITLOGIC_NEG_INF;   // largest off the record
+        for (int v = lane; v < V; v += 32) mo = fmaxf(mo, x[v]);
+        mo = warp_largest(mo);
+        float m = mo;
         for (int k = lane; k < K; k += 32)
             if (entries[k].v >= 0) m = fmaxf(m, entries[k].z);
         m = warp_largest(m);
         if (m == BITLOGIC_NEG_INF) m = 0.f;
         const float cy = kLog2E * a.inv_tau;
+        const bool off_record = mo > BITLOGIC_NEG_INF;
+        if (!off_record) mo = m;   // of a sum of 0, or of NaN
+        const float to_row = exp2_unit((mo - m) * cy), to_row_z = exp2_unit((mo - m) * kLog2E);
         float rest = 0.f, member = 0.f, sz = 0.f;
 #pragma unroll 4
         for (int v = lane; v < V; v += 32) {
-            const float d = x[v] - m;
+            const float d = x[v] - mo;
             rest += exp2_unit(d * cy);
             if (TWO) sz += exp2_unit(d * kLog2E);
         }
+        if (TWO) sz *= to_row_z;
         for (int k = lane; k < K; k += 32) {
             float q_class;
             if (first_of(k, q_class)) {
@@ -820,29 +859,29 @@ distill_narrow_kernel(const T* Z, T* dZ, Distill a) {
             }
         }
         rest = warp_add(rest);
-        const float s = rest + warp_add(member);
+        const float s = rest * to_row + warp_add(member);
         sz = TWO ? warp_add(sz) : s;
         if (s == 0.f) {
             counts = false;   // every class masked
         } else {
-            const float qr = a.teacher_lse && any && rest > 0.f ? q_left : 0.f;
+            const float qr = a.teacher_lse && any && off_record ? q_left : 0.f;
             const float log_s = logf(s);
             float kl = 0.f;
             for (int k = lane; k < K; k += 32)
                 if (entries[k].q > 0.f) kl += entries[k].q * (entries[k].logq - ((entries[k].z - m) * a.inv_tau - log_s));
             kl = warp_add(kl);
-            if (qr > 0.f) kl += qr * (logf(qr) - logf(rest / s));
+            if (qr > 0.f) kl += qr * (logf(qr) - ((mo - m) * a.inv_tau + logf(rest) - log_s));
             loss = a.kd != 0.f ? a.kd * kl : 0.f;
             if (label_ok) loss += a.ce * (logf(sz) - (z_label - m));
             if (s != s) loss = s;
             if (dZ) {
                 const float ay = wt * a.grad_scale * a.kd * a.inv_tau, az = label_ok ? wt * a.grad_scale * a.ce : 0.f;
-                const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) / s - (qr > 0.f ? qr / rest : 0.f));
-                const float iz = label_ok ? az / sz : 0.f;
+                const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) * to_row / s - (qr > 0.f ? qr / rest : 0.f));
+                const float iz = label_ok ? az / sz : 0.f, iz_off = iz * to_row_z;
 #pragma unroll 4
                 for (int v = lane; v < V; v += 32) {
-                    const float d = x[v] - m;
-                    x[v] = TWO ? exp2_unit(d * cy) * off + exp2_unit(d * kLog2E) * iz : exp2_unit(d * cy) * (off + iz);
+                    const float d = x[v] - mo;
+                    x[v] = TWO ? exp2_unit(d * cy) * off + exp2_unit(d * kLog2E) * iz_off : exp2_unit(d * cy) * (off + iz_off);
                 }
                 __syncwarp();
                 for (int k = lane; k < K; k += 32) {
@@ -855,7 +894,7 @@ distill_narrow_kernel(const T* Z, T* dZ, Distill a) {
                     }
                 }
                 if (lane == 0 && label_ok && !label_on)
-                    x[label] = exp2_unit((z_label - m) * cy) * off + exp2_unit((z_label - m) * kLog2E) * iz - az;
+                    x[label] = exp2_unit((z_label - mo) * cy) * off + exp2_unit((z_label - mo) * kLog2E) * iz_off - az;
             }
         }
     }
