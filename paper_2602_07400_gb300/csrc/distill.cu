@@ -51,6 +51,11 @@ __device__ __forceinline__ Pair teacher_log(float val, const Distill& a, float l
     const Pair p = exact_product(val, a.inv_tau2.hi);
     return pair_add(Pair{p.hi, fmaf(val, a.inv_tau2.lo, p.lo)}, Pair{-lse, 0.f});
 }
+// An entry's logit over tau less the largest one's: the difference first, which
+// keeps the digits that entries of large logits differ in.
+__device__ __forceinline__ float below_largest(float val, float largest, const Distill& a) {
+    return (val - (isinf(largest) ? 0.f : largest)) * a.inv_tau;
+}
 // max(0, 1 - Q)
 __device__ __forceinline__ float left_of(Pair Q) { return fmaxf(pair_add(Pair{1.f, 0.f}, Pair{-Q.hi, -Q.lo}).hi, 0.f); }
 
@@ -162,18 +167,18 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
         if (lane == 0) dbuf[warp] = q2;
         __syncthreads();
     } else {   // softmax over the record
-        const float wm = warp_largest(t);
+        const float own = ev >= 0 ? tval : BITLOGIC_NEG_INF, wm = warp_largest(own);
         if (lane == 0) tbuf[warp] = wm;
         __syncthreads();
         float tm = tbuf[0];
         for (int w = 1; w < kRowWarps; ++w) tm = fmaxf(tm, tbuf[w]);
-        const float ts = isinf(tm) ? 0.f : tm, ws = warp_add(exp2_unit((t - ts) * kLog2E));
+        const float d = below_largest(own, tm, a), ws = warp_add(exp2_unit(d * kLog2E));
         if (lane == 0) nbuf[warp] = ws;
         __syncthreads();
         float sum = 0.f;
         for (int w = 0; w < kRowWarps; ++w) sum += nbuf[w];
-        logq = t - (ts + logf(sum));
-        q = t == BITLOGIC_NEG_INF ? 0.f : exp2_unit(logq * kLog2E);
+        logq = d - logf(sum);
+        q = own == BITLOGIC_NEG_INF ? 0.f : exp2_unit(logq * kLog2E);
         const float wq = warp_add(q);
         if (lane == 0) qbuf[warp] = wq;
     }
@@ -484,18 +489,18 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
         }
         __syncthreads();
     } else {   // softmax over the record
-        const float wm = warp_largest(t);
+        const float own = ev >= 0 ? tval : BITLOGIC_NEG_INF, wm = warp_largest(own);
         if (lane == 0) tbuf[warp] = wm;
         __syncthreads();
         float tm = tbuf[0];
         for (int w = 1; w < kTileWarps; ++w) tm = fmaxf(tm, tbuf[w]);
-        const float ts = isinf(tm) ? 0.f : tm, ws = warp_add(exp2_unit((t - ts) * kLog2E));
+        const float d = below_largest(own, tm, a), ws = warp_add(exp2_unit(d * kLog2E));
         if (lane == 0) nbuf[warp] = ws;
         __syncthreads();
         float sum = 0.f;
         for (int w = 0; w < kTileWarps; ++w) sum += nbuf[w];
-        logq = t - (ts + logf(sum));
-        q = t == BITLOGIC_NEG_INF ? 0.f : exp2_unit(logq * kLog2E);
+        logq = d - logf(sum);
+        q = own == BITLOGIC_NEG_INF ? 0.f : exp2_unit(logq * kLog2E);
         const float wq = warp_add(q);
         if (lane == 0) qbuf[warp] = wq;
     }
@@ -762,7 +767,7 @@ distill_narrow_kernel(const T* Z, T* dZ, Distill a) {
                     entries[k].v = v = -1;
                     entries[k].logq = BITLOGIC_NEG_INF;
                 }
-                tm = fmaxf(tm, entries[k].logq * a.inv_tau);
+                tm = fmaxf(tm, entries[k].logq);
             }
             any |= __ballot_sync(0xffffffffu, v >= 0);
             label_on |= __ballot_sync(0xffffffffu, label_ok && v == label);
@@ -786,15 +791,15 @@ distill_narrow_kernel(const T* Z, T* dZ, Distill a) {
             q_left = left_of(sum);
         } else {
             tm = warp_largest(tm);
-            const float ts = isinf(tm) ? 0.f : tm;
             float sum = 0.f;
-            for (int k = lane; k < K; k += 32) sum += exp2_unit((entries[k].logq * a.inv_tau - ts) * kLog2E);
-            const float log_sum = ts + logf(warp_add(sum));
+            for (int k = lane; k < K; k += 32) sum += exp2_unit(below_largest(entries[k].logq, tm, a) * kLog2E);
+            const float log_sum = logf(warp_add(sum));
             for (int k = lane; k < K; k += 32) {
-                const float t = entries[k].logq * a.inv_tau;
+                const float t = entries[k].logq;
                 if (t != BITLOGIC_NEG_INF) {
-                    entries[k].logq = t - log_sum;
-                    entries[k].q = exp2_unit((t - log_sum) * kLog2E);
+                    const float logq = below_largest(t, tm, a) - log_sum;
+                    entries[k].logq = logq;
+                    entries[k].q = exp2_unit(logq * kLog2E);
                     Q += entries[k].q;
                 }
             }

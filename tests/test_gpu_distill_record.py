@@ -1,0 +1,45 @@
+"""Distillation against records whose values are large: only their differences
+count, so neither a loss nor a gradient may lose digits to their size."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import logits_ref as ref
+from test_gpu_distill_remainder import on_gpu, row64
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BASES = [0.0, 6e3, 1e5, 2.0 ** 25, -(2.0 ** 25), -1e30]
+STEPS = [[0, 0, 0, 0, 0], [0, -4, -8, 4, 4], [0, 0, -64, -64, -400]]
+
+
+def large_records(V, device):
+    """A row per base and pattern of differences (whole multiples of 4: exact in
+    fp32 up to 2^25; -1e30 swallows them)."""
+    g = torch.Generator().manual_seed(V)
+    T = len(BASES) * len(STEPS)
+    x = torch.randn(T, V, generator=g) * 2
+    idx = torch.stack([torch.randperm(V, generator=g)[:5] for _ in range(T)]).to(torch.int32)
+    val = torch.tensor([[b + s for s in steps] for b in BASES for steps in STEPS], dtype=torch.float32)
+    return x.to(device), val.to(device), idx.to(device)
+
+
+def check_large(call, x, val, idx, tau):
+    row, grad = call(x, val, idx, None, None, tau, 1.0, 0.0, 1.0)
+    z, v64, i64 = ref.values(x), val.double().cpu().numpy(), idx.cpu().numpy().astype(np.int64)
+    v64 -= v64.max(axis=1, keepdims=True)   # a softmax of them is the same
+    for t in range(x.shape[0]):
+        l, g, mag = row64(z[t], v64[t], i64[t], None, None, 0.125, tau, 1.0, 0.0, 1.0)
+        # terms: q ln q with differences up to 408 / tau, and the student's logits
+        size = 1 + 408 / tau + np.abs(z[t]).max() + math.log(x.shape[1])
+        assert abs(row[t] - l) <= 2.0 ** -20 * size * tau * max(tau, 1.0), (t, row[t], l)
+        bad = ~(np.abs(grad[t] - g) <= 2e-5 * mag + 2.0 ** -24 * np.abs(g) + 1e-37)
+        assert not bad.any(), (t, np.flatnonzero(bad)[:5], grad[t][bad][:5], g[bad][:5])
+
+
+@pytest.mark.parametrize("V", [12, 1000, 3000, 70000, 430001])
+@pytest.mark.parametrize("tau", [1.0, 2.0, 0.7])
+def test_large_values_of_a_record(V, tau):
+    check_large(on_gpu("rows"), *large_records(V, DEV), tau)
