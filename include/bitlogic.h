@@ -601,10 +601,12 @@ int bitlogic_top_logits(const void* X, int32_t dtype, int64_t T, int32_t V, int6
  *                with the same strides, and overlap Z in no other way.
  * A row of weight 0 has loss and gradient 0 whatever its logits hold, and so
  * has a row whose logits are all -inf.  A row without entries has no teacher
- * term.  A teacher value of -inf has q = 0.  A class that is on the record more
- * than once counts with the sum of its q.  A masked class has gradient
- * -q times its factor, and a loss of +inf where q > 0 or where it is the
- * label.  A row with a NaN or +inf logit has NaN in its loss and gradient.
+ * term.  A teacher value of -inf has q = 0; one whose a_k exceeds teacher_lse
+ * by more than 88 (a record of another temperature) leaves neither loss nor
+ * gradient finite.  A class that is on the record more than once counts with
+ * the sum of its q.  A masked class has gradient -q times its factor, and a
+ * loss of +inf where q > 0 or where it is the label.  A row with a NaN or +inf
+ * logit has NaN in its loss and gradient.
  * A class or label of V or more raises the device flag and is ignored.
  * Sums run in a fixed order: results are the same from run to run.
  * Returns BITLOGIC_ERR_NULL, BITLOGIC_ERR_SHAPE, BITLOGIC_ERR_DTYPE,

@@ -433,11 +433,13 @@ __device__ __forceinline__ Pair warp_add(Pair v) {
 }
 
 
-// e^x to about 2^-44 of itself, for x of a few ulps above 0 at most: x = n ln 2
-// + r, and the exponential series of r (|r| <= 0.35), whose terms from r^7 / 7!
-// on (below 2e-7) are summed in fp32.
+// e^x to about 2^-44 of itself; 0 below -80 and +inf above 88 (2^n is built from
+// n's bits).  x = n ln 2 + r with ln 2 in parts whose first n times is exact (Cody
+// and Waite's reduction), and the exponential series of r (|r| <= 0.35), whose
+// terms from r^7 / 7! on (below 2e-7) are summed in fp32.
 __device__ __forceinline__ Pair exp_pair(Pair x) {
     if (!(x.hi > -80.f)) return {x.hi != x.hi ? x.hi : 0.f, 0.f};
+    if (x.hi > 88.f) return {HUGE_VALF, 0.f};
     const float n = rintf(x.hi * kLog2E);
     // ln 2 in parts of 11, 24 and 24 bits: n times the first is exact
     constexpr double kLn2Exact = 0.693147180559945309417;

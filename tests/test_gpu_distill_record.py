@@ -43,3 +43,30 @@ def check_large(call, x, val, idx, tau):
 @pytest.mark.parametrize("tau", [1.0, 2.0, 0.7])
 def test_large_values_of_a_record(V, tau):
     check_large(on_gpu("rows"), *large_records(V, DEV), tau)
+
+
+@pytest.mark.parametrize("V", [12, 1000, 3000, 70000, 430001])
+def test_values_far_above_the_log_sum_exp_show(V):
+    """A record under a log-sum-exp that is not its own: q = exp(a) as long as
+    fp32 holds it, and no finite loss or gradient beyond."""
+    above = [0.5, 3.0, 60.0, 87.0, 90.0, 100.0, 177.5, 1e4]
+    T = len(above)
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn(T, V, generator=g).to(DEV)
+    idx = torch.randint(0, V, (T, 1), generator=g).to(torch.int32).to(DEV)
+    val = torch.tensor(above, dtype=torch.float32, device=DEV)[:, None] + 2.0
+    lse = torch.full((T,), 2.0, device=DEV)
+    row, grad = on_gpu("rows")(x, val, idx, lse, None, 1.0, 1.0, 0.0, 1.0)
+    z, v64 = ref.values(x), val.double().cpu().numpy()
+    for t, a in enumerate(above):
+        if a > 88:
+            assert not np.isfinite(row[t]) and not np.isfinite(grad[t]).any(), a
+            continue
+        l, gr, mag = row64(z[t], v64[t], idx[t].cpu().numpy().astype(np.int64), 2.0, None, 0.125, 1.0, 1.0, 0.0, 1.0)
+        # q is as exact as its exponent, off by a 2^-24 at most, beside the loss's own terms
+        size = 1 + a + np.abs(z[t]).max() + math.log(V)
+        if abs(l) > np.finfo(np.float32).max:   # past what a loss is held in
+            assert row[t] == math.inf
+        else:
+            assert abs(row[t] - l) <= (2.0 ** -20 + a * 2.0 ** -24) * size * math.exp(a), (a, row[t], l)
+        assert (np.abs(grad[t] - gr) <= (2e-5 + a * 2.0 ** -24) * mag + 1e-37).all(), a
