@@ -606,7 +606,8 @@ int bitlogic_top_logits(const void* X, int32_t dtype, int64_t T, int32_t V, int6
  * gradient finite.  A class that is on the record more than once counts with
  * the sum of its q.  A masked class has gradient -q times its factor, and a
  * loss of +inf where q > 0 or where it is the label.  A row with a NaN or +inf
- * logit has NaN in its loss and gradient.
+ * logit, or with a NaN in its teacher_lse or among its entries' values, has NaN
+ * in its loss and gradient.
  * A class or label of V or more raises the device flag and is ignored.
  * Sums run in a fixed order: results are the same from run to run.
  * Returns BITLOGIC_ERR_NULL, BITLOGIC_ERR_SHAPE, BITLOGIC_ERR_DTYPE,

@@ -384,7 +384,7 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
         if (qr > 0.f) kl += qr * (logf(qr) - ((m_off - m) * a.inv_tau + log_about(oy, rest) - log_s));
         float loss = a.kd != 0.f ? a.kd * kl : 0.f;   // a loss of +inf without weight is none
         if (label_ok) loss += a.ce * (log_about(rz, sz) - (z_label - m));
-        a.row_loss[row] = s != s ? s : loss;
+        a.row_loss[row] = s != s ? s : Q != Q ? Q : loss;
     }
 }
 
@@ -709,7 +709,7 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
         if (qr > 0.f) kl += qr * (logf(qr) - ((m_off - m) * a.inv_tau + log_about(oy, rest) - log_s));
         float loss = a.kd != 0.f ? a.kd * kl : 0.f;
         if (label_ok) loss += a.ce * (log_about(bz, sz) - (zl - m));
-        a.row_loss[row] = s != s ? s : loss;
+        a.row_loss[row] = s != s ? s : Q != Q ? Q : loss;
     }
 }
 
@@ -879,6 +879,7 @@ distill_narrow_kernel(const T* Z, T* dZ, Distill a) {
             loss = a.kd != 0.f ? a.kd * kl : 0.f;
             if (label_ok) loss += a.ce * (logf(sz) - (z_label - m));
             if (s != s) loss = s;
+            else if (Q != Q) loss = Q;
             if (dZ) {
                 const float ay = wt * a.grad_scale * a.kd * a.inv_tau, az = label_ok ? wt * a.grad_scale * a.ce : 0.f;
                 const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) * to_row / s - (qr > 0.f ? qr / rest : 0.f));

@@ -70,3 +70,30 @@ def test_values_far_above_the_log_sum_exp_show(V):
         else:
             assert abs(row[t] - l) <= (2.0 ** -20 + a * 2.0 ** -24) * size * math.exp(a), (a, row[t], l)
         assert (np.abs(grad[t] - gr) <= (2e-5 + a * 2.0 ** -24) * mag + 1e-37).all(), a
+
+
+@pytest.mark.parametrize("V", [12, 1000, 3000, 70000, 430001])
+def test_nan_of_a_record_shows(V):
+    """A NaN among a row's entries, or in its log-sum-exp, is in the row's loss
+    and gradient and in no other row's; a place without an entry is not read."""
+    T, nan = 6, math.nan
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn(T, V, generator=g).to(DEV)
+    idx = torch.stack([torch.randperm(V, generator=g)[:4] for _ in range(T)]).to(torch.int32).to(DEV)
+    val = torch.randn(T, 4, generator=g).to(DEV)
+    lse = torch.full((T,), 3.0, device=DEV)
+    call = on_gpu("rows")
+    for own in (None, lse):
+        v, i = val.clone(), idx.clone()
+        v[1, 2] = nan
+        v[2, :] = nan
+        v[3, 3], i[3, 3] = nan, -1
+        want = [False, True, True, False, False, False]
+        if own is not None:
+            own = own.clone()
+            own[4] = nan
+            want[4] = True
+        row, grad = call(x, v, i, own, None, 1.0, 1.0, 0.0, 1.0)
+        for t in range(T):
+            assert np.isnan(row[t]) == want[t], (t, row)
+            assert (np.isnan(grad[t]).all() if want[t] else np.isfinite(grad[t]).all()), t
