@@ -933,14 +933,21 @@ distill_narrow_kernel(const T* Z, T* dZ, Distill a) {
 // 51.7 us, in four 55.9 us).
 constexpr int kTileFit = 100 * 1024, kTileMost = 208 * 1024, kTileLeast = 8 * 1024;
 
+// Shared memory of the kernels for rows of few classes and for rows streamed twice.
+inline size_t narrow_bytes(int V, int K) { return kNarrowWarps * (K * sizeof(NarrowEntry) + narrow_row_floats(V) * sizeof(float)); }
+inline size_t row_bytes(int V, int element) {
+    // a thread's mask bits, by 32 of its pieces, and a bit per place of the row
+    const long long pieces = slice_bytes(V, element, 1) / 16, words = (pieces + 32 * kRowThreads - 1) / (32 * kRowThreads);
+    return (size_t)(words * kRowThreads + (pieces * (16 / element) + 31) / 32) * 4;
+}
+
 template <typename T, bool TWO>
 int launch_distill(const T* z, T* dz, const Distill& a, cudaStream_t stream) {
     cudaError_t e;
     const int blocks = blocks_per_row(a.T, a.V, sizeof(T), kTileFit, kTileMost, kTileLeast);
     if (a.V <= kNarrow) {
-        const size_t smem = kNarrowWarps * (a.K * sizeof(NarrowEntry) + narrow_row_floats(a.V) * sizeof(float));
-        e = launch_rows(distill_narrow_kernel<T, TWO>, (a.T + kNarrowWarps - 1) / kNarrowWarps, 1, kNarrowWarps * 32, smem,
-                        stream, z, dz, a);
+        e = launch_rows(distill_narrow_kernel<T, TWO>, (a.T + kNarrowWarps - 1) / kNarrowWarps, 1, kNarrowWarps * 32,
+                        narrow_bytes(a.V, a.K), narrow_bytes(kNarrow, kMaxTop), stream, z, dz, a);
     } else if (blocks > 0) {
         // (bf16: 9024 rows of 6644 classes 57.2 us in 64 threads, 63.1 in 128,
         // 96.7 in 256; 8192 rows of 16384 classes 100.4, 97.7 and 114.8 us)
@@ -949,12 +956,10 @@ int launch_distill(const T* z, T* dz, const Distill& a, cudaStream_t stream) {
                     : a.K <= 128 && bytes <= 40 * 1024 ? distill_tile_kernel<T, TWO, 128>
                                                        : distill_tile_kernel<T, TWO, 256>;
         const int threads = a.K <= 64 && bytes <= 16 * 1024 ? 64 : a.K <= 128 && bytes <= 40 * 1024 ? 128 : 256;
-        e = launch_rows(kern, a.T, blocks, threads, (size_t)bytes, stream, z, dz, a);
+        e = launch_rows(kern, a.T, blocks, threads, (size_t)bytes, kTileMost, stream, z, dz, a);
     } else {
-        // a thread's mask bits, by 32 of its pieces, and a bit per place of the row
-        const long long pieces = slice_bytes(a.V, sizeof(T), 1) / 16, words = (pieces + 32 * kRowThreads - 1) / (32 * kRowThreads);
-        const size_t smem = (size_t)(words * kRowThreads + (pieces * (16 / sizeof(T)) + 31) / 32) * 4;
-        e = launch_rows(distill_row_kernel<T, TWO>, a.T, 1, kRowThreads, smem, stream, z, dz, a);
+        e = launch_rows(distill_row_kernel<T, TWO>, a.T, 1, kRowThreads, row_bytes(a.V, sizeof(T)),
+                        row_bytes(kMaxClasses, sizeof(T)), stream, z, dz, a);
     }
     return e == cudaSuccess ? launch_status() : (int)BITLOGIC_ERR_CUDA;
 }

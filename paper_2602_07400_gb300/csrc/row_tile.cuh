@@ -484,12 +484,15 @@ inline int blocks_per_row(long long T, long long V, int element, long long fit, 
 }
 
 // Launch of a kernel over T rows with `blocks` blocks (one cluster) per row,
-// as a programmatic dependent launch (see launch_dependent).
+// as a programmatic dependent launch (see launch_dependent).  The limit on a
+// kernel's shared memory belongs to the kernel, not to the call, and calls come
+// from any thread: it is set to `most`, the largest `smem` that the kernel is ever
+// launched with, and so never below what a launch of another thread needs.
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch_rows(void (*kernel)(KArgs...), long long T, int blocks, int threads, size_t smem,
+inline cudaError_t launch_rows(void (*kernel)(KArgs...), long long T, int blocks, int threads, size_t smem, size_t most,
                                cudaStream_t stream, Args... args) {
     if (smem > 4 * 1024) {   // with the kernels' own arrays perhaps past the 48 KB that need no leave
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchConfig_t cfg = {};

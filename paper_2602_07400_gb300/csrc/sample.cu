@@ -1393,6 +1393,12 @@ sample_narrow_kernel(const T* __restrict__ X, long long ld, int V, long long row
 // their lists.
 constexpr int kTileFit = 40 * 1024, kTileMost = 184 * 1024, kTileLeast = 8 * 1024;
 
+// Shared memory of the chunks' weights of a row.
+inline size_t chunk_bytes(int V, int element) {
+    const long long pieces = slice_bytes(V, element, 1) / 16, batches = (pieces + 4 * kSampleThreads - 1) / (4 * kSampleThreads);
+    return (size_t)(2 + kSampleWarps * batches) * 8;
+}
+
 template <typename T>
 int launch_sample(const T* x, long long T_, int V, long long ld, const Settings& set, const Draw& out,
                   cudaStream_t stream) {
@@ -1400,7 +1406,7 @@ int launch_sample(const T* x, long long T_, int V, long long ld, const Settings&
     if (V <= kNarrow) {
         auto kern = V <= 32 ? sample_narrow_kernel<T, 1> : V <= 128 ? sample_narrow_kernel<T, 4>
                   : V <= 256 ? sample_narrow_kernel<T, 8> : V <= 512 ? sample_narrow_kernel<T, 16> : sample_narrow_kernel<T, 32>;
-        e = launch_rows(kern, (T_ + kNarrowWarps - 1) / kNarrowWarps, 1, kNarrowWarps * 32, 0, stream, x, ld, V, T_, set, out);
+        e = launch_rows(kern, (T_ + kNarrowWarps - 1) / kNarrowWarps, 1, kNarrowWarps * 32, 0, 0, stream, x, ld, V, T_, set, out);
     } else {
         // where a cluster per row is faster (50001 fp32 and 131072 bf16 classes:
         // top_k at 60 rows 21 and 21.6 against 18.1 and 19.9 us in a block each,
@@ -1410,11 +1416,10 @@ int launch_sample(const T* x, long long T_, int V, long long ld, const Settings&
         const int blocks = T_ <= few ? blocks_per_row(T_, V, sizeof(T), kTileFit, kTileMost, kTileLeast) : 0;
         if (blocks > 1) {
             e = launch_rows(sample_tile_kernel<T>, T_, blocks, kSampleThreads, (size_t)slice_bytes(V, sizeof(T), blocks),
-                            stream, x, ld, V, set, out);
+                            kTileMost, stream, x, ld, V, set, out);
         } else {
-            const long long pieces = slice_bytes(V, sizeof(T), 1) / 16, batches = (pieces + 4 * kSampleThreads - 1) / (4 * kSampleThreads);
-            e = launch_rows(sample_row_kernel<T>, T_, 1, kSampleThreads, (size_t)(2 + kSampleWarps * batches) * 8, stream, x, ld, V,
-                            set, out);
+            e = launch_rows(sample_row_kernel<T>, T_, 1, kSampleThreads, chunk_bytes(V, sizeof(T)),
+                            chunk_bytes(kMaxClasses, sizeof(T)), stream, x, ld, V, set, out);
         }
     }
     return e == cudaSuccess ? launch_status() : (int)BITLOGIC_ERR_CUDA;

@@ -539,21 +539,21 @@ int launch_top(const T* x, long long T_, int V, long long ld, const TopOut& o, c
     cudaError_t e;
     if (V <= kNarrow) {
         const long long grid = (T_ + kNarrowWarps - 1) / kNarrowWarps;
-        const size_t smem = (size_t)kNarrowWarps * o.K * 8;
+        const size_t smem = (size_t)kNarrowWarps * o.K * 8, most = (size_t)kNarrowWarps * kMaxTop * 8;
         auto kern = V <= 32 ? top_narrow_kernel<T, 1> : V <= 128 ? top_narrow_kernel<T, 4>
                   : V <= 256 ? top_narrow_kernel<T, 8> : V <= 512 ? top_narrow_kernel<T, 16> : top_narrow_kernel<T, 32>;
-        e = launch_rows(kern, grid, 1, kNarrowWarps * 32, smem, stream, x, ld, V, T_, o);
+        e = launch_rows(kern, grid, 1, kNarrowWarps * 32, smem, most, stream, x, ld, V, T_, o);
     } else {
         const int blocks = 2 * T_ <= sm_count() ? blocks_per_row(T_, V, sizeof(T), kTileFit, kTileMost, kTileLeast) : 0;
         if (blocks > 1) {
-            e = launch_rows(top_tile_kernel<T>, T_, blocks, kTopThreads, (size_t)slice_bytes(V, sizeof(T), blocks), stream,
-                            x, ld, V, o);
+            e = launch_rows(top_tile_kernel<T>, T_, blocks, kTopThreads, (size_t)slice_bytes(V, sizeof(T), blocks),
+                            kTileMost, stream, x, ld, V, o);
         } else {
             // short rows in 128 threads, of which an SM holds more blocks (bf16,
             // 2000 rows: 4096 classes 20.8 against 30.0 us in 256, 16384 classes
             // 35.1 against 36.5, 32768 classes 51.4 against 49.4)
             const bool is_short = V * (long long)sizeof(T) <= 32 * 1024;
-            e = launch_rows(is_short ? top_row_kernel<T, 128> : top_row_kernel<T, 256>, T_, 1, is_short ? 128 : 256, 0, stream,
+            e = launch_rows(is_short ? top_row_kernel<T, 128> : top_row_kernel<T, 256>, T_, 1, is_short ? 128 : 256, 0, 0, stream,
                             x, ld, V, o);
         }
     }
