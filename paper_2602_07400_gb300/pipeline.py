@@ -373,9 +373,13 @@ class TrainStep:
         else:
             bitlogic_lut_forward_node(self.y1, n.conn2, n.theta2, self.y2, self.node, stream)
         mark("forward2")
-        bitlogic_head_loss_ex(self.y2, self.labels, self.C, self.tau, self.loss, self.ws_head,
-                              logits=self.logits, dY_grouped=self.dyg, stream=stream)
+        self._head(self.labels, stream)
         mark("head")
+
+    def _head(self, labels, stream):
+        """Logits, loss and class gradients of the last forward."""
+        bitlogic_head_loss_ex(self.y2, labels, self.C, self.tau, self.loss, self.ws_head,
+                              logits=self.logits, dY_grouped=self.dyg, stream=stream)
 
     def backward(self, stream=None, mark=_nomark):
         n = self.net
@@ -544,17 +548,16 @@ class DistillStep(TrainStep):
         # what the head takes for a sample without a label
         self._head_labels = torch.zeros_like(self.labels)
 
+    def _head(self, labels, stream):
+        # the head's own loss and gradients are overwritten by forward(); it
+        # takes labels in range, whatever the samples carry
+        super()._head(self._head_labels, stream)
+
     def forward(self, stream=None, mark=_nomark):
-        # the head's own loss and gradients are overwritten below; it takes
-        # labels in range, whatever the samples carry
-        labels, self.labels = self.labels, self._head_labels
-        try:
-            super().forward(stream, mark)
-        finally:
-            self.labels = labels
+        super().forward(stream, mark)
         t = self.teacher
         bitlogic_distill_loss(self.logits, t.val, t.idx, self.row_loss, self.loss, self.dyg.t(),
-                              teacher_lse=t.lse if self.tail else None, labels=labels, row_weight=self.row_weight,
+                              teacher_lse=t.lse if self.tail else None, labels=self.labels, row_weight=self.row_weight,
                               temperature=t.temperature, kd_weight=self.kd_weight, ce_weight=self.ce_weight,
                               grad_scale=1.0 / self.tau, stream=stream)
         mark("distill")
