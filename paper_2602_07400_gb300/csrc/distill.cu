@@ -999,7 +999,8 @@ extern "C" int bitlogic_distill_loss(const void* Z, int32_t dtype, int64_t T, in
     if (dZ) {
         // rows and classes of the gradient apart from each other
         if (ldg < 1 || incg < 1 || ldg > (1LL << 40) || incg > (1LL << 40)) return BITLOGIC_ERR_SHAPE;
-        if (T > 1 && V > 1 && ldg < (V - 1) * incg + 1 && incg < (T - 1) * ldg + 1) return BITLOGIC_ERR_SHAPE;
+        // (the rows' extent by division: the product of T and ldg may pass 64 bits)
+        if (T > 1 && V > 1 && ldg < (V - 1) * incg + 1 && (incg - 1) / ldg < T - 1) return BITLOGIC_ERR_SHAPE;
         if (reinterpret_cast<uintptr_t>(dZ) % logit_bytes(dtype)) return BITLOGIC_ERR_ALIGN;
     }
     const double inv_tau = 1.0 / (double)temperature;
