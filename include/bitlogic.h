@@ -569,7 +569,8 @@ typedef enum {
  * when the row has a NaN, +inf when it has +inf and no NaN.
  * Returns BITLOGIC_ERR_NULL, BITLOGIC_ERR_SHAPE, BITLOGIC_ERR_DTYPE,
  * BITLOGIC_ERR_ALIGN, BITLOGIC_ERR_HYPER (temperature not positive and
- * finite), BITLOGIC_ERR_CUDA. */
+ * finite, or below 4.3e-39, where log2(e) / temperature passes fp32),
+ * BITLOGIC_ERR_CUDA. */
 int bitlogic_top_logits(const void* X, int32_t dtype, int64_t T, int32_t V, int64_t ld, int32_t K,
                         float temperature, float* val, int32_t* idx, float* lse, cudaStream_t stream);
 
@@ -611,8 +612,9 @@ int bitlogic_top_logits(const void* X, int32_t dtype, int64_t T, int32_t V, int6
  * A class or label of V or more raises the device flag and is ignored.
  * Sums run in a fixed order: results are the same from run to run.
  * Returns BITLOGIC_ERR_NULL, BITLOGIC_ERR_SHAPE, BITLOGIC_ERR_DTYPE,
- * BITLOGIC_ERR_ALIGN, BITLOGIC_ERR_HYPER (temperature not positive and finite,
- * a weight or scale not finite), BITLOGIC_ERR_CUDA. */
+ * BITLOGIC_ERR_ALIGN, BITLOGIC_ERR_HYPER (temperature as above, a weight or
+ * scale not finite, kd_weight temperature^2 past fp32 or below it),
+ * BITLOGIC_ERR_CUDA. */
 int bitlogic_distill_loss(const void* Z, int32_t dtype, int64_t T, int32_t V, int64_t ld,
                           const float* teacher_val, const int32_t* teacher_idx, int32_t K,
                           const float* teacher_lse, const int32_t* labels, const float* row_weight,

@@ -992,9 +992,10 @@ extern "C" int bitlogic_distill_loss(const void* Z, int32_t dtype, int64_t T, in
                                      cudaStream_t stream) {
     if (int st = check_logits(Z, dtype, false, T, V, ld)) return st;
     if (K < 1 || K > kMaxTop) return BITLOGIC_ERR_SHAPE;
-    if (!(temperature > 0.f) || isinf(temperature) || !isfinite(kd_weight) || !isfinite(ce_weight) ||
-        !isfinite(grad_scale))
+    if (!temperature_ok(temperature) || !isfinite(kd_weight) || !isfinite(ce_weight) || !isfinite(grad_scale))
         return BITLOGIC_ERR_HYPER;
+    const float kd = kd_weight * temperature * temperature;   // of the divergence
+    if (!isfinite(kd) || (kd == 0.f) != (kd_weight == 0.f)) return BITLOGIC_ERR_HYPER;
     if (!loss || (T > 0 && (!teacher_val || !teacher_idx || !row_loss))) return BITLOGIC_ERR_NULL;
     if (dZ) {
         // rows and classes of the gradient apart from each other
@@ -1007,7 +1008,7 @@ extern "C" int bitlogic_distill_loss(const void* Z, int32_t dtype, int64_t T, in
     Distill a = {T, V, K, ld, teacher_val, teacher_idx, teacher_lse, labels, row_weight,
                  {(float)inv_tau, (float)(inv_tau - (double)(float)inv_tau)},
                  1.0f / temperature,
-                 kd_weight * temperature * temperature, ce_weight, row_loss, ldg, incg, grad_scale};
+                 kd, ce_weight, row_loss, ldg, incg, grad_scale};
     if (T > 0) {
         const int st = with_logit_type(dtype, false, [&](auto* type) {
             using E = std::remove_const_t<std::remove_pointer_t<decltype(type)>>;

@@ -173,6 +173,10 @@ inline int with_logit_type(int dtype, bool whole, F f) {
 
 inline int logit_bytes(int dtype) { return dtype == BITLOGIC_F32 || dtype == BITLOGIC_I32 ? 4 : 2; }
 
+// Whether a temperature is positive and finite, and so is its inverse times
+// log2(e), the slope of a row's powers.
+inline bool temperature_ok(float temperature) { return temperature > 0.f && isfinite(temperature) && isfinite(kLog2E / temperature); }
+
 // Checks of a matrix of logits that the three operators share.
 inline int check_logits(const void* X, int dtype, bool whole, int64_t T, int32_t V, int64_t ld) {
     if (dtype < BITLOGIC_F32 || dtype > BITLOGIC_I32 || (dtype == BITLOGIC_I32 && !whole)) return BITLOGIC_ERR_DTYPE;

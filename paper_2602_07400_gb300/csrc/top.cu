@@ -569,7 +569,7 @@ extern "C" int bitlogic_top_logits(const void* X, int32_t dtype, int64_t T, int3
                                    float temperature, float* val, int32_t* idx, float* lse, cudaStream_t stream) {
     if (int st = check_logits(X, dtype, true, T, V, ld)) return st;
     if (K < 1 || K > kMaxTop || K > V) return BITLOGIC_ERR_SHAPE;
-    if (!(temperature > 0.f) || isinf(temperature)) return BITLOGIC_ERR_HYPER;
+    if (!temperature_ok(temperature)) return BITLOGIC_ERR_HYPER;
     if (T == 0) return BITLOGIC_OK;
     if (!val || !idx) return BITLOGIC_ERR_NULL;
     const TopOut o = {K, 1.0f / temperature, val, idx, lse};
