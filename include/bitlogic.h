@@ -549,8 +549,10 @@ int bitlogic_adamw_update(float* theta, float* m, float* v, const float* grad, i
  *          is held in fp32 or wider.  In BITLOGIC_I32 the lowest int stands
  *          for -inf.
  * -inf marks a class that is masked.  Any other number, the type's lowest
- * among them, is an ordinary logit.  No call needs a workspace, and results do
- * not depend on the rows around a row. */
+ * among them, is an ordinary logit.  No call needs a workspace.  A record's
+ * values and classes and a draw do not depend on the rows around a row; the
+ * number of rows may choose the order in which a row's log-sum-exp, loss and
+ * gradient are summed, and so their last bits. */
 typedef enum {
     BITLOGIC_F32 = 0,
     BITLOGIC_BF16 = 1,
