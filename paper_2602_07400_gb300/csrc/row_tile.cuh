@@ -32,8 +32,9 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 // Another block's shared memory may be touched only once that block runs: each
 // block of a cluster reports at its kernel's start, behind which it asks for its
 // slice, and waits for the others just before its first store to one of them.
+// The report orders no memory, so it does not wait for loads on their way.
 __device__ __forceinline__ void report_running(unsigned blocks) {
-    if (blocks > 1) cluster_arrive();
+    if (blocks > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void wait_all_running(unsigned blocks) {
     if (blocks > 1) cluster_wait();
