@@ -62,8 +62,19 @@ __device__ __forceinline__ float left_of(Pair Q) { return fmaxf(pair_add(Pair{1.
 // ln of a sum of powers about a base, less the base's own logit over tau.
 __device__ __forceinline__ float log_about(const PowerBase& p, float sum) { return kLn2 * (log2f(sum) - p.exponent(p.m)); }
 
-// The factor from a base off the record to the row's, 0 where no class is off it.
-__device__ __forceinline__ float factor_of(const PowerBase& off, const PowerBase& row) { return off.none ? 0.f : off.to(row); }
+// The bases about a logit at tau (y) and at 1 (z): for two softmaxes far alike, as
+// one pass takes the powers of both; else the same, since labels come with tau = 1.
+template <bool TWO>
+struct Bases {
+    PowerBase y, z;
+    __device__ __forceinline__ Bases(float largest, float cy) : y(largest, cy), z(largest, TWO ? kLog2E : cy) {
+        if (TWO) {
+            const PowerBase at_tau = y;
+            y = far_alike(y, z);
+            z = far_alike(z, at_tau);
+        }
+    }
+};
 
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
 
@@ -293,7 +304,8 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
         m = fmaxf(m, mbuf[w]);
     }
     m = fmaxf(m, m_off);
-    const PowerBase ry(m, cy), rz(m, kLog2E), ny(m_off, cy), nz(m_off, kLog2E), oy = far_alike(ny, nz), oz = far_alike(nz, ny);
+    const Bases<TWO> off_bases(m_off, cy);
+    const PowerBase ry(m, cy), rz(m, TWO ? kLog2E : cy), &oy = off_bases.y, &oz = off_bases.z;
     {
         float ra, rb, sa, sb;
         unpack2(add2(y0, y1), ra, rb);
@@ -317,7 +329,8 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
         if (a.teacher_lse) q_sum = pair_add(q_sum, dbuf[w]);
         else Q += qbuf[w];
     }
-    s += rest * oy.to(ry);
+    const float to_row = oy.to(ry);
+    s += rest * to_row;
     if (!TWO) sz = s;   // tau = 1 where a label is
     if (a.teacher_lse) {
         Q = q_sum.hi;
@@ -333,8 +346,9 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
     const float kl_part = warp_add(q > 0.f ? q * (logq - ((zk - m) * a.inv_tau - log_s)) : 0.f);
     if (lane == 0) kbuf[warp] = kl_part;
     const float ay = wt * a.grad_scale * a.kd * a.inv_tau, az = label_ok ? wt * a.grad_scale * a.ce : 0.f;
-    const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) * factor_of(oy, ry) / s - (qr > 0.f ? qr / rest : 0.f));
-    const float iz = label_ok ? az / sz : 0.f, iz_off = iz * factor_of(oz, rz), fy = TWO ? off : off + iz_off;
+    const float p_off = oy.none ? 0.f : to_row;   // the factor F, 0 where no class is off the record
+    const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) * p_off / s - (qr > 0.f ? qr / rest : 0.f));
+    const float iz = label_ok ? az / sz : 0.f, iz_off = iz * (!TWO ? p_off : oz.none ? 0.f : oz.to(rz)), fy = TWO ? off : off + iz_off;
     if (g) {
         auto gradient = [&](const auto& py, const auto& pz) {
             const f32x2 fy2 = pack2(fy, fy), fz2 = pack2(iz_off, iz_off);
@@ -563,7 +577,8 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     // powers of the slice
     const float cy = kLog2E * a.inv_tau;
     {
-        const PowerBase by(m_off, cy), bz(m_off, kLog2E), ey = far_alike(by, bz), ez = far_alike(bz, by), my(m, cy), mz(m, kLog2E);
+        const Bases<TWO> e(m_off, cy);
+        const PowerBase &ey = e.y, &ez = e.z, my(m, cy), mz(m, kLog2E);
         f32x2 r0 = 0, r1 = 0, s0 = 0, s1 = 0;   // two zeros each
         auto sums = [&](const auto& py, const auto& pz) {
 #pragma unroll 2
@@ -622,18 +637,24 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
         m = fmaxf(m, stats[b].m);
         m_off = fmaxf(m_off, stats[b].m_off);
     }
-    const PowerBase by(m, cy), bz(m, kLog2E), ny(m_off, cy), nz(m_off, kLog2E), oy = far_alike(ny, nz), oz = far_alike(nz, ny);
-    float rest = 0.f, s = 0.f, sz = 0.f, zl = 0.f;
-    Pair q_sum = {0.f, 0.f};
-    for (unsigned b = 0; b < blocks; ++b) {
-        const DistillStats& o = stats[b];
-        rest += o.rest * far_alike(PowerBase(o.m_off, cy), PowerBase(o.m_off, kLog2E)).to(oy);
-        s += o.member * PowerBase(o.m, cy).to(by);
-        if (TWO) sz += o.sz * PowerBase(o.m, kLog2E).to(bz);
-        if (a.teacher_lse) q_sum = pair_add(q_sum, o.q);
-        if (o.has_label) zl = o.z_label;
+    const Bases<TWO> off_bases(m_off, cy);
+    const PowerBase by(m, cy), bz(m, TWO ? kLog2E : cy), &oy = off_bases.y, &oz = off_bases.z;
+    float rest = stats[0].rest, s = stats[0].member, sz = stats[0].sz, zl = stats[0].z_label;
+    Pair q_sum = stats[0].q;
+    if (blocks > 1) {   // from the blocks' bases
+        rest = s = sz = 0.f;
+        q_sum = {0.f, 0.f};
+        for (unsigned b = 0; b < blocks; ++b) {
+            const DistillStats& o = stats[b];
+            rest += o.rest * Bases<TWO>(o.m_off, cy).y.to(oy);
+            s += o.member * PowerBase(o.m, cy).to(by);
+            if (TWO) sz += o.sz * PowerBase(o.m, kLog2E).to(bz);
+            if (a.teacher_lse) q_sum = pair_add(q_sum, o.q);
+            if (o.has_label) zl = o.z_label;
+        }
     }
-    s += rest * oy.to(by);
+    const float to_row = oy.to(by);
+    s += rest * to_row;
     if (!TWO) sz = s;   // tau = 1 where a label is
     const bool empty = s == 0.f;   // every class masked
     float qr = 0.f;
@@ -655,8 +676,9 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
         zero_row();
     } else if (g) {
         const float ay = wt * a.grad_scale * a.kd * a.inv_tau, az = label_ok ? wt * a.grad_scale * a.ce : 0.f;
-        const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) * factor_of(oy, by) / s - (qr > 0.f ? qr / rest : 0.f));
-        const float iz = label_ok ? az / sz : 0.f, iz_off = iz * factor_of(oz, bz), fy = TWO ? off : off + iz_off;
+        const float p_off = oy.none ? 0.f : to_row;   // the factor F, 0 where no class is off the record
+        const float on = ay * (Q + qr) / s, off = ay * ((Q + qr) * p_off / s - (qr > 0.f ? qr / rest : 0.f));
+        const float iz = label_ok ? az / sz : 0.f, iz_off = iz * (!TWO ? p_off : oz.none ? 0.f : oz.to(bz)), fy = TWO ? off : off + iz_off;
         auto gradient = [&](const auto& py, const auto& pz) {
             const f32x2 fy2 = pack2(fy, fy), fz2 = pack2(iz_off, iz_off);
             uint4* to16 = wide ? reinterpret_cast<uint4*>(g + slice.first) : tile16;   // written at whole pieces
