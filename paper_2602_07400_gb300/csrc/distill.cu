@@ -62,6 +62,13 @@ __device__ __forceinline__ float left_of(Pair Q) { return fmaxf(pair_add(Pair{1.
 // ln of a sum of powers about a base, less the base's own logit over tau.
 __device__ __forceinline__ float log_about(const PowerBase& p, float sum) { return kLn2 * (log2f(sum) - p.exponent(p.m)); }
 
+// ln r of the classes off the record, r = S F / s: the quotient's own logarithm,
+// which keeps the digits of an r near 1, as long as fp32 holds the quotient; else
+// from the logits (`below`: the largest off the record less the row's, over tau).
+__device__ __forceinline__ float log_remainder(float r, float below, float log_rest, float log_s) {
+    return r > 1e-30f ? logf(r) : below + log_rest - log_s;
+}
+
 // The bases about a logit at tau (y) and at 1 (z): for two softmaxes far alike, as
 // one pass takes the powers of both; else the same, since labels come with tau = 1.
 template <bool TWO>
@@ -395,7 +402,7 @@ distill_row_kernel(const T* Z, T* dZ, Distill a) {
     if (tid == 0) {
         float kl = 0.f;
         for (int w = 0; w < kRowWarps; ++w) kl += kbuf[w];
-        if (qr > 0.f) kl += qr * (logf(qr) - ((m_off - m) * a.inv_tau + log_about(oy, rest) - log_s));
+        if (qr > 0.f) kl += qr * (logf(qr) - log_remainder(rest * to_row / s, (m_off - m) * a.inv_tau, log_about(oy, rest), log_s));
         float loss = a.kd != 0.f ? a.kd * kl : 0.f;   // a loss of +inf without weight is none
         if (label_ok) loss += a.ce * (log_about(rz, sz) - (z_label - m));
         a.row_loss[row] = s != s ? s : Q != Q ? Q : loss;
@@ -728,7 +735,7 @@ distill_tile_kernel(const T* Z, T* dZ, Distill a) {
     if (rank == 0 && tid == 0 && !empty) {
         float kl = 0.f;
         for (unsigned b = 0; b < blocks * kTileWarps; ++b) kl += kl_part[b];
-        if (qr > 0.f) kl += qr * (logf(qr) - ((m_off - m) * a.inv_tau + log_about(oy, rest) - log_s));
+        if (qr > 0.f) kl += qr * (logf(qr) - log_remainder(rest * to_row / s, (m_off - m) * a.inv_tau, log_about(oy, rest), log_s));
         float loss = a.kd != 0.f ? a.kd * kl : 0.f;
         if (label_ok) loss += a.ce * (log_about(bz, sz) - (zl - m));
         a.row_loss[row] = s != s ? s : Q != Q ? Q : loss;
@@ -897,7 +904,7 @@ distill_narrow_kernel(const T* Z, T* dZ, Distill a) {
             for (int k = lane; k < K; k += 32)
                 if (entries[k].q > 0.f) kl += entries[k].q * (entries[k].logq - ((entries[k].z - m) * a.inv_tau - log_s));
             kl = warp_add(kl);
-            if (qr > 0.f) kl += qr * (logf(qr) - ((mo - m) * a.inv_tau + logf(rest) - log_s));
+            if (qr > 0.f) kl += qr * (logf(qr) - log_remainder(rest * to_row / s, (mo - m) * a.inv_tau, logf(rest), log_s));
             loss = a.kd != 0.f ? a.kd * kl : 0.f;
             if (label_ok) loss += a.ce * (logf(sz) - (z_label - m));
             if (s != s) loss = s;
