@@ -20,8 +20,9 @@
 // q_r / r overflows before.  With S that sum and F = 2^(base off the record - base
 // of the row), r = S F / s and p_v = power F / s, power about the base off the
 // record, so the gradient there is power ((sum_k q_k + q_r) F / s - q_r / S).
-// Logarithms are taken as (z - m) / tau less that of the sum about the row's largest
-// m (and r's with the largest off the record for z): c z overflows before they do.
+// Logarithms of probabilities are taken as (z - m) / tau less that of the sum about
+// the row's largest m, since c z overflows before they do; ln r likewise, from the
+// largest off the record, where fp32 does not hold r.
 // Where every class off the record is masked, q_r = 0.
 //
 // Bound by reading the logits and writing the gradient once.
@@ -86,8 +87,9 @@ struct Bases {
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
 
 // Rows too long for the shared memory of a cluster: a block per row, which
-// streams it from memory once for the statistics and a second time, most of it
-// from L2, for the gradient (8192 x 131072 bf16: 907 us, the tile kernel 881).
+// streams it once for the statistics and a second time for the gradient, from
+// memory again where the rows in flight exceed L2 (8192 x 131072 bf16, which go
+// by the tile kernel: 915 us here, 868 there).
 // The classes on the record are marked in a bit map by place, and the pieces that
 // hold any in a mask per thread; the marked ones are taken out of their sums.
 template <typename T, bool TWO>
@@ -957,9 +959,9 @@ distill_narrow_kernel(const T* Z, T* dZ, Distill a) {
 // Blocks per row.  Slices up to 100 KB (two blocks on an SM) beat more and
 // shorter ones: what a block does besides its bytes takes 5 us or more, and the
 // more so the more blocks exchange statistics (bf16, 2^30 logits in all: rows of
-// 64 KB in one block 758 us, of 128 KB in two 835, of 256 KB in four 895; the
-// 256 KB rows in eight slices of 32 KB 1115 us; 509 fp32 rows of 200 KB in two
-// 51.7 us, in four 55.9 us).
+// 64 KB in one block 740 us, of 128 KB in two 813, of 256 KB in four 868; the
+// 256 KB rows in eight slices of 32 KB 927 us; 509 fp32 rows of 200 KB are too
+// few waves for it to matter: in two 53.6 us, in four 52.4 us).
 constexpr int kTileFit = 100 * 1024, kTileMost = 208 * 1024, kTileLeast = 8 * 1024;
 
 // Shared memory of the kernels for rows of few classes and for rows streamed twice.
@@ -978,8 +980,8 @@ int launch_distill(const T* z, T* dz, const Distill& a, cudaStream_t stream) {
         e = launch_rows(distill_narrow_kernel<T, TWO>, (a.T + kNarrowWarps - 1) / kNarrowWarps, 1, kNarrowWarps * 32,
                         narrow_bytes(a.V, a.K), narrow_bytes(kNarrow, kMaxTop), stream, z, dz, a);
     } else if (blocks > 0) {
-        // (bf16: 9024 rows of 6644 classes 57.2 us in 64 threads, 63.1 in 128,
-        // 96.7 in 256; 8192 rows of 16384 classes 100.4, 97.7 and 114.8 us)
+        // (bf16: 9024 rows of 6644 classes 55.6 us in 64 threads, 66.5 in 128,
+        // 100 in 256; 8192 rows of 16384 classes 103, 102 and 111 us)
         const long long bytes = slice_bytes(a.V, sizeof(T), blocks);
         auto kern = a.K <= 64 && bytes <= 16 * 1024    ? distill_tile_kernel<T, TWO, 64>
                     : a.K <= 128 && bytes <= 40 * 1024 ? distill_tile_kernel<T, TWO, 128>

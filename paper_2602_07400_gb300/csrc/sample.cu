@@ -877,7 +877,8 @@ struct SampleRowShared {
 //
 // Many rows, of any length: a block per row.  It streams the row once from
 // memory for the largest and for the maxima of 2048 groups; what else a row
-// needs streams it again from L2:
+// needs streams it again, in part from L2 (four rows of 256 KB on every SM exceed
+// it: 1024 x 131072 bf16 under mixed settings read 405 MB of DRAM for 268 MB):
 //   top_k up to 1024 (and greedy rows): the groups that reach the bound are
 //     read again, and their entries cut and drawn among as a list;
 //   top_p alone: the mass of the row; then its bins of 1/64 octave down to
@@ -1409,9 +1410,9 @@ int launch_sample(const T* x, long long T_, int V, long long ld, const Settings&
         e = launch_rows(kern, (T_ + kNarrowWarps - 1) / kNarrowWarps, 1, kNarrowWarps * 32, 0, 0, stream, x, ld, V, T_, set, out);
     } else {
         // where a cluster per row is faster (50001 fp32 and 131072 bf16 classes:
-        // top_k at 60 rows 21 and 21.6 against 18.1 and 19.9 us in a block each,
-        // top_p at 100 rows 51.7 and 93 against 63 and 125 us, at 250 rows 115
-        // and 193 against 74 and 151)
+        // top_k at 60 rows 21.4 and 21.6 against 17.1 and 18.7 us in a block each,
+        // top_p at 100 rows 50.4 and 89 against 58 and 112 us, at 250 rows 111
+        // and 180 against 68 and 131)
         const long long few = set.top_p ? sm_count() : sm_count() / 4;
         const int blocks = T_ <= few ? blocks_per_row(T_, V, sizeof(T), kTileFit, kTileMost, kTileLeast) : 0;
         if (blocks > 1) {

@@ -137,10 +137,11 @@ struct TopRowShared {
 
 // Many rows, of any length: a block per row, which streams it once, keeping
 // eight running maxima per thread.  Joined by twos, and in two parts each, the
-// 2048 maxima of the row's groups of pieces give a bound that K logits reach, and the groups whose maximum
-// reaches it are read again (a sixteenth of a row of 2^17 bf16 at K = 128), from
-// L2, for the entries: little more than K for logits in no particular order.  A
-// row on which more than 2048 pass is selected from memory.  Taking entries
+// 2048 maxima of the row's groups of pieces give a bound that K logits reach, and
+// the groups whose maximum reaches it are read again (a sixteenth of a row of 2^17
+// bf16 at K = 128; in part from L2: DRAM reads are 1.16 of the logits) for the
+// entries: little more than K for logits in no particular order.  A row on which
+// more than 2048 pass is selected from memory.  Taking entries
 // while streaming, under a bound from the row's beginning that is raised as it
 // goes, met four times as many and took 554 us where this takes 221 us
 // (4096 x 131072 bf16).
@@ -528,9 +529,9 @@ top_narrow_kernel(const T* __restrict__ X, long long ld, int V, long long rows, 
 }
 
 // Few rows go by clusters, so that several SMs share one (16 rows of 2^17 bf16
-// 9.7 against 17.2 us in a block each, 64 rows 13.5 against 17.6); from half a
-// row per SM on a block per row is faster (100 rows 17.6 against 20.3 us, 4096
-// rows 221 against 490).  Slices of at most kTileFit bytes leave room for three
+// 10.1 against 16.2 us in a block each, 64 rows 13.5 against 16.5); from half a
+// row per SM on a block per row is faster (100 rows 16.6 against 20.6 us, 4096
+// rows 220 against 510).  Slices of at most kTileFit bytes leave room for three
 // blocks on an SM.
 constexpr int kTileFit = 56 * 1024, kTileMost = 200 * 1024, kTileLeast = 8 * 1024;
 
