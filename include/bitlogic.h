@@ -59,7 +59,7 @@ typedef enum {
     BITLOGIC_ERR_TOO_LARGE = -10, /* sizes beyond bitlogic_head_loss_noalloc's fixed scratch */
     BITLOGIC_ERR_HYPER = -11,     /* optimizer or loss hyperparameter out of range */
     BITLOGIC_ERR_NODE = -12,      /* unknown node form */
-    BITLOGIC_ERR_DTYPE = -13      /* logit type unknown, or not taken by the call */
+    BITLOGIC_ERR_DTYPE = -13      /* element type unknown, or not taken by the call */
 } bitlogic_status_t;
 
 /* Node forms of the LightLUT parameterization (§2 "Gradient-based LUT
@@ -651,6 +651,160 @@ int bitlogic_distill_loss(const void* Z, int32_t dtype, int64_t T, int32_t V, in
 int bitlogic_sample_logits(const void* X, int32_t dtype, int64_t T, int32_t V, int64_t ld, const float* u,
                            const float* temperature, const int32_t* top_k, const float* top_p,
                            const float* min_p, int32_t* token, float* logprob, cudaStream_t stream);
+
+/* The classes that a draw keeps of every row under the settings of
+ * bitlogic_sample_logits, as bitlogic_verify_drafts reads them: the last one in the
+ * order (value descending, class ascending), so that the classes kept are those
+ * with X[t][v] > floor[t], and those equal to it up to class last[t].
+ *   X, dtype, T, V, ld, temperature, top_k, top_p, min_p  as there
+ *   floor  device fp32 [T], last device int32 [T]: -inf and -1 (all classes) where
+ *          nothing is set to cut the row (top_k <= 0 or >= V, top_p >= 1 or NaN,
+ *          min_p not > 0), and where no class ranks; a temperature that is not > 0,
+ *          and a row with +inf, count as top_k = 1
+ * Returns BITLOGIC_ERR_NULL, BITLOGIC_ERR_SHAPE, BITLOGIC_ERR_DTYPE,
+ * BITLOGIC_ERR_ALIGN, BITLOGIC_ERR_CUDA. */
+int bitlogic_support_logits(const void* X, int32_t dtype, int64_t T, int32_t V, int64_t ld,
+                            const float* temperature, const int32_t* top_k, const float* top_p,
+                            const float* min_p, float* floor, int32_t* last, cudaStream_t stream);
+
+/* Drafted classes accepted or rejected by a target's logits and given random
+ * numbers, and the class that follows the accepted ones: what goes out is
+ * distributed as the target's own draws, whatever the drafts are.
+ * S sequences; sequence s has the drafts first[s] .. first[s+1] - 1 (none to any
+ * number) of D in all, and one target row more than drafts, the rows
+ * first[s] + s .. first[s+1] + s: row first[s] + s + i holds the logits from
+ * which draft i would be drawn, the last one those behind the last draft.  With
+ * p the softmax of a target row's kept logits over its temperature, and q that
+ * of a draft's row, draft i is accepted iff
+ *   u[first[s] + i] q(token) < p(token),   q(token) = exp(draft_logprob)
+ * and accepted[s] counts the drafts before the first that is not.  next_token[s]
+ * is drawn with draw_u[s] from the row behind the accepted: all drafts accepted,
+ * as bitlogic_sample_logits draws from its kept logits; a draft refused, from
+ *   w_v = 2^40 max(0, p_v - q_v) rounded to a whole number, p_v = e_v / sum e,
+ * q_v likewise, both rounded to fp32: the first class whose weights up to and
+ * including its own exceed floor(draw_u sum) (e and the sums as in
+ * bitlogic_sample_logits, so the draw does not depend on the batch; where no
+ * weight is left, from p).
+ *   target       device [S + D] rows of V classes, as X above (any dtype)
+ *   temperature  device fp32 [S + D] or NULL (1); not > 0: p is all on the first
+ *                of the largest
+ *   floor, last  device fp32 and int32 [S + D], both or neither: the classes kept
+ *                (bitlogic_support_logits); NULL: all
+ *   first        device int32 [S + 1], not falling, first[0] >= 0, first[S] <= D.
+ *                Drafts and rows behind first[S] are not read, so that a batch
+ *                may be shorter than its buffers.  A sequence whose places break
+ *                this raises the device flag: accepted 0, next_token -1,
+ *                logprob -inf
+ *   token        device int32 [D]; a class outside [0, V) raises the device flag
+ *                and is refused
+ *   u, draw_u    device fp32 [D] and [S], in [0, 1) (clamped; NaN reads 0; 24
+ *                bits after the point count).  The numbers of the tests and of
+ *                the draw are independent
+ *   draft        device [D] rows of V classes, of draft_dtype, row i that from
+ *                which draft i was drawn, or NULL: drafts that were not drawn (q
+ *                is all on the token)
+ *   draft_logprob      device fp32 [D], the draw's own logarithm of q(token);
+ *                      with draft, and only then
+ *   draft_temperature, draft_floor, draft_last  the draft's settings, as above
+ *                      (a temperature not > 0: q is all on the token)
+ *   accepted     device int32 [S];  next_token device int32 [S], -1 when the
+ *                row's kept logits are all -inf or NaN
+ *   logprob      device fp32 [S] or NULL: ln p(next_token)
+ *   workspace    device, 16-byte aligned, bitlogic_verify_drafts_workspace(S, D, V)
+ *                bytes (0 for few classes: NULL); used on `stream` until the call's
+ *                work is done, so calls that may run at once, two captured graphs
+ *                among them, take one each
+ * A target row with +inf has p all on the first of those; a draft row with +inf
+ * has q all on the token.  Returns BITLOGIC_ERR_NULL (also for one of a pair
+ * without the other), BITLOGIC_ERR_SHAPE, BITLOGIC_ERR_DTYPE, BITLOGIC_ERR_ALIGN,
+ * BITLOGIC_ERR_WORKSPACE, BITLOGIC_ERR_CUDA. */
+size_t bitlogic_verify_drafts_workspace(int64_t S, int64_t D, int32_t V);
+int bitlogic_verify_drafts(const void* target, int32_t dtype, int64_t S, int64_t D, int32_t V, int64_t ld,
+                           const float* temperature, const float* floor, const int32_t* last, const int32_t* first,
+                           const int32_t* token, const float* u, const float* draw_u, const void* draft,
+                           int32_t draft_dtype, int64_t draft_ld, const float* draft_logprob,
+                           const float* draft_temperature, const float* draft_floor, const int32_t* draft_last,
+                           int32_t* accepted, int32_t* next_token, float* logprob, void* workspace,
+                           size_t workspace_bytes, cudaStream_t stream);
+
+/* Dropout from a counter-based generator, with the addition of a residual:
+ *   out[r][c] = (number >= round(p 2^32) ? X[r][c] / (1 - p) : 0) + residual[r][c]
+ * in fp32, rounded once.  Nothing is stored: the gradient is the same call on the
+ * output's gradient, without the residual.  `number`, 32 bits, of element
+ * i = r C + c comes from Philox4x32-10 (Salmon, Moraes, Dror and Shaw, 2011)
+ * under the key `seed`: half-word i mod 8 (low half of word 0, high half of word
+ * 0, low half of word 1, ...) of the counter (i / 8 low, i / 8 high, step,
+ * 2 site) is its high half, that of (i / 8 low, i / 8 high, step, 2 site + 1) its
+ * low half.  So a value's fate depends on seed, step, site and i, not on strides,
+ * types or how the work is split.
+ *   X, residual, out  device [R] rows of C values of dtype (BITLOGIC_F32,
+ *            BITLOGIC_BF16, BITLOGIC_F16), rows ld* >= C values apart, aligned to
+ *            the value; residual may be NULL; out may be X or residual with the
+ *            same stride, and overlap them in no other way
+ *   counter  device int64 [2]: seed, and step (its low 32 bits count).  Read by the
+ *            kernel, so a captured graph drops anew when the caller advances step
+ *   p        in [0, 1), below 1 - 2^-33; site >= 0: a further number for each place
+ *            of a step that drops
+ * A dropped value counts 0 whatever it holds.  R or C of 0 is a no-op.
+ * Returns BITLOGIC_ERR_NULL, BITLOGIC_ERR_SHAPE (R C or R ld past 2^40),
+ * BITLOGIC_ERR_DTYPE, BITLOGIC_ERR_ALIGN, BITLOGIC_ERR_HYPER, BITLOGIC_ERR_CUDA. */
+int bitlogic_dropout(const void* X, int32_t dtype, int64_t R, int64_t C, int64_t ldx, const void* residual,
+                     int64_t ldr, void* out, int64_t ldo, const int64_t* counter, double p, int32_t site,
+                     cudaStream_t stream);
+
+/* Rows over their root mean square, in 8 bits: hidden states of another model as
+ * the uint8 samples that the encoder reads, or as e4m3 with scales.
+ *   h = X + residual,  y_j = h_j weight_j / sqrt(mean_j h_j^2 + eps)   in fp32
+ *   BITLOGIC_CODES  out_j = 128 + y_j / s rounded to a whole number, in [1, 255]
+ *                   (NaN: 128)
+ *   BITLOGIC_E4M3   out_j = y_j / s rounded to e4m3, at most 448 (NaN: NaN)
+ * (ties to even) with s = fixed_scale where that is > 0, else the largest |y| of
+ * the row, or of every `group` columns, over 127 (codes) or 448 (e4m3), which goes
+ * to scale[t][j / group].  Where that largest |y| is below 2^-100 it counts as 0:
+ * scale 0, out at zero.  A NaN shows in the scale.
+ *   X, residual, total  device [T] rows of d values of dtype (BITLOGIC_F32, _BF16,
+ *            _F16), ld* >= d values apart, aligned to the value; residual may be
+ *            NULL; total or NULL: h rounded to dtype; it may be X or residual with
+ *            the same stride, and overlap them in no other way
+ *   weight   device [d] of weight_dtype (dtype or BITLOGIC_F32), or NULL: 1
+ *   out      device bytes [T] rows of d, ldo >= d apart
+ *   scale    device fp32 [T][ceil(d / group)] ([T] for group 0); not used, and may
+ *            be NULL, with a fixed scale
+ *   group    0: the row; or 16, 32, 64, 128 or 256
+ * 1 <= d <= 32768; T == 0 is a no-op.  Returns BITLOGIC_ERR_NULL,
+ * BITLOGIC_ERR_SHAPE, BITLOGIC_ERR_DTYPE, BITLOGIC_ERR_ALIGN, BITLOGIC_ERR_HYPER
+ * (eps not positive and finite; fixed_scale negative, not finite, or its inverse
+ * past fp32), BITLOGIC_ERR_CUDA. */
+typedef enum {
+    BITLOGIC_CODES = 0,
+    BITLOGIC_E4M3 = 1
+} bitlogic_bytes_t;
+int bitlogic_norm_bytes(const void* X, int32_t dtype, int64_t T, int32_t d, int64_t ldx, const void* residual,
+                        int64_t ldr, void* total, int64_t ldt, const void* weight, int32_t weight_dtype, float eps,
+                        int32_t form, void* out, int64_t ldo, float* scale, int32_t group, float fixed_scale,
+                        cudaStream_t stream);
+
+/* Gradient of the norm above, the rounding to 8 bits passed as if it were not
+ * there: with H the rows that were normed (its `total`) and dY the gradient of y,
+ *   g = dY weight,  xh = H r,  r = 1 / sqrt(mean H^2 + eps)
+ *   dX = r (g - xh mean(g xh)) + residual_grad,   dweight = sum_t dY xh
+ * dX is the gradient of X and of the residual alike; residual_grad (or NULL) is
+ * what reaches H by its own way.
+ *   dY, H, residual_grad, dX  device [T] rows of d values of dtype, as above; dX may
+ *            be any of the three with the same stride, and overlap them in no
+ *            other way
+ *   dweight  device fp32 [d] or NULL; sums run in a fixed order.  T == 0: zeros
+ *   workspace  device, 16-byte aligned, bitlogic_norm_backward_workspace(T, d) bytes
+ *            (NULL without dweight); calls that may run at once, two captured
+ *            graphs among them, take one each
+ * Returns BITLOGIC_ERR_NULL, BITLOGIC_ERR_SHAPE, BITLOGIC_ERR_DTYPE,
+ * BITLOGIC_ERR_ALIGN, BITLOGIC_ERR_HYPER, BITLOGIC_ERR_WORKSPACE,
+ * BITLOGIC_ERR_CUDA. */
+size_t bitlogic_norm_backward_workspace(int64_t T, int32_t d);
+int bitlogic_norm_backward(const void* dY, int32_t dtype, int64_t T, int32_t d, int64_t ldy, const void* H, int64_t ldh,
+                           const void* weight, int32_t weight_dtype, const void* residual_grad, int64_t ldr, float eps,
+                           void* dX, int64_t ldx, float* dweight, void* workspace, size_t workspace_bytes,
+                           cudaStream_t stream);
 
 /* Table discretization (§3: every surrogate discretizes to a 2^n-entry
  * truth table; App. C.1 extracts it once per layer): bit a of table[j] is 1

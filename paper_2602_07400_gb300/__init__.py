@@ -34,6 +34,8 @@ __all__ = [
     "bitlogic_lut_forward_codes", "bitlogic_codes_decode", "bitlogic_lut_forward_coded",
     "bitlogic_lut_backward_coded", "bitlogic_corner_reduce", "code_bytes",
     "bitlogic_top_logits", "bitlogic_distill_loss", "bitlogic_sample_logits", "LOGIT_TYPES", "MAX_TOP",
+    "bitlogic_support_logits", "bitlogic_verify_drafts", "bitlogic_verify_drafts_workspace", "bitlogic_dropout",
+    "bitlogic_norm_bytes", "bitlogic_norm_backward", "bitlogic_norm_backward_workspace", "ROW_TYPES", "BYTE_TYPES",
     "bitlogic_head_loss", "bitlogic_binarize_tables", "bitlogic_pack_bits",
     "bitlogic_hard_forward", "bitlogic_build_csr", "bitlogic_csr_positions", "bitlogic_degree_order",
     "bitlogic_device_error",
@@ -54,6 +56,11 @@ NODE_FORMS = {"soft": 0, "st": 1}
 # types of a matrix of logits (bitlogic_dtype_t); int32 counts are taken by
 # bitlogic_top_logits and bitlogic_sample_logits
 LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.int32: 3}
+
+# types of rows of activations (bitlogic_dtype_t without the counts), and the
+# 8-bit forms of a norm's output (bitlogic_bytes_t)
+ROW_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+BYTE_TYPES = {torch.uint8: 0, torch.float8_e4m3fn: 1}
 
 # entries of a teacher's record per row, at most
 MAX_TOP = 256
@@ -132,6 +139,16 @@ _SIGS = {
     "bitlogic_distill_loss": ([_P, _I32, _I64, _I32, _I64, _P, _P, _I32, _P, _P, _P, _F32, _F32, _F32, _P, _P, _P,
                                _I64, _I64, _F32, _P], ctypes.c_int),
     "bitlogic_sample_logits": ([_P, _I32, _I64, _I32, _I64, _P, _P, _P, _P, _P, _P, _P, _P], ctypes.c_int),
+    "bitlogic_support_logits": ([_P, _I32, _I64, _I32, _I64, _P, _P, _P, _P, _P, _P, _P], ctypes.c_int),
+    "bitlogic_verify_drafts_workspace": ([_I64, _I64, _I32], _SZ),
+    "bitlogic_verify_drafts": ([_P, _I32, _I64, _I64, _I32, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _I32, _I64, _P, _P,
+                                _P, _P, _P, _P, _P, _P, _SZ, _P], ctypes.c_int),
+    "bitlogic_dropout": ([_P, _I32, _I64, _I64, _I64, _P, _I64, _P, _I64, _P, ctypes.c_double, _I32, _P], ctypes.c_int),
+    "bitlogic_norm_bytes": ([_P, _I32, _I64, _I32, _I64, _P, _I64, _P, _I64, _P, _I32, _F32, _I32, _P, _I64, _P, _I32,
+                             _F32, _P], ctypes.c_int),
+    "bitlogic_norm_backward_workspace": ([_I64, _I32], _SZ),
+    "bitlogic_norm_backward": ([_P, _I32, _I64, _I32, _I64, _P, _I64, _P, _I32, _P, _I64, _F32, _P, _I64, _P, _P, _SZ, _P],
+                               ctypes.c_int),
     "bitlogic_binarize_tables": ([_P, _I32, _I32, _P, _P], ctypes.c_int),
     "bitlogic_pack_bits": ([_P, _I64, _I32, _P, _I32, _P, _P], ctypes.c_int),
     "bitlogic_hard_forward": ([_P, _I32, _I64, _P, _P, _I32, _I32, _P, _I32, _P, _P, _P],
@@ -962,6 +979,209 @@ def bitlogic_sample_logits(logits: torch.Tensor, u: torch.Tensor, token: torch.T
     _check("bitlogic_sample_logits", load().bitlogic_sample_logits(
         _ptr(logits), code, T, V, ld, _ptr(u), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
         _ptr(token), _ptr(logprob), _stream(stream)))
+
+
+def bitlogic_support_logits(logits: torch.Tensor, floor: torch.Tensor, last: torch.Tensor,
+                            temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+                            top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, stream=None):
+    """The classes of every row of ``logits`` [T, V] that bitlogic_sample_logits
+    draws among under the same settings: those above floor fp32 [T], and those
+    equal to it up to class last int32 [T] (-inf and -1: all)."""
+    code, T, V, ld = _logits(logits, "logits")
+    _need(floor, "floor", torch.float32, (T,))
+    _need(last, "last", torch.int32, (T,))
+    _optional(temperature, "temperature", torch.float32, (T,))
+    _optional(top_k, "top_k", torch.int32, (T,))
+    _optional(top_p, "top_p", torch.float32, (T,))
+    _optional(min_p, "min_p", torch.float32, (T,))
+    _check("bitlogic_support_logits", load().bitlogic_support_logits(
+        _ptr(logits), code, T, V, ld, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(floor), _ptr(last),
+        _stream(stream)))
+
+
+def _optional(t, name: str, dtype: torch.dtype, shape: Tuple[int, ...]):
+    if t is not None:
+        _need(t, name, dtype, shape)
+
+
+def _workspace(t: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous():
+        raise TypeError("workspace must be a contiguous uint8 CUDA tensor")
+    return t.data_ptr(), t.numel()
+
+
+def bitlogic_verify_drafts_workspace(S: int, D: int, V: int) -> int:
+    """Bytes of a workspace for S sequences with D drafts in all over V classes
+    (0: none is needed)."""
+    return int(load().bitlogic_verify_drafts_workspace(S, D, V))
+
+
+def bitlogic_verify_drafts(target: torch.Tensor, first: torch.Tensor, token: torch.Tensor, u: torch.Tensor,
+                           draw_u: torch.Tensor, accepted: torch.Tensor, next_token: torch.Tensor,
+                           workspace: Optional[torch.Tensor] = None, logprob: Optional[torch.Tensor] = None,
+                           draft: Optional[torch.Tensor] = None, draft_logprob: Optional[torch.Tensor] = None,
+                           temperature: Optional[torch.Tensor] = None, floor: Optional[torch.Tensor] = None,
+                           last: Optional[torch.Tensor] = None, draft_temperature: Optional[torch.Tensor] = None,
+                           draft_floor: Optional[torch.Tensor] = None, draft_last: Optional[torch.Tensor] = None,
+                           stream=None):
+    """Accepts or refuses the drafted classes token int32 [D] of S sequences by
+    the logits ``target`` [S + D, V] and the random numbers u fp32 [D], and draws
+    the class behind the accepted ones with draw_u fp32 [S]: accepted int32 [S],
+    next_token int32 [S], and its logarithm logprob fp32 [S].  Sequence s has the
+    drafts first[s] .. first[s + 1] - 1 (first int32 [S + 1]) and the target rows
+    first[s] + s .. first[s + 1] + s.  ``draft`` [D, V] are the logits that the
+    drafts were drawn from and draft_logprob fp32 [D] their draws' logarithms;
+    without them the drafts count as certain.  Per row of either, each optional:
+    temperature fp32, and floor fp32 with last int32 as bitlogic_support_logits
+    gives them."""
+    code, R, V, ld = _logits(target, "target")
+    D = token.shape[0] if isinstance(token, torch.Tensor) and token.dim() == 1 else 0
+    S = R - D
+    if S < 0:
+        raise ValueError(f"target: expected a row per draft and one per sequence, got {R} rows for {D} drafts")
+    _need(first, "first", torch.int32, (S + 1,))
+    _need(token, "token", torch.int32, (D,))
+    _need(u, "u", torch.float32, (D,))
+    _need(draw_u, "draw_u", torch.float32, (S,))
+    _need(accepted, "accepted", torch.int32, (S,))
+    _need(next_token, "next_token", torch.int32, (S,))
+    _optional(logprob, "logprob", torch.float32, (S,))
+    _optional(temperature, "temperature", torch.float32, (R,))
+    _optional(floor, "floor", torch.float32, (R,))
+    _optional(last, "last", torch.int32, (R,))
+    _optional(draft_logprob, "draft_logprob", torch.float32, (D,))
+    _optional(draft_temperature, "draft_temperature", torch.float32, (D,))
+    _optional(draft_floor, "draft_floor", torch.float32, (D,))
+    _optional(draft_last, "draft_last", torch.int32, (D,))
+    dcode, dld = 0, V
+    if draft is not None:
+        dcode, DR, DV, dld = _logits(draft, "draft")
+        if (DR, DV) != (D, V):
+            raise ValueError(f"draft: expected shape {(D, V)}, got {(DR, DV)}")
+    ws, ws_bytes = _workspace(workspace)
+    _check("bitlogic_verify_drafts", load().bitlogic_verify_drafts(
+        _ptr(target), code, S, D, V, ld, _ptr(temperature), _ptr(floor), _ptr(last), _ptr(first), _ptr(token), _ptr(u),
+        _ptr(draw_u), _ptr(draft), dcode, dld, _ptr(draft_logprob), _ptr(draft_temperature), _ptr(draft_floor),
+        _ptr(draft_last), _ptr(accepted), _ptr(next_token), _ptr(logprob), ws, ws_bytes, _stream(stream)))
+
+
+def _rows(x: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> Tuple[int, int]:
+    """Type code and row stride of a matrix of activations whose columns are
+    adjacent (rows may lie apart), of the type and shape of ``like``."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    code = ROW_TYPES.get(x.dtype)
+    if code is None:
+        raise TypeError(f"{name}: expected one of {[str(t) for t in ROW_TYPES]}, got {x.dtype}")
+    if like is not None and x.dtype != like.dtype:
+        raise TypeError(f"{name}: expected {like.dtype}, got {x.dtype}")
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be on a CUDA device")
+    if x.dim() != 2:
+        raise ValueError(f"{name}: expected [rows, columns], got {x.dim()} dimensions")
+    if like is not None and x.shape != like.shape:
+        raise ValueError(f"{name}: expected shape {tuple(like.shape)}, got {tuple(x.shape)}")
+    return code, _row_stride(x, name)
+
+
+def _row_stride(x: torch.Tensor, name: str) -> int:
+    R, C = x.shape
+    ld, inc = x.stride()
+    if C > 1 and R > 0 and inc != 1:
+        raise ValueError(f"{name}: the columns of a row must be adjacent (stride 1)")
+    return max(ld, C) if R <= 1 else ld
+
+
+def bitlogic_dropout(x: torch.Tensor, out: torch.Tensor, counter: torch.Tensor, p: float, site: int = 0,
+                     residual: Optional[torch.Tensor] = None, stream=None):
+    """``out`` = ``x`` [R, C] (fp32, bf16 or fp16) with every value dropped with
+    probability p and the others divided by 1 - p, plus ``residual``.  counter
+    int64 [2] on the device holds seed and step; with the same counter, site and
+    p the gradient of x is the same call on the gradient of out.  ``out`` may be
+    x or residual."""
+    code, ldx = _rows(x, "x")
+    _, ldo = _rows(out, "out", x)
+    ldr = x.shape[1]
+    if residual is not None:
+        _, ldr = _rows(residual, "residual", x)
+    _need(counter, "counter", torch.int64, (2,))
+    R, C = x.shape
+    _check("bitlogic_dropout", load().bitlogic_dropout(
+        _ptr(x), code, R, C, ldx, _ptr(residual), ldr, _ptr(out), ldo, _ptr(counter), float(p), int(site),
+        _stream(stream)))
+
+
+def _norm_weight(weight: Optional[torch.Tensor], x: torch.Tensor) -> int:
+    if weight is None:
+        return ROW_TYPES[x.dtype]
+    if not isinstance(weight, torch.Tensor):
+        raise TypeError("weight must be a torch.Tensor")
+    _need(weight, "weight", torch.float32 if weight.dtype == torch.float32 else x.dtype, (x.shape[1],))
+    return ROW_TYPES[weight.dtype]
+
+
+def bitlogic_norm_bytes(x: torch.Tensor, out: torch.Tensor, scale: Optional[torch.Tensor] = None,
+                        weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                        total: Optional[torch.Tensor] = None, group: int = 0, fixed_scale: float = 0.0,
+                        eps: float = 1e-6, stream=None):
+    """Rows of ``x`` + ``residual`` [T, d] (fp32, bf16 or fp16) over their root
+    mean square, times ``weight`` [d], in 8 bits into ``out`` [T, d]: uint8 codes
+    128 + y / scale, as the encoder reads samples, or float8_e4m3fn.  Scales go to
+    scale fp32 [T, groups] (a group: ``group`` columns, 0 the row) unless
+    ``fixed_scale`` is given; the sum x + residual goes to ``total`` (it may be x
+    or residual)."""
+    code, ldx = _rows(x, "x")
+    T, d = x.shape
+    ldr = ldt = d
+    if residual is not None:
+        _, ldr = _rows(residual, "residual", x)
+    if total is not None:
+        _, ldt = _rows(total, "total", x)
+    wcode = _norm_weight(weight, x)
+    if not isinstance(out, torch.Tensor):
+        raise TypeError("out must be a torch.Tensor")
+    form = BYTE_TYPES.get(out.dtype)
+    if form is None:
+        raise TypeError(f"out: expected one of {[str(t) for t in BYTE_TYPES]}, got {out.dtype}")
+    if not out.is_cuda:
+        raise ValueError("out must be on a CUDA device")
+    if out.shape != x.shape:
+        raise ValueError(f"out: expected shape {tuple(x.shape)}, got {tuple(out.shape)}")
+    group = int(group)
+    if scale is not None:
+        _need(scale, "scale", torch.float32, (T, -(-d // group) if group > 0 else 1))
+    _check("bitlogic_norm_bytes", load().bitlogic_norm_bytes(
+        _ptr(x), code, T, d, ldx, _ptr(residual), ldr, _ptr(total), ldt, _ptr(weight), wcode, float(eps), form, _ptr(out),
+        _row_stride(out, "out"), _ptr(scale), group, float(fixed_scale), _stream(stream)))
+
+
+def bitlogic_norm_backward_workspace(T: int, d: int) -> int:
+    """Bytes of a workspace for the weight's gradient."""
+    return int(load().bitlogic_norm_backward_workspace(T, d))
+
+
+def bitlogic_norm_backward(dy: torch.Tensor, h: torch.Tensor, dx: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                           dweight: Optional[torch.Tensor] = None, residual_grad: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, eps: float = 1e-6, stream=None):
+    """Gradient of bitlogic_norm_bytes at the rows ``h`` (its total) from ``dy``
+    [T, d], the rounding to 8 bits passed as if it were not there: into ``dx`` that
+    of x and of the residual alike, plus ``residual_grad``, and into dweight fp32
+    [d] that of the weight.  ``dx`` may be dy, h or residual_grad."""
+    code, ldy = _rows(dy, "dy")
+    T, d = dy.shape
+    _, ldh = _rows(h, "h", dy)
+    _, ldx = _rows(dx, "dx", dy)
+    ldr = d
+    if residual_grad is not None:
+        _, ldr = _rows(residual_grad, "residual_grad", dy)
+    wcode = _norm_weight(weight, dy)
+    _optional(dweight, "dweight", torch.float32, (d,))
+    ws, ws_bytes = _workspace(workspace)
+    _check("bitlogic_norm_backward", load().bitlogic_norm_backward(
+        _ptr(dy), code, T, d, ldy, _ptr(h), ldh, _ptr(weight), wcode, _ptr(residual_grad), ldr, float(eps), _ptr(dx), ldx,
+        _ptr(dweight), ws, ws_bytes, _stream(stream)))
 
 
 def bitlogic_binarize_tables(theta: torch.Tensor, table: torch.Tensor, stream=None):

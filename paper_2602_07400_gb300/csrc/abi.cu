@@ -36,6 +36,7 @@ extern "C" int bitlogic_internal_index_error_lut_bytes(cudaStream_t);
 extern "C" int bitlogic_internal_index_error_lut_codes(cudaStream_t);
 extern "C" int bitlogic_internal_index_error_lut_packed(cudaStream_t);
 extern "C" int bitlogic_internal_index_error_distill(cudaStream_t);
+extern "C" int bitlogic_internal_index_error_verify(cudaStream_t);
 
 extern "C" const char* bitlogic_status_string(int code) {
     switch (code) {
@@ -52,7 +53,7 @@ extern "C" const char* bitlogic_status_string(int code) {
         case BITLOGIC_ERR_TOO_LARGE: return "sizes exceed the fixed scratch of the allocation-free entry point";
         case BITLOGIC_ERR_HYPER: return "optimizer or loss hyperparameter out of range";
         case BITLOGIC_ERR_NODE: return "unknown node form";
-        case BITLOGIC_ERR_DTYPE: return "logit type unknown or not taken by the call";
+        case BITLOGIC_ERR_DTYPE: return "element type unknown or not taken by the call";
         default: return "unknown status";
     }
 }
@@ -106,7 +107,7 @@ extern "C" int bitlogic_degree_order(const int32_t* off_host, int32_t n, int32_t
 
 extern "C" int bitlogic_device_error(cudaStream_t stream) {
     int worst = BITLOGIC_OK;
-    const int r[11] = {bitlogic_internal_index_error_lut_soft(stream),
+    const int r[12] = {bitlogic_internal_index_error_lut_soft(stream),
                       bitlogic_internal_index_error_head(stream),
                       bitlogic_internal_index_error_encode(stream),
                       bitlogic_internal_index_error_hard(stream),
@@ -116,7 +117,8 @@ extern "C" int bitlogic_device_error(cudaStream_t stream) {
                       bitlogic_internal_index_error_lut_bytes(stream),
                       bitlogic_internal_index_error_lut_codes(stream),
                        bitlogic_internal_index_error_lut_packed(stream),
-                      bitlogic_internal_index_error_distill(stream)};
+                      bitlogic_internal_index_error_distill(stream),
+                      bitlogic_internal_index_error_verify(stream)};
     for (int v : r) {
         if (v == BITLOGIC_ERR_CUDA) return v;
         if (v != BITLOGIC_OK) worst = v;

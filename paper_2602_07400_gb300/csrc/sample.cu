@@ -11,9 +11,17 @@
 // The weights are whole numbers, so every sum is exact: the draw depends on
 // the row and its settings alone, not on the batch, the split of a row over
 // threads or the order of additions.  Bound by reading the logits once.
+//
+// The same kernels give a row's support, the last class kept in the order (value
+// descending, class ascending) (kSupport): they stop where the cut is known.
+// support.cu compiles this file for that entry point, so that the two compile at
+// once.
 #include <cfloat>
 
 #include "row_tile.cuh"
+#include "weights.cuh"
+
+#pragma nv_diag_suppress 128   // loops behind a support's return are not reached
 
 namespace bitlogic {
 namespace {
@@ -31,7 +39,24 @@ struct Settings {
 struct Draw {
     int* token;
     float* logprob;
+    float* floor;   // of a support: the logit of the last class kept
+    int* last;      // and the class
 };
+
+template <bool kSupport>
+__device__ __forceinline__ void put_nothing(const Draw& out, long long row) {
+    if constexpr (kSupport) {
+        out.floor[row] = BITLOGIC_NEG_INF;
+        out.last[row] = -1;
+    } else {
+        out.token[row] = -1;
+        if (out.logprob) out.logprob[row] = BITLOGIC_NEG_INF;
+    }
+}
+__device__ __forceinline__ void put_support(const Draw& out, long long row, float floor, int last) {
+    out.floor[row] = floor;
+    out.last[row] = last;
+}
 
 // A row's settings as the draw uses them.
 struct RowSettings {
@@ -46,7 +71,7 @@ struct RowSettings {
         p = p < 1.0f ? fmaxf(p, 0.f) : 1.0f;
         floor_e = s.min_p ? s.min_p[row] : 0.0f;
         floor_e = floor_e > 0.f ? fminf(floor_e, 1.0f) : 0.f;
-        u = s.u[row];
+        u = s.u ? s.u[row] : 0.f;
         u = u > 0.f ? fminf(u, 0.99999994f) : 0.f;
     }
 };
@@ -66,35 +91,6 @@ struct Power {
     // for any but +inf: 0 for -inf and NaN (0 slope included)
     __device__ __forceinline__ float of(float z) const {
         return z > BITLOGIC_NEG_INF ? exp2_unit((z - m) * slope) : 0.f;
-    }
-};
-
-// Sums of weights w = rint(2^40 e), 0 <= e <= 1, of at most 1024 of them, in
-// fp32 and 32-bit integer operations: 16 + e rounds e to a multiple of 2^-19,
-// the remainder is exact, and 1.5 2^23 + 2^40 remainder rounds it to a whole
-// number as rint does; so w = 2^21 high + low with the offsets of the two
-// floats' bits taken off, in arithmetic modulo 2^32.
-struct WeightSum {
-    uint32_t high = 0, low = 0;
-    __device__ __forceinline__ void add(f32x2 e) {
-        const f32x2 c16 = pack2(16.0f, 16.0f), scale = pack2(1099511627776.0f, 1099511627776.0f),
-                    whole = pack2(12582912.0f, 12582912.0f);
-        const f32x2 t = add2(e, c16), r = sub2(e, sub2(t, c16)), u = fma2(r, scale, whole);
-        float a, b;
-        unpack2(t, a, b);
-        high += __float_as_uint(a) + __float_as_uint(b) - 2u * 0x41800000u;
-        unpack2(u, a, b);
-        low += __float_as_uint(a) + __float_as_uint(b) - 2u * 0x4b400000u;
-    }
-    __device__ __forceinline__ unsigned long long total() const {
-        return ((unsigned long long)high << 21) + (unsigned long long)(long long)(int)low;
-    }
-    // the sum over a warp (of at most 1024 weights), in every lane
-    __device__ __forceinline__ unsigned long long warp_total() const {
-        WeightSum s;
-        s.high = __reduce_add_sync(0xffffffffu, high);
-        s.low = __reduce_add_sync(0xffffffffu, low);
-        return s.total();
     }
 };
 
@@ -143,9 +139,85 @@ __device__ __forceinline__ unsigned long long warp_upto(unsigned long long v, in
     return v;
 }
 
+// A logit below which no power exceeds e (some of those above it may not).
+__device__ __forceinline__ float logit_below(float e, const Power& p) {
+    return p.slope > 0.f ? p.m - fabsf(p.m) * 1e-6f - (0.02f - 1.000001f * log2f(e)) / p.slope : BITLOGIC_NEG_INF;
+}
+
+// The last class kept of a row read from memory: at a cut whose power min_p lets
+// through the last of its ties, else the last of the classes above the cut with
+// e >= min_p.  Called by the whole block.
+template <typename T>
+__device__ void last_kept(const T* __restrict__ x, int V, const Cut& cut, const RowSettings& set, const Power& power,
+                          long long row, const Draw& out, StreamScratch* sc) {
+    using P = Piece<T>;
+    constexpr int N = P::N;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const RowSlice<T> slice(x, V, 0, 1);
+    const uint4* from = reinterpret_cast<const uint4*>(x + slice.first);
+    auto piece = [&](int j) {
+        return j >= slice.whole0() && j < slice.whole1(V) ? __ldcg(from + j) : end_piece(x, V, slice.first + j * N);
+    };
+    const float z_cut = cut.key == kNoCut ? BITLOGIC_NEG_INF : key_logit(cut.key);
+    if (cut.ties && power(z_cut) >= set.floor_e) {
+        // every warp a contiguous part of the row: its ties
+        const int part = (slice.n + kSampleWarps - 1) / kSampleWarps, j0 = min(slice.n, warp * part), j1 = min(slice.n, j0 + part);
+        auto ties_of = [&](int j, float (&z)[N]) {
+            unsigned same = 0;
+            if (j < j1) {
+                P::load(piece(j), z);
+#pragma unroll
+                for (int i = 0; i < N; ++i) same += z[i] == z_cut;
+            }
+            return same;
+        };
+        float z[N];
+        unsigned eq = 0;
+        for (int j = j0 + lane; j < j1; j += 32) eq += ties_of(j, z);
+        eq = __reduce_add_sync(0xffffffffu, eq);
+        __syncthreads();
+        if (lane == 0) sc->ties[warp] = eq;
+        __syncthreads();
+        unsigned long long left = cut.ties;
+        for (int w = 0; w < warp; ++w) left -= sc->ties[w] < left ? sc->ties[w] : left;
+        if (left == 0 || left > eq) return;
+        for (int b = j0; b < j1; b += 32) {   // the warp that holds it: a piece per lane, in order
+            const unsigned same = ties_of(b + lane, z);
+            const unsigned upto = (unsigned)warp_upto(same, lane);
+            if (upto >= left && upto - same < left) {
+                unsigned n = (unsigned)left - (upto - same);
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (z[i] == z_cut && --n == 0) put_support(out, row, z_cut + 0.0f, slice.first + (b + lane) * N + i);
+            }
+            const unsigned all = __shfl_sync(0xffffffffu, upto, 31);
+            if (all >= left) return;
+            left -= all;
+        }
+        return;
+    }
+    const float z_min = set.floor_e > 0.f ? logit_below(set.floor_e, power) : BITLOGIC_NEG_INF;
+    unsigned long long best = 0;   // ~key << 32 | class, of the least key
+    for (int j = tid; j < slice.n; j += kSampleThreads) {
+        const uint4 u = piece(j);
+        if (P::largest_of(u) >= z_min) {
+            float z[N];
+            P::load(u, z);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (z[i] > z_cut && power(z[i]) >= set.floor_e) {
+                    const unsigned long long c = ((unsigned long long)~logit_key(z[i]) << 32) | (uint32_t)(slice.first + j * N + i);
+                    best = c > best ? c : best;
+                }
+        }
+    }
+    best = block_max(best, sc->mass);
+    if (tid == 0) put_support(out, row, key_logit(~(uint32_t)(best >> 32)), (int)(uint32_t)best);
+}
+
 // The draw of a row read from memory in every pass, for any row and settings.
 // Called by the whole block.
-template <typename T>
+template <typename T, bool kSupport>
 __device__ void sample_of_stream(const T* __restrict__ x, int V, RowSettings set, long long row, const Draw& out,
                                  StreamScratch* sc) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -153,10 +225,7 @@ __device__ void sample_of_stream(const T* __restrict__ x, int V, RowSettings set
     for (int v = tid; v < V; v += kSampleThreads) m = fmaxf(m, logit_value(x[v]));
     m = block_largest(m, sc->fbuf, kSampleWarps);
     if (m == BITLOGIC_NEG_INF) {   // nothing to draw from
-        if (tid == 0) {
-            out.token[row] = -1;
-            if (out.logprob) out.logprob[row] = BITLOGIC_NEG_INF;
-        }
+        if (tid == 0) put_nothing<kSupport>(out, row);
         return;
     }
     const Power power(m, set);
@@ -194,6 +263,10 @@ __device__ void sample_of_stream(const T* __restrict__ x, int V, RowSettings set
             const unsigned long long wt = draw_weight(power(key_logit(cut.key)));
             cut.ties = wt ? (want - above + wt - 1) / wt : 1;
         }
+    }
+    if constexpr (kSupport) {
+        last_kept(x, V, cut, set, power, row, out, sc);
+        return;
     }
     // every warp a contiguous part of the row: its weight above the cut, and its ties
     const int part = (V + kSampleWarps - 1) / kSampleWarps, v0 = min(V, warp * part), v1 = min(V, v0 + part);
@@ -296,7 +369,8 @@ struct SampleShared {
     int kept[kSampleWarps];
     struct Found {
         uint32_t key;
-        unsigned ties, slow, pad;
+        unsigned ties, slow;
+        int last;   // class
     } found;
     int bin;
     unsigned n_list, n_local, base;
@@ -312,11 +386,6 @@ __device__ __forceinline__ float bin_mass(unsigned units, int b) {
     return (float)units * __uint_as_float((unsigned)(127 - 14 - b / kBinsPerOctave) << 23);
 }
 __device__ __forceinline__ float bin_above(int b) { return __uint_as_float(0x3fffffffu - ((unsigned)b << 17)); }
-
-// A logit below which no power exceeds e (some of those above it may not).
-__device__ __forceinline__ float logit_below(float e, const Power& p) {
-    return p.slope > 0.f ? p.m - fabsf(p.m) * 1e-6f - (0.02f - 1.000001f * log2f(e)) / p.slope : BITLOGIC_NEG_INF;
-}
 
 // The bins in which a mass is reached from the largest power down, into *bin: 4
 // times the bin (the last one if none), and 1 or 2 where the mass comes so near
@@ -401,6 +470,7 @@ __device__ __forceinline__ void find_cut(unsigned long long* list, unsigned list
             found->key = key;
             found->ties = ties;
             found->slow = 0u;
+            found->last = (int)~(uint32_t)list[i];
         }
         run += w;
     }
@@ -410,7 +480,7 @@ __device__ __forceinline__ void find_cut(unsigned long long* list, unsigned list
 // The first block's work where the row's first k classes are all on its list:
 // the cut by rank and mass on the sorted list, then the draw among the kept
 // sorted by class.
-template <typename S>
+template <bool kSupport, typename S>
 __device__ void sample_of_list(S* s, unsigned n, const RowSettings& set, const Power& power, long long row,
                                const Draw& out) {
     constexpr int kPer = kListTop / kSampleThreads;
@@ -435,7 +505,7 @@ __device__ void sample_of_list(S* s, unsigned n, const RowSettings& set, const P
 #pragma unroll
     for (int q = 0; q < kPer; ++q) {
         const int i = tid * kPer + q;
-        if (i < k && (set.p >= 1.0f || before < want)) kept = i + 1;
+        if (i < k && (set.p >= 1.0f || before < want) && (!kSupport || e[q] >= set.floor_e)) kept = i + 1;
         before += w[q];
     }
     // the kept are a run from the front: its length
@@ -444,6 +514,10 @@ __device__ void sample_of_list(S* s, unsigned n, const RowSettings& set, const P
     if ((tid & 31) == 0) s->kept[tid >> 5] = kept;
     __syncthreads();
     for (int v = 0; v < kSampleWarps; ++v) kept = max(kept, s->kept[v]);
+    if constexpr (kSupport) {
+        if (tid == 0) put_support(out, row, key_logit((uint32_t)(s->list[kept - 1] >> 32)), (int)~(uint32_t)s->list[kept - 1]);
+        return;
+    }
     // by class: ~class << 32 | key falls as the class rises
     const int size2 = power_of_two(kept);
     for (int i = tid; i < size2; i += kSampleThreads) {
@@ -485,7 +559,7 @@ __device__ void sample_of_list(S* s, unsigned n, const RowSettings& set, const P
 //   neither: the last step alone.
 // A larger top_k, and a list that overflows (long runs of equal logits), are
 // drawn from memory by the first block.
-template <typename T>
+template <typename T, bool kSupport>
 __global__ void __launch_bounds__(kSampleThreads)
 sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settings, Draw out) {
     using P = Piece<T>;
@@ -544,10 +618,7 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
         bound = min(bound, s.stats[b].bound);
     }
     if (m == BITLOGIC_NEG_INF) {   // nothing to draw from
-        if (rank == 0 && tid == 0) {
-            out.token[row] = -1;
-            if (out.logprob) out.logprob[row] = BITLOGIC_NEG_INF;
-        }
+        if (rank == 0 && tid == 0) put_nothing<kSupport>(out, row);
         return;
     }
     const Power power(m, set);
@@ -587,11 +658,19 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
         if (rank != 0) return;
         const unsigned n = s.n_list;
         __syncthreads();
-        if (listed && n <= kList) sample_of_list(&s, n, set, power, row, out);
-        else sample_of_stream(x, V, set, row, out, &s.stream);
+        if (listed && n <= kList) sample_of_list<kSupport>(&s, n, set, power, row, out);
+        else sample_of_stream<T, kSupport>(x, V, set, row, out, &s.stream);
         return;
     }
 
+    if constexpr (kSupport) {
+        if (set.p >= 1.0f) {   // min_p alone, or nothing
+            if (rank != 0) return;
+            if (set.floor_e > 0.f) last_kept(x, V, Cut{kNoCut, 0}, set, power, row, out, &s.stream);
+            else if (tid == 0) put_nothing<true>(out, row);
+            return;
+        }
+    }
     // every warp a contiguous part of the slice, so that sums follow the order
     // of classes
     const int run_of = (slice.n + kSampleWarps - 1) / kSampleWarps, j0 = min(slice.n, warp * run_of),
@@ -698,7 +777,7 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
             unsigned long long first = 0;
             for (unsigned b = 0; b < blocks; ++b) first += s.sums[b].mass;
             const unsigned listed = s.n_list;
-            if (tid == 0) s.found = {0u, 0u, 1u, 0u};   // not found: from memory
+            if (tid == 0) s.found = {0u, 0u, 1u, -1};   // not found: from memory
             __syncthreads();
             if (listed <= kList && listed > 0 && first < want)
                 find_cut(s.list, listed, first, want, power, s.scan.sums, &s.found, [](unsigned long long, float, unsigned long long) {});
@@ -707,11 +786,19 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
         }
         row_barrier();
         if (s.found.slow) {
-            if (rank == 0) sample_of_stream(x, V, set, row, out, &s.stream);
+            if (rank == 0) sample_of_stream<T, kSupport>(x, V, set, row, out, &s.stream);
             return;
         }
         cut = {s.found.key, s.found.ties};
         z_cut = key_logit(cut.key);
+        if constexpr (kSupport) {
+            if (rank != 0) return;
+            const int last = s.found.last;
+            __syncthreads();
+            if (power.of(z_cut) < set.floor_e) last_kept(x, V, cut, set, power, row, out, &s.stream);
+            else if (tid == 0) put_support(out, row, z_cut, last);
+            return;
+        }
     }
 
     // kept weights and ties, by warp and by block
@@ -868,6 +955,7 @@ struct SampleRowShared {
     struct {
         uint32_t key;
         unsigned ties, slow;
+        int last;   // class
     } found;
 };
 
@@ -886,7 +974,7 @@ struct SampleRowShared {
 //     by chunk, and that bin's entries as a list, in which the cut is found;
 //   neither: the weights by chunk.
 // The chunk that holds the draw is read once more by a warp.
-template <typename T>
+template <typename T, bool kSupport>
 __global__ void __launch_bounds__(kSampleThreads, 4)
 sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings settings, Draw out) {
     using P = Piece<T>;
@@ -937,10 +1025,7 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
     for (int i = 0; i < 8; ++i) m = fmaxf(m, P::value(mx[i]));
     m = block_largest(m, s.fbuf, kSampleWarps);
     if (m == BITLOGIC_NEG_INF) {   // nothing to draw from
-        if (tid == 0) {
-            out.token[row] = -1;
-            if (out.logprob) out.logprob[row] = BITLOGIC_NEG_INF;
-        }
+        if (tid == 0) put_nothing<kSupport>(out, row);
         return;
     }
     const Power power(m, set);
@@ -952,7 +1037,7 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
     };
     if (set.k < V) {
         if (set.k > kListTop) {
-            sample_of_stream(x, V, set, row, out, &s.stream);
+            sample_of_stream<T, kSupport>(x, V, set, row, out, &s.stream);
             return;
         }
         float part[8];
@@ -985,13 +1070,20 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
         __syncthreads();
         const unsigned n = s.n;
         __syncthreads();
-        if (n <= kRowList) sample_of_list(&s, n, set, power, row, out);
-        else sample_of_stream(x, V, set, row, out, &s.stream);
+        if (n <= kRowList) sample_of_list<kSupport>(&s, n, set, power, row, out);
+        else sample_of_stream<T, kSupport>(x, V, set, row, out, &s.stream);
         return;
     }
 
     Cut cut = {kNoCut, 0};
     float z_cut = BITLOGIC_NEG_INF;   // kept: above it, and the first ties at it
+    if constexpr (kSupport) {
+        if (set.p >= 1.0f) {   // min_p alone, or nothing
+            if (set.floor_e > 0.f) last_kept(x, V, cut, set, power, row, out, &s.stream);
+            else if (tid == 0) put_nothing<true>(out, row);
+            return;
+        }
+    }
     stream.load(0, ua);
     stream.load(1, ub);
     if (set.p < 1.0f) {
@@ -1106,7 +1198,7 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
                 if (e > e_list && e <= e_above) list_entry(z, v);
             }
         }
-        if (tid == 0) s.found = {0u, 0u, 1u};   // not found: from memory
+        if (tid == 0) s.found = {0u, 0u, 1u, -1};   // not found: from memory
         __syncthreads();
         const unsigned listed = s.n;
         __syncthreads();
@@ -1118,11 +1210,16 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
                 }
             });
         if (s.found.slow) {
-            sample_of_stream(x, V, set, row, out, &s.stream);
+            sample_of_stream<T, kSupport>(x, V, set, row, out, &s.stream);
             return;
         }
         cut = {s.found.key, s.found.ties};
         z_cut = key_logit(cut.key);
+        if constexpr (kSupport) {
+            if (power.of(z_cut) < set.floor_e) last_kept(x, V, cut, set, power, row, out, &s.stream);
+            else if (tid == 0) put_support(out, row, z_cut, s.found.last);
+            return;
+        }
     } else {
         stream_row([&](const uint4 (&u)[4], int q) {
             WeightSum ws;
@@ -1239,7 +1336,7 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
 // WeightSum), so that a warp's sums are two 32-bit reductions.
 constexpr int kNarrow = 1024, kNarrowWarps = 8;
 
-template <typename T, int PER>
+template <typename T, int PER, bool kSupport>
 __global__ void __launch_bounds__(kNarrowWarps * 32)
 sample_narrow_kernel(const T* __restrict__ X, long long ld, int V, long long rows, Settings settings, Draw out) {
     constexpr int kKeyBits = sizeof(T) == 2 ? 19 : 32;   // leading bits of a key that differ (fp16 fills 19)
@@ -1257,10 +1354,7 @@ sample_narrow_kernel(const T* __restrict__ X, long long ld, int V, long long row
     for (int i = 0; i < PER; ++i) m = fmaxf(m, z[i]);
     m = warp_largest(m);
     if (m == BITLOGIC_NEG_INF) {   // nothing to draw from
-        if (lane == 0) {
-            out.token[row] = -1;
-            if (out.logprob) out.logprob[row] = BITLOGIC_NEG_INF;
-        }
+        if (lane == 0) put_nothing<kSupport>(out, row);
         return;
     }
     const Power power(m, set);
@@ -1354,9 +1448,34 @@ sample_narrow_kernel(const T* __restrict__ X, long long ld, int V, long long row
             cut.ties = wt ? (want - above + wt - 1) / wt : 1;
         }
     }
-    // kept weights, then the draw: the 32 classes it falls in, and the class
     unsigned left = (unsigned)cut.ties;
     const float floor_e = set.floor_e;
+    if constexpr (kSupport) {
+        if (set.k >= V && set.p >= 1.0f && floor_e == 0.f) {
+            if (lane == 0) put_nothing<true>(out, row);
+            return;
+        }
+        // the least key kept, and the last of its classes
+        uint32_t least = 0xffffffffu;
+        unsigned last = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const bool same = cut.ties && key[i] == cut.key;
+            const unsigned mask = __ballot_sync(0xffffffffu, same);
+            const bool kept = ranks(key[i]) && (key[i] > cut.key || (same && __popc(mask & ((1u << lane) - 1u)) < left)) &&
+                              (floor_e == 0.f || power(key_logit(key[i])) >= floor_e);
+            left -= min(left, (unsigned)__popc(mask));
+            if (kept && key[i] <= least) {
+                least = key[i];
+                last = 32 * i + lane;
+            }
+        }
+        const uint32_t all = __reduce_min_sync(0xffffffffu, least);
+        last = __reduce_max_sync(0xffffffffu, least == all ? last : 0u);
+        if (lane == 0) put_support(out, row, key_logit(all), (int)last);
+        return;
+    }
+    // kept weights, then the draw: the 32 classes it falls in, and the class
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const bool same = cut.ties && key[i] == cut.key;
@@ -1400,13 +1519,13 @@ inline size_t chunk_bytes(int V, int element) {
     return (size_t)(2 + kSampleWarps * batches) * 8;
 }
 
-template <typename T>
+template <typename T, bool kSupport>
 int launch_sample(const T* x, long long T_, int V, long long ld, const Settings& set, const Draw& out,
                   cudaStream_t stream) {
     cudaError_t e;
     if (V <= kNarrow) {
-        auto kern = V <= 32 ? sample_narrow_kernel<T, 1> : V <= 128 ? sample_narrow_kernel<T, 4>
-                  : V <= 256 ? sample_narrow_kernel<T, 8> : V <= 512 ? sample_narrow_kernel<T, 16> : sample_narrow_kernel<T, 32>;
+        auto kern = V <= 32 ? sample_narrow_kernel<T, 1, kSupport> : V <= 128 ? sample_narrow_kernel<T, 4, kSupport>
+                  : V <= 256 ? sample_narrow_kernel<T, 8, kSupport> : V <= 512 ? sample_narrow_kernel<T, 16, kSupport> : sample_narrow_kernel<T, 32, kSupport>;
         e = launch_rows(kern, (T_ + kNarrowWarps - 1) / kNarrowWarps, 1, kNarrowWarps * 32, 0, 0, stream, x, ld, V, T_, set, out);
     } else {
         // where a cluster per row is faster (50001 fp32 and 131072 bf16 classes:
@@ -1416,10 +1535,10 @@ int launch_sample(const T* x, long long T_, int V, long long ld, const Settings&
         const long long few = set.top_p ? sm_count() : sm_count() / 4;
         const int blocks = T_ <= few ? blocks_per_row(T_, V, sizeof(T), kTileFit, kTileMost, kTileLeast) : 0;
         if (blocks > 1) {
-            e = launch_rows(sample_tile_kernel<T>, T_, blocks, kSampleThreads, (size_t)slice_bytes(V, sizeof(T), blocks),
+            e = launch_rows(sample_tile_kernel<T, kSupport>, T_, blocks, kSampleThreads, (size_t)slice_bytes(V, sizeof(T), blocks),
                             kTileMost, stream, x, ld, V, set, out);
         } else {
-            e = launch_rows(sample_row_kernel<T>, T_, 1, kSampleThreads, chunk_bytes(V, sizeof(T)),
+            e = launch_rows(sample_row_kernel<T, kSupport>, T_, 1, kSampleThreads, chunk_bytes(V, sizeof(T)),
                             chunk_bytes(kMaxClasses, sizeof(T)), stream, x, ld, V, set, out);
         }
     }
@@ -1431,6 +1550,7 @@ int launch_sample(const T* x, long long T_, int V, long long ld, const Settings&
 
 using namespace bitlogic;
 
+#ifndef BITLOGIC_SUPPORT_UNIT
 extern "C" int bitlogic_sample_logits(const void* X, int32_t dtype, int64_t T, int32_t V, int64_t ld, const float* u,
                                       const float* temperature, const int32_t* top_k, const float* top_p,
                                       const float* min_p, int32_t* token, float* logprob, cudaStream_t stream) {
@@ -1438,8 +1558,24 @@ extern "C" int bitlogic_sample_logits(const void* X, int32_t dtype, int64_t T, i
     if (T == 0) return BITLOGIC_OK;
     if (!u || !token) return BITLOGIC_ERR_NULL;
     const Settings set = {u, temperature, top_k, top_p, min_p};
-    const Draw out = {token, logprob};
+    const Draw out = {token, logprob, nullptr, nullptr};
     return with_logit_type(dtype, true, [&](auto* type) {
-        return launch_sample(static_cast<decltype(type)>(X), T, V, ld, set, out, stream);
+        return launch_sample<std::remove_const_t<std::remove_pointer_t<decltype(type)>>, false>(
+            static_cast<decltype(type)>(X), T, V, ld, set, out, stream);
     });
 }
+#else
+extern "C" int bitlogic_support_logits(const void* X, int32_t dtype, int64_t T, int32_t V, int64_t ld,
+                                       const float* temperature, const int32_t* top_k, const float* top_p,
+                                       const float* min_p, float* floor, int32_t* last, cudaStream_t stream) {
+    if (int st = check_logits(X, dtype, true, T, V, ld)) return st;
+    if (T == 0) return BITLOGIC_OK;
+    if (!floor || !last) return BITLOGIC_ERR_NULL;
+    const Settings set = {nullptr, temperature, top_k, top_p, min_p};
+    const Draw out = {nullptr, nullptr, floor, last};
+    return with_logit_type(dtype, true, [&](auto* type) {
+        return launch_sample<std::remove_const_t<std::remove_pointer_t<decltype(type)>>, true>(
+            static_cast<decltype(type)>(X), T, V, ld, set, out, stream);
+    });
+}
+#endif

@@ -8,7 +8,9 @@ evaluation (App. C.1): binarize tables, encode + pack, hard layer 1, hard
 layer 2 with the fused popcount head and argmax.  ``DistillStep`` is the
 training step of a student that learns from a teacher's recorded answers
 (``TeacherRecord``), and ``HardInfer.draw`` answers by chance instead of the
-argmax.  Buffers are allocated once
+argmax.  ``Features`` turns hidden states of another model into the samples that
+either reads, and ``DraftCheck`` has a larger model check answers as drafts.
+Buffers are allocated once
 (torch provides the device memory); every step only enqueues library calls
 on the current stream, so a step can be captured once as a CUDA graph and
 replayed (``capture``), which removes the host work between the launches.
@@ -32,11 +34,18 @@ from . import (NODE_FORMS, bitlogic_adamw_update, bitlogic_binarize_tables, bitl
                bitlogic_lut_backward_bitrows, bitrow_words, bitlogic_degree_order,
                bitlogic_lut_forward_codes, bitlogic_lut_forward_coded, bitlogic_lut_backward_coded,
                bitlogic_corner_reduce, bitlogic_codes_decode, code_bytes,
-               bitlogic_top_logits, bitlogic_distill_loss, bitlogic_sample_logits)
+               bitlogic_top_logits, bitlogic_distill_loss, bitlogic_sample_logits,
+               bitlogic_support_logits, bitlogic_verify_drafts, bitlogic_verify_drafts_workspace,
+               bitlogic_dropout, bitlogic_norm_bytes, bitlogic_norm_backward, bitlogic_norm_backward_workspace)
 
 
 def _nomark(name: str) -> None:
     return None
+
+
+def _on(stream):
+    """Context in which torch's own operations run on ``stream``."""
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
 
 
 def fit_quantile_thresholds(batches, b: int, stream=None) -> list:
@@ -223,14 +232,33 @@ class TrainStep:
     no multiple of four ``dy1`` too.  Set ``keep_dy1`` to also write dY1 in
     every step (e.g. to check it).  ``node`` picks the
     LightLUT form of both layers: "soft", or "st" (hard table samples in the
-    forward, straight-through gradient to the logits)."""
+    forward, straight-through gradient to the logits).
+
+    With ``dropout`` > 0 every value of layer 1's output is dropped with that
+    probability and the others are divided by 1 - dropout (bitlogic_dropout, in
+    place; the mask is drawn again for the gradient).  A node is linear in each of
+    its inputs, so over the masks its mean is the node of the whole inputs where
+    they are distinct, which is what ``HardInfer`` deploys.  ``drop_counter``
+    (int64 [2] on the device: ``seed`` and a step that ``update`` advances) gives
+    the mask; ranks of a data-parallel run take different seeds.  The step then
+    keeps layer 1's output and its gradient as fp32 rows (neither ``through``,
+    ``fuse_dy1`` nor ``codes1``)."""
 
     def __init__(self, net: Network, B: int, d: int, thresholds: Sequence[int], C: int,
                  tau: float, want_dx1: bool = False, keep_dy1: bool = False,
                  fuse_dy1: Optional[bool] = None, csr_order: bool = True, node: str = "soft",
                  through: Optional[bool] = None, bytes1: Optional[bool] = None,
-                 bits1: Optional[bool] = None, device="cuda", codes1: Optional[bool] = None):
+                 bits1: Optional[bool] = None, device="cuda", codes1: Optional[bool] = None,
+                 dropout: float = 0.0, seed: int = 0):
         dev = torch.device(device)
+        self.dropout = float(dropout)
+        if not 0.0 <= self.dropout < 1.0:
+            raise ValueError("dropout must lie in [0, 1)")
+        if self.dropout:
+            if through or fuse_dy1 or codes1:
+                raise ValueError("dropout needs layer 1's output and gradient as fp32 rows: no through, fuse_dy1 or codes1")
+            through = fuse_dy1 = codes1 = False
+            self.drop_counter = torch.tensor([int(seed), 0], dtype=torch.int64, device=dev)
         if node not in NODE_FORMS:
             raise ValueError(f"node must be one of {sorted(NODE_FORMS)}")
         self.node = node
@@ -368,6 +396,9 @@ class TrainStep:
             mark("encode")
             bitlogic_lut_forward_node(self.bits, n.conn1, n.theta1, self.y1, self.node, stream)
         mark("forward1")
+        if self.dropout:
+            bitlogic_dropout(self._y1, self._y1, self.drop_counter, self.dropout, stream=stream)
+            mark("dropout")
         if self.codes1:
             bitlogic_lut_forward_coded(self.codes, self.table1, n.conn2, n.theta2, self.y2, self.node, stream)
         else:
@@ -431,6 +462,9 @@ class TrainStep:
         else:
             bitlogic_csr_reduce(self.edges2, n.off2, edge2, self._dy1, stream)
             mark("csr2")
+            if self.dropout:
+                bitlogic_dropout(self._dy1, self._dy1, self.drop_counter, self.dropout, stream=stream)
+                mark("dropout_bwd")
             if self.bits1:
                 bitlogic_lut_backward_bitrows(self.bits, self.B, n.conn1, n.theta1, self.dth1, nd, dY=self._dy1,
                                               stream=stream)
@@ -482,17 +516,22 @@ class TrainStep:
                               weight_decay, stream)
         bitlogic_adamw_update(n.theta2, self.opt_m2, self.opt_v2, self.dth2, self.opt_step, lr, betas, eps,
                               weight_decay, stream)
+        if self.dropout:
+            with _on(stream):
+                self.drop_counter[1:].add_(1)
         mark("update")
 
     # kernels one run() launches: encode 1, forwards 2, head 2, backwards 2
     # (+ the CSR reduction of layer 2's terms unless fused or recomputed, +
     # the layer-1 CSR reduction when the input gradient is wanted; on corner
-    # codes + decode, terms and CSR reduction when dY1 is kept)
+    # codes + decode, terms and CSR reduction when dY1 is kept; + both
+    # directions of dropout)
     @property
     def kernels_per_run(self) -> int:
         if self.codes1:
             return 7 + (3 if self._dy1 is not None else 0)
-        return 7 + (0 if (self.fuse_dy1 or self.through) else 1) + (1 if self.dbits is not None else 0)
+        return (7 + (0 if (self.fuse_dy1 or self.through) else 1) + (1 if self.dbits is not None else 0)
+                + (2 if self.dropout else 0))
 
 
 class TeacherRecord:
@@ -514,7 +553,7 @@ class TeacherRecord:
         its logits are the counts divided by it)."""
         bitlogic_top_logits(logits, self.val, self.idx, self.lse, temperature=self.temperature * unit, stream=stream)
         if unit != 1.0:
-            with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            with _on(stream):
                 self.val.div_(unit)
 
     def load(self, val: torch.Tensor, idx: torch.Tensor, lse: torch.Tensor, non_blocking: bool = False):
@@ -522,6 +561,70 @@ class TeacherRecord:
         self.val.copy_(val, non_blocking=non_blocking)
         self.idx.copy_(idx, non_blocking=non_blocking)
         self.lse.copy_(lse, non_blocking=non_blocking)
+
+
+class Features:
+    """Hidden states of another model as the 8-bit samples that the encoder reads:
+    rows [B, d] (fp32, bf16 or fp16), with a residual added, over their root mean
+    square, times ``weight`` (fp32 or the rows' type [d], or None), as codes
+    128 + y / ``scale``, in 1 .. 255.  The scale is the same for all rows, so that
+    thresholds mean the same everywhere; ``fit_quantile_thresholds`` takes the codes
+    as it takes pixels."""
+
+    def __init__(self, d: int, scale: float = 4.0 / 127.0, weight: Optional[torch.Tensor] = None, eps: float = 1e-6):
+        if not scale > 0:
+            raise ValueError("scale must be positive")
+        self.d, self.scale, self.weight, self.eps = int(d), float(scale), weight, float(eps)
+
+    def take(self, hidden: torch.Tensor, x: torch.Tensor, residual: Optional[torch.Tensor] = None,
+             total: Optional[torch.Tensor] = None, stream=None):
+        """The codes of ``hidden`` (+ ``residual``; the sum into ``total``) into the
+        samples ``x`` uint8 [B, d], e.g. those of a step or of a hard pass."""
+        bitlogic_norm_bytes(hidden, x, weight=self.weight, residual=residual, total=total, fixed_scale=self.scale,
+                            eps=self.eps, stream=stream)
+
+    def backward(self, dy: torch.Tensor, total: torch.Tensor, dx: torch.Tensor, dweight: Optional[torch.Tensor] = None,
+                 residual_grad: Optional[torch.Tensor] = None, stream=None):
+        """From the gradient ``dy`` of the rows before their rounding to codes, that
+        of ``hidden`` and of the residual (alike) into ``dx``, and of the weight into
+        dweight fp32 [d], at the rows ``total``."""
+        ws = None
+        if dweight is not None:
+            with _on(stream):
+                ws = torch.empty(bitlogic_norm_backward_workspace(*dy.shape), dtype=torch.uint8, device=dy.device)
+        bitlogic_norm_backward(dy, total, dx, weight=self.weight, dweight=dweight, residual_grad=residual_grad,
+                               workspace=ws, eps=self.eps, stream=stream)
+
+
+class DraftCheck:
+    """Drafted answers of a small network checked by a larger model: up to S
+    sequences with up to D drafts in all over V classes.
+
+    ``first`` (int32 [S + 1]) says where each sequence's drafts begin, ``token``
+    (int32 [D]) and ``logprob`` (fp32 [D]) take the drafts and the logarithms of
+    their draws (e.g. HardInfer.draw(u, check.token, check.logprob)); after ``run``
+    ``accepted`` (int32 [S]) counts those that stand, and ``next_token`` (int32 [S])
+    is the class behind them, ``next_logprob`` its logarithm."""
+
+    def __init__(self, S: int, D: int, V: int, device="cuda"):
+        dev = torch.device(device)
+        self.S, self.D, self.V = int(S), int(D), int(V)
+        i32, f32 = dict(dtype=torch.int32, device=dev), dict(dtype=torch.float32, device=dev)
+        self.first = torch.zeros(S + 1, **i32)
+        self.token, self.logprob = torch.zeros(D, **i32), torch.zeros(D, **f32)
+        self.accepted, self.next_token = torch.zeros(S, **i32), torch.zeros(S, **i32)
+        self.next_logprob = torch.zeros(S, **f32)
+        self.workspace = torch.empty(bitlogic_verify_drafts_workspace(S, D, V), dtype=torch.uint8, device=dev)
+
+    def run(self, target: torch.Tensor, u: torch.Tensor, draw_u: torch.Tensor, draft: Optional[torch.Tensor] = None,
+            stream=None, **settings):
+        """``target`` [S + D, V] and ``draft`` [D, V] (None: drafts that were not
+        drawn) are logits of any type, u fp32 [D] and draw_u fp32 [S] random numbers;
+        settings (temperature, floor, last and their draft_ forms) as in
+        bitlogic_verify_drafts."""
+        bitlogic_verify_drafts(target, self.first, self.token, u, draw_u, self.accepted, self.next_token, self.workspace,
+                               logprob=self.next_logprob, draft=draft,
+                               draft_logprob=self.logprob if draft is not None else None, stream=stream, **settings)
 
 
 class DistillStep(TrainStep):
@@ -744,6 +847,14 @@ class HardInfer:
         head's tau times the softmax temperature)."""
         bitlogic_sample_logits(self.counts, u, token, logprob, temperature=temperature, top_k=top_k, top_p=top_p,
                                min_p=min_p, stream=stream)
+
+    def support(self, floor: torch.Tensor, last: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+                top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                min_p: Optional[torch.Tensor] = None, stream=None):
+        """The classes that ``draw`` keeps of the last pass's counts under the same
+        settings, into floor fp32 [N] and last int32 [N] (bitlogic_support_logits)."""
+        bitlogic_support_logits(self.counts, floor, last, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p,
+                                stream=stream)
 
     def capture(self, binarize: bool = True) -> torch.cuda.CUDAGraph:
         """One hard pass (with the table binarization when ``binarize``) as a
