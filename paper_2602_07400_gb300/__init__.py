@@ -988,20 +988,25 @@ def bitlogic_support_logits(logits: torch.Tensor, floor: torch.Tensor, last: tor
     draws among under the same settings: those above floor fp32 [T], and those
     equal to it up to class last int32 [T] (-inf and -1: all)."""
     code, T, V, ld = _logits(logits, "logits")
-    _need(floor, "floor", torch.float32, (T,))
-    _need(last, "last", torch.int32, (T,))
-    _optional(temperature, "temperature", torch.float32, (T,))
-    _optional(top_k, "top_k", torch.int32, (T,))
-    _optional(top_p, "top_p", torch.float32, (T,))
-    _optional(min_p, "min_p", torch.float32, (T,))
+    n = (T,)
     _check("bitlogic_support_logits", load().bitlogic_support_logits(
-        _ptr(logits), code, T, V, ld, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(floor), _ptr(last),
-        _stream(stream)))
+        logits.data_ptr(), code, T, V, ld, _vector(temperature, "temperature", torch.float32, n),
+        _vector(top_k, "top_k", torch.int32, n), _vector(top_p, "top_p", torch.float32, n),
+        _vector(min_p, "min_p", torch.float32, n), _required(floor, "floor", torch.float32, n),
+        _required(last, "last", torch.int32, n), _stream(stream)))
 
 
-def _optional(t, name: str, dtype: torch.dtype, shape: Tuple[int, ...]):
-    if t is not None:
-        _need(t, name, dtype, shape)
+def _required(t: torch.Tensor, name: str, dtype: torch.dtype, shape: Tuple[int, ...]) -> int:
+    """The address of a tensor that _need accepts (one pass over its attributes:
+    a call with twenty of them is short on the device)."""
+    if t.__class__ is torch.Tensor and t.dtype is dtype and t.is_cuda and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    _need(t, name, dtype, shape)
+    return t.data_ptr()
+
+
+def _vector(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape: Tuple[int, ...]) -> Optional[int]:
+    return None if t is None else _required(t, name, dtype, shape)
 
 
 def _workspace(t: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
@@ -1041,49 +1046,46 @@ def bitlogic_verify_drafts(target: torch.Tensor, first: torch.Tensor, token: tor
     S = R - D
     if S < 0:
         raise ValueError(f"target: expected a row per draft and one per sequence, got {R} rows for {D} drafts")
-    _need(first, "first", torch.int32, (S + 1,))
-    _need(token, "token", torch.int32, (D,))
-    _need(u, "u", torch.float32, (D,))
-    _need(draw_u, "draw_u", torch.float32, (S,))
-    _need(accepted, "accepted", torch.int32, (S,))
-    _need(next_token, "next_token", torch.int32, (S,))
-    _optional(logprob, "logprob", torch.float32, (S,))
-    _optional(temperature, "temperature", torch.float32, (R,))
-    _optional(floor, "floor", torch.float32, (R,))
-    _optional(last, "last", torch.int32, (R,))
-    _optional(draft_logprob, "draft_logprob", torch.float32, (D,))
-    _optional(draft_temperature, "draft_temperature", torch.float32, (D,))
-    _optional(draft_floor, "draft_floor", torch.float32, (D,))
-    _optional(draft_last, "draft_last", torch.int32, (D,))
-    dcode, dld = 0, V
+    f32, i32, nr, nd, ns = torch.float32, torch.int32, (R,), (D,), (S,)
+    dptr, dcode, dld = None, 0, V
     if draft is not None:
         dcode, DR, DV, dld = _logits(draft, "draft")
-        if (DR, DV) != (D, V):
+        if DR != D or DV != V:
             raise ValueError(f"draft: expected shape {(D, V)}, got {(DR, DV)}")
+        dptr = draft.data_ptr()
     ws, ws_bytes = _workspace(workspace)
     _check("bitlogic_verify_drafts", load().bitlogic_verify_drafts(
-        _ptr(target), code, S, D, V, ld, _ptr(temperature), _ptr(floor), _ptr(last), _ptr(first), _ptr(token), _ptr(u),
-        _ptr(draw_u), _ptr(draft), dcode, dld, _ptr(draft_logprob), _ptr(draft_temperature), _ptr(draft_floor),
-        _ptr(draft_last), _ptr(accepted), _ptr(next_token), _ptr(logprob), ws, ws_bytes, _stream(stream)))
+        target.data_ptr(), code, S, D, V, ld, _vector(temperature, "temperature", f32, nr), _vector(floor, "floor", f32, nr),
+        _vector(last, "last", i32, nr), _required(first, "first", i32, (S + 1,)), _required(token, "token", i32, nd),
+        _required(u, "u", f32, nd), _required(draw_u, "draw_u", f32, ns), dptr, dcode, dld,
+        _vector(draft_logprob, "draft_logprob", f32, nd), _vector(draft_temperature, "draft_temperature", f32, nd),
+        _vector(draft_floor, "draft_floor", f32, nd), _vector(draft_last, "draft_last", i32, nd),
+        _required(accepted, "accepted", i32, ns), _required(next_token, "next_token", i32, ns),
+        _vector(logprob, "logprob", f32, ns), ws, ws_bytes, _stream(stream)))
 
 
-def _rows(x: torch.Tensor, name: str, like: Optional[torch.Tensor] = None) -> Tuple[int, int]:
-    """Type code and row stride of a matrix of activations whose columns are
-    adjacent (rows may lie apart), of the type and shape of ``like``."""
+def _rows(x: torch.Tensor, name: str, dtype: Optional[torch.dtype] = None, shape=None) -> Tuple[int, int]:
+    """Address and row stride of a matrix of activations whose columns are
+    adjacent (rows may lie apart), of a type and shape where they are given."""
+    if x.__class__ is torch.Tensor and x.is_cuda and (x.dtype is dtype if dtype is not None else x.dtype in ROW_TYPES):
+        s = x.shape
+        if s == shape if shape is not None else len(s) == 2:
+            ld, inc = x.stride()
+            if inc == 1 and s[0] > 1:
+                return x.data_ptr(), ld
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    code = ROW_TYPES.get(x.dtype)
-    if code is None:
+    if x.dtype not in ROW_TYPES:
         raise TypeError(f"{name}: expected one of {[str(t) for t in ROW_TYPES]}, got {x.dtype}")
-    if like is not None and x.dtype != like.dtype:
-        raise TypeError(f"{name}: expected {like.dtype}, got {x.dtype}")
+    if dtype is not None and x.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {x.dtype}")
     if not x.is_cuda:
         raise ValueError(f"{name} must be on a CUDA device")
     if x.dim() != 2:
         raise ValueError(f"{name}: expected [rows, columns], got {x.dim()} dimensions")
-    if like is not None and x.shape != like.shape:
-        raise ValueError(f"{name}: expected shape {tuple(like.shape)}, got {tuple(x.shape)}")
-    return code, _row_stride(x, name)
+    if shape is not None and x.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
+    return x.data_ptr(), _row_stride(x, name)
 
 
 def _row_stride(x: torch.Tensor, name: str) -> int:
@@ -1094,6 +1096,10 @@ def _row_stride(x: torch.Tensor, name: str) -> int:
     return max(ld, C) if R <= 1 else ld
 
 
+def _rows_or_none(x: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape) -> Tuple[Optional[int], int]:
+    return (None, shape[1]) if x is None else _rows(x, name, dtype, shape)
+
+
 def bitlogic_dropout(x: torch.Tensor, out: torch.Tensor, counter: torch.Tensor, p: float, site: int = 0,
                      residual: Optional[torch.Tensor] = None, stream=None):
     """``out`` = ``x`` [R, C] (fp32, bf16 or fp16) with every value dropped with
@@ -1101,25 +1107,23 @@ def bitlogic_dropout(x: torch.Tensor, out: torch.Tensor, counter: torch.Tensor, 
     int64 [2] on the device holds seed and step; with the same counter, site and
     p the gradient of x is the same call on the gradient of out.  ``out`` may be
     x or residual."""
-    code, ldx = _rows(x, "x")
-    _, ldo = _rows(out, "out", x)
-    ldr = x.shape[1]
-    if residual is not None:
-        _, ldr = _rows(residual, "residual", x)
-    _need(counter, "counter", torch.int64, (2,))
-    R, C = x.shape
+    px, ldx = _rows(x, "x")
+    dtype, shape = x.dtype, x.shape
+    po, ldo = _rows(out, "out", dtype, shape)
+    pr, ldr = _rows_or_none(residual, "residual", dtype, shape)
+    R, C = shape
     _check("bitlogic_dropout", load().bitlogic_dropout(
-        _ptr(x), code, R, C, ldx, _ptr(residual), ldr, _ptr(out), ldo, _ptr(counter), float(p), int(site),
+        px, ROW_TYPES[dtype], R, C, ldx, pr, ldr, po, ldo, _required(counter, "counter", torch.int64, (2,)), float(p), int(site),
         _stream(stream)))
 
 
-def _norm_weight(weight: Optional[torch.Tensor], x: torch.Tensor) -> int:
+def _norm_weight(weight: Optional[torch.Tensor], dtype: torch.dtype, d: int) -> Tuple[Optional[int], int]:
     if weight is None:
-        return ROW_TYPES[x.dtype]
+        return None, 0
     if not isinstance(weight, torch.Tensor):
         raise TypeError("weight must be a torch.Tensor")
-    _need(weight, "weight", torch.float32 if weight.dtype == torch.float32 else x.dtype, (x.shape[1],))
-    return ROW_TYPES[weight.dtype]
+    wide = weight.dtype is torch.float32
+    return _required(weight, "weight", torch.float32 if wide else dtype, (d,)), 0 if wide else ROW_TYPES[dtype]
 
 
 def bitlogic_norm_bytes(x: torch.Tensor, out: torch.Tensor, scale: Optional[torch.Tensor] = None,
@@ -1132,14 +1136,12 @@ def bitlogic_norm_bytes(x: torch.Tensor, out: torch.Tensor, scale: Optional[torc
     scale fp32 [T, groups] (a group: ``group`` columns, 0 the row) unless
     ``fixed_scale`` is given; the sum x + residual goes to ``total`` (it may be x
     or residual)."""
-    code, ldx = _rows(x, "x")
-    T, d = x.shape
-    ldr = ldt = d
-    if residual is not None:
-        _, ldr = _rows(residual, "residual", x)
-    if total is not None:
-        _, ldt = _rows(total, "total", x)
-    wcode = _norm_weight(weight, x)
+    px, ldx = _rows(x, "x")
+    dtype, shape = x.dtype, x.shape
+    T, d = shape
+    pr, ldr = _rows_or_none(residual, "residual", dtype, shape)
+    pt, ldt = _rows_or_none(total, "total", dtype, shape)
+    pw, wcode = _norm_weight(weight, dtype, d)
     if not isinstance(out, torch.Tensor):
         raise TypeError("out must be a torch.Tensor")
     form = BYTE_TYPES.get(out.dtype)
@@ -1147,14 +1149,13 @@ def bitlogic_norm_bytes(x: torch.Tensor, out: torch.Tensor, scale: Optional[torc
         raise TypeError(f"out: expected one of {[str(t) for t in BYTE_TYPES]}, got {out.dtype}")
     if not out.is_cuda:
         raise ValueError("out must be on a CUDA device")
-    if out.shape != x.shape:
-        raise ValueError(f"out: expected shape {tuple(x.shape)}, got {tuple(out.shape)}")
+    if out.shape != shape:
+        raise ValueError(f"out: expected shape {tuple(shape)}, got {tuple(out.shape)}")
     group = int(group)
-    if scale is not None:
-        _need(scale, "scale", torch.float32, (T, -(-d // group) if group > 0 else 1))
     _check("bitlogic_norm_bytes", load().bitlogic_norm_bytes(
-        _ptr(x), code, T, d, ldx, _ptr(residual), ldr, _ptr(total), ldt, _ptr(weight), wcode, float(eps), form, _ptr(out),
-        _row_stride(out, "out"), _ptr(scale), group, float(fixed_scale), _stream(stream)))
+        px, ROW_TYPES[dtype], T, d, ldx, pr, ldr, pt, ldt, pw, wcode, float(eps), form, out.data_ptr(), _row_stride(out, "out"),
+        _vector(scale, "scale", torch.float32, (T, -(-d // group) if group > 0 else 1)), group, float(fixed_scale),
+        _stream(stream)))
 
 
 def bitlogic_norm_backward_workspace(T: int, d: int) -> int:
@@ -1169,19 +1170,17 @@ def bitlogic_norm_backward(dy: torch.Tensor, h: torch.Tensor, dx: torch.Tensor, 
     [T, d], the rounding to 8 bits passed as if it were not there: into ``dx`` that
     of x and of the residual alike, plus ``residual_grad``, and into dweight fp32
     [d] that of the weight.  ``dx`` may be dy, h or residual_grad."""
-    code, ldy = _rows(dy, "dy")
-    T, d = dy.shape
-    _, ldh = _rows(h, "h", dy)
-    _, ldx = _rows(dx, "dx", dy)
-    ldr = d
-    if residual_grad is not None:
-        _, ldr = _rows(residual_grad, "residual_grad", dy)
-    wcode = _norm_weight(weight, dy)
-    _optional(dweight, "dweight", torch.float32, (d,))
+    py, ldy = _rows(dy, "dy")
+    dtype, shape = dy.dtype, dy.shape
+    T, d = shape
+    ph, ldh = _rows(h, "h", dtype, shape)
+    px, ldx = _rows(dx, "dx", dtype, shape)
+    pr, ldr = _rows_or_none(residual_grad, "residual_grad", dtype, shape)
+    pw, wcode = _norm_weight(weight, dtype, d)
     ws, ws_bytes = _workspace(workspace)
     _check("bitlogic_norm_backward", load().bitlogic_norm_backward(
-        _ptr(dy), code, T, d, ldy, _ptr(h), ldh, _ptr(weight), wcode, _ptr(residual_grad), ldr, float(eps), _ptr(dx), ldx,
-        _ptr(dweight), ws, ws_bytes, _stream(stream)))
+        py, ROW_TYPES[dtype], T, d, ldy, ph, ldh, pw, wcode, pr, ldr, float(eps), px, ldx,
+        _vector(dweight, "dweight", torch.float32, (d,)), ws, ws_bytes, _stream(stream)))
 
 
 def bitlogic_binarize_tables(theta: torch.Tensor, table: torch.Tensor, stream=None):

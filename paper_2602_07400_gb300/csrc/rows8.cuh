@@ -5,7 +5,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include "common.cuh"
+#include "packed.cuh"
 
 namespace bitlogic {
 
@@ -115,6 +115,25 @@ __device__ __forceinline__ void store_eight(T* p, int n, bool vec, const float (
             if (i < n) p[i] = from_f32<T>(v[i]);
     }
 }
+
+// Eight values as four pairs, for packed arithmetic.
+template <typename T>
+__device__ __forceinline__ void pairs_of(const Eight<T>& e, f32x2 (&z)[4]) {
+    float v[8];
+    e.get(v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = pack2(v[2 * i], v[2 * i + 1]);
+}
+template <typename T>
+__device__ __forceinline__ Eight<T> eight_of(const f32x2 (&z)[4]) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(z[i], v[2 * i], v[2 * i + 1]);
+    Eight<T> e;
+    e.set(v);
+    return e;
+}
+__device__ __forceinline__ f32x2 twice(float v) { return pack2(v, v); }
 
 inline int row_type_bytes(int dtype) { return dtype == BITLOGIC_F32 ? 4 : 2; }
 

@@ -163,12 +163,12 @@ verify_sums_kernel(Rows rows, int V, Drafts d, int parts, Part* __restrict__ out
         for (int i = 0; i < H; ++i) {
             float a, b;
             unpack2(mul2(sub2(z[i], mm), cc), a, b);
-            acc = add2(acc, pack2(fmaxf(exp2_unit(a), 0.f), fmaxf(exp2_unit(b), 0.f)));
+            acc = add2(acc, pack2(exp2_unit(a), exp2_unit(b)));
         }
         return acc;
     };
     auto add_kept = [&](const uint4& u, int j) {
-        if (!(P::largest_of(u) >= rule.floor)) return;
+        if (P::largest_of(u) < rule.floor) return;
         float z[N], top = BITLOGIC_NEG_INF;
         P::load(u, z);
 #pragma unroll
@@ -184,14 +184,17 @@ verify_sums_kernel(Rows rows, int V, Drafts d, int parts, Part* __restrict__ out
         sum += part;
     };
 
-    if (rule.greedy) {
-        largest_class();
-    } else if (rule.floor > BITLOGIC_NEG_INF || rule.floor != rule.floor) {
+    auto sum_kept = [&]() {
         stream_row([&](const uint4 (&u)[4], int q) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) add_kept(u[i], stream.piece(q, i));
         });
         if (j_end >= 0) add_kept(u_end, j_end);
+    };
+    if (rule.greedy) {
+        largest_class();
+    } else if (rule.floor > BITLOGIC_NEG_INF || rule.floor != rule.floor) {
+        sum_kept();
     } else {
         stream_row([&](const uint4 (&u)[4], int) {
             typename P::Max top = P::lowest();
@@ -235,9 +238,18 @@ verify_sums_kernel(Rows rows, int V, Drafts d, int parts, Part* __restrict__ out
         m = s[0].m;
         sum = s[0].sum;
         cls = s[0].cls;
+#pragma unroll
         for (int w = 1; w < kVerifyWarps; ++w) join(s[w].m, s[w].sum, s[w].cls);
     };
     join_block();
+    if (sum != sum && !(m > FLT_MAX)) {   // a NaN among the logits, which counts nothing
+        m = BITLOGIC_NEG_INF;
+        sum = 0.f;
+        stream.load(0, ua);
+        stream.load(1, ub);
+        sum_kept();
+        join_block();
+    }
     if (!rule.greedy && m > FLT_MAX) {   // the first of +inf takes it all
         m = BITLOGIC_NEG_INF;
         cls = INT_MAX;
@@ -251,53 +263,96 @@ verify_sums_kernel(Rows rows, int V, Drafts d, int parts, Part* __restrict__ out
 
 // ------------------------------------------------------------------- draw --
 
-// Eight classes from v0 on; -inf past the row's end.
-template <typename T>
-__device__ __forceinline__ void octet(const T* x, int v0, int V, bool aligned, float (&z)[8]) {
-    if (aligned && v0 + 8 <= V) {
-        constexpr int N = Piece<T>::N;
-        float part[N];
-#pragma unroll
-        for (int h = 0; h < 8 / N; ++h) {
-            Piece<T>::load(__ldcg(reinterpret_cast<const uint4*>(x + v0) + h), part);
-#pragma unroll
-            for (int i = 0; i < N; ++i) z[h * N + i] = part[i];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = v0 + i < V ? logit_value(x[v0 + i]) : BITLOGIC_NEG_INF;
-    }
-}
+// A row of any type, its kept logits eight at a time: 32 lanes' eights make a
+// chunk.  Where the row starts on 16 bytes a lane's eight classes are side by
+// side (`along`), two loads at most; else they lie 32 apart, so that the lanes of
+// a load are side by side.  Loads come before conversions, so that a warp has
+// many on their way.
+struct Raw {
+    uint32_t w[8];
+};
 
-// A row of any type, its kept logits eight at a time.
 struct RowReader {
-    const void* x;
+    const unsigned char* x;
     int dtype, V;
-    bool aligned;
+    bool wide, aligned, cut;
     RowRule rule;
-    __device__ __forceinline__ RowReader(const Rows& rows, long long row, int V_) : dtype(rows.dtype), V(V_), rule(rows, row) {
-        x = static_cast<const unsigned char*>(rows.x) + row * rows.ld * (dtype == BITLOGIC_F32 || dtype == BITLOGIC_I32 ? 4 : 2);
+    __device__ __forceinline__ RowReader(const Rows& rows, long long row, int V_)
+        : dtype(rows.dtype), V(V_), wide(rows.dtype == BITLOGIC_F32 || rows.dtype == BITLOGIC_I32), rule(rows, row) {
+        x = static_cast<const unsigned char*>(rows.x) + row * rows.ld * (wide ? 4 : 2);
         aligned = (reinterpret_cast<uintptr_t>(x) & 15u) == 0;
-    }
-    __device__ __forceinline__ void load(int v0, float (&z)[8]) const {
-        switch (dtype) {
-            case BITLOGIC_F32: octet(static_cast<const float*>(x), v0, V, aligned, z); break;
-            case BITLOGIC_BF16: octet(static_cast<const __nv_bfloat16*>(x), v0, V, aligned, z); break;
-            case BITLOGIC_F16: octet(static_cast<const __half*>(x), v0, V, aligned, z); break;
-            default: octet(static_cast<const int*>(x), v0, V, aligned, z); break;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = rule.kept(z[i], v0 + i);
+        cut = !(rule.floor == BITLOGIC_NEG_INF);
     }
     __device__ __forceinline__ float at(int v) const {
         float z;
         switch (dtype) {
-            case BITLOGIC_F32: z = static_cast<const float*>(x)[v]; break;
-            case BITLOGIC_BF16: z = logit_value(static_cast<const __nv_bfloat16*>(x)[v]); break;
-            case BITLOGIC_F16: z = logit_value(static_cast<const __half*>(x)[v]); break;
-            default: z = logit_value(static_cast<const int*>(x)[v]); break;
+            case BITLOGIC_F32: z = reinterpret_cast<const float*>(x)[v]; break;
+            case BITLOGIC_BF16: z = logit_value(reinterpret_cast<const __nv_bfloat16*>(x)[v]); break;
+            case BITLOGIC_F16: z = logit_value(reinterpret_cast<const __half*>(x)[v]); break;
+            default: z = logit_value(reinterpret_cast<const int*>(x)[v]); break;
         }
         return rule.kept(z, v);
+    }
+    static __device__ __forceinline__ int place(int q, int lane, int i, bool along) { return q * kChunk + (along ? 8 * lane + i : 32 * i + lane); }
+    __device__ __forceinline__ bool full(int q) const { return (q + 1) * kChunk <= V; }
+    __device__ __forceinline__ Raw load(int q, int lane, bool along) const {
+        Raw r;
+        if (along && aligned && full(q)) {
+            const uint4* p = reinterpret_cast<const uint4*>(x + (size_t)(q * kChunk + 8 * lane) * (wide ? 4 : 2));
+            const uint4 a = p[0];
+            if (wide) {
+                const uint4 b = p[1];
+                r = {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+            } else {
+                r = {{a.x, a.y, a.z, a.w, 0u, 0u, 0u, 0u}};
+            }
+        } else if (wide) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int v = place(q, lane, i, along);
+                r.w[i] = v < V ? reinterpret_cast<const uint32_t*>(x)[v] : 0u;
+            }
+        } else {
+            uint32_t h[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int v = place(q, lane, i, along);
+                h[i] = v < V ? reinterpret_cast<const unsigned short*>(x)[v] : 0u;
+            }
+            r = {{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16, 0u, 0u, 0u, 0u}};
+        }
+        return r;
+    }
+    // their values; -inf for what is not kept
+    __device__ __forceinline__ void kept(const Raw& r, int q, int lane, bool along, float (&z)[8]) const {
+        const uint4 a = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]), b = make_uint4(r.w[4], r.w[5], r.w[6], r.w[7]);
+        float h[4];
+        if (dtype == BITLOGIC_BF16) {
+            Piece<__nv_bfloat16>::load(a, z);
+        } else if (dtype == BITLOGIC_F16) {
+            Piece<__half>::load(a, z);
+        } else if (dtype == BITLOGIC_F32) {
+            Piece<float>::load(a, h);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] = h[i];
+            Piece<float>::load(b, h);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[4 + i] = h[i];
+        } else {
+            Piece<int>::load(a, h);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] = h[i];
+            Piece<int>::load(b, h);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[4 + i] = h[i];
+        }
+        if (cut || !full(q)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int v = place(q, lane, i, along);
+                z[i] = v < V ? rule.kept(z[i], v) : BITLOGIC_NEG_INF;
+            }
+        }
     }
 };
 
@@ -314,6 +369,36 @@ struct Weigher {
         // no multiply-add: the differences are those of the rounded shares
         const float p = __fmul_rn(e, inv), q = one >= 0 ? (v == one ? 1.f : 0.f) : __fmul_rn(draft.power(zd, dm), dinv);
         return fmaxf(__fsub_rn(p, q), 0.f);
+    }
+    // two powers about m, rounded as power() rounds one
+    static __device__ __forceinline__ f32x2 powers(const RowRule& rule, float a, float b, float m) {
+        unpack2(mul2(sub2(pack2(a, b), pack2(m, m)), pack2(rule.slope, rule.slope)), a, b);
+        return pack2(fmaxf(exp2_unit(a), 0.f), fmaxf(exp2_unit(b), 0.f));
+    }
+    // The weights of a lane's eight logits of chunk q; q(one) = 1 leaves nothing.
+    __device__ __forceinline__ WeightSum eight(const float (&z)[8], const float (&zd)[8], bool spread, int q, int lane,
+                                               bool along) const {
+        WeightSum ws;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            f32x2 e = powers(target, z[i], z[i + 1], m);
+            if (rest) {
+                e = mul2(e, pack2(inv, inv));
+                if (spread) {
+                    e = sub2(e, mul2(powers(draft, zd[i], zd[i + 1], dm), pack2(dinv, dinv)));
+                    float a, b;
+                    unpack2(e, a, b);
+                    e = pack2(fmaxf(a, 0.f), fmaxf(b, 0.f));
+                } else if (one >= 0 && q == one / kChunk) {
+                    float a, b;
+                    unpack2(e, a, b);
+                    const int v0 = RowReader::place(q, lane, i, along), v1 = RowReader::place(q, lane, i + 1, along);
+                    e = pack2(v0 == one ? 0.f : a, v1 == one ? 0.f : b);
+                }
+            }
+            ws.add(e);
+        }
+        return ws;
     }
 };
 
@@ -351,19 +436,21 @@ __device__ __forceinline__ float share_in(const Part& p, const RowRule& rule, fl
     return rule.power(z, p.m) / p.sum;
 }
 
-__global__ void __launch_bounds__(kVerifyThreads)
+__global__ void __launch_bounds__(kVerifyThreads, 3)
 verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Part* __restrict__ sums, Verdict out) {
     extern __shared__ __align__(16) unsigned char raw[];
     unsigned long long* chunks = reinterpret_cast<unsigned long long*>(raw);
     __shared__ DrawShared s;
-    grid_dependency_wait();
-    allow_dependent_launch();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const unsigned rank = cluster_rank(), blocks = cluster_size();
     const long long seq = blockIdx.x / blocks;
+    // What the call's caller wrote may be read before the wait: the kernel before
+    // this one let it start only once its own wait was over.
     const long long first = d.first[seq], end = d.first[seq + 1];
     const bool writes = rank == 0 && tid == 0;
     if (first < 0 || end < first || end > d.D || end > d.first[d.S]) {   // alike in all blocks
+        grid_dependency_wait();
+        allow_dependent_launch();
         if (writes) {
             flag_index_error();
             out.accepted[seq] = 0;
@@ -376,6 +463,7 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
     // the drafts before the first that is refused, a warp each
     const long long k = end - first;
     long long a = 0;
+    bool waited = false;   // for the rows' sums
     for (; a < k; a += kVerifyWarps) {
         const long long i = a + warp;
         bool refuse = false;
@@ -385,9 +473,11 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
             const int v = d.token[j];
             const bool known = v >= 0 && v < V;
             if (!known && rank == 0 && lane == 0) flag_index_error();
-            const float z = known ? reader.at(v) : BITLOGIC_NEG_INF;
+            const float z = known ? reader.at(v) : BITLOGIC_NEG_INF, u = d.u[j], q = d.logprob ? expf(d.logprob[j]) : 1.f;
+            if (!waited) grid_dependency_wait();
+            waited = true;
             const Part p = join_parts(sums + row * parts, parts, reader.rule, lane);
-            refuse = !(known && passes(d.u[j], d.logprob ? expf(d.logprob[j]) : 1.f, share_in(p, reader.rule, z, v)));
+            refuse = !(known && passes(u, q, share_in(p, reader.rule, z, v)));
         }
         if (lane == 0) s.refused[warp] = refuse;
         __syncthreads();
@@ -399,6 +489,8 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
             break;
         }
     }
+    if (!waited) grid_dependency_wait();
+    allow_dependent_launch();
     a = a < k ? a : k;
     const long long row = first + seq + a, j = first + a;
     const RowReader reader(target, row, V);
@@ -431,25 +523,43 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
             __syncthreads();
         }
     };
+    // two chunks of a warp at a time to `use`, of the target where `with_target` and
+    // of the draft where `with_draft`; what is not read is masked
+    const bool along = reader.aligned && (!spread || other.aligned);
+    auto each_chunk = [&](bool with_target, bool with_draft, auto&& use) {
+        for (int q = q0 + warp; q < q1; q += 2 * kVerifyWarps) {
+            const int q2 = q + kVerifyWarps;
+            const bool two = q2 < q1;
+            Raw a0, a1, b0, b1;
+            if (with_target) a0 = reader.load(q, lane, along);
+            if (with_draft) b0 = other.load(q, lane, along);
+            if (with_target && two) a1 = reader.load(q2, lane, along);
+            if (with_draft && two) b1 = other.load(q2, lane, along);
+            float z[8], zd[8];
+            if (with_target) reader.kept(a0, q, lane, along, z);
+            if (with_draft) other.kept(b0, q, lane, along, zd);
+            use(q, z, zd);
+            if (two) {
+                if (with_target) reader.kept(a1, q2, lane, along, z);
+                if (with_draft) other.kept(b1, q2, lane, along, zd);
+                use(q2, z, zd);
+            }
+        }
+    };
     // the chunks' weights into `chunks`; every thread gets the block's sum
     auto sum_chunks = [&](bool with_draft, float* draft_top) {
         unsigned long long mass = 0;
         float top = BITLOGIC_NEG_INF;
-        for (int q = q0 + warp; q < q1; q += kVerifyWarps) {
-            const int v0 = q * kChunk + 8 * lane;
-            float z[8], zd[8];
-            reader.load(v0, z);
-            if (with_draft) other.load(v0, zd);
-            WeightSum ws;
+        each_chunk(true, with_draft, [&](int q, const float (&z)[8], const float (&zd)[8]) {
+            const WeightSum ws = weigh.eight(z, zd, with_draft, q, lane, along);
+            if (draft_top && with_draft) {
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                ws.add(pack2(weigh(z[i], with_draft ? zd[i] : 0.f, v0 + i), weigh(z[i + 1], with_draft ? zd[i + 1] : 0.f, v0 + i + 1)));
-                if (with_draft) top = fmaxf(top, fmaxf(zd[i], zd[i + 1]));
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, zd[i]);
             }
             const unsigned long long w = ws.warp_total();
             if (lane == 0) chunks[q - q0] = w;
             mass += w;
-        }
+        });
         if (draft_top) *draft_top = block_largest(top, s.fbuf, kVerifyWarps);
         __syncthreads();
         if (lane == 0) s.warp_mass[warp] = mass;
@@ -480,16 +590,13 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
         }
         if (spread && weigh.dm > BITLOGIC_NEG_INF) {
             unsigned long long sum = 0;
-            for (int q = q0 + warp; q < q1; q += kVerifyWarps) {
-                const int v0 = q * kChunk + 8 * lane;
-                float zd[8];
-                other.load(v0, zd);
+            each_chunk(false, true, [&](int, const float (&)[8], const float (&zd)[8]) {
                 WeightSum ws;
 #pragma unroll
                 for (int i = 0; i < 8; i += 2)
-                    ws.add(pack2(weigh.draft.power(zd[i], weigh.dm), weigh.draft.power(zd[i + 1], weigh.dm)));
+                    ws.add(Weigher::powers(weigh.draft, zd[i], zd[i + 1], weigh.dm));
                 sum += ws.total();
-            }
+            });
             sum = block_add(sum, s.warp_mass, kVerifyWarps);
             if (tid < (int)blocks) put_in_block(&s.draft[rank], tid, DrawShared::Stats{sum, 0.f, 0u});
             barrier();
@@ -538,10 +645,11 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
     }
     __syncthreads();
     if (warp != 0) return;
-    const int v0 = s.chunk * kChunk + 8 * lane;
+    // side by side, so that lanes follow the order of classes
+    const int q = s.chunk, v0 = q * kChunk + 8 * lane;
     float z[8], zd[8];
-    reader.load(v0, z);
-    if (weigh.rest && spread) other.load(v0, zd);
+    reader.kept(reader.load(q, lane, true), q, lane, true, z);
+    if (weigh.rest && spread) other.kept(other.load(q, lane, true), q, lane, true, zd);
     unsigned long long w[8], sum = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -690,18 +798,18 @@ verify_narrow_kernel(Rows target, Rows draft, int V, Drafts d, Verdict out) {
     }
 }
 
-// Parts of a row: as many as keep two blocks on every SM, of at least 4 KB.
+// Parts of a row: as many as keep two to four blocks on every SM, of at least 4 KB.
 inline int row_parts(long long rows, int V, int element) {
     int parts = 1;
-    while (parts < kMaxParts && rows * parts <= sm_count() && (long long)V * element / (2 * parts) >= 4096) parts *= 2;
+    while (parts < kMaxParts && rows * parts <= 2 * sm_count() && (long long)V * element / (2 * parts) >= 4096) parts *= 2;
     return parts;
 }
 
-// Blocks of a sequence's draw: as many as the SMs have room for, of at least
-// 4096 classes.
+// Blocks of a sequence's draw: as many as keep up to eight on every SM, of at
+// least 2048 classes.
 inline int draw_blocks(long long S, int V) {
     int c = 1;
-    while (c < kMaxCluster && S * c * 2 <= sm_count() && V / (2 * c) >= 4096) c *= 2;
+    while (c < kMaxCluster && S * c * 2 <= 8 * sm_count() && V / (2 * c) >= 2048) c *= 2;
     return c;
 }
 
