@@ -1071,8 +1071,8 @@ def _rows(x: torch.Tensor, name: str, dtype: Optional[torch.dtype] = None, shape
         s = x.shape
         if s == shape if shape is not None else len(s) == 2:
             ld, inc = x.stride()
-            if inc == 1 and s[0] > 1:
-                return x.data_ptr(), ld
+            if inc == 1:
+                return x.data_ptr(), ld if s[0] > 1 or ld > s[1] else s[1]
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if x.dtype not in ROW_TYPES:
@@ -1117,6 +1117,23 @@ def bitlogic_dropout(x: torch.Tensor, out: torch.Tensor, counter: torch.Tensor, 
         _stream(stream)))
 
 
+def _byte_rows(x: torch.Tensor, name: str, shape) -> Tuple[int, int, int]:
+    """Address, row stride and form (bitlogic_bytes_t) of rows in 8 bits."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    form = BYTE_TYPES.get(x.dtype)
+    if form is None:
+        raise TypeError(f"{name}: expected one of {[str(t) for t in BYTE_TYPES]}, got {x.dtype}")
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be on a CUDA device")
+    if x.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(x.shape)}")
+    ld, inc = x.stride()
+    if inc == 1 and ld >= shape[1]:
+        return x.data_ptr(), ld, form
+    return x.data_ptr(), _row_stride(x, name), form
+
+
 def _norm_weight(weight: Optional[torch.Tensor], dtype: torch.dtype, d: int) -> Tuple[Optional[int], int]:
     if weight is None:
         return None, 0
@@ -1142,18 +1159,10 @@ def bitlogic_norm_bytes(x: torch.Tensor, out: torch.Tensor, scale: Optional[torc
     pr, ldr = _rows_or_none(residual, "residual", dtype, shape)
     pt, ldt = _rows_or_none(total, "total", dtype, shape)
     pw, wcode = _norm_weight(weight, dtype, d)
-    if not isinstance(out, torch.Tensor):
-        raise TypeError("out must be a torch.Tensor")
-    form = BYTE_TYPES.get(out.dtype)
-    if form is None:
-        raise TypeError(f"out: expected one of {[str(t) for t in BYTE_TYPES]}, got {out.dtype}")
-    if not out.is_cuda:
-        raise ValueError("out must be on a CUDA device")
-    if out.shape != shape:
-        raise ValueError(f"out: expected shape {tuple(shape)}, got {tuple(out.shape)}")
+    po, ldo, form = _byte_rows(out, "out", shape)
     group = int(group)
     _check("bitlogic_norm_bytes", load().bitlogic_norm_bytes(
-        px, ROW_TYPES[dtype], T, d, ldx, pr, ldr, pt, ldt, pw, wcode, float(eps), form, out.data_ptr(), _row_stride(out, "out"),
+        px, ROW_TYPES[dtype], T, d, ldx, pr, ldr, pt, ldt, pw, wcode, float(eps), form, po, ldo,
         _vector(scale, "scale", torch.float32, (T, -(-d // group) if group > 0 else 1)), group, float(fixed_scale),
         _stream(stream)))
 

@@ -10,6 +10,7 @@
 namespace bitlogic {
 
 // The loads do not go through the read-only path: an output may be the input.
+// load_once and store_once mark what L2 need not keep.
 template <typename T> struct Eight;
 
 template <> struct Eight<float> {
@@ -26,6 +27,10 @@ template <> struct Eight<float> {
         *reinterpret_cast<uint4*>(p) = a;
         *reinterpret_cast<uint4*>(p + 4) = b;
     }
+    __device__ __forceinline__ void store_once(float* p) const {
+        __stcs(reinterpret_cast<uint4*>(p), a);
+        __stcs(reinterpret_cast<uint4*>(p) + 1, b);
+    }
     __device__ __forceinline__ void get(float (&v)[8]) const {
         v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
         v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
@@ -40,6 +45,7 @@ template <> struct Eight<__nv_bfloat16> {
     __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint4*>(p); }
     __device__ __forceinline__ void load_once(const __nv_bfloat16* p) { a = __ldcs(reinterpret_cast<const uint4*>(p)); }
     __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = a; }
+    __device__ __forceinline__ void store_once(__nv_bfloat16* p) const { __stcs(reinterpret_cast<uint4*>(p), a); }
     static __device__ __forceinline__ void two(uint32_t u, float& x, float& y) {
         x = __uint_as_float(u << 16);
         y = __uint_as_float(u & 0xffff0000u);
@@ -63,6 +69,7 @@ template <> struct Eight<__half> {
     __device__ __forceinline__ void load(const __half* p) { a = *reinterpret_cast<const uint4*>(p); }
     __device__ __forceinline__ void load_once(const __half* p) { a = __ldcs(reinterpret_cast<const uint4*>(p)); }
     __device__ __forceinline__ void store(__half* p) const { *reinterpret_cast<uint4*>(p) = a; }
+    __device__ __forceinline__ void store_once(__half* p) const { __stcs(reinterpret_cast<uint4*>(p), a); }
     static __device__ __forceinline__ void two(uint32_t u, float& x, float& y) {
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u));
         x = f.x;
