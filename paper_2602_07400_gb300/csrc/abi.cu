@@ -37,6 +37,7 @@ extern "C" int bitlogic_internal_index_error_lut_codes(cudaStream_t);
 extern "C" int bitlogic_internal_index_error_lut_packed(cudaStream_t);
 extern "C" int bitlogic_internal_index_error_distill(cudaStream_t);
 extern "C" int bitlogic_internal_index_error_verify(cudaStream_t);
+extern "C" int bitlogic_internal_index_error_verify_draw(cudaStream_t);
 
 extern "C" const char* bitlogic_status_string(int code) {
     switch (code) {
@@ -107,7 +108,7 @@ extern "C" int bitlogic_degree_order(const int32_t* off_host, int32_t n, int32_t
 
 extern "C" int bitlogic_device_error(cudaStream_t stream) {
     int worst = BITLOGIC_OK;
-    const int r[12] = {bitlogic_internal_index_error_lut_soft(stream),
+    const int r[13] = {bitlogic_internal_index_error_lut_soft(stream),
                       bitlogic_internal_index_error_head(stream),
                       bitlogic_internal_index_error_encode(stream),
                       bitlogic_internal_index_error_hard(stream),
@@ -118,7 +119,8 @@ extern "C" int bitlogic_device_error(cudaStream_t stream) {
                       bitlogic_internal_index_error_lut_codes(stream),
                        bitlogic_internal_index_error_lut_packed(stream),
                       bitlogic_internal_index_error_distill(stream),
-                      bitlogic_internal_index_error_verify(stream)};
+                      bitlogic_internal_index_error_verify(stream),
+                      bitlogic_internal_index_error_verify_draw(stream)};
     for (int v : r) {
         if (v == BITLOGIC_ERR_CUDA) return v;
         if (v != BITLOGIC_OK) worst = v;

@@ -1,0 +1,112 @@
+// What the kernels of the draft check share (verify.cu, verify_draw.cu).
+#pragma once
+
+#include <cfloat>
+
+#include "row_tile.cuh"
+#include "weights.cuh"
+
+namespace bitlogic {
+
+constexpr int kVerifyThreads = 256, kVerifyWarps = kVerifyThreads / 32;
+constexpr int kMaxParts = 32;
+constexpr int kVerifyNarrow = 1024;   // classes of a row in a warp's registers
+constexpr int kChunk = 256;           // classes whose weights are summed together
+constexpr float kWhole = 1099511627776.0f;   // 2^40
+
+// A matrix of logits with the settings of its rows.
+struct Rows {
+    const void* x;
+    int dtype;
+    long long ld;
+    const float* temperature;
+    const float* floor;   // kept: z > floor, or z == floor up to class `last`
+    const int* last;
+};
+struct Drafts {
+    const int* first;        // [S + 1]
+    const int* token;        // [D]
+    const float* logprob;    // [D] or NULL: 0
+    const float* u;          // [D]
+    const float* draw_u;     // [S]
+    long long S, D;
+};
+struct Verdict {
+    int* accepted;
+    int* next_token;
+    float* logprob;
+};
+
+// The largest kept logit of a part of a row, the sum of the powers about it, and
+// the first class of that logit (in greedy rows and where it is +inf).
+struct Part {
+    float m, sum;
+    int cls, pad;
+};
+
+struct RowRule {
+    float slope, floor;
+    int last;
+    bool greedy;
+    __device__ __forceinline__ RowRule(const Rows& r, long long row) {
+        const float temp = r.temperature ? r.temperature[row] : 1.0f;
+        greedy = !(temp > 0.f);
+        slope = greedy ? 0.f : fminf((1.0f / temp) * kLog2E, FLT_MAX);
+        floor = r.floor ? r.floor[row] : BITLOGIC_NEG_INF;
+        last = r.last ? r.last[row] : -1;
+    }
+    __device__ __forceinline__ bool keeps(float z, int v) const { return z > floor || (z == floor && v <= last); }
+    __device__ __forceinline__ float kept(float z, int v) const { return keeps(z, v) ? z : BITLOGIC_NEG_INF; }
+    // e of a kept logit about m; 0 for -inf and NaN
+    __device__ __forceinline__ float power(float z, float m) const { return fmaxf(exp2_unit((z - m) * slope), 0.f); }
+};
+
+// u as the tests use it: 24 bits in [0, 1), NaN reads 0.
+__device__ __forceinline__ float unit_of(float u) { return u > 0.f ? floorf(fminf(u, 0.99999994f) * 16777216.0f) * 5.9604645e-08f : 0.f; }
+
+__device__ __forceinline__ bool passes(float u, float q, float p) { return unit_of(u) * q < p; }
+
+// The sum of v over the lanes below this one and itself.
+__device__ __forceinline__ unsigned long long lanes_upto(unsigned long long v, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long t = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += t;
+    }
+    return v;
+}
+
+// The kept logit of class v of a row of any type.
+__device__ __forceinline__ float kept_logit(const Rows& rows, const RowRule& rule, long long row, int v) {
+    const long long at = row * rows.ld + v;
+    float z;
+    switch (rows.dtype) {
+        case BITLOGIC_F32: z = static_cast<const float*>(rows.x)[at]; break;
+        case BITLOGIC_BF16: z = logit_value(static_cast<const __nv_bfloat16*>(rows.x)[at]); break;
+        case BITLOGIC_F16: z = logit_value(static_cast<const __half*>(rows.x)[at]); break;
+        default: z = logit_value(static_cast<const int*>(rows.x)[at]); break;
+    }
+    return rule.kept(z, v);
+}
+
+// What a row of the target and the draft refused there leave for the draw.
+struct Weigher {
+    RowRule target, draft;
+    float m, inv, dm, dinv;   // largest logits, and 2^40 / the sum of the weights
+    int one;                  // the class that q has all of, or -1
+    bool rest;                // max(0, p - q), or p's own weights
+
+    __device__ __forceinline__ float operator()(float z, float zd, int v) const {
+        const float e = target.power(z, m);
+        if (!rest) return e;
+        // no multiply-add: the differences are those of the rounded shares
+        const float p = __fmul_rn(e, inv), q = one >= 0 ? (v == one ? 1.f : 0.f) : __fmul_rn(draft.power(zd, dm), dinv);
+        return fmaxf(__fsub_rn(p, q), 0.f);
+    }
+};
+
+// The draw behind the accepted drafts of every sequence (verify_draw.cu).
+cudaError_t launch_verify_draw(const Rows& target, const Rows& draft, int V, const Drafts& d, int parts, const Part* sums,
+                               const Verdict& out, cudaStream_t stream);
+
+}  // namespace bitlogic

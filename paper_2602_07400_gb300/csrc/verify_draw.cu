@@ -1,0 +1,440 @@
+// The draw behind the accepted drafts: a sequence per block or cluster (verify.cu
+// has the mathematics).
+//
+// Once the refused draft is known, the target's row and the draft's come into the
+// shared memory of the sequence's blocks, a slice each, where they are gone over
+// three times: the target's weights and the draft's largest logit, the draft's
+// weights, and what max(0, p - q) leaves, by chunks of 256 classes; the chunk that
+// holds the draw is then looked at class by class.  Bound by instructions: some 30
+// for each class of a refused row.
+#include "verify.cuh"
+
+namespace bitlogic {
+namespace {
+
+// A chunk's logits are held eight to a lane.  Where both rows start on 16 bytes a
+// lane's classes are side by side (`along`) and come by vectors; else they lie 32
+// apart, so that the lanes of a load are side by side.
+__device__ __forceinline__ int place(int q, int lane, int i, bool along) { return q * kChunk + (along ? 8 * lane + i : 32 * i + lane); }
+
+// A block's part of a row, classes c0 to c1, in shared memory or where it is.
+template <typename T>
+struct Slice {
+    static constexpr int N = Piece<T>::N;
+    const T* at;     // of class 0, in whichever memory
+    const T* x;      // the row
+    int V;
+    bool aligned, cut;
+    RowRule rule;
+
+    __device__ __forceinline__ Slice(const Rows& rows, long long row, int V_)
+        : at(static_cast<const T*>(rows.x) + row * rows.ld), x(at), V(V_), aligned((reinterpret_cast<uintptr_t>(x) & 15u) == 0),
+          rule(rows, row) {
+        cut = !(rule.floor == BITLOGIC_NEG_INF);
+    }
+    // Copies to `tile`; finish with cp_async_wait<0>() and a barrier.
+    __device__ __forceinline__ void copy(T* tile, int c0, int c1, int tid) {
+        const int shift = (int)((reinterpret_cast<uintptr_t>(x + c0) & 15u) / sizeof(T)), first = c0 - shift;   // class of the first place
+        const int n = c1 > c0 ? (shift + c1 - c0 + N - 1) / N : 0;
+        const T* from = x + first;   // read at whole pieces only
+        for (int j = tid; j < n; j += kVerifyThreads) {
+            const int v = first + j * N;
+            if (v >= 0 && v + N <= V) {
+                cp_async16(tile + j * N, from + j * N);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (v + i >= 0 && v + i < V) tile[j * N + i] = x[v + i];
+            }
+        }
+        at = tile - first;
+    }
+    // the kept logits of chunk q; -inf for what is not kept and past the row's end
+    __device__ __forceinline__ void load(int q, int lane, bool along, float (&z)[8]) const {
+        const bool full = (q + 1) * kChunk <= V;
+        if (along && full) {
+            const uint4* p = reinterpret_cast<const uint4*>(at + q * kChunk + 8 * lane);
+            float part[N];
+#pragma unroll
+            for (int h = 0; h < 8 / N; ++h) {
+                Piece<T>::load(p[h], part);
+#pragma unroll
+                for (int i = 0; i < N; ++i) z[h * N + i] = part[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int v = place(q, lane, i, along);
+                z[i] = v < V ? logit_value(at[v]) : BITLOGIC_NEG_INF;
+            }
+        }
+        if (cut) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = rule.kept(z[i], place(q, lane, i, along));
+        }
+    }
+};
+
+// WeightSum (weights.cuh) of eight weights a lane, the offsets of the floats' bits
+// taken off a warp's sum at once.
+struct EightSum {
+    uint32_t high = 0, low = 0;
+    __device__ __forceinline__ void add(f32x2 e) {
+        const f32x2 c16 = pack2(16.0f, 16.0f), scale = pack2(kWhole, kWhole), whole = pack2(12582912.0f, 12582912.0f);
+        const f32x2 t = add2(e, c16), u = fma2(sub2(e, sub2(t, c16)), scale, whole);
+        float a, b;
+        unpack2(t, a, b);
+        high += __float_as_uint(a) + __float_as_uint(b);
+        unpack2(u, a, b);
+        low += __float_as_uint(a) + __float_as_uint(b);
+    }
+    __device__ __forceinline__ unsigned long long warp_total() const {
+        WeightSum s;
+        s.high = __reduce_add_sync(0xffffffffu, high) - 256u * 0x41800000u;
+        s.low = __reduce_add_sync(0xffffffffu, low) - 256u * 0x4b400000u;
+        return s.total();
+    }
+};
+
+// Two powers about m, rounded as RowRule::power rounds one.
+__device__ __forceinline__ f32x2 two_powers(const RowRule& rule, float a, float b, float m) {
+    unpack2(mul2(sub2(pack2(a, b), pack2(m, m)), pack2(rule.slope, rule.slope)), a, b);
+    return pack2(fmaxf(exp2_unit(a), 0.f), fmaxf(exp2_unit(b), 0.f));
+}
+
+struct DrawShared {
+    struct Stats {
+        unsigned long long mass;
+        float m;
+        unsigned pad;
+    } target[kMaxCluster], draft[kMaxCluster];
+    struct Mass {
+        unsigned long long mass;
+    } rest[kMaxCluster];
+    unsigned long long warp_mass[kVerifyWarps];
+    float fbuf[kVerifyWarps];
+    int refused[kVerifyWarps];
+    int chunk;
+    unsigned long long before;
+};
+
+// The parts of a row joined, in order, by a warp; every lane gets the result.
+__device__ __forceinline__ Part join_parts(const Part* parts, int n, const RowRule& rule, int lane) {
+    Part p = {BITLOGIC_NEG_INF, 0.f, INT_MAX, 0};
+    if (lane < n) p = parts[lane];
+    const float m = warp_largest(p.m);
+    float sum = p.m > BITLOGIC_NEG_INF && !rule.greedy && m <= FLT_MAX ? p.sum * exp2_unit((p.m - m) * rule.slope) : 0.f;
+    sum = warp_add(sum);
+    const int cls = (int)__reduce_min_sync(0xffffffffu, p.m == m ? (unsigned)p.cls : (unsigned)INT_MAX);
+    return {m, sum, cls, 0};
+}
+
+// The target's probability of class v.
+__device__ __forceinline__ float share_in(const Part& p, const RowRule& rule, float z, int v) {
+    if (!(p.m > BITLOGIC_NEG_INF)) return 0.f;
+    if (rule.greedy || p.m > FLT_MAX) return v == p.cls ? 1.f : 0.f;
+    return rule.power(z, p.m) / p.sum;
+}
+
+// Shared memory behind the chunks' weights: the slices of both rows, of any
+// alignment.
+__host__ __device__ __forceinline__ size_t tile_offset(int chunks) { return ((size_t)chunks * 8 + 15) / 16 * 16; }
+__host__ __device__ __forceinline__ size_t tile_bytes(int chunks, int element) { return (size_t)chunks * kChunk * element + 32; }
+
+template <typename T, typename Q>
+__global__ void __launch_bounds__(kVerifyThreads, 3)
+verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Part* __restrict__ sums, Verdict out, bool tiled) {
+    extern __shared__ __align__(16) unsigned char raw[];
+    unsigned long long* chunks = reinterpret_cast<unsigned long long*>(raw);
+    __shared__ DrawShared s;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const unsigned rank = cluster_rank(), blocks = cluster_size();
+    const long long seq = blockIdx.x / blocks;
+    // What the call's caller wrote may be read before the wait: the kernel before
+    // this one let it start only once its own wait was over.
+    const long long first = d.first[seq], end = d.first[seq + 1];
+    const bool writes = rank == 0 && tid == 0;
+    if (first < 0 || end < first || end > d.D || end > d.first[d.S]) {   // alike in all blocks
+        grid_dependency_wait();
+        allow_dependent_launch();
+        if (writes) {
+            flag_index_error();
+            out.accepted[seq] = 0;
+            out.next_token[seq] = -1;
+            if (out.logprob) out.logprob[seq] = BITLOGIC_NEG_INF;
+        }
+        return;
+    }
+    report_running(blocks);
+    // the drafts before the first that is refused, a warp each
+    const long long k = end - first;
+    long long a = 0;
+    bool waited = false;   // for the rows' sums
+    for (; a < k; a += kVerifyWarps) {
+        const long long i = a + warp;
+        bool refuse = false;
+        if (i < k) {
+            const long long j = first + i, row = j + seq;
+            const RowRule rule(target, row);
+            const int v = d.token[j];
+            const bool known = v >= 0 && v < V;
+            if (!known && rank == 0 && lane == 0) flag_index_error();
+            const float z = known ? kept_logit(target, rule, row, v) : BITLOGIC_NEG_INF, u = d.u[j], q = d.logprob ? expf(d.logprob[j]) : 1.f;
+            if (!waited) grid_dependency_wait();
+            waited = true;
+            const Part p = join_parts(sums + row * parts, parts, rule, lane);
+            refuse = !(known && passes(u, q, share_in(p, rule, z, v)));
+        }
+        if (lane == 0) s.refused[warp] = refuse;
+        __syncthreads();
+        int w = 0;
+        while (w < kVerifyWarps && !s.refused[w]) ++w;
+        __syncthreads();
+        if (w < kVerifyWarps) {
+            a += w;
+            break;
+        }
+    }
+    if (!waited) grid_dependency_wait();
+    allow_dependent_launch();
+    a = a < k ? a : k;
+    const long long row = first + seq + a, j = first + a;
+    Slice<T> mine_t(target, row, V);
+    const Part p = join_parts(sums + row * parts, parts, mine_t.rule, lane);
+    if (writes) out.accepted[seq] = (int)a;
+    const bool sure = mine_t.rule.greedy || !(p.m > BITLOGIC_NEG_INF) || p.m > FLT_MAX;
+    if (sure) {   // one class, or none; alike in all blocks
+        if (writes) {
+            const bool none = !(p.m > BITLOGIC_NEG_INF);
+            out.next_token[seq] = none ? -1 : p.cls;
+            if (out.logprob) out.logprob[seq] = none ? BITLOGIC_NEG_INF : 0.f;
+        }
+        wait_all_running(blocks);
+        return;
+    }
+    const bool refused = a < k;
+    Slice<Q> mine_q(draft.x && refused ? draft : target, draft.x && refused ? j : row, V);   // not read unless it is the draft's
+    Weigher weigh = {mine_t.rule, mine_q.rule, p.m, 0.f, 0.f, 0.f, -1, false};
+    if (refused && (!draft.x || mine_q.rule.greedy)) weigh.one = d.token[j];
+    bool spread = refused && draft.x && !mine_q.rule.greedy;   // q is over the draft's row
+
+    // the block's chunks of the row, a warp each in turn
+    const int all = (V + kChunk - 1) / kChunk, per = (all + (int)blocks - 1) / (int)blocks;
+    const int q0 = min(all, (int)rank * per), q1 = min(all, q0 + per);
+    auto barrier = [&]() {
+        if (blocks > 1) {
+            cluster_arrive();
+            cluster_wait();
+        } else {
+            __syncthreads();
+        }
+    };
+    const bool along = mine_t.aligned && (!spread || mine_q.aligned);
+    if (tiled) {
+        T* tile = reinterpret_cast<T*>(raw + tile_offset(per));
+        const int c0 = q0 * kChunk, c1 = min(V, q1 * kChunk);
+        mine_t.copy(tile, c0, c1, tid);
+        if (spread) mine_q.copy(reinterpret_cast<Q*>(raw + tile_offset(per) + tile_bytes(per, sizeof(T))), c0, c1, tid);
+        cp_async_commit();
+        cp_async_wait<0>();
+        __syncthreads();
+    }
+    // the chunks' weights into `chunks`; every thread gets the block's sum
+    auto sum_chunks = [&](bool with_draft, float* draft_top) {
+        unsigned long long mass = 0;
+        float top = BITLOGIC_NEG_INF;
+        for (int q = q0 + warp; q < q1; q += kVerifyWarps) {
+            float z[8], zd[8];
+            mine_t.load(q, lane, along, z);
+            if (with_draft) mine_q.load(q, lane, along, zd);
+            EightSum ws;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                f32x2 e = two_powers(mine_t.rule, z[i], z[i + 1], weigh.m);
+                if (weigh.rest) {
+                    e = mul2(e, pack2(weigh.inv, weigh.inv));
+                    float a, b;
+                    if (with_draft) {
+                        e = sub2(e, mul2(two_powers(mine_q.rule, zd[i], zd[i + 1], weigh.dm), pack2(weigh.dinv, weigh.dinv)));
+                        unpack2(e, a, b);
+                        e = pack2(fmaxf(a, 0.f), fmaxf(b, 0.f));
+                    } else if (weigh.one >= 0 && q == weigh.one / kChunk) {   // q(one) = 1 leaves nothing
+                        unpack2(e, a, b);
+                        e = pack2(place(q, lane, i, along) == weigh.one ? 0.f : a, place(q, lane, i + 1, along) == weigh.one ? 0.f : b);
+                    }
+                }
+                ws.add(e);
+            }
+            if (draft_top && with_draft) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, zd[i]);
+            }
+            const unsigned long long w = ws.warp_total();
+            if (lane == 0) chunks[q - q0] = w;
+            mass += w;
+        }
+        if (draft_top) *draft_top = block_largest(top, s.fbuf, kVerifyWarps);
+        __syncthreads();
+        if (lane == 0) s.warp_mass[warp] = mass;
+        __syncthreads();
+        unsigned long long t = 0;
+        for (int w = 0; w < kVerifyWarps; ++w) t += s.warp_mass[w];
+        return t;
+    };
+
+    // p's own weights, and the draft's largest logit
+    float top = BITLOGIC_NEG_INF;
+    unsigned long long mine = sum_chunks(spread, &top);
+    wait_all_running(blocks);
+    if (tid < (int)blocks) put_in_block(&s.target[rank], tid, DrawShared::Stats{mine, top, 0u});
+    barrier();
+    unsigned long long mass = 0, before = 0;
+    for (unsigned b = 0; b < blocks; ++b) {
+        if (b == rank) before = mass;
+        mass += s.target[b].mass;
+        weigh.dm = b == 0 ? s.target[b].m : fmaxf(weigh.dm, s.target[b].m);
+    }
+    const unsigned long long whole = mass;
+    if (refused) {
+        weigh.inv = kWhole / (float)whole;
+        if (spread && weigh.dm > FLT_MAX) {   // a draft of +inf: all of q is on the class drawn
+            weigh.one = d.token[j];
+            spread = false;
+        }
+        if (spread && weigh.dm > BITLOGIC_NEG_INF) {
+            unsigned long long sum = 0;
+            for (int q = q0 + warp; q < q1; q += kVerifyWarps) {
+                float zd[8];
+                mine_q.load(q, lane, along, zd);
+                EightSum ws;
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) ws.add(two_powers(mine_q.rule, zd[i], zd[i + 1], weigh.dm));
+                sum += ws.warp_total();
+            }
+            sum = lane == 0 ? sum : 0ull;
+            sum = block_add(sum, s.warp_mass, kVerifyWarps);
+            if (tid < (int)blocks) put_in_block(&s.draft[rank], tid, DrawShared::Stats{sum, 0.f, 0u});
+            barrier();
+            unsigned long long t = 0;
+            for (unsigned b = 0; b < blocks; ++b) t += s.draft[b].mass;
+            weigh.dinv = kWhole / (float)t;
+        }   // a draft without classes: q is 0
+        if (spread && !(weigh.dm > BITLOGIC_NEG_INF)) weigh.dm = 0.f;
+        weigh.rest = true;
+        mine = sum_chunks(spread, nullptr);
+        if (tid < (int)blocks) put_in_block(&s.rest[rank], tid, DrawShared::Mass{mine});
+        barrier();
+        mass = before = 0;
+        for (unsigned b = 0; b < blocks; ++b) {
+            if (b == rank) before = mass;
+            mass += s.rest[b].mass;
+        }
+        if (mass == 0) {   // p and q differ by less than their roundings
+            weigh.rest = false;
+            mine = sum_chunks(false, nullptr);
+            for (unsigned b = 0; b < blocks; ++b) {
+                if (b == rank) before = mass;
+                mass += s.target[b].mass;
+            }
+        }
+    }
+    const unsigned long long goal = share_of(mass, unit_of(d.draw_u[seq]));
+    if (goal < before || goal >= before + mine) return;   // another block's
+
+    // the chunk that holds the draw: a run of chunks per thread
+    const int n = q1 - q0, run = (n + kVerifyThreads - 1) / kVerifyThreads;
+    const int i0 = min(n, tid * run), i1 = min(n, i0 + run);
+    unsigned long long own = 0;
+    for (int i = i0; i < i1; ++i) own += chunks[i];
+    const unsigned long long upto = lanes_upto(own, lane);
+    __syncthreads();
+    if (lane == 31) s.warp_mass[warp] = upto;
+    __syncthreads();
+    unsigned long long at = before + upto - own;
+    for (int w = 0; w < warp; ++w) at += s.warp_mass[w];
+    if (goal >= at && goal < at + own) {
+        int i = i0;
+        while (goal >= at + chunks[i]) at += chunks[i++];
+        s.chunk = q0 + i;
+        s.before = at;
+    }
+    __syncthreads();
+    if (warp != 0) return;
+    // side by side, so that lanes follow the order of classes
+    const int q = s.chunk, v0 = q * kChunk + 8 * lane;
+    float z[8], zd[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        z[i] = v0 + i < V ? mine_t.rule.kept(logit_value(mine_t.at[v0 + i]), v0 + i) : BITLOGIC_NEG_INF;
+        zd[i] = weigh.rest && spread && v0 + i < V ? mine_q.rule.kept(logit_value(mine_q.at[v0 + i]), v0 + i) : BITLOGIC_NEG_INF;
+    }
+    unsigned long long w[8], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        w[i] = draw_weight(weigh(z[i], zd[i], v0 + i));
+        sum += w[i];
+    }
+    unsigned long long at_lane = s.before + lanes_upto(sum, lane) - sum;
+    if (goal < at_lane || goal >= at_lane + sum) return;
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        at_lane += w[i];
+        if (!found && at_lane > goal) {
+            found = true;
+            out.next_token[seq] = v0 + i;
+            if (out.logprob) out.logprob[seq] = logf((float)draw_weight(mine_t.rule.power(z[i], p.m)) / (float)whole);
+        }
+    }
+}
+
+// Blocks of a sequence's draw: slices of 16384 classes (64 KB of two bf16 rows, three
+// blocks on an SM), and with few sequences as many as the SMs have room for, of at
+// least 2048.
+inline int draw_blocks(long long S, int V) {
+    int c = 1;
+    while (c < kMaxCluster && (V / c > 16384 || (S * c * 2 <= 4 * sm_count() && V / (2 * c) >= 2048))) c *= 2;
+    return c;
+}
+
+constexpr size_t kDrawShared = 200 * 1024;
+
+template <typename T, typename Q>
+cudaError_t launch_draw(const Rows& target, const Rows& draft, int V, const Drafts& d, int parts, const Part* sums, const Verdict& out,
+                        cudaStream_t stream) {
+    const int blocks = draw_blocks(d.S, V), all = (V + kChunk - 1) / kChunk, per = (all + blocks - 1) / blocks;
+    const size_t tiles = tile_offset(per) + tile_bytes(per, sizeof(T)) + (draft.x ? tile_bytes(per, sizeof(Q)) : 0);
+    const bool tiled = tiles <= kDrawShared;
+    return launch_rows(verify_draw_kernel<T, Q>, d.S, blocks, kVerifyThreads, tiled ? tiles : (size_t)per * 8, kDrawShared, stream, target,
+                       draft, V, d, parts, sums, out, tiled);
+}
+
+template <typename T>
+cudaError_t launch_draw_of(const Rows& target, const Rows& draft, int V, const Drafts& d, int parts, const Part* sums, const Verdict& out,
+                           cudaStream_t stream) {
+    if (!draft.x) return launch_draw<T, T>(target, draft, V, d, parts, sums, out, stream);
+    switch (draft.dtype) {
+        case BITLOGIC_F32: return launch_draw<T, float>(target, draft, V, d, parts, sums, out, stream);
+        case BITLOGIC_BF16: return launch_draw<T, __nv_bfloat16>(target, draft, V, d, parts, sums, out, stream);
+        case BITLOGIC_F16: return launch_draw<T, __half>(target, draft, V, d, parts, sums, out, stream);
+        default: return launch_draw<T, int>(target, draft, V, d, parts, sums, out, stream);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_verify_draw(const Rows& target, const Rows& draft, int V, const Drafts& d, int parts, const Part* sums,
+                               const Verdict& out, cudaStream_t stream) {
+    switch (target.dtype) {
+        case BITLOGIC_F32: return launch_draw_of<float>(target, draft, V, d, parts, sums, out, stream);
+        case BITLOGIC_BF16: return launch_draw_of<__nv_bfloat16>(target, draft, V, d, parts, sums, out, stream);
+        case BITLOGIC_F16: return launch_draw_of<__half>(target, draft, V, d, parts, sums, out, stream);
+        default: return launch_draw_of<int>(target, draft, V, d, parts, sums, out, stream);
+    }
+}
+
+}  // namespace bitlogic
+
+using namespace bitlogic;
+
+BITLOGIC_ERROR_READER(verify_draw)
