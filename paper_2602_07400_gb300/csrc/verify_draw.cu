@@ -49,7 +49,16 @@ struct Slice {
         }
         at = tile - first;
     }
-    // the kept logits of chunk q; -inf for what is not kept and past the row's end
+    // Masks what is not kept of classes c0 to c1 in the tile; copied and with a
+    // barrier before and behind.
+    __device__ __forceinline__ void mask(int c0, int c1, int tid) const {
+        T* own = const_cast<T*>(at);
+        for (int v = c0 + tid; v < c1; v += kVerifyThreads)
+            if (!rule.keeps(logit_value(own[v]), v)) own[v] = masked_logit<T>();
+    }
+    // the kept logits of chunk q (kMasked: what is not kept is masked already); -inf
+    // past the row's end
+    template <bool kMasked>
     __device__ __forceinline__ void load(int q, int lane, bool along, float (&z)[8]) const {
         const bool full = (q + 1) * kChunk <= V;
         if (along && full) {
@@ -68,7 +77,7 @@ struct Slice {
                 z[i] = v < V ? logit_value(at[v]) : BITLOGIC_NEG_INF;
             }
         }
-        if (cut) {
+        if (!kMasked) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) z[i] = rule.kept(z[i], place(q, lane, i, along));
         }
@@ -113,19 +122,26 @@ struct DrawShared {
     } rest[kMaxCluster];
     unsigned long long warp_mass[kVerifyWarps];
     float fbuf[kVerifyWarps];
-    int refused[kVerifyWarps];
+    int stop;                              // the first draft refused
+    struct {
+        float m;
+        int cls;
+    } row[kVerifyThreads];                 // of a round's rows
     int chunk;
     unsigned long long before;
 };
 
-// The parts of a row joined, in order, by a warp; every lane gets the result.
-__device__ __forceinline__ Part join_parts(const Part* parts, int n, const RowRule& rule, int lane) {
-    Part p = {BITLOGIC_NEG_INF, 0.f, INT_MAX, 0};
-    if (lane < n) p = parts[lane];
-    const float m = warp_largest(p.m);
-    float sum = p.m > BITLOGIC_NEG_INF && !rule.greedy && m <= FLT_MAX ? p.sum * exp2_unit((p.m - m) * rule.slope) : 0.f;
-    sum = warp_add(sum);
-    const int cls = (int)__reduce_min_sync(0xffffffffu, p.m == m ? (unsigned)p.cls : (unsigned)INT_MAX);
+// The parts of a row joined by as many neighbouring lanes (a power of two of them);
+// each gets the result.
+__device__ __forceinline__ Part join_parts(const Part& own, int parts, const RowRule& rule) {
+    float m = own.m;
+    for (int o = parts >> 1; o > 0; o >>= 1) m = fmaxf(m, shuffle_xor(m, o));
+    float sum = own.m > BITLOGIC_NEG_INF && !rule.greedy && m <= FLT_MAX ? own.sum * exp2_unit((own.m - m) * rule.slope) : 0.f;
+    int cls = own.m == m ? own.cls : INT_MAX;
+    for (int o = parts >> 1; o > 0; o >>= 1) {
+        sum += shuffle_xor(sum, o);
+        cls = min(cls, shuffle_xor(cls, o));
+    }
     return {m, sum, cls, 0};
 }
 
@@ -141,9 +157,9 @@ __device__ __forceinline__ float share_in(const Part& p, const RowRule& rule, fl
 __host__ __device__ __forceinline__ size_t tile_offset(int chunks) { return ((size_t)chunks * 8 + 15) / 16 * 16; }
 __host__ __device__ __forceinline__ size_t tile_bytes(int chunks, int element) { return (size_t)chunks * kChunk * element + 32; }
 
-template <typename T, typename Q>
+template <typename T, typename Q, bool kTiled>
 __global__ void __launch_bounds__(kVerifyThreads, 3)
-verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Part* __restrict__ sums, Verdict out, bool tiled) {
+verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Part* __restrict__ sums, Verdict out) {
     extern __shared__ __align__(16) unsigned char raw[];
     unsigned long long* chunks = reinterpret_cast<unsigned long long*>(raw);
     __shared__ DrawShared s;
@@ -166,41 +182,44 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
         return;
     }
     report_running(blocks);
-    // the drafts before the first that is refused, a warp each
+    // the drafts before the first that is refused: a row by `parts` lanes, as many as
+    // the block has at a time
     const long long k = end - first;
-    long long a = 0;
+    const int round = kVerifyThreads / parts;
+    long long a = k, base = 0;
     bool waited = false;   // for the rows' sums
-    for (; a < k; a += kVerifyWarps) {
-        const long long i = a + warp;
-        bool refuse = false;
-        if (i < k) {
-            const long long j = first + i, row = j + seq;
+    for (;; base += round) {
+        const long long i = base + tid / parts;   // the row behind the last draft is among them
+        if (tid == 0) s.stop = kVerifyThreads;
+        __syncthreads();
+        if (base + (tid & ~31) / parts <= k) {    // alike in a warp
+            const bool real = i <= k, test = i < k;
+            const long long j = first + i, row = first + seq + (real ? i : 0);
             const RowRule rule(target, row);
-            const int v = d.token[j];
+            const int v = test ? d.token[j] : -1;
             const bool known = v >= 0 && v < V;
-            if (!known && rank == 0 && lane == 0) flag_index_error();
-            const float z = known ? kept_logit(target, rule, row, v) : BITLOGIC_NEG_INF, u = d.u[j], q = d.logprob ? expf(d.logprob[j]) : 1.f;
+            const bool leads = (tid & (parts - 1)) == 0;
+            const float z = known ? kept_logit(target, rule, row, v) : BITLOGIC_NEG_INF, u = test ? d.u[j] : 0.f,
+                        q = test && d.logprob ? expf(d.logprob[j]) : 1.f;
             if (!waited) grid_dependency_wait();
             waited = true;
-            const Part p = join_parts(sums + row * parts, parts, rule, lane);
-            refuse = !(known && passes(u, q, share_in(p, rule, z, v)));
+            const Part p = join_parts(sums[row * parts + (tid & (parts - 1))], parts, rule);
+            if (leads && real) s.row[tid / parts] = {p.m, p.cls};
+            if (leads && test) {
+                if (!known && rank == 0) flag_index_error();
+                if (!(known && passes(u, q, share_in(p, rule, z, v)))) atomicMin(&s.stop, tid / parts);
+            }
         }
-        if (lane == 0) s.refused[warp] = refuse;
         __syncthreads();
-        int w = 0;
-        while (w < kVerifyWarps && !s.refused[w]) ++w;
+        if (s.stop < kVerifyThreads) a = base + s.stop;
+        if (a < base + round) break;   // refused here, or the last row is here
         __syncthreads();
-        if (w < kVerifyWarps) {
-            a += w;
-            break;
-        }
     }
     if (!waited) grid_dependency_wait();
     allow_dependent_launch();
-    a = a < k ? a : k;
     const long long row = first + seq + a, j = first + a;
     Slice<T> mine_t(target, row, V);
-    const Part p = join_parts(sums + row * parts, parts, mine_t.rule, lane);
+    const Part p = {s.row[a - base].m, 0.f, s.row[a - base].cls, 0};
     if (writes) out.accepted[seq] = (int)a;
     const bool sure = mine_t.rule.greedy || !(p.m > BITLOGIC_NEG_INF) || p.m > FLT_MAX;
     if (sure) {   // one class, or none; alike in all blocks
@@ -230,7 +249,7 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
         }
     };
     const bool along = mine_t.aligned && (!spread || mine_q.aligned);
-    if (tiled) {
+    if (kTiled) {
         T* tile = reinterpret_cast<T*>(raw + tile_offset(per));
         const int c0 = q0 * kChunk, c1 = min(V, q1 * kChunk);
         mine_t.copy(tile, c0, c1, tid);
@@ -238,34 +257,42 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
         cp_async_commit();
         cp_async_wait<0>();
         __syncthreads();
+        if (mine_t.cut || (spread && mine_q.cut)) {   // alike in all blocks
+            if (mine_t.cut) mine_t.mask(c0, c1, tid);
+            if (spread && mine_q.cut) mine_q.mask(c0, c1, tid);
+            __syncthreads();
+        }
     }
     // the chunks' weights into `chunks`; every thread gets the block's sum
-    auto sum_chunks = [&](bool with_draft, float* draft_top) {
+    using Yes = std::true_type;
+    using No = std::false_type;
+    auto sum_chunks = [&](auto rest, auto with_draft, float* draft_top) {
+        constexpr bool kRest = decltype(rest)::value, kDraft = decltype(with_draft)::value;
         unsigned long long mass = 0;
         float top = BITLOGIC_NEG_INF;
         for (int q = q0 + warp; q < q1; q += kVerifyWarps) {
             float z[8], zd[8];
-            mine_t.load(q, lane, along, z);
-            if (with_draft) mine_q.load(q, lane, along, zd);
+            mine_t.template load<kTiled>(q, lane, along, z);
+            if (kDraft) mine_q.template load<kTiled>(q, lane, along, zd);
             EightSum ws;
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
                 f32x2 e = two_powers(mine_t.rule, z[i], z[i + 1], weigh.m);
-                if (weigh.rest) {
+                if (kRest) {
                     e = mul2(e, pack2(weigh.inv, weigh.inv));
                     float a, b;
-                    if (with_draft) {
+                    if (kDraft) {
                         e = sub2(e, mul2(two_powers(mine_q.rule, zd[i], zd[i + 1], weigh.dm), pack2(weigh.dinv, weigh.dinv)));
                         unpack2(e, a, b);
                         e = pack2(fmaxf(a, 0.f), fmaxf(b, 0.f));
-                    } else if (weigh.one >= 0 && q == weigh.one / kChunk) {   // q(one) = 1 leaves nothing
+                    } else {   // q(one) = 1 leaves nothing
                         unpack2(e, a, b);
                         e = pack2(place(q, lane, i, along) == weigh.one ? 0.f : a, place(q, lane, i + 1, along) == weigh.one ? 0.f : b);
                     }
                 }
                 ws.add(e);
             }
-            if (draft_top && with_draft) {
+            if (!kRest && kDraft) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) top = fmaxf(top, zd[i]);
             }
@@ -284,7 +311,7 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
 
     // p's own weights, and the draft's largest logit
     float top = BITLOGIC_NEG_INF;
-    unsigned long long mine = sum_chunks(spread, &top);
+    unsigned long long mine = spread ? sum_chunks(No(), Yes(), &top) : sum_chunks(No(), No(), &top);
     wait_all_running(blocks);
     if (tid < (int)blocks) put_in_block(&s.target[rank], tid, DrawShared::Stats{mine, top, 0u});
     barrier();
@@ -305,7 +332,7 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
             unsigned long long sum = 0;
             for (int q = q0 + warp; q < q1; q += kVerifyWarps) {
                 float zd[8];
-                mine_q.load(q, lane, along, zd);
+                mine_q.template load<kTiled>(q, lane, along, zd);
                 EightSum ws;
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) ws.add(two_powers(mine_q.rule, zd[i], zd[i + 1], weigh.dm));
@@ -321,7 +348,7 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
         }   // a draft without classes: q is 0
         if (spread && !(weigh.dm > BITLOGIC_NEG_INF)) weigh.dm = 0.f;
         weigh.rest = true;
-        mine = sum_chunks(spread, nullptr);
+        mine = spread ? sum_chunks(Yes(), Yes(), nullptr) : sum_chunks(Yes(), No(), nullptr);
         if (tid < (int)blocks) put_in_block(&s.rest[rank], tid, DrawShared::Mass{mine});
         barrier();
         mass = before = 0;
@@ -331,7 +358,7 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
         }
         if (mass == 0) {   // p and q differ by less than their roundings
             weigh.rest = false;
-            mine = sum_chunks(false, nullptr);
+            mine = sum_chunks(No(), No(), nullptr);
             for (unsigned b = 0; b < blocks; ++b) {
                 if (b == rank) before = mass;
                 mass += s.target[b].mass;
@@ -405,8 +432,8 @@ cudaError_t launch_draw(const Rows& target, const Rows& draft, int V, const Draf
     const int blocks = draw_blocks(d.S, V), all = (V + kChunk - 1) / kChunk, per = (all + blocks - 1) / blocks;
     const size_t tiles = tile_offset(per) + tile_bytes(per, sizeof(T)) + (draft.x ? tile_bytes(per, sizeof(Q)) : 0);
     const bool tiled = tiles <= kDrawShared;
-    return launch_rows(verify_draw_kernel<T, Q>, d.S, blocks, kVerifyThreads, tiled ? tiles : (size_t)per * 8, kDrawShared, stream, target,
-                       draft, V, d, parts, sums, out, tiled);
+    return launch_rows(tiled ? verify_draw_kernel<T, Q, true> : verify_draw_kernel<T, Q, false>, d.S, blocks, kVerifyThreads,
+                       tiled ? tiles : (size_t)per * 8, kDrawShared, stream, target, draft, V, d, parts, sums, out);
 }
 
 template <typename T>
