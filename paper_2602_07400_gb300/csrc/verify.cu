@@ -10,10 +10,10 @@
 // draft's draw, so of the draft's logits only the refused row is read; the
 // target's rows are read once.  Bound by that reading.
 //
-//   verify_sums_kernel    a row (or, where rows are few, a part of one) per
-//                         block: its largest logit and the sum of its powers
-//                         about it, in one pass: every thread keeps a running
-//                         maximum and rescales its sum when that rises
+//   verify_rows_kernel    a row (verify_parts_kernel, where rows are few: a part of
+//                         one) per block: its largest logit and the sum of its
+//                         powers about it, in one pass: every thread keeps a
+//                         running maximum and rescales its sum when that rises
 //   verify_draw_kernel    (verify_draw.cu) a sequence per block or cluster: the
 //                         accepted drafts from the rows' sums, then the draw in
 //                         whole-number weights, whose sums are exact in any order
@@ -26,19 +26,14 @@ namespace {
 
 // ------------------------------------------------------------ rows' sums --
 
+// Part `which` of `parts` of a row, by the whole block; every thread gets it.
 template <typename T>
-__global__ void __launch_bounds__(kVerifyThreads, 4)
-verify_sums_kernel(Rows rows, int V, Drafts d, int parts, Part* __restrict__ out) {
+__device__ __forceinline__ Part sum_part(const Rows& rows, long long row, int V, unsigned which, unsigned parts, Part* s) {
     using P = Piece<T>;
     constexpr int N = P::N, H = N / 2;
-    __shared__ Part s[kVerifyWarps];
-    grid_dependency_wait();
-    allow_dependent_launch();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const long long row = blockIdx.x / (unsigned)parts;
-    if (row >= (long long)d.first[d.S] + d.S) return;   // behind the last sequence
     const T* x = static_cast<const T*>(rows.x) + row * rows.ld;
-    const RowSlice<T> slice(x, V, blockIdx.x % (unsigned)parts, (unsigned)parts);
+    const RowSlice<T> slice(x, V, which, parts);
     const PieceStream<T, kVerifyThreads> stream(x, slice, V, tid);
     uint4 ua[4], ub[4];
     stream.load(0, ua);
@@ -187,7 +182,66 @@ verify_sums_kernel(Rows rows, int V, Drafts d, int parts, Part* __restrict__ out
         largest_class();
         join_block();
     }
-    if (tid == 0) out[blockIdx.x] = {m, sum, cls, 0};
+    return {m, sum, cls, 0};
+}
+
+// Rows in parts, where they are few; what the parts say of a draft is put together
+// by the draw.
+template <typename T>
+__global__ void __launch_bounds__(kVerifyThreads, 4)
+verify_parts_kernel(Rows rows, int V, Drafts d, int parts, Part* __restrict__ out) {
+    __shared__ Part s[kVerifyWarps];
+    grid_dependency_wait();
+    allow_dependent_launch();
+    const long long row = blockIdx.x / (unsigned)parts;
+    if (row >= (long long)d.first[d.S] + d.S) return;   // behind the last sequence
+    const Part p = sum_part<T>(rows, row, V, blockIdx.x % (unsigned)parts, (unsigned)parts, s);
+    if (threadIdx.x == 0) out[blockIdx.x] = p;
+}
+
+// Whole rows: block b takes row b / S of sequence b % S, and every `turns`-th one
+// behind it.  The row's draft is decided here (Part.refused), and where rows come
+// in several waves `stop` takes each sequence's first refused draft known so far:
+// the rows behind it say nothing about the outcome and are not read.  Whether a
+// block sees a refusal in time changes its work, never a result (256 x 7 drafts of
+// 131072 bf16 classes: XX us with all rows read, XX without those).
+template <typename T>
+__global__ void __launch_bounds__(kVerifyThreads, 4)
+verify_rows_kernel(Rows rows, int V, Drafts d, int turns, int* stop, Part* __restrict__ out) {
+    __shared__ Part s[kVerifyWarps];
+    grid_dependency_wait();
+    allow_dependent_launch();
+    const long long seq = blockIdx.x % (unsigned)d.S;
+    Places at;
+    if (!at.read(d, seq)) return;
+    for (long long i = blockIdx.x / (unsigned)d.S; i <= at.count; i += turns) {
+        __syncthreads();   // the buffers of the row before are free
+        if (stop) {
+            __shared__ int seen;
+            if (threadIdx.x == 0) seen = *(volatile int*)(stop + seq);
+            __syncthreads();
+            if (seen < i) return;
+        }
+        const long long row = at.first + seq + i, j = at.first + i;
+        Part p = sum_part<T>(rows, row, V, 0u, 1u, s);
+        if (threadIdx.x == 0) {
+            if (i < at.count) {
+                const RowRule rule(rows, row);
+                const int v = d.token[j];
+                const bool known = v >= 0 && v < V;
+                const float z = known ? kept_logit(rows, rule, row, v) : BITLOGIC_NEG_INF, q = d.logprob ? expf(d.logprob[j]) : 1.f;
+                p.refused = !(known && passes(d.u[j], q, share_in(p, rule, z, v)));
+                if (p.refused && stop) atomicMin(stop + seq, (int)i);
+            }
+            out[row] = p;
+        }
+    }
+}
+
+__global__ void verify_start_kernel(int* stop, long long S) {
+    dependent_kernel_start();
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i < S) stop[i] = INT_MAX;
 }
 
 // ------------------------------------------------------------ few classes --
@@ -201,8 +255,8 @@ verify_narrow_kernel(Rows target, Rows draft, int V, Drafts d, Verdict out) {
     allow_dependent_launch();
     const long long seq = (long long)blockIdx.x * kVerifyWarps + warp;
     if (seq >= d.S) return;
-    const long long first = d.first[seq], end = d.first[seq + 1];
-    if (first < 0 || end < first || end > d.D || end > d.first[d.S]) {
+    Places at;
+    if (!at.read(d, seq)) {
         if (lane == 0) {
             flag_index_error();
             out.accepted[seq] = 0;
@@ -211,6 +265,7 @@ verify_narrow_kernel(Rows target, Rows draft, int V, Drafts d, Verdict out) {
         }
         return;
     }
+    const long long first = at.first, end = at.first + at.count;
     float z[PER], m = BITLOGIC_NEG_INF;
     unsigned long long whole = 0;
     int sure = -1;   // the class that p has all of
@@ -335,7 +390,15 @@ int launch_verify(const Rows& target, const Rows& draft, int V, const Drafts& d,
     } else {
         const long long rows = d.S + d.D;
         const int parts = row_parts(rows, V, sizeof(T));
-        e = launch_rows(verify_sums_kernel<T>, rows * parts, 1, kVerifyThreads, 0, 0, stream, target, V, d, parts, ws);
+        if (parts > 1) {
+            e = launch_rows(verify_parts_kernel<T>, rows * parts, 1, kVerifyThreads, 0, 0, stream, target, V, d, parts, ws);
+        } else {
+            const long long turns = (rows + d.S - 1) / d.S, blocks = turns * d.S;
+            int* stop = blocks > 2 * 4 * sm_count() ? reinterpret_cast<int*>(ws + rows * kMaxParts) : nullptr;
+            e = stop ? launch_dependent(verify_start_kernel, (unsigned)((d.S + 255) / 256), 256, 0, stream, stop, d.S) : cudaSuccess;
+            if (e == cudaSuccess)
+                e = launch_rows(verify_rows_kernel<T>, blocks, 1, kVerifyThreads, 0, 0, stream, target, V, d, (int)turns, stop, ws);
+        }
         if (e == cudaSuccess) e = launch_verify_draw(target, draft, V, d, parts, ws, out, stream);
     }
     return e == cudaSuccess ? launch_status() : (int)BITLOGIC_ERR_CUDA;
@@ -350,7 +413,7 @@ BITLOGIC_ERROR_READER(verify)
 
 extern "C" size_t bitlogic_verify_drafts_workspace(int64_t S, int64_t D, int32_t V) {
     if (S < 1 || D < 0 || V <= kVerifyNarrow || S > (1LL << 30) || D > (1LL << 30)) return 0;
-    return (size_t)(S + D) * kMaxParts * sizeof(Part);
+    return (size_t)(S + D) * kMaxParts * sizeof(Part) + ((size_t)S * 4 + 15) / 16 * 16;
 }
 
 extern "C" int bitlogic_verify_drafts(const void* target, int32_t dtype, int64_t S, int64_t D, int32_t V, int64_t ld,

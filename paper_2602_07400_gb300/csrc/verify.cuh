@@ -31,6 +31,16 @@ struct Drafts {
     const float* draw_u;     // [S]
     long long S, D;
 };
+// A sequence's places; read() is false where they break the rules.
+struct Places {
+    long long first, count;
+    __device__ __forceinline__ bool read(const Drafts& d, long long seq) {
+        const long long end = d.first[seq + 1];
+        first = d.first[seq];
+        count = end - first;
+        return first >= 0 && count >= 0 && end <= d.D && end <= d.first[d.S];
+    }
+};
 struct Verdict {
     int* accepted;
     int* next_token;
@@ -41,7 +51,8 @@ struct Verdict {
 // the first class of that logit (in greedy rows and where it is +inf).
 struct Part {
     float m, sum;
-    int cls, pad;
+    int cls;
+    int refused;   // of a whole row: whether its draft is
 };
 
 struct RowRule {
@@ -74,6 +85,13 @@ __device__ __forceinline__ unsigned long long lanes_upto(unsigned long long v, i
         if (lane >= o) v += t;
     }
     return v;
+}
+
+// The target's probability of class v.
+__device__ __forceinline__ float share_in(const Part& p, const RowRule& rule, float z, int v) {
+    if (!(p.m > BITLOGIC_NEG_INF)) return 0.f;
+    if (rule.greedy || p.m > FLT_MAX) return v == p.cls ? 1.f : 0.f;
+    return rule.power(z, p.m) / p.sum;
 }
 
 // The kept logit of class v of a row of any type.

@@ -17,56 +17,61 @@ namespace {
 // apart, so that the lanes of a load are side by side.
 __device__ __forceinline__ int place(int q, int lane, int i, bool along) { return q * kChunk + (along ? 8 * lane + i : 32 * i + lane); }
 
-// A block's part of a row, classes c0 to c1, in shared memory or where it is.
-template <typename T>
+extern __shared__ __align__(16) unsigned char draw_shared[];
+
+// A block's part of a row, classes c0 to c1, in shared memory (kTiled) or where it is.
+template <typename T, bool kTiled>
 struct Slice {
     static constexpr int N = Piece<T>::N;
-    const T* at;     // of class 0, in whichever memory
     const T* x;      // the row
+    int tile;        // of class 0 in the shared memory: its place in values
     int V;
     bool aligned, cut;
     RowRule rule;
 
     __device__ __forceinline__ Slice(const Rows& rows, long long row, int V_)
-        : at(static_cast<const T*>(rows.x) + row * rows.ld), x(at), V(V_), aligned((reinterpret_cast<uintptr_t>(x) & 15u) == 0),
+        : x(static_cast<const T*>(rows.x) + row * rows.ld), tile(0), V(V_), aligned((reinterpret_cast<uintptr_t>(x) & 15u) == 0),
           rule(rows, row) {
         cut = !(rule.floor == BITLOGIC_NEG_INF);
     }
-    // Copies to `tile`; finish with cp_async_wait<0>() and a barrier.
-    __device__ __forceinline__ void copy(T* tile, int c0, int c1, int tid) {
+    __device__ __forceinline__ T* shared() const { return reinterpret_cast<T*>(draw_shared); }
+    __device__ __forceinline__ T at(int v) const { return kTiled ? shared()[tile + v] : x[v]; }
+    // Copies to `place` bytes into the shared memory; finish with cp_async_wait<0>()
+    // and a barrier.
+    __device__ __forceinline__ void copy(size_t place, int c0, int c1, int tid) {
         const int shift = (int)((reinterpret_cast<uintptr_t>(x + c0) & 15u) / sizeof(T)), first = c0 - shift;   // class of the first place
         const int n = c1 > c0 ? (shift + c1 - c0 + N - 1) / N : 0;
         const T* from = x + first;   // read at whole pieces only
+        tile = (int)(place / sizeof(T)) - first;
+        T* to = shared() + place / sizeof(T);
         for (int j = tid; j < n; j += kVerifyThreads) {
             const int v = first + j * N;
             if (v >= 0 && v + N <= V) {
-                cp_async16(tile + j * N, from + j * N);
+                cp_async16(to + j * N, from + j * N);
             } else {
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    if (v + i >= 0 && v + i < V) tile[j * N + i] = x[v + i];
+                    if (v + i >= 0 && v + i < V) to[j * N + i] = x[v + i];
             }
         }
-        at = tile - first;
     }
     // Masks what is not kept of classes c0 to c1 in the tile; copied and with a
     // barrier before and behind.
     __device__ __forceinline__ void mask(int c0, int c1, int tid) const {
-        T* own = const_cast<T*>(at);
         for (int v = c0 + tid; v < c1; v += kVerifyThreads)
-            if (!rule.keeps(logit_value(own[v]), v)) own[v] = masked_logit<T>();
+            if (!rule.keeps(logit_value(at(v)), v)) shared()[tile + v] = masked_logit<T>();
     }
-    // the kept logits of chunk q (kMasked: what is not kept is masked already); -inf
+    // the kept logits of chunk q (what is not kept is masked in a tile already); -inf
     // past the row's end
-    template <bool kMasked>
     __device__ __forceinline__ void load(int q, int lane, bool along, float (&z)[8]) const {
         const bool full = (q + 1) * kChunk <= V;
         if (along && full) {
-            const uint4* p = reinterpret_cast<const uint4*>(at + q * kChunk + 8 * lane);
+            const int v0 = q * kChunk + 8 * lane;
             float part[N];
 #pragma unroll
             for (int h = 0; h < 8 / N; ++h) {
-                Piece<T>::load(p[h], part);
+                if (kTiled) Piece<T>::load(*reinterpret_cast<const uint4*>(shared() + tile + v0 + h * N), part);
+                else Piece<T>::load(*reinterpret_cast<const uint4*>(x + v0 + h * N), part);
 #pragma unroll
                 for (int i = 0; i < N; ++i) z[h * N + i] = part[i];
             }
@@ -74,10 +79,10 @@ struct Slice {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int v = place(q, lane, i, along);
-                z[i] = v < V ? logit_value(at[v]) : BITLOGIC_NEG_INF;
+                z[i] = v < V ? logit_value(at(v)) : BITLOGIC_NEG_INF;
             }
         }
-        if (!kMasked) {
+        if (!kTiled) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) z[i] = rule.kept(z[i], place(q, lane, i, along));
         }
@@ -145,13 +150,6 @@ __device__ __forceinline__ Part join_parts(const Part& own, int parts, const Row
     return {m, sum, cls, 0};
 }
 
-// The target's probability of class v.
-__device__ __forceinline__ float share_in(const Part& p, const RowRule& rule, float z, int v) {
-    if (!(p.m > BITLOGIC_NEG_INF)) return 0.f;
-    if (rule.greedy || p.m > FLT_MAX) return v == p.cls ? 1.f : 0.f;
-    return rule.power(z, p.m) / p.sum;
-}
-
 // Shared memory behind the chunks' weights: the slices of both rows, of any
 // alignment.
 __host__ __device__ __forceinline__ size_t tile_offset(int chunks) { return ((size_t)chunks * 8 + 15) / 16 * 16; }
@@ -160,17 +158,16 @@ __host__ __device__ __forceinline__ size_t tile_bytes(int chunks, int element) {
 template <typename T, typename Q, bool kTiled>
 __global__ void __launch_bounds__(kVerifyThreads, 3)
 verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Part* __restrict__ sums, Verdict out) {
-    extern __shared__ __align__(16) unsigned char raw[];
-    unsigned long long* chunks = reinterpret_cast<unsigned long long*>(raw);
+    unsigned long long* chunks = reinterpret_cast<unsigned long long*>(draw_shared);
     __shared__ DrawShared s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const unsigned rank = cluster_rank(), blocks = cluster_size();
     const long long seq = blockIdx.x / blocks;
     // What the call's caller wrote may be read before the wait: the kernel before
     // this one let it start only once its own wait was over.
-    const long long first = d.first[seq], end = d.first[seq + 1];
     const bool writes = rank == 0 && tid == 0;
-    if (first < 0 || end < first || end > d.D || end > d.first[d.S]) {   // alike in all blocks
+    Places where;
+    if (!where.read(d, seq)) {   // alike in all blocks
         grid_dependency_wait();
         allow_dependent_launch();
         if (writes) {
@@ -184,7 +181,7 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
     report_running(blocks);
     // the drafts before the first that is refused: a row by `parts` lanes, as many as
     // the block has at a time
-    const long long k = end - first;
+    const long long first = where.first, k = where.count;
     const int round = kVerifyThreads / parts;
     long long a = k, base = 0;
     bool waited = false;   // for the rows' sums
@@ -195,20 +192,24 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
         if (base + (tid & ~31) / parts <= k) {    // alike in a warp
             const bool real = i <= k, test = i < k;
             const long long j = first + i, row = first + seq + (real ? i : 0);
-            const RowRule rule(target, row);
-            const int v = test ? d.token[j] : -1;
-            const bool known = v >= 0 && v < V;
             const bool leads = (tid & (parts - 1)) == 0;
-            const float z = known ? kept_logit(target, rule, row, v) : BITLOGIC_NEG_INF, u = test ? d.u[j] : 0.f,
-                        q = test && d.logprob ? expf(d.logprob[j]) : 1.f;
-            if (!waited) grid_dependency_wait();
-            waited = true;
-            const Part p = join_parts(sums[row * parts + (tid & (parts - 1))], parts, rule);
-            if (leads && real) s.row[tid / parts] = {p.m, p.cls};
-            if (leads && test) {
-                if (!known && rank == 0) flag_index_error();
-                if (!(known && passes(u, q, share_in(p, rule, z, v)))) atomicMin(&s.stop, tid / parts);
+            if (parts == 1) {   // decided where the row was read
+                if (!waited) grid_dependency_wait();
+                const Part p = sums[row];
+                if (real) s.row[tid] = {p.m, p.cls};
+                if (test && p.refused) atomicMin(&s.stop, tid);
+            } else {
+                const RowRule rule(target, row);
+                const int v = test ? d.token[j] : -1;
+                const bool known = v >= 0 && v < V;
+                const float z = known ? kept_logit(target, rule, row, v) : BITLOGIC_NEG_INF, u = test ? d.u[j] : 0.f,
+                            q = test && d.logprob ? expf(d.logprob[j]) : 1.f;
+                if (!waited) grid_dependency_wait();
+                const Part p = join_parts(sums[row * parts + (tid & (parts - 1))], parts, rule);
+                if (leads && real) s.row[tid / parts] = {p.m, p.cls};
+                if (leads && test && !(known && passes(u, q, share_in(p, rule, z, v)))) atomicMin(&s.stop, tid / parts);
             }
+            waited = true;
         }
         __syncthreads();
         if (s.stop < kVerifyThreads) a = base + s.stop;
@@ -218,9 +219,12 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
     if (!waited) grid_dependency_wait();
     allow_dependent_launch();
     const long long row = first + seq + a, j = first + a;
-    Slice<T> mine_t(target, row, V);
+    Slice<T, kTiled> mine_t(target, row, V);
     const Part p = {s.row[a - base].m, 0.f, s.row[a - base].cls, 0};
-    if (writes) out.accepted[seq] = (int)a;
+    if (writes) {
+        out.accepted[seq] = (int)a;
+        if (a < k && (d.token[j] < 0 || d.token[j] >= V)) flag_index_error();
+    }
     const bool sure = mine_t.rule.greedy || !(p.m > BITLOGIC_NEG_INF) || p.m > FLT_MAX;
     if (sure) {   // one class, or none; alike in all blocks
         if (writes) {
@@ -232,7 +236,7 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
         return;
     }
     const bool refused = a < k;
-    Slice<Q> mine_q(draft.x && refused ? draft : target, draft.x && refused ? j : row, V);   // not read unless it is the draft's
+    Slice<Q, kTiled> mine_q(draft.x && refused ? draft : target, draft.x && refused ? j : row, V);   // not read unless it is the draft's
     Weigher weigh = {mine_t.rule, mine_q.rule, p.m, 0.f, 0.f, 0.f, -1, false};
     if (refused && (!draft.x || mine_q.rule.greedy)) weigh.one = d.token[j];
     bool spread = refused && draft.x && !mine_q.rule.greedy;   // q is over the draft's row
@@ -250,10 +254,9 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
     };
     const bool along = mine_t.aligned && (!spread || mine_q.aligned);
     if (kTiled) {
-        T* tile = reinterpret_cast<T*>(raw + tile_offset(per));
         const int c0 = q0 * kChunk, c1 = min(V, q1 * kChunk);
-        mine_t.copy(tile, c0, c1, tid);
-        if (spread) mine_q.copy(reinterpret_cast<Q*>(raw + tile_offset(per) + tile_bytes(per, sizeof(T))), c0, c1, tid);
+        mine_t.copy(tile_offset(per), c0, c1, tid);
+        if (spread) mine_q.copy(tile_offset(per) + tile_bytes(per, sizeof(T)), c0, c1, tid);
         cp_async_commit();
         cp_async_wait<0>();
         __syncthreads();
@@ -272,8 +275,8 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
         float top = BITLOGIC_NEG_INF;
         for (int q = q0 + warp; q < q1; q += kVerifyWarps) {
             float z[8], zd[8];
-            mine_t.template load<kTiled>(q, lane, along, z);
-            if (kDraft) mine_q.template load<kTiled>(q, lane, along, zd);
+            mine_t.load(q, lane, along, z);
+            if (kDraft) mine_q.load(q, lane, along, zd);
             EightSum ws;
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
@@ -332,7 +335,7 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
             unsigned long long sum = 0;
             for (int q = q0 + warp; q < q1; q += kVerifyWarps) {
                 float zd[8];
-                mine_q.template load<kTiled>(q, lane, along, zd);
+                mine_q.load(q, lane, along, zd);
                 EightSum ws;
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) ws.add(two_powers(mine_q.rule, zd[i], zd[i + 1], weigh.dm));
@@ -392,8 +395,8 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
     float z[8], zd[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        z[i] = v0 + i < V ? mine_t.rule.kept(logit_value(mine_t.at[v0 + i]), v0 + i) : BITLOGIC_NEG_INF;
-        zd[i] = weigh.rest && spread && v0 + i < V ? mine_q.rule.kept(logit_value(mine_q.at[v0 + i]), v0 + i) : BITLOGIC_NEG_INF;
+        z[i] = v0 + i < V ? mine_t.rule.kept(logit_value(mine_t.at(v0 + i)), v0 + i) : BITLOGIC_NEG_INF;
+        zd[i] = weigh.rest && spread && v0 + i < V ? mine_q.rule.kept(logit_value(mine_q.at(v0 + i)), v0 + i) : BITLOGIC_NEG_INF;
     }
     unsigned long long w[8], sum = 0;
 #pragma unroll
