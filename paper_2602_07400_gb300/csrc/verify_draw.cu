@@ -121,10 +121,7 @@ struct DrawShared {
         unsigned long long mass;
         float m;
         unsigned pad;
-    } target[kMaxCluster], draft[kMaxCluster];
-    struct Mass {
-        unsigned long long mass;
-    } rest[kMaxCluster];
+    } target[kMaxCluster], draft[kMaxCluster], rest[kMaxCluster];
     unsigned long long warp_mass[kVerifyWarps];
     float fbuf[kVerifyWarps];
     int stop;                              // the first draft refused
@@ -266,10 +263,39 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
             __syncthreads();
         }
     }
-    // the chunks' weights into `chunks`; every thread gets the block's sum
+    // the sum and the largest over the block's warps to all blocks, and theirs here
+    bool met = false;
+    auto tell = [&](unsigned long long mass, float top, DrawShared::Stats* to) {
+        if (lane == 0) {
+            s.warp_mass[warp] = mass;
+            s.fbuf[warp] = top;
+        }
+        __syncthreads();
+        if (!met) wait_all_running(blocks);
+        met = true;
+        if (tid < (int)blocks) {
+            DrawShared::Stats own = {0ull, s.fbuf[0], 0u};
+            for (int w = 0; w < kVerifyWarps; ++w) {
+                own.mass += s.warp_mass[w];
+                own.m = fmaxf(own.m, s.fbuf[w]);
+            }
+            put_in_block(to + rank, tid, own);
+        }
+        barrier();
+    };
+    // the mass of the blocks before this one, and of all
+    auto add_up = [&](const DrawShared::Stats* of, unsigned long long* before) {
+        unsigned long long all = 0;
+        for (unsigned b = 0; b < blocks; ++b) {
+            if (b == rank) *before = all;
+            all += of[b].mass;
+        }
+        return all;
+    };
+    // the chunks' weights into `chunks`, and what they come to told
     using Yes = std::true_type;
     using No = std::false_type;
-    auto sum_chunks = [&](auto rest, auto with_draft, float* draft_top) {
+    auto sum_chunks = [&](auto rest, auto with_draft, DrawShared::Stats* to) {
         constexpr bool kRest = decltype(rest)::value, kDraft = decltype(with_draft)::value;
         unsigned long long mass = 0;
         float top = BITLOGIC_NEG_INF;
@@ -303,30 +329,18 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
             if (lane == 0) chunks[q - q0] = w;
             mass += w;
         }
-        if (draft_top) *draft_top = block_largest(top, s.fbuf, kVerifyWarps);
-        __syncthreads();
-        if (lane == 0) s.warp_mass[warp] = mass;
-        __syncthreads();
-        unsigned long long t = 0;
-        for (int w = 0; w < kVerifyWarps; ++w) t += s.warp_mass[w];
-        return t;
+        tell(mass, warp_largest(top), to);
     };
 
     // p's own weights, and the draft's largest logit
-    float top = BITLOGIC_NEG_INF;
-    unsigned long long mine = spread ? sum_chunks(No(), Yes(), &top) : sum_chunks(No(), No(), &top);
-    wait_all_running(blocks);
-    if (tid < (int)blocks) put_in_block(&s.target[rank], tid, DrawShared::Stats{mine, top, 0u});
-    barrier();
-    unsigned long long mass = 0, before = 0;
-    for (unsigned b = 0; b < blocks; ++b) {
-        if (b == rank) before = mass;
-        mass += s.target[b].mass;
-        weigh.dm = b == 0 ? s.target[b].m : fmaxf(weigh.dm, s.target[b].m);
-    }
+    if (spread) sum_chunks(No(), Yes(), s.target);
+    else sum_chunks(No(), No(), s.target);
+    unsigned long long before = 0, mass = add_up(s.target, &before), mine = s.target[rank].mass;
     const unsigned long long whole = mass;
     if (refused) {
         weigh.inv = kWhole / (float)whole;
+        weigh.dm = s.target[0].m;
+        for (unsigned b = 1; b < blocks; ++b) weigh.dm = fmaxf(weigh.dm, s.target[b].m);
         if (spread && weigh.dm > FLT_MAX) {   // a draft of +inf: all of q is on the class drawn
             weigh.one = d.token[j];
             spread = false;
@@ -341,31 +355,21 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
                 for (int i = 0; i < 8; i += 2) ws.add(two_powers(mine_q.rule, zd[i], zd[i + 1], weigh.dm));
                 sum += ws.warp_total();
             }
-            sum = lane == 0 ? sum : 0ull;
-            sum = block_add(sum, s.warp_mass, kVerifyWarps);
-            if (tid < (int)blocks) put_in_block(&s.draft[rank], tid, DrawShared::Stats{sum, 0.f, 0u});
-            barrier();
-            unsigned long long t = 0;
-            for (unsigned b = 0; b < blocks; ++b) t += s.draft[b].mass;
-            weigh.dinv = kWhole / (float)t;
+            tell(sum, 0.f, s.draft);
+            unsigned long long unused;
+            weigh.dinv = kWhole / (float)add_up(s.draft, &unused);
         }   // a draft without classes: q is 0
         if (spread && !(weigh.dm > BITLOGIC_NEG_INF)) weigh.dm = 0.f;
         weigh.rest = true;
-        mine = spread ? sum_chunks(Yes(), Yes(), nullptr) : sum_chunks(Yes(), No(), nullptr);
-        if (tid < (int)blocks) put_in_block(&s.rest[rank], tid, DrawShared::Mass{mine});
-        barrier();
-        mass = before = 0;
-        for (unsigned b = 0; b < blocks; ++b) {
-            if (b == rank) before = mass;
-            mass += s.rest[b].mass;
-        }
+        if (spread) sum_chunks(Yes(), Yes(), s.rest);
+        else sum_chunks(Yes(), No(), s.rest);
+        mass = add_up(s.rest, &before);
+        mine = s.rest[rank].mass;
         if (mass == 0) {   // p and q differ by less than their roundings
             weigh.rest = false;
-            mine = sum_chunks(No(), No(), nullptr);
-            for (unsigned b = 0; b < blocks; ++b) {
-                if (b == rank) before = mass;
-                mass += s.target[b].mass;
-            }
+            sum_chunks(No(), No(), s.draft);   // which every block has read
+            mass = add_up(s.draft, &before);
+            mine = s.draft[rank].mass;
         }
     }
     const unsigned long long goal = share_of(mass, unit_of(d.draw_u[seq]));
