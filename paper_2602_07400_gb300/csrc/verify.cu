@@ -166,7 +166,9 @@ __device__ __forceinline__ Part sum_part(const Rows& rows, long long row, int V,
         for (int w = 1; w < kVerifyWarps; ++w) join(s[w].m, s[w].sum, s[w].cls);
     };
     join_block();
+    int flags = 0;
     if (sum != sum && !(m > FLT_MAX)) {   // a NaN among the logits, which counts nothing
+        flags = kHasNan;
         m = BITLOGIC_NEG_INF;
         sum = 0.f;
         stream.load(0, ua);
@@ -182,7 +184,7 @@ __device__ __forceinline__ Part sum_part(const Rows& rows, long long row, int V,
         largest_class();
         join_block();
     }
-    return {m, sum, cls, 0};
+    return {m, sum, cls, flags};
 }
 
 // Rows in parts, where they are few; what the parts say of a draft is put together
@@ -200,7 +202,7 @@ verify_parts_kernel(Rows rows, int V, Drafts d, int parts, Part* __restrict__ ou
 }
 
 // Whole rows: block b takes row b / S of sequence b % S, and every `turns`-th one
-// behind it.  The row's draft is decided here (Part.refused), and where rows come
+// behind it.  The row's draft is decided here (kRefused), and where rows come
 // in several waves `stop` takes each sequence's first refused draft known so far:
 // the rows behind it say nothing about the outcome and are not read.  Whether a
 // block sees a refusal in time changes its work, never a result (256 x 7 drafts of
@@ -230,8 +232,9 @@ verify_rows_kernel(Rows rows, int V, Drafts d, int turns, int* stop, Part* __res
                 const int v = d.token[j];
                 const bool known = v >= 0 && v < V;
                 const float z = known ? kept_logit(rows, rule, row, v) : BITLOGIC_NEG_INF, q = d.logprob ? expf(d.logprob[j]) : 1.f;
-                p.refused = !(known && passes(d.u[j], q, share_in(p, rule, z, v)));
-                if (p.refused && stop) atomicMin(stop + seq, (int)i);
+                const bool refused = !(known && passes(d.u[j], q, share_in(p, rule, z, v)));
+                if (refused) p.flags |= kRefused;
+                if (refused && stop) atomicMin(stop + seq, (int)i);
             }
             out[row] = p;
         }

@@ -52,8 +52,10 @@ struct Verdict {
 struct Part {
     float m, sum;
     int cls;
-    int refused;   // of a whole row: whether its draft is
+    int flags;   // kRefused (whole rows: the draft of the row), kHasNan
 };
+
+constexpr int kRefused = 1, kHasNan = 2;
 
 struct RowRule {
     float slope, floor;
@@ -62,7 +64,8 @@ struct RowRule {
     __device__ __forceinline__ RowRule(const Rows& r, long long row) {
         const float temp = r.temperature ? r.temperature[row] : 1.0f;
         greedy = !(temp > 0.f);
-        slope = greedy ? 0.f : fminf((1.0f / temp) * kLog2E, FLT_MAX);
+        // not 0, so that -inf has no power at any temperature
+        slope = greedy ? 0.f : fmaxf(fminf((1.0f / temp) * kLog2E, FLT_MAX), FLT_MIN);
         floor = r.floor ? r.floor[row] : BITLOGIC_NEG_INF;
         last = r.last ? r.last[row] : -1;
     }

@@ -110,10 +110,23 @@ struct EightSum {
     }
 };
 
-// Two powers about m, rounded as RowRule::power rounds one.
+// The largest of three, NaN where one is.
+__device__ __forceinline__ float largest_or_nan(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float warp_largest_or_nan(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = largest_or_nan(v, shuffle_xor(v, o), v);
+    return v;
+}
+
+// Two powers about m, rounded as RowRule::power rounds one, of logits among which
+// there is no NaN.
 __device__ __forceinline__ f32x2 two_powers(const RowRule& rule, float a, float b, float m) {
     unpack2(mul2(sub2(pack2(a, b), pack2(m, m)), pack2(rule.slope, rule.slope)), a, b);
-    return pack2(fmaxf(exp2_unit(a), 0.f), fmaxf(exp2_unit(b), 0.f));
+    return pack2(exp2_unit(a), exp2_unit(b));
 }
 
 struct DrawShared {
@@ -121,13 +134,13 @@ struct DrawShared {
         unsigned long long mass;
         float m;
         unsigned pad;
-    } target[kMaxCluster], draft[kMaxCluster], rest[kMaxCluster];
+    } target[kMaxCluster], nan[kMaxCluster], draft[kMaxCluster], rest[kMaxCluster];
     unsigned long long warp_mass[kVerifyWarps];
     float fbuf[kVerifyWarps];
     int stop;                              // the first draft refused
     struct {
         float m;
-        int cls;
+        int cls, flags;
     } row[kVerifyThreads];                 // of a round's rows
     int chunk;
     unsigned long long before;
@@ -139,12 +152,13 @@ __device__ __forceinline__ Part join_parts(const Part& own, int parts, const Row
     float m = own.m;
     for (int o = parts >> 1; o > 0; o >>= 1) m = fmaxf(m, shuffle_xor(m, o));
     float sum = own.m > BITLOGIC_NEG_INF && !rule.greedy && m <= FLT_MAX ? own.sum * exp2_unit((own.m - m) * rule.slope) : 0.f;
-    int cls = own.m == m ? own.cls : INT_MAX;
+    int cls = own.m == m ? own.cls : INT_MAX, flags = own.flags;
     for (int o = parts >> 1; o > 0; o >>= 1) {
         sum += shuffle_xor(sum, o);
         cls = min(cls, shuffle_xor(cls, o));
+        flags |= shuffle_xor(flags, o);
     }
-    return {m, sum, cls, 0};
+    return {m, sum, cls, flags};
 }
 
 // Shared memory behind the chunks' weights: the slices of both rows, of any
@@ -193,8 +207,8 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
             if (parts == 1) {   // decided where the row was read
                 if (!waited) grid_dependency_wait();
                 const Part p = sums[row];
-                if (real) s.row[tid] = {p.m, p.cls};
-                if (test && p.refused) atomicMin(&s.stop, tid);
+                if (real) s.row[tid] = {p.m, p.cls, p.flags};
+                if (test && (p.flags & kRefused)) atomicMin(&s.stop, tid);
             } else {
                 const RowRule rule(target, row);
                 const int v = test ? d.token[j] : -1;
@@ -203,7 +217,7 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
                             q = test && d.logprob ? expf(d.logprob[j]) : 1.f;
                 if (!waited) grid_dependency_wait();
                 const Part p = join_parts(sums[row * parts + (tid & (parts - 1))], parts, rule);
-                if (leads && real) s.row[tid / parts] = {p.m, p.cls};
+                if (leads && real) s.row[tid / parts] = {p.m, p.cls, p.flags};
                 if (leads && test && !(known && passes(u, q, share_in(p, rule, z, v)))) atomicMin(&s.stop, tid / parts);
             }
             waited = true;
@@ -217,7 +231,8 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
     allow_dependent_launch();
     const long long row = first + seq + a, j = first + a;
     Slice<T, kTiled> mine_t(target, row, V);
-    const Part p = {s.row[a - base].m, 0.f, s.row[a - base].cls, 0};
+    const Part p = {s.row[a - base].m, 0.f, s.row[a - base].cls, s.row[a - base].flags};
+    if (p.flags & kHasNan) mine_t.cut = true;   // a NaN is not kept
     if (writes) {
         out.accepted[seq] = (int)a;
         if (a < k && (d.token[j] < 0 || d.token[j] >= V)) flag_index_error();
@@ -277,7 +292,7 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
             DrawShared::Stats own = {0ull, s.fbuf[0], 0u};
             for (int w = 0; w < kVerifyWarps; ++w) {
                 own.mass += s.warp_mass[w];
-                own.m = fmaxf(own.m, s.fbuf[w]);
+                own.m = largest_or_nan(own.m, s.fbuf[w], s.fbuf[w]);
             }
             put_in_block(to + rank, tid, own);
         }
@@ -308,14 +323,15 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
             for (int i = 0; i < 8; i += 2) {
                 f32x2 e = two_powers(mine_t.rule, z[i], z[i + 1], weigh.m);
                 if (kRest) {
-                    e = mul2(e, pack2(weigh.inv, weigh.inv));
                     float a, b;
-                    if (kDraft) {
-                        e = sub2(e, mul2(two_powers(mine_q.rule, zd[i], zd[i + 1], weigh.dm), pack2(weigh.dinv, weigh.dinv)));
-                        unpack2(e, a, b);
-                        e = pack2(fmaxf(a, 0.f), fmaxf(b, 0.f));
+                    unpack2(e, a, b);
+                    a = __fmul_rn(a, weigh.inv);
+                    b = __fmul_rn(b, weigh.inv);
+                    if (kDraft) {   // the shares rounded before their difference, as Weigher does
+                        float qa, qb;
+                        unpack2(two_powers(mine_q.rule, zd[i], zd[i + 1], weigh.dm), qa, qb);
+                        e = pack2(fmaxf(__fsub_rn(a, __fmul_rn(qa, weigh.dinv)), 0.f), fmaxf(__fsub_rn(b, __fmul_rn(qb, weigh.dinv)), 0.f));
                     } else {   // q(one) = 1 leaves nothing
-                        unpack2(e, a, b);
                         e = pack2(place(q, lane, i, along) == weigh.one ? 0.f : a, place(q, lane, i + 1, along) == weigh.one ? 0.f : b);
                     }
                 }
@@ -323,13 +339,13 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
             }
             if (!kRest && kDraft) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) top = fmaxf(top, zd[i]);
+                for (int i = 0; i < 8; i += 2) top = largest_or_nan(top, zd[i], zd[i + 1]);
             }
             const unsigned long long w = ws.warp_total();
             if (lane == 0) chunks[q - q0] = w;
             mass += w;
         }
-        tell(mass, warp_largest(top), to);
+        tell(mass, warp_largest_or_nan(top), to);
     };
 
     // p's own weights, and the draft's largest logit
@@ -339,8 +355,18 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
     const unsigned long long whole = mass;
     if (refused) {
         weigh.inv = kWhole / (float)whole;
-        weigh.dm = s.target[0].m;
-        for (unsigned b = 1; b < blocks; ++b) weigh.dm = fmaxf(weigh.dm, s.target[b].m);
+        auto draft_top = [&](const DrawShared::Stats* of) {
+            float t = of[0].m;
+            for (unsigned b = 1; b < blocks; ++b) t = largest_or_nan(t, of[b].m, of[b].m);
+            return t;
+        };
+        weigh.dm = draft_top(s.target);
+        if (weigh.dm != weigh.dm) {   // a NaN among the draft's logits (only in tiles), which counts nothing
+            mine_q.mask(q0 * kChunk, min(V, q1 * kChunk), tid);
+            __syncthreads();
+            sum_chunks(No(), Yes(), s.nan);
+            weigh.dm = draft_top(s.nan);
+        }
         if (spread && weigh.dm > FLT_MAX) {   // a draft of +inf: all of q is on the class drawn
             weigh.one = d.token[j];
             spread = false;

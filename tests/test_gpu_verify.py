@@ -139,6 +139,39 @@ def test_verify_against_its_definition(counts, V, dtype, draft, pad, shift):
     assert bl.bitlogic_device_error() == 0
 
 
+@pytest.mark.parametrize("counts,V,dtype,draft", [([3] * 400, 1100, "bf16", "bf16"), ([0, 7, 1, 12, 3] * 90, 2050, "f32", "i32"),
+                                                  ([2] * 700, 1500, "f16", None)])
+def test_verify_of_more_rows_than_run_at_once(counts, V, dtype, draft):
+    # rows behind a refused draft may be left unread
+    b = Batch(counts, V, dtype, draft, 1)
+    for _ in range(3):
+        b.ws.fill_(0xFF)
+        b.run().check(range(0, len(counts), 7))
+    assert bl.bitlogic_device_error() == 0
+
+
+@pytest.mark.parametrize("V", [60, 3000, 33000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_draft_with_nan_and_a_refusal_that_leaves_nothing(V, dtype):
+    b = Batch([1] * 40, V, dtype, dtype, 31)
+    b.u.fill_(0.99)                      # refuse where q is not far below p
+    b.draft[::2, 1::3] = float("nan")    # NaN is never drawn: q is 0 there
+    b.run().check()
+    # q as p, but for a draw's logarithm that claims more: what is left of p - q is
+    # nothing, and the next class is drawn from p
+    b = Batch([1] * 40, V, dtype, dtype, 32)
+    at = 2 * torch.arange(40, device="cuda")
+    b.draft = b.target[at].contiguous()
+    b.draft_temperature = b.temperature[at].contiguous()
+    b.lp.fill_(5.0)
+    b.u.fill_(0.999)
+    b.run()
+    token, lp = torch.empty(40, dtype=torch.int32, device="cuda"), torch.empty(40, device="cuda")
+    bl.bitlogic_sample_logits(b.draft, b.draw_u, token, lp, temperature=b.draft_temperature)
+    torch.cuda.synchronize()
+    assert (b.accepted == 0).all() and torch.equal(b.next, token) and torch.equal(b.logprob, lp)
+
+
 @pytest.mark.parametrize("counts,V,dtype,draft", [([3, 0, 2, 5], 33, "bf16", "bf16"), ([4] * 12, 500, "f32", "i32"),
                                                   ([3, 7, 1], 5000, "bf16", "bf16"), ([2, 3], 50001, "f32", None),
                                                   ([2] * 30, 4099, "f16", "f32")])
