@@ -448,25 +448,40 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
     }
 }
 
-// Blocks of a sequence's draw: slices of 16384 classes (64 KB of two bf16 rows, three
-// blocks on an SM), and with few sequences as many as the SMs have room for, of at
-// least 2048.
-inline int draw_blocks(long long S, int V) {
-    int c = 1;
-    while (c < kMaxCluster && (V / c > 16384 || (S * c * 2 <= 4 * sm_count() && V / (2 * c) >= 2048))) c *= 2;
-    return c;
-}
-
 constexpr size_t kDrawShared = 200 * 1024;
+
+// Blocks of a sequence's draw: slices of 16384 classes at most (64 KB of two bf16
+// rows, three blocks on an SM), and with few sequences as many as run at once, of at
+// least 2048.
+struct DrawShape {
+    int blocks, chunks;   // of a sequence, of a block
+    size_t bytes;         // of both slices in shared memory, with the chunks' weights
+};
+inline DrawShape draw_shape(int64_t S, int V, int element, int draft_element) {
+    auto with = [&](int blocks) {
+        const int all = (V + kChunk - 1) / kChunk, per = (all + blocks - 1) / blocks;
+        return DrawShape{blocks, per, tile_offset(per) + tile_bytes(per, element) + (draft_element ? tile_bytes(per, draft_element) : 0)};
+    };
+    auto at_once = [](const DrawShape& s) {
+        const long long per = 227 * 1024 / (long long)(s.bytes + 6 * 1024);
+        return (per < 1 ? 1 : per > 3 ? 3 : per) * sm_count();
+    };
+    DrawShape s = with(1);
+    while (s.blocks < kMaxCluster) {
+        const DrawShape more = with(2 * s.blocks);
+        if (V / s.blocks <= 16384 && (S * more.blocks > at_once(more) || V / more.blocks < 2048)) break;
+        s = more;
+    }
+    return s;
+}
 
 template <typename T, typename Q>
 cudaError_t launch_draw(const Rows& target, const Rows& draft, int V, const Drafts& d, int parts, const Part* sums, const Verdict& out,
                         cudaStream_t stream) {
-    const int blocks = draw_blocks(d.S, V), all = (V + kChunk - 1) / kChunk, per = (all + blocks - 1) / blocks;
-    const size_t tiles = tile_offset(per) + tile_bytes(per, sizeof(T)) + (draft.x ? tile_bytes(per, sizeof(Q)) : 0);
-    const bool tiled = tiles <= kDrawShared;
-    return launch_rows(tiled ? verify_draw_kernel<T, Q, true> : verify_draw_kernel<T, Q, false>, d.S, blocks, kVerifyThreads,
-                       tiled ? tiles : (size_t)per * 8, kDrawShared, stream, target, draft, V, d, parts, sums, out);
+    const DrawShape s = draw_shape(d.S, V, sizeof(T), draft.x ? sizeof(Q) : 0);
+    const bool tiled = s.bytes <= kDrawShared;
+    return launch_rows(tiled ? verify_draw_kernel<T, Q, true> : verify_draw_kernel<T, Q, false>, d.S, s.blocks, kVerifyThreads,
+                       tiled ? s.bytes : (size_t)s.chunks * 8, kDrawShared, stream, target, draft, V, d, parts, sums, out);
 }
 
 template <typename T>
