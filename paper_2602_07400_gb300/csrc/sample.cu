@@ -372,7 +372,7 @@ struct SampleShared {
         unsigned ties, slow;
         int last;   // class
     } found;
-    int bin;
+    int bin, last_bin;
     unsigned n_list, n_local, base;
 };
 
@@ -387,13 +387,17 @@ __device__ __forceinline__ float bin_mass(unsigned units, int b) {
 }
 __device__ __forceinline__ float bin_above(int b) { return __uint_as_float(0x3fffffffu - ((unsigned)b << 17)); }
 
-// The bins in which a mass is reached from the largest power down, into *bin: 4
-// times the bin (the last one if none), and 1 or 2 where the mass comes so near
-// to its beginning or end that the bin before or after it may be the one (the
-// bins' sums are right to some 2^-13).  Called by the whole block.
-__device__ __forceinline__ void find_bin(const unsigned* bins, float goal, int* bin, float* fbuf) {
+// The bins among which a mass is reached from the largest power down, into *bin: the
+// first and, 12 bits up, the last (the last bin of all where there is none).  Every
+// power counts to 2^-16 of itself, and so do the bins' sums: the bins are those that
+// the mass may be reached in if all of them are off by as much, 2^-15 with what
+// fp32 sums add.  (One bin more on either side than the one found left out the cut
+// of one row in some thousands, where bins weigh less than that; a block took 1.5 ms
+// to draw such a row from memory.)  Called by the whole block.
+__device__ __forceinline__ void find_bin(const unsigned* bins, float goal, int* bin, int* last, float* fbuf) {
     constexpr int kPer = (kBins + kSampleThreads - 1) / kSampleThreads;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const float least = goal * (1.0f - 3.0517578e-5f), most = goal * (1.0f + 3.0517578e-5f);
     float sum = 0.f;
     for (int q = 0; q < kPer; ++q) {
         const int b = tid * kPer + q;
@@ -405,25 +409,25 @@ __device__ __forceinline__ void find_bin(const unsigned* bins, float goal, int* 
         if (lane >= o) upto += t;
     }
     if (lane == 31) fbuf[warp] = upto;
-    if (tid == 0) *bin = 4 * (kBins - 1) + 3;
+    if (tid == 0) *bin = *last = kBins - 1;
     __syncthreads();
     float before = upto - sum;
     for (int w = 0; w < warp; ++w) before += fbuf[w];
-    if (before < goal && before + sum >= goal * 0.9999f)
+    if (before * 0.9999f < most && before + sum >= least * 0.9999f)
         for (int q = 0; q < kPer; ++q) {
             const int b = tid * kPer + q;
             if (b < kBins) {
-                const float m = bin_mass(bins[b], b);
-                const float near = goal * 0.0005f;
-                if (before < goal && before + m >= goal)
-                    atomicMin(bin, 4 * b + (goal - before < near) + 2 * (before + m - goal < near));
-                before += m;
+                before += bin_mass(bins[b], b);
+                if (before >= least) atomicMin(bin, b);
+                if (before >= most) atomicMin(last, b);
             }
         }
     __syncthreads();
+    if (tid == 0) *bin |= *last << 12;
+    __syncthreads();
 }
-__device__ __forceinline__ int first_bin(int found) { return max(0, found / 4 - (found & 1)); }
-__device__ __forceinline__ int end_bin(int found) { return min(kBins, found / 4 + 1 + (found >> 1 & 1)); }
+__device__ __forceinline__ int first_bin(int found) { return found & 4095; }
+__device__ __forceinline__ int end_bin(int found) { return min(kBins, (found >> 12) + 1); }
 
 // The sum of v over the block's threads before this one, and over all of them.
 __device__ __forceinline__ unsigned long long block_before(unsigned long long v, unsigned long long* buf,
@@ -553,7 +557,7 @@ __device__ void sample_of_list(S* s, unsigned n, const RowSettings& set, const P
 //   top_k up to 1024 (and greedy rows): the classes that pass a bound which at
 //     least k reach go to the first block, which cuts and draws among them;
 //   top_p alone: the weights by bins of 1/64 octave show where the mass is
-//     reached; the three bins around it go to the first block, which finds the
+//     reached; the bins that it may be reached in go to the first block, which finds the
 //     cut to the class with exact sums; then every block sums its kept weights
 //     in the order of classes and the one that holds the draw finds it;
 //   neither: the last step alone.
@@ -725,7 +729,7 @@ sample_tile_kernel(const T* __restrict__ X, long long ld, int V, Settings settin
             if (s.bins[b]) add_in_block(row_bins + b, 0, s.bins[b]);
         row_barrier();
         if (rank == 0) {
-            find_bin(row_bins, (float)want * (1.0f / 1099511627776.0f), &s.bin, s.fbuf);
+            find_bin(row_bins, (float)want * (1.0f / 1099511627776.0f), &s.bin, &s.last_bin, s.fbuf);
             const int b = s.bin;
             if (tid < (int)blocks) store_in_block(&s.bin, tid, (uint32_t)b);
             if (tid == 0) s.n_list = 0;
@@ -951,7 +955,7 @@ struct SampleRowShared {
     unsigned long long mass[kSampleWarps];
     int kept[kSampleWarps];
     unsigned n, n_groups, ties;
-    int bin;
+    int bin, last_bin;
     struct {
         uint32_t key;
         unsigned ties, slow;
@@ -1138,7 +1142,7 @@ sample_row_kernel(const T* __restrict__ X, long long ld, int V, Settings setting
         stream.load(1, ub);
         count(u_end);
         __syncthreads();
-        find_bin(s.bins, (float)want * (1.0f / 1099511627776.0f), &s.bin, s.fbuf);
+        find_bin(s.bins, (float)want * (1.0f / 1099511627776.0f), &s.bin, &s.last_bin, s.fbuf);
         // the exact mass above the bins found, and its kept part by
         // chunk; the pieces that hold entries of those bins wait until the pass
         // is over (where the bins were)
