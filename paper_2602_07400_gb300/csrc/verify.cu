@@ -108,6 +108,14 @@ __device__ __forceinline__ Part sum_part(const Rows& rows, long long row, int V,
         sum += part;
     };
 
+    // a NaN into the sum, which then is formed again without them
+    auto show_nan = [&](const uint4& u) {
+        float z[N];
+        P::load(u, z);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (z[i] != z[i]) sum = z[i];
+    };
     auto sum_kept = [&]() {
         stream_row([&](const uint4 (&u)[4], int q) {
 #pragma unroll
@@ -125,7 +133,11 @@ __device__ __forceinline__ Part sum_part(const Rows& rows, long long row, int V,
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = P::largest(top, u[i]);
             const float t = P::value(top);
-            if (!(t > BITLOGIC_NEG_INF)) return;
+            if (!(t > BITLOGIC_NEG_INF)) {   // masked, or NaN, which the maximum passes over
+#pragma unroll
+                for (int i = 0; i < 4; ++i) show_nan(u[i]);
+                return;
+            }
             rise(t);
             f32x2 acc = pack2(0.f, 0.f);
 #pragma unroll
@@ -138,7 +150,10 @@ __device__ __forceinline__ Part sum_part(const Rows& rows, long long row, int V,
             unpack2(acc, a, b);
             sum += a + b;
         });
-        if (j_end >= 0) add_kept(u_end, j_end);
+        if (j_end >= 0) {
+            add_kept(u_end, j_end);
+            show_nan(u_end);
+        }
     }
     // over the block
     auto join = [&](float m2, float s2, int c2) {

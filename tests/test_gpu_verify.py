@@ -283,6 +283,40 @@ def test_rows_that_are_masked_infinite_or_greedy(V, dtype):
     assert int(b.accepted[0]) == 0 and int(b.next[0]) == -1
 
 
+@pytest.mark.parametrize("V", [40, 1200, 20011, 60000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_nan_wherever_it_stands(V, dtype, shift):
+    # at the ends of rows, in runs as long as what a thread takes at a time, alone
+    nan = float("nan")
+    b = Batch([1] * 16, V, dtype, dtype, 77, 3 * shift, shift)
+    b.u.fill_(0.97)                      # refused mostly: the draw goes over both rows
+    for x, rows in ((b.target, 2), (b.draft, 1)):
+        for s in range(16):
+            r = rows * s
+            if s % 8 == 0:
+                x[r, 0] = nan
+            elif s % 8 == 1:
+                x[r, V - 1] = nan
+            elif s % 8 == 2:
+                x[r, V // 4: 3 * V // 4] = nan
+            elif s % 8 == 3:
+                x[r, : V // 2] = nan
+                x[r, V // 2: V // 2 + 5] = -float("inf")
+            elif s % 8 == 4:
+                x[r, V // 3] = nan
+            elif s % 8 == 5:
+                x[r, 3:] = nan
+            elif s % 8 == 6:
+                x[r, V // 2:] = nan
+    # tokens that may be drawn
+    ok = b.draft.float()
+    b.token = torch.where(torch.isnan(ok), torch.full_like(ok, -1e30), ok).argmax(1).to(torch.int32)
+    b.lp.fill_(-0.1)
+    b.run().check()
+    assert bl.bitlogic_device_error() == 0
+
+
 def test_u_and_draw_u_outside_their_range_are_clamped():
     for V in (40, 4000):
         b = Batch([1] * 8, V, "f32", "f32", 6)
