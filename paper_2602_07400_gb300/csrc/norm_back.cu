@@ -41,6 +41,8 @@ norm_backward_kernel(const T* dy, long long ldy, const T* h, long long ldh, Weig
     for (int i = 0; i < kVec; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) dw[i][e] = twice(0.f);
+    const WeightSlots<T, kVec> ws = {raw + Slots<T, kVec>::place(4), weight.wide};
+    if (kAhead && weight.w) ws.fill(weight, walk, d);
     if (kAhead) ask(walk.first, 0);
     int turn = 0;
     for (long long row = walk.first; row < rows; row += walk.step, turn ^= 1) {
@@ -72,7 +74,8 @@ norm_backward_kernel(const T* dy, long long ldy, const T* h, long long ldh, Weig
             f32x2 a[4], g[4], w[4];
             values(i, c, a, g);
             if (weight.w) {
-                weight_pairs<T>(weight, c, d - c, w);
+                if (kAhead) ws.get(i, w);
+                else weight_pairs<T>(weight, c, d - c, w);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) g[e] = mul2(g[e], w[e]);
             }
@@ -109,7 +112,8 @@ norm_backward_kernel(const T* dy, long long ldy, const T* h, long long ldh, Weig
 #pragma unroll
             for (int e = 0; e < 4; ++e) dw[i][e] = fma2(g[e], mul2(a[e], root), dw[i][e]);
             if (weight.w) {
-                weight_pairs<T>(weight, c, d - c, w);
+                if (kAhead) ws.get(i, w);
+                else weight_pairs<T>(weight, c, d - c, w);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) g[e] = mul2(g[e], w[e]);
             }
@@ -217,7 +221,7 @@ extern "C" int bitlogic_norm_backward(const void* dY, int32_t dtype, int64_t T, 
             constexpr int kVec = decltype(vecs)::value, kThreads = decltype(most)::value;
             constexpr bool kWarp = decltype(warp)::value;
             const int resident = resident_by_registers(s.threads, kVec, kWarp);
-            const size_t slots = Slots<V, kVec>::bytes(4, s.threads);
+            const size_t slots = Slots<V, kVec>::bytes(4, s.threads) + (weight ? WeightSlots<V, kVec>::bytes(s.threads, wt.wide) : 0);
             const bool ahead = vec && d % 8 == 0 && slots <= kMostShared && row_blocks(T, s) > sm_count();
             auto kern = ahead ? norm_backward_kernel<V, kVec, kWarp, kThreads, true> : norm_backward_kernel<V, kVec, kWarp, kThreads, false>;
             const size_t join = kWarp && partial ? (size_t)(s.threads / 32) * d * 4 : 0;   // dw of a block's warps

@@ -86,8 +86,9 @@ template <typename T, int kVec>
 struct Slots {
     static constexpr int kBytes = 8 * (int)sizeof(T);
     unsigned char* base;
-    __device__ __forceinline__ Slots(unsigned char* raw, int row) : base(raw + (size_t)row * kVec * blockDim.x * kBytes) {}
+    __device__ __forceinline__ Slots(unsigned char* raw, int row) : base(raw + place(row)) {}
     static size_t bytes(int rows, int threads) { return (size_t)rows * kVec * threads * kBytes; }
+    static __device__ __forceinline__ size_t place(int row) { return (size_t)row * kVec * blockDim.x * kBytes; }
     // place `part` of vector i, 16 bytes, lanes side by side
     __device__ __forceinline__ uint4* at(int i, int part) const {
         return reinterpret_cast<uint4*>(base) + ((size_t)i * (kBytes / 16) + part) * blockDim.x + threadIdx.x;
@@ -157,6 +158,53 @@ __device__ __forceinline__ void weight_pairs(const Weight& weight, int c, int n,
     if (weight.wide) read_pairs(static_cast<const float*>(weight.w) + c, n, weight.vec, w);
     else read_pairs(static_cast<const T*>(weight.w) + c, n, weight.vec, w);
 }
+// A thread's own columns of the weight in shared memory for all of its rows, for the
+// gradient, which reads them twice a row: beside rows on their way L1 has no room
+// for them (16384 x 8192 bf16: 195 us with the weight read from L1 and L2, 158 from
+// here; the norm itself, which reads them once, 296 and 304).
+template <typename T, int kVec>
+struct WeightSlots {
+    unsigned char* base;
+    bool wide;
+    static size_t bytes(int threads, bool wide) { return (size_t)kVec * threads * 8 * (wide ? 4 : sizeof(T)); }
+    __device__ __forceinline__ uint4* at(int i, int part) const {
+        return reinterpret_cast<uint4*>(base) + ((size_t)i * (wide || sizeof(T) == 4 ? 2 : 1) + part) * blockDim.x + threadIdx.x;
+    }
+    template <bool kWarp>
+    __device__ __forceinline__ void fill(const Weight& weight, const Walk<kWarp>& walk, int d) const {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const int c = walk.column(i);
+            if (c >= d) continue;
+            if (wide) {
+                f32x2 w[4];
+                read_pairs(static_cast<const float*>(weight.w) + c, 8, weight.vec, w);
+                const Eight<float> e = eight_of<float>(w);
+                *at(i, 0) = e.a;
+                *at(i, 1) = e.b;
+            } else {
+                f32x2 w[4];
+                read_pairs(static_cast<const T*>(weight.w) + c, 8, weight.vec, w);
+                const Eight<T> e = eight_of<T>(w);
+                *at(i, 0) = e.a;
+                if constexpr (sizeof(T) == 4) *at(i, 1) = e.b;
+            }
+        }
+    }
+    __device__ __forceinline__ void get(int i, f32x2 (&w)[4]) const {
+        if (wide) {
+            Eight<float> e;
+            e.a = *at(i, 0);
+            e.b = *at(i, 1);
+            pairs_of(e, w);
+        } else {
+            Eight<T> e;
+            e.a = *at(i, 0);
+            if constexpr (sizeof(T) == 4) e.b = *at(i, 1);
+            pairs_of(e, w);
+        }
+    }
+};
 __device__ __forceinline__ float sum_of(f32x2 v) {
     float a, b;
     unpack2(v, a, b);
