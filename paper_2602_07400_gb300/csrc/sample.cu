@@ -198,18 +198,23 @@ __device__ void last_kept(const T* __restrict__ x, int V, const Cut& cut, const 
     }
     const float z_min = set.floor_e > 0.f ? logit_below(set.floor_e, power) : BITLOGIC_NEG_INF;
     unsigned long long best = 0;   // ~key << 32 | class, of the least key
-    for (int j = tid; j < slice.n; j += kSampleThreads) {
-        const uint4 u = piece(j);
-        if (P::largest_of(u) >= z_min) {
-            float z[N];
-            P::load(u, z);
+    for (int j0 = tid; j0 < slice.n; j0 += 4 * kSampleThreads) {   // four loads on their way
+        uint4 u[4];
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (z[i] > z_cut && power(z[i]) >= set.floor_e) {
-                    const unsigned long long c = ((unsigned long long)~logit_key(z[i]) << 32) | (uint32_t)(slice.first + j * N + i);
-                    best = c > best ? c : best;
-                }
-        }
+        for (int r = 0; r < 4; ++r) u[r] = j0 + r * kSampleThreads < slice.n ? piece(j0 + r * kSampleThreads) : masked_piece<T>();
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (P::largest_of(u[r]) >= z_min) {
+                float z[N];
+                P::load(u[r], z);
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (z[i] > z_cut && power(z[i]) >= set.floor_e) {
+                        const unsigned long long c = ((unsigned long long)~logit_key(z[i]) << 32) |
+                                                     (uint32_t)(slice.first + (j0 + r * kSampleThreads) * N + i);
+                        best = c > best ? c : best;
+                    }
+            }
     }
     best = block_max(best, sc->mass);
     if (tid == 0) put_support(out, row, key_logit(~(uint32_t)(best >> 32)), (int)(uint32_t)best);
@@ -458,7 +463,7 @@ __device__ __forceinline__ void find_cut(unsigned long long* list, unsigned list
                                          Found* found, Kept&& kept) {
     const int tid = threadIdx.x, size = power_of_two(listed), per = ((int)listed + kSampleThreads - 1) / kSampleThreads;
     for (int i = listed + tid; i < size; i += kSampleThreads) list[i] = 0ull;
-    block_sort_falling(list, size);
+    block_sort_falling_256(list, size);
     const int i0 = tid * per, i1 = min((int)listed, i0 + per);
     unsigned long long own = 0, all;
     for (int i = i0; i < i1; ++i) own += draw_weight(power.of(key_logit((uint32_t)(list[i] >> 32))));
@@ -491,7 +496,7 @@ __device__ void sample_of_list(S* s, unsigned n, const RowSettings& set, const P
     const int tid = threadIdx.x;
     const int size = power_of_two(n);
     for (int i = n + tid; i < size; i += kSampleThreads) s->list[i] = 0ull;
-    block_sort_falling(s->list, size);
+    block_sort_falling_256(s->list, size);
     const int k = min((int)n, set.k);   // at most kListTop
     unsigned long long w[kPer], sum = 0, all;
     float e[kPer];
@@ -528,7 +533,7 @@ __device__ void sample_of_list(S* s, unsigned n, const RowSettings& set, const P
         const unsigned long long x = s->list[i];
         s->list[i] = i < kept ? (x << 32) | (x >> 32) : 0ull;
     }
-    block_sort_falling(s->list, size2);
+    block_sort_falling_256(s->list, size2);
     sum = 0;
 #pragma unroll
     for (int q = 0; q < kPer; ++q) {

