@@ -876,6 +876,14 @@ def bitlogic_head_loss_noalloc(Y: torch.Tensor, labels: torch.Tensor, C: int, ta
 def _logits(x: torch.Tensor, name: str) -> Tuple[int, int, int, int]:
     """Type code, rows, classes and row stride of a matrix of logits whose
     classes are adjacent (rows may lie apart)."""
+    # one pass when everything fits
+    if x.__class__ is torch.Tensor and x.is_cuda:
+        code, s = LOGIT_TYPES.get(x.dtype), x.shape
+        if code is not None and len(s) == 2:
+            ld, inc = x.stride()
+            if inc == 1:
+                T, V = s
+                return code, T, V, ld if T > 1 or ld > V else V
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     code = LOGIT_TYPES.get(x.dtype)
