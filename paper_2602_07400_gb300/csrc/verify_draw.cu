@@ -48,15 +48,13 @@ struct Slice {
         const T* from = x + first;   // read at whole pieces only
         tile = (int)(place / sizeof(T)) - first;
         T* to = shared() + place / sizeof(T);
-        for (int j = tid; j < n; j += kVerifyThreads) {
-            const int v = first + j * N;
-            if (v >= 0 && v + N <= V) {
-                cp_async16(to + j * N, from + j * N);
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (v + i >= 0 && v + i < V) to[j * N + i] = x[v + i];
-            }
+        // pieces [w0, w1) lie in the row in full, at most one before and one after do not
+        const int w0 = n > 0 && first < 0 ? 1 : 0, w1 = n > 0 && first + n * N > V ? max(w0, n - 1) : n;
+#pragma unroll 4
+        for (int j = w0 + tid; j < w1; j += kVerifyThreads) cp_async16(to + j * N, from + j * N);
+        if (tid < 2 * N) {
+            const int j = tid < N ? 0 : n - 1, v = first + j * N + tid % N;
+            if (n > 0 && (j < w0 || j >= w1) && v >= 0 && v < V) to[j * N + tid % N] = x[v];
         }
     }
     // Masks what is not kept of classes c0 to c1 in the tile; copied and with a
@@ -106,6 +104,14 @@ struct EightSum {
         unpack2(u, a, b);
         low += __float_as_uint(a) + __float_as_uint(b);
     }
+    // of the `n` weights of a lane (512 at most)
+    __device__ __forceinline__ unsigned long long lane_total(unsigned n) const {
+        WeightSum s;
+        s.high = high - n * 0x41800000u;
+        s.low = low - n * 0x4b400000u;
+        return s.total();
+    }
+    // of the eight of every lane
     __device__ __forceinline__ unsigned long long warp_total() const {
         WeightSum s;
         s.high = __reduce_add_sync(0xffffffffu, high) - 256u * 0x41800000u;
@@ -260,6 +266,7 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
     // the block's chunks of the row, a warp each in turn
     const int all = (V + kChunk - 1) / kChunk, per = (all + (int)blocks - 1) / (int)blocks;
     const int q0 = min(all, (int)rank * per), q1 = min(all, q0 + per);
+    const unsigned visits = q0 + warp < q1 ? (unsigned)(q1 - q0 - warp + kVerifyWarps - 1) / kVerifyWarps : 0u;   // of this warp
     auto barrier = [&]() {
         if (blocks > 1) {
             cluster_arrive();
@@ -311,18 +318,20 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
         }
         return all;
     };
-    // the chunks' weights into `chunks`, and what they come to told
+    // the weights of p, or of what is left of it (`rest`), and what they come to told;
+    // by chunk where a draw may follow (`by_chunk`)
     using Yes = std::true_type;
     using No = std::false_type;
-    auto sum_chunks = [&](auto rest, auto with_draft, DrawShared::Stats* to) {
-        constexpr bool kRest = decltype(rest)::value, kDraft = decltype(with_draft)::value;
+    auto sum_chunks = [&](auto rest, auto with_draft, auto by_chunk, DrawShared::Stats* to) {
+        constexpr bool kRest = decltype(rest)::value, kDraft = decltype(with_draft)::value, kByChunk = decltype(by_chunk)::value;
         unsigned long long mass = 0;
         float top = BITLOGIC_NEG_INF;
+        EightSum ws;
         for (int q = q0 + warp; q < q1; q += kVerifyWarps) {
             float z[8], zd[8];
             mine_t.load(q, lane, along, z);
             if (kDraft) mine_q.load(q, lane, along, zd);
-            EightSum ws;
+            if (kByChunk) ws = EightSum();
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
                 f32x2 e = two_powers(mine_t.rule, z[i], z[i + 1], weigh.m);
@@ -345,16 +354,20 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) top = largest_or_nan(top, zd[i], zd[i + 1]);
             }
-            const unsigned long long w = ws.warp_total();
-            if (lane == 0) chunks[q - q0] = w;
-            mass += w;
+            if (kByChunk) {
+                const unsigned long long w = ws.warp_total();
+                if (lane == 0) chunks[q - q0] = w;
+                mass += w;
+            }
         }
-        tell(mass, warp_largest_or_nan(top), to);
+        if (!kByChunk) mass = warp_add(ws.lane_total(8u * visits));
+        tell(mass, !kRest && kDraft ? warp_largest_or_nan(top) : top, to);
     };
 
     // p's own weights, and the draft's largest logit
-    if (spread) sum_chunks(No(), Yes(), s.target);
-    else sum_chunks(No(), No(), s.target);
+    if (spread) sum_chunks(No(), Yes(), No(), s.target);
+    else if (refused) sum_chunks(No(), No(), No(), s.target);
+    else sum_chunks(No(), No(), Yes(), s.target);
     unsigned long long before = 0, mass = add_up(s.target, &before), mine = s.target[rank].mass;
     const unsigned long long whole = mass;
     if (refused) {
@@ -368,7 +381,7 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
         if (weigh.dm != weigh.dm) {   // a NaN among the draft's logits (only in tiles), which counts nothing
             mine_q.mask(q0 * kChunk, min(V, q1 * kChunk), tid);
             __syncthreads();
-            sum_chunks(No(), Yes(), s.nan);
+            sum_chunks(No(), Yes(), No(), s.nan);
             weigh.dm = draft_top(s.nan);
         }
         if (spread && weigh.dm > FLT_MAX) {   // a draft of +inf: all of q is on the class drawn
@@ -376,28 +389,27 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
             spread = false;
         }
         if (spread && weigh.dm > BITLOGIC_NEG_INF) {
-            unsigned long long sum = 0;
+            EightSum ws;
             for (int q = q0 + warp; q < q1; q += kVerifyWarps) {
                 float zd[8];
                 mine_q.load(q, lane, along, zd);
-                EightSum ws;
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) ws.add(two_powers(mine_q.rule, zd[i], zd[i + 1], weigh.dm));
-                sum += ws.warp_total();
             }
+            const unsigned long long sum = warp_add(ws.lane_total(8u * visits));
             tell(sum, 0.f, s.draft);
             unsigned long long unused;
             weigh.dinv = kWhole / (float)add_up(s.draft, &unused);
         }   // a draft without classes: q is 0
         if (spread && !(weigh.dm > BITLOGIC_NEG_INF)) weigh.dm = 0.f;
         weigh.rest = true;
-        if (spread) sum_chunks(Yes(), Yes(), s.rest);
-        else sum_chunks(Yes(), No(), s.rest);
+        if (spread) sum_chunks(Yes(), Yes(), Yes(), s.rest);
+        else sum_chunks(Yes(), No(), Yes(), s.rest);
         mass = add_up(s.rest, &before);
         mine = s.rest[rank].mass;
         if (mass == 0) {   // p and q differ by less than their roundings
             weigh.rest = false;
-            sum_chunks(No(), No(), s.draft);   // which every block has read
+            sum_chunks(No(), No(), Yes(), s.draft);   // which every block has read
             mass = add_up(s.draft, &before);
             mine = s.draft[rank].mass;
         }
