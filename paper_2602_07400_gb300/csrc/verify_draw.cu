@@ -6,9 +6,9 @@
 // three times: the target's weights and the draft's largest logit, the draft's
 // weights, and what max(0, p - q) leaves, by chunks of 256 classes; the chunk that
 // holds the draw is then looked at class by class.  Bound by instructions and the
-// latency between the cluster's barriers: of the 169 us of 256 x 7 drafts over 131072
-// bf16 classes 82 are the rows' sums, 14 the slices' copies and 22, 19 and 32 the
-// passes, whose instructions alone would issue in half of that.  Slices that stay in
+// latency between the cluster's barriers: of the 162 us of 256 x 7 drafts over 131072
+// bf16 classes 82 are the rows' sums, 14 the slices' copies and 66 the passes, whose
+// instructions alone would issue in half of that.  Slices that stay in
 // L2 in place of shared memory took 217 us, slices of 32768 classes (a block on an
 // SM) 247.
 #include "verify.cuh"
