@@ -7,7 +7,9 @@
  * LUT layer (LightLUT soft or straight-through hard node; fixed connectivity
  * or learnable routing over candidate pools), the group-sum head with
  * temperature and cross-entropy, the AdamW update of the logits, and the
- * hard bit-packed evaluation mode with a popcount group-sum.  Every call is
+ * hard bit-packed evaluation mode with a popcount group-sum.  Beside them stand
+ * operators on rows of logits, and operators that put a network beside a larger
+ * model: its drafts checked, dropout, hidden states in 8 bits.  Every call is
  * a hand-written CUDA kernel sequence enqueued on the caller's stream.
  *
  * Conventions shared by all calls
