@@ -52,7 +52,9 @@ def _check(out, scale, y, group, fixed=0.0):
 
 
 SHAPES = [(1, 1), (2, 7), (3, 8), (5, 16), (4, 100), (1, 255), (33, 256), (7, 1001), (300, 512), (3, 4096), (1, 8192), (2, 8200),
-          (2, 16384), (3, 20001), (2, 32768), (0, 64)]
+          (2, 16384), (3, 20001), (2, 32768), (0, 64),
+          # more rows than run at once: rows come ahead of their turn
+          (2500, 200), (2600, 1024), (400, 2048), (330, 8192), (170, 16384), (160, 20008)]
 
 
 @pytest.mark.gpu
@@ -136,7 +138,7 @@ def test_rows_of_any_size_and_content(dtype):
 
 
 BACK = [(1, 1), (2, 7), (3, 8), (5, 100), (1, 4096), (700, 256), (509, 1001), (33, 8192), (4, 8200), (5, 16384), (3, 20001), (2, 32768),
-        (3000, 33)]
+        (3000, 33), (2500, 200), (2600, 1024), (400, 2048), (700, 8192), (170, 16384), (160, 20008)]
 
 
 @pytest.mark.gpu

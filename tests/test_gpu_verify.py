@@ -128,6 +128,8 @@ CASES = [
     ([1, 9, 0, 4, 12], 5000, "f16", "f32"), ([3] * 20, 7777, "f32", "bf16"), ([2, 0, 7], 50001, "f32", "f32"),
     ([3, 1], 131072, "bf16", None), ([1, 2], 300001, "bf16", "f16"), ([0, 0], 40000, "i32", None),
     ([1] * 200, 2049, "bf16", "i32"),
+    # rows longer than the blocks of a sequence hold
+    ([2], 1 << 20, "f32", "f32"), ([1, 0, 1], 700001, "bf16", "f32"), ([1, 1], 900000, "i32", "bf16"),
 ]
 
 
@@ -174,7 +176,7 @@ def test_a_draft_with_nan_and_a_refusal_that_leaves_nothing(V, dtype):
 
 @pytest.mark.parametrize("counts,V,dtype,draft", [([3, 0, 2, 5], 33, "bf16", "bf16"), ([4] * 12, 500, "f32", "i32"),
                                                   ([3, 7, 1], 5000, "bf16", "bf16"), ([2, 3], 50001, "f32", None),
-                                                  ([2] * 30, 4099, "f16", "f32")])
+                                                  ([2] * 30, 4099, "f16", "f32"), ([1, 1], 600000, "f32", "f32")])
 @pytest.mark.parametrize("cut", [1, 5, 40])
 def test_verify_among_the_classes_kept(counts, V, dtype, draft, cut):
     # bf16 and counts have many equal logits at the cut
