@@ -180,16 +180,33 @@ dropout_kernel(const T* x, long long ldx, const T* residual, long long ldr, T* o
     const long long warps = (long long)gridDim.x * (kDropThreads / 32);
     for (long long w = ((long long)blockIdx.x * kDropThreads + threadIdx.x) >> 5; w * 256 < n; w += warps) {
         const uint32_t keep = keeper((unsigned long long)(w * 32 + lane));
+        // row and column of the lane's first element; its others are 32 columns on
+        const long long e0 = w * 256 + lane;
+        long long row = e0 < 0x100000000LL && cols < 0x100000000LL ? (long long)((uint32_t)e0 / (uint32_t)cols) : e0 / cols;
+        long long col = e0 - row * cols;
+        T v[8], r[8];
+        long long at[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            at[i] = row * ldo + col;
+            if (e0 + 32 * i < n) {
+                v[i] = x[row * ldx + col];
+                if (kResidual) r[i] = residual[row * ldr + col];
+            }
+            col += 32;
+            if (col >= cols) {
+                const long long over = cols >= 32 ? 1 : col / cols;
+                row += over;
+                col -= over * cols;
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint32_t mine = __shfl_sync(0xffffffffu, keep, 4 * i + (lane >> 3));
-            const long long e = w * 256 + 32 * i + lane;
-            if (e < n) {
-                const long long row = e < 0x100000000LL && cols < 0x100000000LL ? (long long)((uint32_t)e / (uint32_t)cols) : e / cols;
-                const long long col = e - row * cols;
-                float v = (mine >> (lane & 7) & 1u) ? to_f32(x[row * ldx + col]) * rule.scale : 0.f;
-                if (kResidual) v += to_f32(residual[row * ldr + col]);
-                out[row * ldo + col] = from_f32<T>(v);
+            if (e0 + 32 * i < n) {
+                float y = (mine >> (lane & 7) & 1u) ? to_f32(v[i]) * rule.scale : 0.f;
+                if (kResidual) y += to_f32(r[i]);
+                out[at[i]] = from_f32<T>(y);
             }
         }
     }

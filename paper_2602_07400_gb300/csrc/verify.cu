@@ -266,7 +266,7 @@ __global__ void verify_start_kernel(int* stop, long long S) {
 
 // A sequence per warp; class 32 i + lane of a row in a lane's register i.
 template <typename T, int PER>
-__global__ void __launch_bounds__(kVerifyThreads)
+__global__ void __launch_bounds__(kVerifyThreads, PER > 16 ? 2 : PER > 4 ? 3 : 4)
 verify_narrow_kernel(Rows target, Rows draft, int V, Drafts d, Verdict out) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     grid_dependency_wait();
@@ -295,10 +295,13 @@ verify_narrow_kernel(Rows target, Rows draft, int V, Drafts d, Verdict out) {
         const int v = j < end ? d.token[j] : 0;
         const bool known = v >= 0 && v < V;
         m = BITLOGIC_NEG_INF;
+        T raw[PER];   // all loads before the first use
+#pragma unroll
+        for (int i = 0; i < PER; ++i) raw[i] = 32 * i + lane < V ? x[32 * i + lane] : T(0);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int c = 32 * i + lane;
-            z[i] = c < V ? rule.kept(logit_value(x[c]), c) : BITLOGIC_NEG_INF;
+            z[i] = c < V ? rule.kept(logit_value(raw[i]), c) : BITLOGIC_NEG_INF;
             m = fmaxf(m, z[i]);
         }
         const float zv = known ? rule.kept(logit_value(x[v]), v) : BITLOGIC_NEG_INF;
@@ -343,10 +346,27 @@ verify_narrow_kernel(Rows target, Rows draft, int V, Drafts d, Verdict out) {
     float zd[PER];
     if (spread) {
         float dm = BITLOGIC_NEG_INF;
+        const bool wide = draft.dtype == BITLOGIC_F32 || draft.dtype == BITLOGIC_I32;
+        uint32_t bits[PER];
+        if (wide) {
+            const uint32_t* x = static_cast<const uint32_t*>(draft.x) + j * draft.ld;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) bits[i] = 32 * i + lane < V ? x[32 * i + lane] : 0u;
+        } else {
+            const unsigned short* x = static_cast<const unsigned short*>(draft.x) + j * draft.ld;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) bits[i] = 32 * i + lane < V ? x[32 * i + lane] : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            zd[i] = draft.dtype == BITLOGIC_BF16  ? __uint_as_float(bits[i] << 16)
+                    : draft.dtype == BITLOGIC_F16 ? __half2float(__ushort_as_half((unsigned short)bits[i]))
+                    : draft.dtype == BITLOGIC_F32 ? __uint_as_float(bits[i])
+                                                  : logit_value((int)bits[i]);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int c = 32 * i + lane;
-            zd[i] = c < V ? kept_logit(draft, other, j, c) : BITLOGIC_NEG_INF;
+            zd[i] = c < V ? other.kept(zd[i], c) : BITLOGIC_NEG_INF;
             dm = fmaxf(dm, zd[i]);
         }
         dm = warp_largest(dm);
