@@ -8,9 +8,13 @@
 // Bound by reading and writing every value once: a block (or, where rows are
 // short, a warp) holds a row in its registers between its reductions, while the
 // next row comes into shared memory.  Sums are fp32, in a fixed order.  32768 rows
-// of 8192 bf16 columns with a residual to e4m3: 296 us, 1.88 GB at 94% of the
+// of 8192 bf16 columns with a residual to e4m3: 295 us, 1.88 GB at 94% of the
 // measured HBM rate; a block per row without the row ahead took 698, and 362 before
-// the arithmetic went by pairs.  One row of 8192 columns: 3.4 us, latency.
+// the arithmetic went by pairs.  16384 such rows with a scale per 128 columns: 169
+// us, and 201 with the groups' scales found among the stores.  Rows that do not lie
+// on 16 bytes go by element, a warp's lanes side by side (16384 x 8191: bf16 316 us,
+// fp32 312; 688 and 878 with eight neighbouring columns to a thread).  One row of
+// 8192 columns: 3.4 us, latency.
 #include <cuda_fp8.h>
 
 #include "norm_rows.cuh"
@@ -63,8 +67,7 @@ __device__ __forceinline__ uint2 to_bytes(const f32x2 (&y)[4], float inv, bool c
     return r;
 }
 
-// kAhead: rows come through shared memory, by vectors that lie in the row in full.
-template <typename T, int kVec, bool kWarp, int kThreads, bool kAhead>
+template <typename T, int kVec, bool kWarp, int kThreads, Way kWay>
 __global__ void __launch_bounds__(kThreads, resident_by_registers(kThreads, kVec, kWarp))
 norm_bytes_kernel(const T* x, long long ldx, const T* residual, long long ldr, T* total, long long ldt, Weight weight,
                   long long rows, int d, float eps, bool vec, bool vec_out, NormOut o) {
@@ -83,28 +86,28 @@ norm_bytes_kernel(const T* x, long long ldx, const T* residual, long long ldr, T
         cp_async_commit();
     };
     const float per = 1.0f / (float)d;
-    if (kAhead) ask(walk.first, 0);
+    if (kWay == kAhead) ask(walk.first, 0);
     int turn = 0;
     for (long long row = walk.first; row < rows; row += walk.step, turn ^= 1) {
-        if (kAhead) {
+        if (kWay == kAhead) {
             ask(row + walk.step, turn ^ 1);
             cp_async_wait<1>();
         }
         f32x2 h[kVec][4], square = twice(0.f);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const int c = walk.column(i);
-            if (kAhead && c >= d) {
+            const int c = walk.template start<kWay>(i);
+            if (kWay == kAhead && c >= d) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) h[i][e] = twice(0.f);
                 continue;
             }
             f32x2 r[4];
-            if (kAhead) xs(turn).get(i, h[i]);
-            else read_pairs(x + row * ldx + c, d - c, vec, h[i]);
+            if (kWay == kAhead) xs(turn).get(i, h[i]);
+            else read_pairs<kWay>(x + row * ldx + c, d - c, vec, h[i]);
             if (residual) {
-                if (kAhead) rs(turn).get(i, r);
-                else read_pairs(residual + row * ldr + c, d - c, vec, r);
+                if (kWay == kAhead) rs(turn).get(i, r);
+                else read_pairs<kWay>(residual + row * ldr + c, d - c, vec, r);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) h[i][e] = add2(h[i][e], r[e]);
             }
@@ -127,17 +130,17 @@ norm_bytes_kernel(const T* x, long long ldx, const T* residual, long long ldr, T
         if (total) {
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
-                const int c = walk.column(i);
-                if (!kAhead) write_pairs(total + row * ldt + c, d - c, vec, h[i]);
+                const int c = walk.template start<kWay>(i);
+                if (kWay != kAhead) write_pairs<kWay>(total + row * ldt + c, d - c, vec, h[i]);
                 else if (c < d) eight_of<T>(h[i]).store(total + row * ldt + c);
             }
         }
         float tops_of[kVec], top = 0.f;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const int c = walk.column(i);
+            const int c = walk.template start<kWay>(i);
             f32x2 w[4];
-            if (weight.w) weight_pairs<T>(weight, c, d - c, w);
+            if (weight.w) weight_pairs<T, kWay>(weight, c, d - c, w);
             tops_of[i] = 0.f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -149,33 +152,41 @@ norm_bytes_kernel(const T* x, long long ldx, const T* residual, long long ldr, T
             }
             top = larger(top, tops_of[i]);
         }
-        float inv = 0.f;
-        if (o.fixed > 0.f) {
-            inv = 1.0f / o.fixed;
-        } else if (o.group == 0) {
-            const float big = __uint_as_float(row_largest<kWarp>(__float_as_uint(top), tops[turn]));
-            inv = inverse_scale(big, o.most);
-            if (walk.t == 0) o.scale[row] = big < kLeast ? 0.f : big / o.most;
+        float inv[kVec];
+        if (kWay == kSpread || o.fixed > 0.f || o.group == 0) {
+            float one;
+            if (o.fixed > 0.f) {
+                one = 1.0f / o.fixed;
+            } else {
+                const float big = __uint_as_float(row_largest<kWarp>(__float_as_uint(top), tops[turn]));
+                one = inverse_scale(big, o.most);
+                if (walk.t == 0) o.scale[row] = big < kLeast ? 0.f : big / o.most;
+            }
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) inv[i] = one;
+        } else {
+            // a group is held by 2 to 32 neighbouring lanes
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                const int c = walk.column(i);
+                uint32_t t = __float_as_uint(tops_of[i]);
+                for (int lanes = o.group >> 4; lanes > 0; lanes >>= 1) t = max(t, __shfl_xor_sync(0xffffffffu, t, lanes));
+                const float big = __uint_as_float(t);
+                inv[i] = inverse_scale(big, o.most);
+                if (c < d && (c & (o.group - 1)) == 0) o.scale[row * o.groups + (c >> (31 - __clz(o.group)))] = big < kLeast ? 0.f : big / o.most;
+            }
         }
         unsigned char* out = static_cast<unsigned char*>(o.out) + row * o.ldo;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const int c = walk.column(i);
-            if (o.fixed <= 0.f && o.group != 0) {
-                // a group is held by 2 to 32 neighbouring lanes
-                uint32_t t = __float_as_uint(tops_of[i]);
-                for (int lanes = o.group >> 4; lanes > 0; lanes >>= 1) t = max(t, __shfl_xor_sync(0xffffffffu, t, lanes));
-                const float big = __uint_as_float(t);
-                inv = inverse_scale(big, o.most);
-                if (c < d && c % o.group == 0) o.scale[row * o.groups + c / o.group] = big < kLeast ? 0.f : big / o.most;
-            }
-            const uint2 b = to_bytes(h[i], inv, o.codes);
-            if (vec_out && c + 8 <= d) {
+            const int c = walk.template start<kWay>(i);
+            const uint2 b = to_bytes(h[i], inv[i], o.codes);
+            if (kWay != kSpread && vec_out && c + 8 <= d) {
                 *reinterpret_cast<uint2*>(out + c) = b;
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (c + e < d) out[c + e] = (unsigned char)((e < 4 ? b.x : b.y) >> (8 * (e & 3)));
+                    if (const int at = c + (kWay == kSpread ? 32 * e : e); at < d) out[at] = (unsigned char)((e < 4 ? b.x : b.y) >> (8 * (e & 3)));
             }
         }
     }
@@ -221,7 +232,11 @@ extern "C" int bitlogic_norm_bytes(const void* X, int32_t dtype, int64_t T, int3
             const int resident = resident_by_registers(s.threads, kVec, kWarp);
             const size_t slots = Slots<V, kVec>::bytes(residual ? 4 : 2, s.threads);
             const bool ahead = vec_in && d % 8 == 0 && slots <= kMostShared && row_blocks(T, s) > sm_count();
-            auto kern = ahead ? norm_bytes_kernel<V, kVec, kWarp, kThreads, true> : norm_bytes_kernel<V, kVec, kWarp, kThreads, false>;
+            // rows off 16 bytes, where no group of columns has to stay with its lanes
+            const bool spread = !vec_in && (group == 0 || fixed_scale > 0.f);
+            auto kern = ahead    ? norm_bytes_kernel<V, kVec, kWarp, kThreads, kAhead>
+                        : spread ? norm_bytes_kernel<V, kVec, kWarp, kThreads, kSpread>
+                                 : norm_bytes_kernel<V, kVec, kWarp, kThreads, kDirect>;
             const size_t smem = ahead ? slots : 0;
             if (allow_shared(kern, smem, kMostShared) != cudaSuccess) return (int)BITLOGIC_ERR_CUDA;
             return done(launch_dependent(kern, (unsigned)resident_blocks(s, resident, smem, T), (unsigned)s.threads, smem, stream,

@@ -9,7 +9,9 @@
 // the end.  Sums are fp32, in a fixed order.  16384 rows of 8192 bf16 columns with a
 // residual's gradient: 158 us, 1.07 GB at the measured HBM rate; 286 with a block's
 // rows read as they are wanted, 217 with rows ahead, 195 with two sums reduced at
-// once.  509 x 1001 fp32: 10 us, latency of two kernels.
+// once.  Rows off 16 bytes go by element, a warp's lanes side by side: 509 x 1001
+// fp32 6.3 us, latency of two kernels, and 16384 x 8191 bf16 494 (10 and 625 with
+// eight neighbouring columns to a thread).
 #include "norm_rows.cuh"
 
 namespace bitlogic {
@@ -18,9 +20,8 @@ namespace {
 constexpr int kNormPartials = 1024;   // rows of partial sums of dw, at most
 
 // dw goes to `partial` [blocks][d], a block's warps joined in order where each has
-// rows.  kAhead: rows come through shared memory, by vectors that lie in the row in
-// full.
-template <typename T, int kVec, bool kWarp, int kThreads, bool kAhead>
+// rows.
+template <typename T, int kVec, bool kWarp, int kThreads, Way kWay>
 __global__ void __launch_bounds__(kThreads, resident_by_registers(kThreads, kVec, kWarp))
 norm_backward_kernel(const T* dy, long long ldy, const T* h, long long ldh, Weight weight, const T* dres, long long lds,
                      T* dx, long long ldx, float* __restrict__ partial, long long rows, int d, float eps, bool vec) {
@@ -45,12 +46,12 @@ norm_backward_kernel(const T* dy, long long ldy, const T* h, long long ldh, Weig
 #pragma unroll
         for (int e = 0; e < 4; ++e) dw[i][e] = twice(0.f);
     const WeightSlots<T, kVec> ws = {raw + Slots<T, kVec>::place(4), weight.wide};
-    if (kAhead && weight.w) ws.fill(weight, walk, d);
-    if (kAhead) ask(walk.first, 0);
+    if (kWay == kAhead && weight.w) ws.fill(weight, walk, d);
+    if (kWay == kAhead) ask(walk.first, 0);
     int turn = 0;
     for (long long row = walk.first; row < rows; row += walk.step, turn ^= 1) {
         Eight<T> extra[kVec];   // of dres, wanted at the row's end
-        if (kAhead) {
+        if (kWay == kAhead) {
             ask(row + walk.step, turn ^ 1);
             if (dres) {
 #pragma unroll
@@ -61,24 +62,24 @@ norm_backward_kernel(const T* dy, long long ldy, const T* h, long long ldh, Weig
         }
         // of vector i: h and dy
         auto values = [&](int i, int c, f32x2 (&a)[4], f32x2 (&g)[4]) {
-            if (kAhead) {
+            if (kWay == kAhead) {
                 as(turn).get(i, a);
                 gs(turn).get(i, g);
             } else {
-                read_pairs(h + row * ldh + c, d - c, vec, a);
-                read_pairs(dy + row * ldy + c, d - c, vec, g);
+                read_pairs<kWay>(h + row * ldh + c, d - c, vec, a);
+                read_pairs<kWay>(dy + row * ldy + c, d - c, vec, g);
             }
         };
         f32x2 squares = twice(0.f), alongs = twice(0.f);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const int c = walk.column(i);
-            if (kAhead && c >= d) continue;
+            const int c = walk.template start<kWay>(i);
+            if (kWay == kAhead && c >= d) continue;
             f32x2 a[4], g[4], w[4];
             values(i, c, a, g);
             if (weight.w) {
-                if (kAhead) ws.get(i, w);
-                else weight_pairs<T>(weight, c, d - c, w);
+                if (kWay == kAhead) ws.get(i, w);
+                else weight_pairs<T, kWay>(weight, c, d - c, w);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) g[e] = mul2(g[e], w[e]);
             }
@@ -93,7 +94,7 @@ norm_backward_kernel(const T* dy, long long ldy, const T* h, long long ldh, Weig
         float square = sum_of(squares), along = sum_of(alongs);
         row_add_two<kWarp>(square, along, sums[turn]);
         const float rstd = row_rstd(square, per, eps, [&](float by) {
-            float s = 0.f;
+            float s = 0.f;   // of the row's columns in any order: by lanes of eight
             for (int i = 0; i < kVec; ++i) {
                 const int c = walk.column(i);
                 float a[8];
@@ -108,29 +109,29 @@ norm_backward_kernel(const T* dy, long long ldy, const T* h, long long ldh, Weig
         const f32x2 back = twice(-(along * rstd * per * rstd)), root = twice(rstd);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            const int c = walk.column(i);
-            if (kAhead && c >= d) continue;
+            const int c = walk.template start<kWay>(i);
+            if (kWay == kAhead && c >= d) continue;
             f32x2 a[4], g[4], w[4], v[4];
             values(i, c, a, g);
 #pragma unroll
             for (int e = 0; e < 4; ++e) dw[i][e] = fma2(g[e], mul2(a[e], root), dw[i][e]);
             if (weight.w) {
-                if (kAhead) ws.get(i, w);
-                else weight_pairs<T>(weight, c, d - c, w);
+                if (kWay == kAhead) ws.get(i, w);
+                else weight_pairs<T, kWay>(weight, c, d - c, w);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) g[e] = mul2(g[e], w[e]);
             }
             if (dres) {
-                if (kAhead) pairs_of(extra[i], v);
-                else read_pairs(dres + row * lds + c, d - c, vec, v);
+                if (kWay == kAhead) pairs_of(extra[i], v);
+                else read_pairs<kWay>(dres + row * lds + c, d - c, vec, v);
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const f32x2 q = fma2(a[e], back, g[e]);
                 v[e] = dres ? fma2(q, root, v[e]) : mul2(q, root);
             }
-            if (kAhead) eight_of<T>(v).store(dx + row * ldx + c);
-            else write_pairs(dx + row * ldx + c, d - c, vec, v);
+            if (kWay == kAhead) eight_of<T>(v).store(dx + row * ldx + c);
+            else write_pairs<kWay>(dx + row * ldx + c, d - c, vec, v);
         }
     }
     if (!partial) return;
@@ -142,8 +143,8 @@ norm_backward_kernel(const T* dy, long long ldy, const T* h, long long ldh, Weig
     }
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-        const int c = walk.column(i);
-        write_pairs(own + c, d - c, d % 8 == 0, dw[i]);
+        const int c = walk.template start<kWay>(i);
+        write_pairs<kWay>(own + c, d - c, d % 8 == 0, dw[i]);
     }
     if (kWarp) {
         __syncthreads();
@@ -226,7 +227,9 @@ extern "C" int bitlogic_norm_backward(const void* dY, int32_t dtype, int64_t T, 
             const int resident = resident_by_registers(s.threads, kVec, kWarp);
             const size_t slots = Slots<V, kVec>::bytes(4, s.threads) + (weight ? WeightSlots<V, kVec>::bytes(s.threads, wt.wide) : 0);
             const bool ahead = vec && d % 8 == 0 && slots <= kMostShared && row_blocks(T, s) > sm_count();
-            auto kern = ahead ? norm_backward_kernel<V, kVec, kWarp, kThreads, true> : norm_backward_kernel<V, kVec, kWarp, kThreads, false>;
+            auto kern = ahead ? norm_backward_kernel<V, kVec, kWarp, kThreads, kAhead>
+                        : vec ? norm_backward_kernel<V, kVec, kWarp, kThreads, kDirect>
+                              : norm_backward_kernel<V, kVec, kWarp, kThreads, kSpread>;
             const size_t join = kWarp && partial ? (size_t)(s.threads / 32) * d * 4 : 0;   // dw of a block's warps
             const size_t smem = std::max(ahead ? slots : 0, join);
             if (allow_shared(kern, smem, kMostShared) != cudaSuccess) return (int)BITLOGIC_ERR_CUDA;

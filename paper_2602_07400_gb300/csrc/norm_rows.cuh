@@ -62,9 +62,16 @@ __device__ __forceinline__ uint32_t row_largest(uint32_t v, uint32_t* buf) {
     return __reduce_max_sync(0xffffffffu, lane < warps ? buf[lane] : 0u);
 }
 
+// How a thread comes to a row's values.
+enum Way {
+    kDirect,   // as they are wanted, by vectors of 16 bytes where these lie so
+    kAhead,    // through shared memory, a row ahead, by vectors that lie in the row in full
+    kSpread,   // by element, a warp's lanes side by side
+};
+
 // How a block walks over rows: one at a time by all its threads, or one by each
 // warp (kWarp).  A thread of a row holds the vectors of eight columns t,
-// t + threads, ... of it.
+// t + threads, ... of it; with kSpread the same 256 columns of a warp go by lanes.
 template <bool kWarp>
 struct Walk {
     int t, threads;
@@ -77,6 +84,11 @@ struct Walk {
         step = kWarp ? (long long)gridDim.x * warps : gridDim.x;
     }
     __device__ __forceinline__ int column(int i) const { return 8 * (i * threads + t); }
+    // the first of the eight, and how far apart they are
+    template <Way kWay>
+    __device__ __forceinline__ int start(int i) const {
+        return kWay == kSpread ? 8 * (i * threads + (t & ~31)) + (t & 31) : column(i);
+    }
 };
 
 // A thread's own places in shared memory for a row on its way: the row after next
@@ -122,10 +134,17 @@ __device__ __forceinline__ float row_rstd(float sum, float per, float eps, Again
     return rsqrtf(again(kBy) * per) * kBy;
 }
 
-// A vector of a row read by vector or by element: 0 past the row's end.
-template <typename T>
+// A thread's eight values of a row, the first at p and n columns from the row's
+// end: 0 past that.
+template <Way kWay = kDirect, typename T>
 __device__ __forceinline__ void read_pairs(const T* p, int n, bool vec, f32x2 (&z)[4]) {
-    if (vec && n >= 8) {
+    if constexpr (kWay == kSpread) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 32 * i < n ? to_f32(p[32 * i]) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = pack2(v[2 * i], v[2 * i + 1]);
+    } else if (vec && n >= 8) {
         Eight<T> e;
         e.load(p);
         pairs_of(e, z);
@@ -136,9 +155,17 @@ __device__ __forceinline__ void read_pairs(const T* p, int n, bool vec, f32x2 (&
         for (int i = 0; i < 4; ++i) z[i] = pack2(v[2 * i], v[2 * i + 1]);
     }
 }
-template <typename T>
+template <Way kWay = kDirect, typename T>
 __device__ __forceinline__ void write_pairs(T* p, int n, bool vec, const f32x2 (&z)[4]) {
-    if (vec && n >= 8) {
+    if constexpr (kWay == kSpread) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float a, b;
+            unpack2(z[i], a, b);
+            if (64 * i < n) p[64 * i] = from_f32<T>(a);
+            if (64 * i + 32 < n) p[64 * i + 32] = from_f32<T>(b);
+        }
+    } else if (vec && n >= 8) {
         eight_of<T>(z).store(p);
     } else {
         float v[8];
@@ -153,10 +180,10 @@ struct Weight {
     const void* w;
     bool wide, vec;   // fp32; on 16 bytes
 };
-template <typename T>
+template <typename T, Way kWay>
 __device__ __forceinline__ void weight_pairs(const Weight& weight, int c, int n, f32x2 (&w)[4]) {
-    if (weight.wide) read_pairs(static_cast<const float*>(weight.w) + c, n, weight.vec, w);
-    else read_pairs(static_cast<const T*>(weight.w) + c, n, weight.vec, w);
+    if (weight.wide) read_pairs<kWay>(static_cast<const float*>(weight.w) + c, n, weight.vec, w);
+    else read_pairs<kWay>(static_cast<const T*>(weight.w) + c, n, weight.vec, w);
 }
 // A thread's own columns of the weight in shared memory for all of its rows, for the
 // gradient, which reads them twice a row: beside rows on their way L1 has no room
