@@ -1,4 +1,6 @@
 """Draft verification and row supports on the GPU against their 64-bit forms."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -372,6 +374,23 @@ def test_no_sequences_and_no_drafts():
                               e(0, torch.int32), e(0, torch.int32))
     Batch([0, 0, 0], 5000, "bf16", "bf16", 1).run().check()
     assert bl.bitlogic_device_error() == 0
+
+
+@pytest.mark.parametrize("V", [77, 2500])
+def test_settings_of_drafts_that_are_none_are_not_read(V):
+    """A caller of the C entry keeps its buffers' addresses when a step has no drafts."""
+    b = Batch([0, 0, 0], V, "f32", None, 3)
+    b.run().check()
+    want = b.next.clone()
+    b.next.fill_(-9)
+    ws = torch.empty(bl.bitlogic_verify_drafts_workspace(3, 0, V) or 16, dtype=torch.uint8, device="cuda")
+    kept, last = _f32(np.zeros(4)), _i32(np.zeros(4))
+    p = lambda t: None if t is None else ctypes.c_void_p(t.data_ptr())   # noqa: E731
+    st = bl.load().bitlogic_verify_drafts(p(b.target), 0, 3, 0, V, b.target.stride(0), p(b.temperature), None, None, p(b.first), None, None,
+                                          p(b.draw_u), None, 0, V, p(kept), p(kept), p(kept), p(last), p(b.accepted), p(b.next), None,
+                                          p(ws), ws.numel(), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+    torch.cuda.synchronize()
+    assert st == 0 and torch.equal(b.next, want) and b.accepted.tolist() == [0, 0, 0]
 
 
 def test_graphs_streams_and_workspaces():
