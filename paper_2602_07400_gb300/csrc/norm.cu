@@ -13,7 +13,7 @@
 // the arithmetic went by pairs.  16384 such rows with a scale per 128 columns: 169
 // us, and 201 with the groups' scales found among the stores.  Rows that do not lie
 // on 16 bytes go by element, a warp's lanes side by side (16384 x 8191: bf16 316 us,
-// fp32 312; 688 and 878 with eight neighbouring columns to a thread).  One row of
+// fp32 333; 688 and 878 with eight neighbouring columns to a thread).  One row of
 // 8192 columns: 3.4 us, latency.
 #include <cuda_fp8.h>
 
