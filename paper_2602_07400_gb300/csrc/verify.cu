@@ -76,8 +76,8 @@ __device__ __forceinline__ Part sum_part(const Rows& rows, long long row, int V,
         if (j_end >= 0) first_largest(u_end, j_end);
     };
     auto rise = [&](float to) {
-        if (to > m) {
-            sum = m > BITLOGIC_NEG_INF ? sum * exp2_unit((m - to) * rule.slope) : 0.f;
+        if (to > m) {   // about -inf the sum is 0, or the NaN of a masked batch, which stays
+            sum *= exp2_unit((m - to) * rule.slope);
             m = to;
         }
     };
