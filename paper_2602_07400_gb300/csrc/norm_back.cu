@@ -12,12 +12,32 @@
 // once.  Rows off 16 bytes go by element, a warp's lanes side by side: 509 x 1001
 // fp32 6.3 us, latency of two kernels, and 16384 x 8191 bf16 494 (10 and 625 with
 // eight neighbouring columns to a thread).
+#include <cfloat>
+
 #include "norm_rows.cuh"
 
 namespace bitlogic {
 namespace {
 
 constexpr int kNormPartials = 1024;   // rows of partial sums of dw, at most
+constexpr float k2m96 = 0x1p-96f, k2m72 = 0x1p-72f;
+
+// The two sums of a row again where fp32 does not hold them, of numbers brought
+// nearer: the squares of 2^-96 h, and h and g by 2^-72 each, which leaves the largest
+// term of a sum past 2^128 above 2^-31.  Rare, so not unrolled.
+template <typename T>
+__device__ __forceinline__ float2 sums_again(const T* h, const T* dy, Weight weight, int t, int threads, int d) {
+    float squares = 0.f, along = 0.f;
+#pragma unroll 1
+    for (int c = t; c < d; c += threads) {
+        const float a = to_f32(h[c]);
+        float g = to_f32(dy[c]);
+        if (weight.w) g *= weight.wide ? static_cast<const float*>(weight.w)[c] : to_f32(static_cast<const T*>(weight.w)[c]);
+        squares = fmaf(a * k2m96, a * k2m96, squares);
+        along = fmaf(a * k2m72, g * k2m72, along);
+    }
+    return make_float2(squares, along);
+}
 
 // dw goes to `partial` [blocks][d], a block's warps joined in order where each has
 // rows.
@@ -26,7 +46,7 @@ __global__ void __launch_bounds__(kThreads, resident_by_registers(kThreads, kVec
 norm_backward_kernel(const T* dy, long long ldy, const T* h, long long ldh, Weight weight, const T* dres, long long lds,
                      T* dx, long long ldx, float* __restrict__ partial, long long rows, int d, float eps, bool vec) {
     extern __shared__ __align__(16) unsigned char raw[];
-    __shared__ float sums[2][64], again_sums[32];
+    __shared__ float sums[2][64], again_sums[64];
     dependent_kernel_start();
     const Walk<kWarp> walk;
     const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
@@ -93,20 +113,20 @@ norm_backward_kernel(const T* dy, long long ldy, const T* h, long long ldh, Weig
         // row's barrier is passed
         float square = sum_of(squares), along = sum_of(alongs);
         row_add_two<kWarp>(square, along, sums[turn]);
-        const float rstd = row_rstd(square, per, eps, [&](float by) {
-            float s = 0.f;   // of the row's columns in any order: by lanes of eight
-            for (int i = 0; i < kVec; ++i) {
-                const int c = walk.column(i);
-                float a[8];
-                load_eight(h + row * ldh + c, d - c, false, a);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s = fmaf(a[e] * by, a[e] * by, s);
-            }
+        float rstd = rsqrtf(fmaf(square, per, eps)), mean = along * rstd * per;   // mean(g xh)
+        const bool wide = isinf(square), far = !(fabsf(along) <= FLT_MAX);
+        if (wide || far) {
+            const float2 s = sums_again(h + row * ldh, dy + row * ldy, weight, walk.t, walk.threads, d);
+            float near_square = s.x, near_along = s.y;
             if (!kWarp) __syncthreads();
-            return row_add<kWarp>(s, again_sums);
-        });
-        // xh mean(g xh) = h (rstd^2 mean(g h))
-        const f32x2 back = twice(-(along * rstd * per * rstd)), root = twice(rstd);
+            row_add_two<kWarp>(near_square, near_along, again_sums);
+            const float root = wide ? rsqrtf(near_square * per) : rstd;   // of 2^-96 h where `wide`
+            if (wide) rstd = root * k2m96;
+            mean = (far ? near_along : along) * per * root;
+            if (far) mean = wide ? mean * 0x1p48f : mean * 0x1p72f * 0x1p72f;
+            else mean *= k2m96;
+        }
+        const f32x2 along_xh = twice(-mean), root = twice(rstd);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
             const int c = walk.template start<kWay>(i);
@@ -114,7 +134,10 @@ norm_backward_kernel(const T* dy, long long ldy, const T* h, long long ldh, Weig
             f32x2 a[4], g[4], w[4], v[4];
             values(i, c, a, g);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) dw[i][e] = fma2(g[e], mul2(a[e], root), dw[i][e]);
+            for (int e = 0; e < 4; ++e) {
+                a[e] = mul2(a[e], root);   // xh
+                dw[i][e] = fma2(g[e], a[e], dw[i][e]);
+            }
             if (weight.w) {
                 if (kWay == kAhead) ws.get(i, w);
                 else weight_pairs<T, kWay>(weight, c, d - c, w);
@@ -127,7 +150,7 @@ norm_backward_kernel(const T* dy, long long ldy, const T* h, long long ldh, Weig
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const f32x2 q = fma2(a[e], back, g[e]);
+                const f32x2 q = fma2(a[e], along_xh, g[e]);
                 v[e] = dres ? fma2(q, root, v[e]) : mul2(q, root);
             }
             if (kWay == kAhead) eight_of<T>(v).store(dx + row * ldx + c);
