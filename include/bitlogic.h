@@ -684,9 +684,10 @@ int bitlogic_support_logits(const void* X, int32_t dtype, int64_t T, int32_t V, 
  * as bitlogic_sample_logits draws from its kept logits; a draft refused, from
  *   w_v = 2^40 max(0, p_v - q_v) rounded to a whole number, p_v = e_v / sum e,
  * q_v likewise, both rounded to fp32: the first class whose weights up to and
- * including its own exceed floor(draw_u sum) (e and the sums as in
- * bitlogic_sample_logits, so the draw does not depend on the batch; where no
- * weight is left, from p).
+ * including its own exceed floor(draw_u sum) (where no weight is left, from p).
+ * e and the sums are those of bitlogic_sample_logits, and p(token) of the test is
+ * e over the same sum, in fp32 as u q is: neither a verdict nor the draw depends on
+ * the batch.  S and D up to 2^24.
  *   target       device [S + D] rows of V classes, as X above (any dtype)
  *   temperature  device fp32 [S + D] or NULL (1); not > 0: p is all on the first
  *                of the largest

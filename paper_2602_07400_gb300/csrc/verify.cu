@@ -224,7 +224,7 @@ verify_parts_kernel(Rows rows, int V, Drafts d, int parts, Part* __restrict__ ou
 // 131072 bf16 classes: 189 us with all rows read, 169 without those).
 template <typename T>
 __global__ void __launch_bounds__(kVerifyThreads, 4)
-verify_rows_kernel(Rows rows, int V, Drafts d, int turns, int* stop, Part* __restrict__ out) {
+verify_rows_kernel(Rows rows, int V, Drafts d, int turns, float error, int* stop, Part* __restrict__ out) {
     __shared__ Part s[kVerifyWarps];
     grid_dependency_wait();
     allow_dependent_launch();
@@ -241,18 +241,32 @@ verify_rows_kernel(Rows rows, int V, Drafts d, int turns, int* stop, Part* __res
         }
         const long long row = at.first + seq + i, j = at.first + i;
         Part p = sum_part<T>(rows, row, V, 0u, 1u, s);
-        if (threadIdx.x == 0) {
-            if (i < at.count) {
-                const RowRule rule(rows, row);
+        if (i < at.count) {
+            __shared__ unsigned long long buf[kVerifyWarps];
+            __shared__ int border;   // the drafted class, where its share is near the bar
+            const RowRule rule(rows, row);
+            float bar = 0.f;
+            bool refused = false;
+            if (threadIdx.x == 0) {
                 const int v = d.token[j];
                 const bool known = v >= 0 && v < V;
-                const float z = known ? kept_logit(rows, rule, row, v) : BITLOGIC_NEG_INF, q = d.logprob ? expf(d.logprob[j]) : 1.f;
-                const bool refused = !(known && passes(d.u[j], q, share_in(p, rule, z, v)));
-                if (refused) p.flags |= kRefused;
-                if (refused && stop) atomicMin(stop + seq, (int)i);
+                const float z = known ? kept_logit(rows, rule, row, v) : BITLOGIC_NEG_INF, q = d.logprob ? expf(d.logprob[j]) : 1.f,
+                            share = share_in(p, rule, z, v);
+                bar = bar_of(d.u[j], q);
+                refused = !(known && bar < share);
+                border = known && by_sum(p, rule) && near_bar(bar, share, error) ? v : -1;
             }
-            out[row] = p;
+            __syncthreads();
+            if (border >= 0) {
+                const float share = whole_share(static_cast<const T*>(rows.x) + row * rows.ld, V, rule, p.m, border, buf);
+                refused = !(bar < share);
+            }
+            if (threadIdx.x == 0 && refused) {
+                p.flags |= kRefused;
+                if (stop) atomicMin(stop + seq, (int)i);
+            }
         }
+        if (threadIdx.x == 0) out[row] = p;
     }
 }
 
@@ -328,7 +342,7 @@ verify_narrow_kernel(Rows target, Rows draft, int V, Drafts d, Verdict out) {
         if (!known && lane == 0) flag_index_error();
         float p = 0.f;
         if (known && m > BITLOGIC_NEG_INF) p = sure >= 0 ? (v == sure ? 1.f : 0.f) : rule.power(zv, m) / ((float)whole * (1.0f / kWhole));
-        if (!(known && passes(d.u[j], d.logprob ? expf(d.logprob[j]) : 1.f, p))) {
+        if (!(known && bar_of(d.u[j], d.logprob ? expf(d.logprob[j]) : 1.f) < p)) {
             refused = true;
             break;
         }
@@ -431,6 +445,7 @@ int launch_verify(const Rows& target, const Rows& draft, int V, const Drafts& d,
     } else {
         const long long rows = d.S + d.D;
         const int parts = row_parts(rows, V, sizeof(T));
+        const float error = sum_error(V, sizeof(T), parts);
         if (parts > 1) {
             e = launch_rows(verify_parts_kernel<T>, rows * parts, 1, kVerifyThreads, 0, 0, stream, target, V, d, parts, ws);
         } else {
@@ -438,9 +453,9 @@ int launch_verify(const Rows& target, const Rows& draft, int V, const Drafts& d,
             int* stop = blocks > 2 * 4 * sm_count() ? reinterpret_cast<int*>(ws + rows * kMaxParts) : nullptr;
             e = stop ? launch_dependent(verify_start_kernel, (unsigned)((d.S + 255) / 256), 256, 0, stream, stop, d.S) : cudaSuccess;
             if (e == cudaSuccess)
-                e = launch_rows(verify_rows_kernel<T>, blocks, 1, kVerifyThreads, 0, 0, stream, target, V, d, (int)turns, stop, ws);
+                e = launch_rows(verify_rows_kernel<T>, blocks, 1, kVerifyThreads, 0, 0, stream, target, V, d, (int)turns, error, stop, ws);
         }
-        if (e == cudaSuccess) e = launch_verify_draw(target, draft, V, d, parts, ws, out, stream);
+        if (e == cudaSuccess) e = launch_verify_draw(target, draft, V, d, parts, error, ws, out, stream);
     }
     return e == cudaSuccess ? launch_status() : (int)BITLOGIC_ERR_CUDA;
 }

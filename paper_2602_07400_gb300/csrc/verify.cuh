@@ -78,7 +78,8 @@ struct RowRule {
 // u as the tests use it: 24 bits in [0, 1), NaN reads 0.
 __device__ __forceinline__ float unit_of(float u) { return u > 0.f ? floorf(fminf(u, 0.99999994f) * 16777216.0f) * 5.9604645e-08f : 0.f; }
 
-__device__ __forceinline__ bool passes(float u, float q, float p) { return unit_of(u) * q < p; }
+// What a draft's test compares p with: u q.
+__device__ __forceinline__ float bar_of(float u, float q) { return unit_of(u) * q; }
 
 // The sum of v over the lanes below this one and itself.
 __device__ __forceinline__ unsigned long long lanes_upto(unsigned long long v, int lane) {
@@ -95,6 +96,32 @@ __device__ __forceinline__ float share_in(const Part& p, const RowRule& rule, fl
     if (!(p.m > BITLOGIC_NEG_INF)) return 0.f;
     if (rule.greedy || p.m > FLT_MAX) return v == p.cls ? 1.f : 0.f;
     return rule.power(z, p.m) / p.sum;
+}
+
+// How far the fp32 sum of a row's parts is off, relatively: in units of 2^-24 less
+// than 24 a batch (a rise of the maximum and an addition a piece at most, 6 each, four
+// pieces) and 190 (the joins 120, the exponents 44, the powers and the whole weights'
+// roundings 26); taken are 32 and 512, 2^-14 for 131072 bf16 classes.
+inline float sum_error(int V, int element, int parts) {
+    const int batches = ((V / (16 / element) + 2) / parts + 1) / (4 * kVerifyThreads) + 1;
+    return (float)(4 * batches + 64) / (float)(1 << 21);
+}
+// A share of which that may turn the verdict is found again from the sum in whole
+// numbers, which is the same in any order; so a verdict goes by its row alone.
+__device__ __forceinline__ bool near_bar(float bar, float p, float error) { return p > 0.f && fabsf(bar - p) <= p * error; }
+// Whether a row's shares come from a sum.
+__device__ __forceinline__ bool by_sum(const Part& p, const RowRule& rule) { return !rule.greedy && p.m <= FLT_MAX; }
+
+// The share of class v of a row by its sum in whole numbers about the largest logit m.
+// Called by the whole block; `buf`: a value per warp.  Rare, and out of the callers'
+// registers.
+template <typename T>
+__device__ __noinline__ float whole_share(const T* x, int V, RowRule rule, float m, int v, unsigned long long* buf) {
+    unsigned long long sum = 0;
+#pragma unroll 4
+    for (int c = threadIdx.x; c < V; c += kVerifyThreads) sum += draw_weight(rule.power(rule.kept(logit_value(x[c]), c), m));
+    sum = block_add(sum, buf, kVerifyWarps);
+    return rule.power(rule.kept(logit_value(x[v]), v), m) / ((float)sum * (1.0f / kWhole));
 }
 
 // The kept logit of class v of a row of any type.
@@ -127,7 +154,7 @@ struct Weigher {
 };
 
 // The draw behind the accepted drafts of every sequence (verify_draw.cu).
-cudaError_t launch_verify_draw(const Rows& target, const Rows& draft, int V, const Drafts& d, int parts, const Part* sums,
-                               const Verdict& out, cudaStream_t stream);
+cudaError_t launch_verify_draw(const Rows& target, const Rows& draft, int V, const Drafts& d, int parts, float error,
+                               const Part* sums, const Verdict& out, cudaStream_t stream);
 
 }  // namespace bitlogic

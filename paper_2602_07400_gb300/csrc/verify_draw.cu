@@ -147,7 +147,9 @@ struct DrawShared {
     } target[kMaxCluster], nan[kMaxCluster], draft[kMaxCluster], rest[kMaxCluster];
     unsigned long long warp_mass[kVerifyWarps];
     float fbuf[kVerifyWarps];
-    int stop;                              // the first draft refused
+    int stop, near;                        // of a round, the first draft refused and the first near its bar
+    float bar;
+    int token;                             // of the draft near its bar
     struct {
         float m;
         int cls, flags;
@@ -178,7 +180,7 @@ __host__ __device__ __forceinline__ size_t tile_bytes(int chunks, int element) {
 
 template <typename T, typename Q, bool kTiled>
 __global__ void __launch_bounds__(kVerifyThreads, 3)
-verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Part* __restrict__ sums, Verdict out) {
+verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, float error, const Part* __restrict__ sums, Verdict out) {
     unsigned long long* chunks = reinterpret_cast<unsigned long long*>(draw_shared);
     __shared__ DrawShared s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -208,7 +210,10 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
     bool waited = false;   // for the rows' sums
     for (;; base += round) {
         const long long i = base + tid / parts;   // the row behind the last draft is among them
-        if (tid == 0) s.stop = kVerifyThreads;
+        float bar = 0.f;
+        int v = -1;
+        bool near = false;
+        if (tid == 0) s.stop = s.near = kVerifyThreads;
         __syncthreads();
         if (base + (tid & ~31) / parts <= k) {    // alike in a warp
             const bool real = i <= k, test = i < k;
@@ -221,18 +226,40 @@ verify_draw_kernel(Rows target, Rows draft, int V, Drafts d, int parts, const Pa
                 if (test && (p.flags & kRefused)) atomicMin(&s.stop, tid);
             } else {
                 const RowRule rule(target, row);
-                const int v = test ? d.token[j] : -1;
+                v = test ? d.token[j] : -1;
                 const bool known = v >= 0 && v < V;
                 const float z = known ? kept_logit(target, rule, row, v) : BITLOGIC_NEG_INF, u = test ? d.u[j] : 0.f,
                             q = test && d.logprob ? expf(d.logprob[j]) : 1.f;
                 if (!waited) grid_dependency_wait();
                 const Part p = join_parts(sums[row * parts + (tid & (parts - 1))], parts, rule);
                 if (leads && real) s.row[tid / parts] = {p.m, p.cls, p.flags};
-                if (leads && test && !(known && passes(u, q, share_in(p, rule, z, v)))) atomicMin(&s.stop, tid / parts);
+                const float share = share_in(p, rule, z, v);
+                bar = bar_of(u, q);
+                near = leads && test && known && by_sum(p, rule) && near_bar(bar, share, error);
+                if (near) atomicMin(&s.near, tid / parts);
+                else if (leads && test && !(known && bar < share)) atomicMin(&s.stop, tid / parts);
             }
             waited = true;
         }
         __syncthreads();
+        while (__builtin_expect(s.near < s.stop, 0)) {   // in their order; alike in all blocks
+            const int n = s.near;
+            if (near && n == tid / parts) {
+                s.bar = bar;
+                s.token = v;
+            }
+            __syncthreads();
+            const long long border = first + seq + base + n;
+            const float share = whole_share(static_cast<const T*>(target.x) + border * target.ld, V, RowRule(target, border), s.row[n].m,
+                                            s.token, s.warp_mass);
+            if (tid == 0) {
+                if (!(s.bar < share)) s.stop = n;
+                s.near = kVerifyThreads;
+            }
+            __syncthreads();
+            if (near && tid / parts > n) atomicMin(&s.near, tid / parts);
+            __syncthreads();
+        }
         if (s.stop < kVerifyThreads) a = base + s.stop;
         if (a < base + round) break;   // refused here, or the last row is here
         __syncthreads();
@@ -492,35 +519,35 @@ inline DrawShape draw_shape(int64_t S, int V, int element, int draft_element) {
 }
 
 template <typename T, typename Q>
-cudaError_t launch_draw(const Rows& target, const Rows& draft, int V, const Drafts& d, int parts, const Part* sums, const Verdict& out,
-                        cudaStream_t stream) {
+cudaError_t launch_draw(const Rows& target, const Rows& draft, int V, const Drafts& d, int parts, float error, const Part* sums,
+                        const Verdict& out, cudaStream_t stream) {
     const DrawShape s = draw_shape(d.S, V, sizeof(T), draft.x ? sizeof(Q) : 0);
     const bool tiled = s.bytes <= kDrawShared;
     return launch_rows(tiled ? verify_draw_kernel<T, Q, true> : verify_draw_kernel<T, Q, false>, d.S, s.blocks, kVerifyThreads,
-                       tiled ? s.bytes : (size_t)s.chunks * 8, kDrawShared, stream, target, draft, V, d, parts, sums, out);
+                       tiled ? s.bytes : (size_t)s.chunks * 8, kDrawShared, stream, target, draft, V, d, parts, error, sums, out);
 }
 
 template <typename T>
-cudaError_t launch_draw_of(const Rows& target, const Rows& draft, int V, const Drafts& d, int parts, const Part* sums, const Verdict& out,
-                           cudaStream_t stream) {
-    if (!draft.x) return launch_draw<T, T>(target, draft, V, d, parts, sums, out, stream);
+cudaError_t launch_draw_of(const Rows& target, const Rows& draft, int V, const Drafts& d, int parts, float error, const Part* sums,
+                           const Verdict& out, cudaStream_t stream) {
+    if (!draft.x) return launch_draw<T, T>(target, draft, V, d, parts, error, sums, out, stream);
     switch (draft.dtype) {
-        case BITLOGIC_F32: return launch_draw<T, float>(target, draft, V, d, parts, sums, out, stream);
-        case BITLOGIC_BF16: return launch_draw<T, __nv_bfloat16>(target, draft, V, d, parts, sums, out, stream);
-        case BITLOGIC_F16: return launch_draw<T, __half>(target, draft, V, d, parts, sums, out, stream);
-        default: return launch_draw<T, int>(target, draft, V, d, parts, sums, out, stream);
+        case BITLOGIC_F32: return launch_draw<T, float>(target, draft, V, d, parts, error, sums, out, stream);
+        case BITLOGIC_BF16: return launch_draw<T, __nv_bfloat16>(target, draft, V, d, parts, error, sums, out, stream);
+        case BITLOGIC_F16: return launch_draw<T, __half>(target, draft, V, d, parts, error, sums, out, stream);
+        default: return launch_draw<T, int>(target, draft, V, d, parts, error, sums, out, stream);
     }
 }
 
 }  // namespace
 
-cudaError_t launch_verify_draw(const Rows& target, const Rows& draft, int V, const Drafts& d, int parts, const Part* sums,
+cudaError_t launch_verify_draw(const Rows& target, const Rows& draft, int V, const Drafts& d, int parts, float error, const Part* sums,
                                const Verdict& out, cudaStream_t stream) {
     switch (target.dtype) {
-        case BITLOGIC_F32: return launch_draw_of<float>(target, draft, V, d, parts, sums, out, stream);
-        case BITLOGIC_BF16: return launch_draw_of<__nv_bfloat16>(target, draft, V, d, parts, sums, out, stream);
-        case BITLOGIC_F16: return launch_draw_of<__half>(target, draft, V, d, parts, sums, out, stream);
-        default: return launch_draw_of<int>(target, draft, V, d, parts, sums, out, stream);
+        case BITLOGIC_F32: return launch_draw_of<float>(target, draft, V, d, parts, error, sums, out, stream);
+        case BITLOGIC_BF16: return launch_draw_of<__nv_bfloat16>(target, draft, V, d, parts, error, sums, out, stream);
+        case BITLOGIC_F16: return launch_draw_of<__half>(target, draft, V, d, parts, error, sums, out, stream);
+        default: return launch_draw_of<int>(target, draft, V, d, parts, error, sums, out, stream);
     }
 }
 
