@@ -384,7 +384,7 @@ struct SampleShared {
 // Bins of the powers e, falling: by the exponent and the 6 leading bits of the
 // mantissa, so that the powers above bin b are those with e > bin_above(b); bin
 // 64 is the first below 1.  A power counts its mantissa's 15 leading bits, so
-// that a bin of 2^17 of them sums in 32 bits and is right to 2^-14 of itself.
+// that a bin of 2^17 of them sums in 32 bits and is right to 2^-15 of itself.
 __device__ __forceinline__ int bin_of(float e) { return (int)((0x3fffffffu - __float_as_uint(e)) >> 17); }   // 2^-41 <= e <= 1
 __device__ __forceinline__ unsigned bin_units(float e) { return (((__float_as_uint(e) & 0x7fffffu) | 0x800000u) + 256u) >> 9; }
 __device__ __forceinline__ float bin_mass(unsigned units, int b) {
@@ -394,15 +394,18 @@ __device__ __forceinline__ float bin_above(int b) { return __uint_as_float(0x3ff
 
 // The bins among which a mass is reached from the largest power down, into *bin: the
 // first and, 12 bits up, the last (the last bin of all where there is none).  Every
-// power counts to 2^-16 of itself, and so do the bins' sums: the bins are those that
-// the mass may be reached in if all of them are off by as much, 2^-15 with what
-// fp32 sums add.  (One bin more on either side than the one found left out the cut
-// of one row in some thousands, where bins weigh less than that; a block took 1.5 ms
-// to draw such a row from memory.)  Called by the whole block.
+// power counts to 2^-15 of itself (half a unit of 2^14 or more), and so do the bins'
+// sums; fp32 sums and goal and the weights' own roundings add less than 2^-18: the
+// bins are those that the mass may be reached in if they are off by both.  No more,
+// as a bin of many equal powers beside the cut overflows the list.  (One bin more on
+// either side than the one found left out the cut of one row in some thousands, where
+// bins weigh less than that; a block took 1.5 ms to draw such a row from memory.)
+// Called by the whole block.
 __device__ __forceinline__ void find_bin(const unsigned* bins, float goal, int* bin, int* last, float* fbuf) {
     constexpr int kPer = (kBins + kSampleThreads - 1) / kSampleThreads;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const float least = goal * (1.0f - 3.0517578e-5f), most = goal * (1.0f + 3.0517578e-5f);
+    constexpr float kOff = 0x1p-15f + 0x1p-18f;
+    const float least = goal * (1.0f - kOff), most = goal * (1.0f + kOff);
     float sum = 0.f;
     for (int q = 0; q < kPer; ++q) {
         const int b = tid * kPer + q;
