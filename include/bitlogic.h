@@ -697,7 +697,8 @@ int bitlogic_support_logits(const void* X, int32_t dtype, int64_t T, int32_t V, 
  *                Drafts and rows behind first[S] are not read, so that a batch
  *                may be shorter than its buffers.  A sequence whose places break
  *                this raises the device flag: accepted 0, next_token -1,
- *                logprob -inf
+ *                logprob -inf; what others get that share rows through it counts
+ *                for nothing
  *   token        device int32 [D]; a class outside [0, V) is refused, and raises
  *                the device flag if no draft before it is
  *   u, draw_u    device fp32 [D] and [S], in [0, 1) (clamped; NaN reads 0; 24

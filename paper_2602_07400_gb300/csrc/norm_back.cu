@@ -6,11 +6,12 @@
 // Bound by reading and writing every value once: persistent blocks (or, where rows
 // are short, warps) read a row's values twice from shared memory, into which the
 // next row comes meanwhile, and keep their columns' part of dw in registers until
-// the end.  Sums are fp32, in a fixed order.  16384 rows of 8192 bf16 columns with a
-// residual's gradient: 158 us, 1.07 GB at the measured HBM rate; 286 with a block's
-// rows read as they are wanted, 217 with rows ahead, 195 with two sums reduced at
-// once.  Rows off 16 bytes go by element, a warp's lanes side by side: 509 x 1001
-// fp32 6.3 us, latency of two kernels, and 16384 x 8191 bf16 494 (10 and 625 with
+// the end.  Sums are fp32, in a fixed order; where one passes fp32 both are formed
+// again of numbers brought nearer (sums_again).  16384 rows of 8192 bf16 columns with
+// a residual's gradient: 160 us, 1.07 GB at 99% of the measured HBM rate; 286 with a
+// block's rows read as they are wanted, 217 with rows ahead, 195 with two sums reduced
+// at once.  Rows off 16 bytes go by element, a warp's lanes side by side: 509 x 1001
+// fp32 6.3 us, latency of two kernels, and 16384 x 8191 bf16 340 (10 and 625 with
 // eight neighbouring columns to a thread).
 #include <cfloat>
 

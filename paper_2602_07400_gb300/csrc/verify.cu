@@ -8,7 +8,8 @@
 //
 // so that every class that goes out is distributed as p.  q(d_i) comes from the
 // draft's draw, so of the draft's logits only the refused row is read; the
-// target's rows are read once.  Bound by that reading.
+// target's rows are read once, and again where u q is so near p that the fp32 sum
+// does not decide (near_bar).  Bound by that reading.
 //
 //   verify_rows_kernel    a row (verify_parts_kernel, where rows are few: a part of
 //                         one) per block: its largest logit and the sum of its

@@ -242,7 +242,10 @@ class TrainStep:
     (int64 [2] on the device: ``seed`` and a step that ``update`` advances) gives
     the mask; ranks of a data-parallel run take different seeds.  The step then
     keeps layer 1's output and its gradient as fp32 rows (neither ``through``,
-    ``fuse_dy1`` nor ``codes1``)."""
+    ``fuse_dy1`` nor ``codes1``: the CIFAR-100-shaped step takes 6.0 ms in place of
+    4.0); ``y1`` holds the values after the drop, ``dy1`` the gradient before it.  With
+    ``dropout`` set to 0 later on, the passes that follow drop nothing (a captured
+    graph keeps what it was captured with)."""
 
     def __init__(self, net: Network, B: int, d: int, thresholds: Sequence[int], C: int,
                  tau: float, want_dx1: bool = False, keep_dy1: bool = False,
@@ -587,7 +590,8 @@ class Features:
                  residual_grad: Optional[torch.Tensor] = None, stream=None):
         """From the gradient ``dy`` of the rows before their rounding to codes, that
         of ``hidden`` and of the residual (alike) into ``dx``, and of the weight into
-        dweight fp32 [d], at the rows ``total``."""
+        dweight fp32 [d], at the rows ``total``.  ``dy`` is the caller's: a step's own
+        gradients end at the wires of the thermometer (TrainStep's ``want_dx1``)."""
         ws = None
         if dweight is not None:
             with _on(stream):
