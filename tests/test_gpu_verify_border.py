@@ -78,3 +78,38 @@ def test_the_border_does_not_move(V, dtype, temp, kind):
             got = _accepted(rows[:k + 1], torch.tensor([0, k], dtype=torch.int32, device="cuda"), tok[:k], u[i0:i0 + k], lp[:k], rows[:k],
                             temperature=T[:k + 1], **{n: one(v, k + 1) for n, v in settings.items()})
             assert int(got) == edge - i0
+
+
+@pytest.mark.parametrize("V,dtype", [(5000, "f32"), (131072, "bf16"), (30011, "f16")])
+@pytest.mark.parametrize("k,others", [(20, 0), (100, 0), (140, 0), (100, 260)])
+def test_many_drafts_at_the_border(V, dtype, k, others):
+    # drafts of one row, those just accepted and the first just refused in any place:
+    # rows in parts, by rounds, and whole rows among those of other sequences
+    g = torch.Generator(device="cuda").manual_seed(V + k)
+    x = (torch.randn(V, generator=g, device="cuda") * 2).to(DTYPES[dtype])
+    token = int(x.float().argmax())
+    p = _exact(x.double().cpu().numpy(), np.float32(1.0), token)
+    lp = float(np.log(p / 0.75))
+    q = float(torch.tensor(lp, dtype=torch.float32).double().exp())
+    S, D = 1 + others, k + others
+    rows = x[None].expand(S + D, V).contiguous()
+    tok, lps = torch.full((D,), token, dtype=torch.int32, device="cuda"), torch.full((D,), lp, device="cuda")
+    # the last u that is accepted, by sequences of one draft
+    at = int(round(p / q * 2 ** 24)) + np.arange(N) - N // 2
+    u = torch.from_numpy((at / 2.0 ** 24).astype(np.float32)).cuda()
+    one = _accepted(x[None].expand(2 * N, V).contiguous(), torch.arange(N + 1, dtype=torch.int32, device="cuda"),
+                    torch.full((N,), token, dtype=torch.int32, device="cuda"), u, torch.full((N,), lp, device="cuda"),
+                    x[None].expand(N, V).contiguous())
+    edge = int(one.sum())
+    yes, no = float(u[edge - 1]), float(u[edge])
+    first = torch.cat([torch.zeros(1), torch.arange(k, D + 1)]).to(torch.int32).cuda()
+    for stop in (0, 1, 7, 15, 16, k // 2, k - 1, k):
+        v = torch.full((D,), 0.3, device="cuda")
+        v[:k:3] = yes
+        v[max(0, stop - 2):stop] = yes
+        if stop < k:
+            v[stop] = no
+            v[stop + 1:k:2] = yes
+            v[stop + 2:k:4] = 0.999
+        got = _accepted(rows, first, tok, v, lps, rows[:D])
+        assert int(got[0]) == stop and (got[1:] == 1).all()
